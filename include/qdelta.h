@@ -94,6 +94,13 @@ typedef struct {
 
 typedef struct CUstream_st *qd_stream;   /* a cudaStream_t */
 
+/* flags of the operators around the delta rule */
+enum {
+    QD_SILU = 32,             /* qdelta_conv_*: y = SiLU(convolution) */
+    QD_SOFTPLUS = 64,         /* qdelta_scan_*: the step is softplus(dt + dt_bias); without it dt + dt_bias as given */
+    QD_RMS = 128              /* qdelta_norm_*: no mean is taken off */
+};
+
 /* Which kernels serve `shape` (the paper has no counterpart; a query for tests and benchmarks):
  * 1 = tensor-core kernels, 0 = fp32-accurate kernels, -1 = invalid or unsupported shape. */
 int qdelta_chunk_path(const qd_shape *shape);
@@ -167,6 +174,82 @@ int qdelta_recurrent_steps(int B, int S, int H, int dk, int dv, int dtype,
                            const void *q, const void *k, const void *v,
                            const void *beta, const void *alpha, const void *lambda,
                            void *state, void *o, unsigned flags, qd_stream stream);
+
+/* ---- operators around the delta rule --------------------------------------------------------------------------
+ * What a recurrent layer runs before, beside and after the calls above.  The conventions at the top of this file hold
+ * (dense device tensors, 16-byte aligned, ordinary stream order, nothing allocated); `dtype` is the type of all tensors but
+ * those given as float.  Gradients of parameters are fp32.  The same call gives the same bits.  Their workspaces hold no
+ * status word. */
+
+/*
+ * Short causal convolution, per channel, before q, k, v (or a scan's input):
+ *     y[b,t,d] = f(bias[d] + sum_j w[d,j] x[b, t - W + 1 + j, d]) ,  j = 0 .. W - 1,  f = SiLU with QD_SILU, else identity
+ *     x, y [B,T,D]   w [D,W]   bias [D] or NULL   W = 2, 3 or 4   T <= 2^30, D <= 2^20
+ * state [B,W-1,D]: the tokens before the first (NULL: zeros); last [B,W-1,D]: the last W - 1 rows of state and x, the state
+ * for the call that goes on from here (NULL: not returned; not the same buffer as state, which other tokens still read).
+ */
+int qdelta_conv_fwd(int B, int T, int D, int W, int dtype, const void *x, const void *w, const void *bias, const void *state,
+                    void *y, void *last, unsigned flags, qd_stream stream);
+
+/* S tokens of every sequence, x, y [B,S,D], `state` [B,W-1,D] updated in place: single tokens, and draft tokens. */
+int qdelta_conv_steps(int B, int S, int D, int W, int dtype, const void *x, const void *w, const void *bias, void *state, void *y,
+                      unsigned flags, qd_stream stream);
+
+size_t qdelta_conv_workspace_bytes(int B, int T, int D, int W, int dtype);      /* of the backward; 0 on an invalid shape */
+
+/* Backward for  L = <y, dy> + <last, dlast>  (dlast NULL: zero).  dx [B,T,D], dstate [B,W-1,D] (NULL: skipped) in `dtype`;
+ * dw [D,W], dbias [D] fp32 (dbias may be NULL only if bias is). */
+int qdelta_conv_bwd(int B, int T, int D, int W, int dtype, const void *x, const void *w, const void *bias, const void *state,
+                    const void *dy, const void *dlast, void *dx, float *dw, float *dbias, void *dstate, void *workspace,
+                    size_t workspace_bytes, unsigned flags, qd_stream stream);
+
+/*
+ * Selective state space scan, N states to a channel:
+ *     h_t = exp(dt_t A) h_{t-1} + dt_t u_t Bm_t ,   y_t = (<Cm_t, h_t> + D u_t) SiLU(z_t)
+ *     u, dt, z, y [B,T,D]   A [D,N] fp32 (not positive where the state is to stay bounded)   D, dt_bias [D] fp32
+ *     Bm, Cm [B,T,G,N], shared by the D / G channels of a group   h0, hT [B,D,N] fp32
+ * D, z, dt_bias, h0 may be NULL (no skip, no factor, no bias, zero state), hT too (not returned).
+ * N from 1 to 64, T <= 2^30, D <= 2^20 a multiple of G.  A forward may need a workspace even if it does not save.
+ */
+typedef struct {
+    int B, T, D, N, G;        /* batch, tokens, channels, states per channel, groups */
+    int dtype;                /* qd_dtype of u, dt, z, y, Bm, Cm and their gradients */
+} qd_scan_shape;
+
+/* 0 on an invalid shape, and for a forward that needs none */
+size_t qdelta_scan_workspace_bytes(const qd_scan_shape *shape, int for_backward);
+
+/* flags: QD_SOFTPLUS, QD_FWD_SAVE_FOR_BWD (with a workspace of the backward's size). */
+int qdelta_scan_fwd(const qd_scan_shape *shape, const void *u, const void *dt, const float *A, const void *Bm, const void *Cm,
+                    const float *D, const void *z, const float *dt_bias, const float *h0, void *y, float *hT,
+                    void *workspace, size_t workspace_bytes, unsigned flags, qd_stream stream);
+
+/* Backward for  L = <y, dy> + <hT, dhT>  (dhT NULL: zero).  Gradients have the shapes of what they belong to; dA, dD, ddt_bias,
+ * dh0 are fp32, the others in `dtype`.  dD, dz, ddt_bias may be NULL only if D, z, dt_bias are; dh0 NULL: skipped.
+ * flags: QD_SOFTPLUS, QD_BWD_REUSE_FWD (the workspace holds what a saving forward of the same inputs left). */
+int qdelta_scan_bwd(const qd_scan_shape *shape, const void *u, const void *dt, const float *A, const void *Bm, const void *Cm,
+                    const float *D, const void *z, const float *dt_bias, const float *h0, const void *dy, const float *dhT,
+                    void *du, void *ddt, float *dA, void *dBm, void *dCm, float *dD, void *dz, float *ddt_bias, float *dh0,
+                    void *workspace, size_t workspace_bytes, unsigned flags, qd_stream stream);
+
+/* shape->T tokens of every sequence with `state` [B,D,N] fp32 updated in place: single tokens, and draft tokens. */
+int qdelta_scan_steps(const qd_scan_shape *shape, const void *u, const void *dt, const float *A, const void *Bm, const void *Cm,
+                      const float *D, const void *z, const float *dt_bias, float *state, void *y, unsigned flags, qd_stream stream);
+
+/*
+ * Layer norm of `rows` rows of `width` elements (1 to 16384), e.g. of a layer's input or of its read-out per head:
+ *     m = mean(x) (0 with QD_RMS),  r = 1 / sqrt(mean((x - m)^2) + eps),  y = (x - m) r weight + bias
+ * weight, bias [width] in `dtype` or NULL.  stats [2, rows] fp32 receives m and r for the backward (NULL: not returned).
+ * eps >= 0 and finite.
+ */
+int qdelta_norm_fwd(long long rows, int width, int dtype, const void *x, const void *weight, const void *bias, void *y, float *stats,
+                    float eps, unsigned flags, qd_stream stream);
+
+size_t qdelta_norm_workspace_bytes(long long rows, int width, int dtype);       /* of the backward; 0 on an invalid shape */
+
+/* Backward for  L = <y, dy>: dx in `dtype`, dweight, dbias [width] fp32 (NULL: skipped).  No workspace is needed without them. */
+int qdelta_norm_bwd(long long rows, int width, int dtype, const void *x, const void *weight, const void *dy, const float *stats,
+                    void *dx, float *dweight, float *dbias, void *workspace, size_t workspace_bytes, unsigned flags, qd_stream stream);
 
 /* Copies the device status word of `workspace` to *status_out (a qd_status) with a blocking
  * 4-byte device-to-host copy on `stream`.  Returns QD_OK or QD_ERR_CUDA / QD_ERR_INVALID_ARG. */

@@ -48,8 +48,8 @@ int check_shape(const qd_shape* s) {
 static bool misaligned(const void* p) { return ((uintptr_t)p & 15) != 0; }
 
 // ---- optional per-stage timing with CUDA events on the launching stream ------------------------
-enum Stage { ST_PREP = 0, ST_CHAIN_FWD, ST_CHAIN_BWD, ST_CHUNK_BWD, ST_DECODE, ST_COUNT };
-static const char* kStageNames[ST_COUNT] = {"prep", "chain_fwd", "chain_bwd", "chunk_bwd", "decode"};
+enum Stage { ST_PREP = 0, ST_CHAIN_FWD, ST_CHAIN_BWD, ST_CHUNK_BWD, ST_DECODE, ST_CONV, ST_SCAN, ST_NORM, ST_COUNT };
+static const char* kStageNames[ST_COUNT] = {"prep", "chain_fwd", "chain_bwd", "chunk_bwd", "decode", "conv", "scan", "norm"};
 struct Pending { cudaEvent_t a, b; int stage; };
 static bool g_profile = false;
 static std::vector<Pending> g_pending;
@@ -64,7 +64,7 @@ static cudaEvent_t get_event() {
     return e;
 }
 
-// Brackets one kernel launch with two events when profiling is on.
+// Brackets one kernel launch (of the operators around the delta rule: one call) with two events when profiling is on.
 struct StageTimer {
     cudaEvent_t a = nullptr, b = nullptr;
     int stage; cudaStream_t s;
@@ -102,6 +102,36 @@ static cudaError_t tc_backward(const ChunkArgs& a) {
     if (parts > 1) return tc_bwd(a, parts);
     const cudaError_t e = timed(ST_CHAIN_BWD, a.stream, [&] { return tc_chain_bwd(a); });
     return e != cudaSuccess ? e : timed(ST_CHUNK_BWD, a.stream, [&] { return tc_chunk_bwd(a); });
+}
+
+// ---- operators around the delta rule: what a shape has to satisfy ---------------------------------------------------
+constexpr long long kMostElements = 1LL << 37;             // of a tensor; what fits the GPU's memory is below it, and grids fit 31 bits
+static int check_conv(int B, int T, int D, int W, int dtype) {
+    if (B <= 0 || T <= 0 || D <= 0 || W <= 0) return QD_ERR_INVALID_ARG;
+    if (dtype != QD_F32 && dtype != QD_BF16) return QD_ERR_UNSUPPORTED;
+    if (W < 2 || W > 4 || T > 1 << 30 || D > 1 << 20) return QD_ERR_UNSUPPORTED;
+    if ((long long)B * T > kMostElements / D) return QD_ERR_UNSUPPORTED;
+    return QD_OK;
+}
+static int check_scan(const qd_scan_shape* s) {
+    if (!s || s->B <= 0 || s->T <= 0 || s->D <= 0 || s->N <= 0 || s->G <= 0) return QD_ERR_INVALID_ARG;
+    if (s->dtype != QD_F32 && s->dtype != QD_BF16) return QD_ERR_UNSUPPORTED;
+    if (s->N > 64 || s->T > 1 << 30 || s->D > 1 << 20 || s->D % s->G) return QD_ERR_UNSUPPORTED;
+    if ((long long)s->B * s->D > 1LL << 30 || (long long)s->B * s->T > kMostElements / ((long long)s->G * s->N) ||
+        (long long)s->B * s->T > kMostElements / s->D)
+        return QD_ERR_UNSUPPORTED;
+    return QD_OK;
+}
+static int check_norm(long long rows, int width, int dtype) {
+    if (rows <= 0 || width <= 0) return QD_ERR_INVALID_ARG;
+    if (dtype != QD_F32 && dtype != QD_BF16) return QD_ERR_UNSUPPORTED;
+    if (width > 16384 || rows > kMostElements / 4 || rows > kMostElements / width) return QD_ERR_UNSUPPORTED;
+    return QD_OK;
+}
+template <size_t N> static bool any_misaligned(const void* const (&ptrs)[N]) {
+    for (const void* p : ptrs)
+        if (p && misaligned(p)) return true;
+    return false;
 }
 
 }  // namespace qd
@@ -266,6 +296,147 @@ int qdelta_recurrent_steps(int B, int S, int H, int dk, int dv, int dtype, const
         }) != cudaSuccess)
         return QD_ERR_CUDA;
     return QD_OK;
+}
+
+int qdelta_conv_fwd(int B, int T, int D, int W, int dtype, const void* x, const void* w, const void* bias, const void* state,
+                    void* y, void* last, unsigned flags, qd_stream stream) {
+    const int rc = check_conv(B, T, D, W, dtype);
+    if (rc != QD_OK) return rc;
+    if (!x || !w || !y || y == x || (last && last == state)) return QD_ERR_INVALID_ARG;
+    const void* const ptrs[] = {x, w, bias, state, y, last};
+    if (any_misaligned(ptrs) || (flags & ~(unsigned)QD_SILU)) return QD_ERR_INVALID_ARG;
+    const cudaStream_t s = (cudaStream_t)stream;
+    const cudaError_t e = timed(ST_CONV, s, [&] { return conv_fwd(B, T, D, W, dtype, x, w, bias, state, y, last, (flags & QD_SILU) != 0, s); });
+    return e == cudaSuccess ? QD_OK : QD_ERR_CUDA;
+}
+
+int qdelta_conv_steps(int B, int S, int D, int W, int dtype, const void* x, const void* w, const void* bias, void* state, void* y,
+                      unsigned flags, qd_stream stream) {
+    const int rc = check_conv(B, S, D, W, dtype);
+    if (rc != QD_OK) return rc;
+    if (!x || !w || !state || !y || y == x) return QD_ERR_INVALID_ARG;
+    const void* const ptrs[] = {x, w, bias, state, y};
+    if (any_misaligned(ptrs) || (flags & ~(unsigned)QD_SILU)) return QD_ERR_INVALID_ARG;
+    const cudaStream_t s = (cudaStream_t)stream;
+    const cudaError_t e = timed(ST_CONV, s, [&] { return conv_fwd(B, S, D, W, dtype, x, w, bias, state, y, state, (flags & QD_SILU) != 0, s); });
+    return e == cudaSuccess ? QD_OK : QD_ERR_CUDA;
+}
+
+size_t qdelta_conv_workspace_bytes(int B, int T, int D, int W, int dtype) {
+    return check_conv(B, T, D, W, dtype) == QD_OK ? conv_bwd_workspace(B, T, D, W, dtype) : 0;
+}
+
+int qdelta_conv_bwd(int B, int T, int D, int W, int dtype, const void* x, const void* w, const void* bias, const void* state,
+                    const void* dy, const void* dlast, void* dx, float* dw, float* dbias, void* dstate, void* workspace,
+                    size_t workspace_bytes, unsigned flags, qd_stream stream) {
+    const int rc = check_conv(B, T, D, W, dtype);
+    if (rc != QD_OK) return rc;
+    if (!x || !w || !dy || !dx || !dw || (bias && !dbias) || dx == x || dx == dy) return QD_ERR_INVALID_ARG;
+    const void* const ptrs[] = {x, w, bias, state, dy, dlast, dx, dw, dbias, dstate, workspace};
+    if (any_misaligned(ptrs) || (flags & ~(unsigned)QD_SILU)) return QD_ERR_INVALID_ARG;
+    if (!workspace || workspace_bytes < conv_bwd_workspace(B, T, D, W, dtype)) return QD_ERR_WORKSPACE;
+    const cudaStream_t s = (cudaStream_t)stream;
+    const cudaError_t e = timed(ST_CONV, s, [&] {
+        return conv_bwd(B, T, D, W, dtype, x, w, bias, state, dy, dlast, dx, dw, dbias, dstate, (float*)workspace, (flags & QD_SILU) != 0, s);
+    });
+    return e == cudaSuccess ? QD_OK : QD_ERR_CUDA;
+}
+
+size_t qdelta_scan_workspace_bytes(const qd_scan_shape* shape, int for_backward) {
+    if (check_scan(shape) != QD_OK) return 0;
+    return for_backward ? scan_bwd_workspace(*shape) : scan_fwd_workspace(*shape, false);
+}
+
+int qdelta_scan_fwd(const qd_scan_shape* shape, const void* u, const void* dt, const float* A, const void* Bm, const void* Cm,
+                    const float* D, const void* z, const float* dt_bias, const float* h0, void* y, float* hT, void* workspace,
+                    size_t workspace_bytes, unsigned flags, qd_stream stream) {
+    const int rc = check_scan(shape);
+    if (rc != QD_OK) return rc;
+    if (!u || !dt || !A || !Bm || !Cm || !y) return QD_ERR_INVALID_ARG;
+    const void* const ptrs[] = {u, dt, A, Bm, Cm, D, z, dt_bias, h0, y, hT, workspace};
+    if (any_misaligned(ptrs) || (flags & ~(unsigned)(QD_SOFTPLUS | QD_FWD_SAVE_FOR_BWD))) return QD_ERR_INVALID_ARG;
+    ScanArgs a{};
+    a.s = *shape;
+    a.save = (flags & QD_FWD_SAVE_FOR_BWD) != 0;
+    a.softplus = (flags & QD_SOFTPLUS) != 0;
+    const size_t need = qdelta_scan_workspace_bytes(shape, a.save ? 1 : 0);
+    if (need && (!workspace || workspace_bytes < need)) return QD_ERR_WORKSPACE;
+    a.u = u; a.dt = dt; a.A = A; a.Bm = Bm; a.Cm = Cm; a.D = D; a.z = z; a.dt_bias = dt_bias; a.h0 = h0; a.y = y; a.hT = hT;
+    a.ws = (char*)workspace;
+    a.stream = (cudaStream_t)stream;
+    return timed(ST_SCAN, a.stream, [&] { return scan_fwd(a); }) == cudaSuccess ? QD_OK : QD_ERR_CUDA;
+}
+
+int qdelta_scan_bwd(const qd_scan_shape* shape, const void* u, const void* dt, const float* A, const void* Bm, const void* Cm,
+                    const float* D, const void* z, const float* dt_bias, const float* h0, const void* dy, const float* dhT, void* du,
+                    void* ddt, float* dA, void* dBm, void* dCm, float* dD, void* dz, float* ddt_bias, float* dh0, void* workspace,
+                    size_t workspace_bytes, unsigned flags, qd_stream stream) {
+    const int rc = check_scan(shape);
+    if (rc != QD_OK) return rc;
+    if (!u || !dt || !A || !Bm || !Cm || !dy || !du || !ddt || !dA || !dBm || !dCm) return QD_ERR_INVALID_ARG;
+    if ((D && !dD) || (z && !dz) || (dt_bias && !ddt_bias)) return QD_ERR_INVALID_ARG;
+    const void* const ptrs[] = {u, dt, A, Bm, Cm, D, z, dt_bias, h0, dy, dhT, du, ddt, dA, dBm, dCm, dD, dz, ddt_bias, dh0, workspace};
+    if (any_misaligned(ptrs) || (flags & ~(unsigned)(QD_SOFTPLUS | QD_BWD_REUSE_FWD))) return QD_ERR_INVALID_ARG;
+    if (!workspace || workspace_bytes < scan_bwd_workspace(*shape)) return QD_ERR_WORKSPACE;
+    ScanArgs a{};
+    a.s = *shape;
+    a.softplus = (flags & QD_SOFTPLUS) != 0;
+    a.u = u; a.dt = dt; a.A = A; a.Bm = Bm; a.Cm = Cm; a.D = D; a.z = z; a.dt_bias = dt_bias; a.h0 = h0;
+    a.ws = (char*)workspace;
+    a.stream = (cudaStream_t)stream;
+    if (!(flags & QD_BWD_REUSE_FWD)) {                     // the states that a saving forward leaves, without its outputs
+        a.save = true;
+        if (timed(ST_SCAN, a.stream, [&] { return scan_fwd(a); }) != cudaSuccess) return QD_ERR_CUDA;
+    }
+    a.dy = dy; a.dhT = dhT; a.du = du; a.ddt = ddt; a.dA = dA; a.dBm = dBm; a.dCm = dCm;
+    a.dD = D ? dD : nullptr; a.dz = dz; a.ddt_bias = dt_bias ? ddt_bias : nullptr; a.dh0 = dh0;
+    return timed(ST_SCAN, a.stream, [&] { return scan_bwd(a); }) == cudaSuccess ? QD_OK : QD_ERR_CUDA;
+}
+
+int qdelta_scan_steps(const qd_scan_shape* shape, const void* u, const void* dt, const float* A, const void* Bm, const void* Cm,
+                      const float* D, const void* z, const float* dt_bias, float* state, void* y, unsigned flags, qd_stream stream) {
+    const int rc = check_scan(shape);
+    if (rc != QD_OK) return rc;
+    if (!u || !dt || !A || !Bm || !Cm || !state || !y) return QD_ERR_INVALID_ARG;
+    const void* const ptrs[] = {u, dt, A, Bm, Cm, D, z, dt_bias, state, y};
+    if (any_misaligned(ptrs) || (flags & ~(unsigned)QD_SOFTPLUS)) return QD_ERR_INVALID_ARG;
+    ScanArgs a{};
+    a.s = *shape;
+    a.softplus = (flags & QD_SOFTPLUS) != 0;
+    a.u = u; a.dt = dt; a.A = A; a.Bm = Bm; a.Cm = Cm; a.D = D; a.z = z; a.dt_bias = dt_bias; a.hT = state; a.y = y;
+    a.stream = (cudaStream_t)stream;
+    return timed(ST_SCAN, a.stream, [&] { return scan_steps(a); }) == cudaSuccess ? QD_OK : QD_ERR_CUDA;
+}
+
+int qdelta_norm_fwd(long long rows, int width, int dtype, const void* x, const void* weight, const void* bias, void* y, float* stats,
+                    float eps, unsigned flags, qd_stream stream) {
+    const int rc = check_norm(rows, width, dtype);
+    if (rc != QD_OK) return rc;
+    if (!x || !y || !(eps >= 0.f) || eps > 3e38f) return QD_ERR_INVALID_ARG;
+    const void* const ptrs[] = {x, weight, bias, y, stats};
+    if (any_misaligned(ptrs) || (flags & ~(unsigned)QD_RMS)) return QD_ERR_INVALID_ARG;
+    const cudaStream_t s = (cudaStream_t)stream;
+    const cudaError_t e = timed(ST_NORM, s, [&] { return norm_fwd(rows, width, dtype, x, weight, bias, y, stats, eps, (flags & QD_RMS) != 0, s); });
+    return e == cudaSuccess ? QD_OK : QD_ERR_CUDA;
+}
+
+size_t qdelta_norm_workspace_bytes(long long rows, int width, int dtype) {
+    return check_norm(rows, width, dtype) == QD_OK ? norm_bwd_workspace(rows, width, dtype) : 0;
+}
+
+int qdelta_norm_bwd(long long rows, int width, int dtype, const void* x, const void* weight, const void* dy, const float* stats, void* dx,
+                    float* dweight, float* dbias, void* workspace, size_t workspace_bytes, unsigned flags, qd_stream stream) {
+    const int rc = check_norm(rows, width, dtype);
+    if (rc != QD_OK) return rc;
+    if (!x || !dy || !stats || !dx) return QD_ERR_INVALID_ARG;
+    const void* const ptrs[] = {x, weight, dy, stats, dx, dweight, dbias, workspace};
+    if (any_misaligned(ptrs) || (flags & ~(unsigned)QD_RMS)) return QD_ERR_INVALID_ARG;
+    if ((dweight || dbias) && (!workspace || workspace_bytes < norm_bwd_workspace(rows, width, dtype))) return QD_ERR_WORKSPACE;
+    const cudaStream_t s = (cudaStream_t)stream;
+    const cudaError_t e = timed(ST_NORM, s, [&] {
+        return norm_bwd(rows, width, dtype, x, weight, dy, stats, dx, dweight, dbias, (float*)workspace, (flags & QD_RMS) != 0, s);
+    });
+    return e == cudaSuccess ? QD_OK : QD_ERR_CUDA;
 }
 
 int qdelta_workspace_status(const void* workspace, int* status_out, qd_stream stream) {

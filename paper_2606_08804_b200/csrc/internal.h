@@ -129,6 +129,41 @@ cudaError_t decode_steps(int B, int S, int H, int dk, int dv, int dtype, const v
                          const void* beta, const void* alpha, const void* lam, void* state, void* o,
                          bool logits, bool norm, bool state_bf16, cudaStream_t stream);
 
+// ---- operators around the delta rule -------------------------------------------------------------------------------------
+// short causal convolution (conv.cu); state == last: decode steps in place
+cudaError_t conv_fwd(int B, int T, int D, int W, int dtype, const void* x, const void* w, const void* bias, const void* state, void* y,
+                     void* last, bool silu, cudaStream_t stream);
+size_t conv_bwd_workspace(int B, int T, int D, int W, int dtype);
+cudaError_t conv_bwd(int B, int T, int D, int W, int dtype, const void* x, const void* w, const void* bias, const void* state,
+                     const void* dy, const void* dlast, void* dx, float* dw, float* dbias, void* dstate, float* part, bool silu,
+                     cudaStream_t stream);
+// layer norm (norm.cu)
+cudaError_t norm_fwd(long long rows, int width, int dtype, const void* x, const void* weight, const void* bias, void* y, float* stats,
+                     float eps, bool rms, cudaStream_t stream);
+size_t norm_bwd_workspace(long long rows, int width, int dtype);
+cudaError_t norm_bwd(long long rows, int width, int dtype, const void* x, const void* weight, const void* dy, const float* stats, void* dx,
+                     float* dweight, float* dbias, float* part, bool rms, cudaStream_t stream);
+// selective scan (scan_fwd.cu, scan_bwd.cu, scan_steps.cu)
+struct ScanArgs {
+    qd_scan_shape s;
+    const void *u, *dt, *Bm, *Cm, *z;
+    const float *A, *D, *dt_bias, *h0;
+    void* y;         // forward: NULL to leave the saved states alone
+    float* hT;       // steps: the state, in place
+    const void* dy;
+    const float* dhT;
+    void *du, *ddt, *dBm, *dCm, *dz;
+    float *dA, *dD, *ddt_bias, *dh0;
+    char* ws;
+    bool softplus, save;
+    cudaStream_t stream;
+};
+size_t scan_fwd_workspace(const qd_scan_shape& s, bool save);
+size_t scan_bwd_workspace(const qd_scan_shape& s);
+cudaError_t scan_fwd(const ScanArgs& a);
+cudaError_t scan_bwd(const ScanArgs& a);
+cudaError_t scan_steps(const ScanArgs& a);
+
 // ---- in-kernel L2 normalisation of q and k (QD_NORM_QK) ------------------------------------------------
 // x^ = x / sqrt(sum x^2 + kNormEps), per token and head.  Its backward: dx = r (dx^ - x^ <x^, dx^>), r = 1/sqrt(sum x^2 + eps).
 constexpr float kNormEps = 1e-6f;

@@ -1,0 +1,144 @@
+// What the kernels around the delta rule (convolution, scan, norm) share: groups of channels in registers, the functions of the
+// gates, and the sum of partial gradients.
+#pragma once
+#include "internal.h"
+#include "sm100.cuh"
+
+namespace qd {
+namespace {
+
+// N consecutive channels of a row.  `vec`: the row's groups are whole and aligned to their size (16 bytes at most); otherwise elements
+// are read one at a time and those from `left` on are 0.  (Ordinary loads, not the read-only path: the kernel before may still be
+// writing when a kernel begins, and a decode step writes the state that it read.)
+template <typename IO, int N> struct Pack { uint32_t w[(N * sizeof(IO) + 3) / 4]; };
+
+template <typename IO, int N>
+__device__ __forceinline__ Pack<IO, N> load_pack(const IO* p, int left, bool vec) {
+    Pack<IO, N> r;
+    constexpr int W = sizeof(r.w) / 4;
+    if (vec && left >= N) {
+        if constexpr (W % 4 == 0) {
+#pragma unroll
+            for (int i = 0; i < W / 4; ++i) {
+                const uint4 t = reinterpret_cast<const uint4*>(p)[i];
+                r.w[4 * i] = t.x; r.w[4 * i + 1] = t.y; r.w[4 * i + 2] = t.z; r.w[4 * i + 3] = t.w;
+            }
+            return r;
+        } else if constexpr (W == 2) {
+            const uint2 t = *reinterpret_cast<const uint2*>(p);
+            r.w[0] = t.x; r.w[1] = t.y;
+            return r;
+        }
+    }
+#pragma unroll
+    for (int i = 0; i < W; ++i) {
+        if constexpr (sizeof(IO) == 4) {
+            r.w[i] = i < left ? __float_as_uint(p[i]) : 0u;
+        } else {
+            const unsigned short* s = reinterpret_cast<const unsigned short*>(p);
+            const uint32_t lo = 2 * i < left ? s[2 * i] : 0, hi = 2 * i + 1 < N && 2 * i + 1 < left ? s[2 * i + 1] : 0;
+            r.w[i] = lo | hi << 16;
+        }
+    }
+    return r;
+}
+template <typename IO, int N>
+__device__ __forceinline__ Pack<IO, N> zero_pack() {
+    Pack<IO, N> r;
+#pragma unroll
+    for (uint32_t& w : r.w) w = 0;
+    return r;
+}
+template <typename IO, int N>
+__device__ __forceinline__ float pick(const Pack<IO, N>& r, int i) {
+    if constexpr (sizeof(IO) == 4) return __uint_as_float(r.w[i]);
+    else return __uint_as_float(i & 1 ? r.w[i >> 1] & 0xffff0000u : r.w[i >> 1] << 16);
+}
+template <typename IO, int N>
+__device__ __forceinline__ void widen(const Pack<IO, N>& r, float (&f)[N]) {
+#pragma unroll
+    for (int i = 0; i < N; ++i) f[i] = pick(r, i);
+}
+template <typename IO, int N>
+__device__ __forceinline__ Pack<IO, N> narrow(const float (&f)[N]) {
+    Pack<IO, N> r;
+    if constexpr (sizeof(IO) == 4) {
+#pragma unroll
+        for (int i = 0; i < N; ++i) r.w[i] = __float_as_uint(f[i]);
+    } else {
+#pragma unroll
+        for (int i = 0; i < (N + 1) / 2; ++i) {
+            const __nv_bfloat162 t = __floats2bfloat162_rn(f[2 * i], 2 * i + 1 < N ? f[2 * i + 1 < N ? 2 * i + 1 : 0] : 0.f);
+            r.w[i] = *reinterpret_cast<const uint32_t*>(&t);
+        }
+    }
+    return r;
+}
+template <typename IO, int N>
+__device__ __forceinline__ void store_pack(IO* p, const Pack<IO, N>& r, int left, bool vec) {
+    constexpr int W = sizeof(r.w) / 4;
+    if (vec && left >= N) {
+        if constexpr (W % 4 == 0) {
+#pragma unroll
+            for (int i = 0; i < W / 4; ++i)
+                reinterpret_cast<uint4*>(p)[i] = make_uint4(r.w[4 * i], r.w[4 * i + 1], r.w[4 * i + 2], r.w[4 * i + 3]);
+            return;
+        } else if constexpr (W == 2) {
+            *reinterpret_cast<uint2*>(p) = make_uint2(r.w[0], r.w[1]);
+            return;
+        }
+    }
+#pragma unroll
+    for (int i = 0; i < N; ++i)
+        if (i < left) {
+            if constexpr (sizeof(IO) == 4) p[i] = __uint_as_float(r.w[i]);
+            else reinterpret_cast<unsigned short*>(p)[i] = (unsigned short)(i & 1 ? r.w[i >> 1] >> 16 : r.w[i >> 1]);
+        }
+}
+
+// The logistic function.  e^{-x} overflows to infinity for x below -88, where the quotient is 0 as it should be.
+__device__ __forceinline__ float sigmoid(float x) { return __fdividef(1.f, 1.f + expf(-x)); }
+
+// 2^x on the special function unit: 2 ulp, and unbiased near x = 0 (mean relative error -5e-9 on (-0.002, -0.001)), which matters where
+// a decay of almost 1 is applied a thousand times.
+__device__ __forceinline__ float exp2_unit(float x) {
+    float y;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+
+// out[col] = sum over p of part[p][col], col < cols, fp32, p in an order that depends on nothing but `parts`.  Column c of the
+// partials is written to out0[c % inner * step0 + c / inner] while c < split, to out1[c - split] behind that.
+__global__ void __launch_bounds__(256) k_sum_parts(const float* part, int parts, long long cols, long long split, long long inner,
+                                                    int step0, float* out0, float* out1) {
+    __shared__ float s[8][33];
+    sm100::grid_dep_wait();
+    sm100::grid_dep_launch();
+    const int x = threadIdx.x & 31, y = threadIdx.x >> 5;
+    const long long c = (long long)blockIdx.x * 32 + x;
+    float a[4] = {0.f, 0.f, 0.f, 0.f};
+    if (c < cols) {
+        int p = y;
+        for (; p + 24 < parts; p += 32)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) a[i] += part[(long long)(p + 8 * i) * cols + c];
+        for (; p < parts; p += 8) a[0] += part[(long long)p * cols + c];
+    }
+    s[y][x] = (a[0] + a[1]) + (a[2] + a[3]);
+    __syncthreads();
+    if (y == 0 && c < cols) {
+        float t = 0.f;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) t += s[i][x];
+        if (c < split) { if (out0) out0[c % inner * step0 + c / inner] = t; }
+        else if (out1) out1[c - split] = t;
+    }
+}
+inline cudaError_t sum_parts(const float* part, int parts, long long cols, long long split, long long inner, int step0, float* out0,
+                             float* out1, cudaStream_t stream) {
+    return launch_overlapped(k_sum_parts, dim3((unsigned)((cols + 31) / 32)), dim3(256), 0, stream, part, parts, cols, split, inner,
+                             step0, out0, out1);
+}
+
+}  // namespace
+}  // namespace qd
