@@ -2,7 +2,7 @@
 
 Argument marshalling only: torch supplies device memory and the current stream; every step of
 the computation runs in the library's CUDA kernels.  The calls that a program makes per step (forward, backward, decode)
-marshal natively (``host/host.cpp``), the others through ctypes.  There is no fallback: if the library has
+marshal natively (``host/*.cpp``), the others through ctypes.  There is no fallback: if the library has
 not been built, or a call returns an error code, an exception is raised.
 """
 import ctypes
@@ -15,17 +15,25 @@ LIB_PATH = os.path.join(_HERE, "libqdelta.so")
 
 QD_F32, QD_BF16 = 0, 1
 QD_FWD_SAVE_FOR_BWD, QD_BWD_REUSE_FWD, QD_COEF_LOGITS, QD_NORM_QK, QD_STATE_BF16 = 1, 2, 4, 8, 16
+QD_SILU, QD_SOFTPLUS, QD_RMS = 32, 64, 128
 
 EXPORTS = ("qdelta_chunk_workspace_bytes", "qdelta_chunk_fwd", "qdelta_chunk_bwd",
            "qdelta_recurrent_step", "qdelta_workspace_status", "qdelta_status_string",
            "qdelta_profile_enable", "qdelta_profile_stage_count", "qdelta_profile_stage_name",
            "qdelta_profile_read", "qdelta_chunk_fwd_static", "qdelta_chunk_path", "qdelta_chunk_parts",
-           "qdelta_recurrent_steps")
+           "qdelta_recurrent_steps", "qdelta_conv_fwd", "qdelta_conv_steps", "qdelta_conv_workspace_bytes", "qdelta_conv_bwd",
+           "qdelta_scan_workspace_bytes", "qdelta_scan_fwd", "qdelta_scan_bwd", "qdelta_scan_steps",
+           "qdelta_norm_fwd", "qdelta_norm_workspace_bytes", "qdelta_norm_bwd")
 
 
 class QdShape(ctypes.Structure):
     _fields_ = [("B", ctypes.c_int), ("T", ctypes.c_int), ("H", ctypes.c_int), ("dk", ctypes.c_int),
                 ("dv", ctypes.c_int), ("chunk", ctypes.c_int), ("dtype", ctypes.c_int)]
+
+
+class QdScanShape(ctypes.Structure):
+    _fields_ = [("B", ctypes.c_int), ("T", ctypes.c_int), ("D", ctypes.c_int), ("N", ctypes.c_int),
+                ("G", ctypes.c_int), ("dtype", ctypes.c_int)]
 
 
 class QdeltaError(RuntimeError):
@@ -77,6 +85,21 @@ def load():
     lib.qdelta_recurrent_step.argtypes = [i] * 5 + [vp] * 8 + [vp]
     lib.qdelta_recurrent_steps.restype = i
     lib.qdelta_recurrent_steps.argtypes = [i] * 6 + [vp] * 8 + [u, vp]
+    ll, f, scan = ctypes.c_longlong, ctypes.c_float, ctypes.POINTER(QdScanShape)
+    lib.qdelta_conv_workspace_bytes.restype = sz
+    lib.qdelta_conv_workspace_bytes.argtypes = [i] * 5
+    lib.qdelta_conv_fwd.argtypes = [i] * 5 + [vp] * 6 + [u, vp]
+    lib.qdelta_conv_steps.argtypes = [i] * 5 + [vp] * 5 + [u, vp]
+    lib.qdelta_conv_bwd.argtypes = [i] * 5 + [vp] * 11 + [sz, u, vp]
+    lib.qdelta_scan_workspace_bytes.restype = sz
+    lib.qdelta_scan_workspace_bytes.argtypes = [scan, i]
+    lib.qdelta_scan_fwd.argtypes = [scan] + [vp] * 12 + [sz, u, vp]
+    lib.qdelta_scan_bwd.argtypes = [scan] + [vp] * 21 + [sz, u, vp]
+    lib.qdelta_scan_steps.argtypes = [scan] + [vp] * 10 + [u, vp]
+    lib.qdelta_norm_workspace_bytes.restype = sz
+    lib.qdelta_norm_workspace_bytes.argtypes = [ll, i, i]
+    lib.qdelta_norm_fwd.argtypes = [ll, i, i] + [vp] * 5 + [f, u, vp]
+    lib.qdelta_norm_bwd.argtypes = [ll, i, i] + [vp] * 8 + [sz, u, vp]
     lib.qdelta_workspace_status.restype = i
     lib.qdelta_workspace_status.argtypes = [vp, ctypes.POINTER(i), vp]
     lib.qdelta_status_string.restype = ctypes.c_char_p
@@ -239,3 +262,62 @@ def recurrent_steps(q, k, v, beta, alpha, lam, state, o=None, logits=False, norm
     reduced-precision state option (QD_STATE_BF16)."""
     flags = (QD_COEF_LOGITS if logits else 0) | (QD_NORM_QK if norm_qk else 0)
     return (_native or _host()).recurrent_steps(q, k, v, beta, alpha, lam, state, o, flags)
+
+
+# ---- operators around the delta rule ------------------------------------------------------------------------------------
+# Tensors are contiguous CUDA tensors of one device, bf16 or fp32 (the type of x or u) unless fp32 is said; a call runs on that
+# device, in its current stream.  Gradients of parameters are fp32.
+
+def conv_fwd(x, w, bias=None, state=None, silu=False, want_state=True):
+    """Short causal convolution per channel.  x [B,T,D], w [D,W] (W = 2, 3, 4), bias [D]; state [B,W-1,D] holds the tokens before
+    the first (None: zeros).  silu=True: SiLU of the sum.  Returns (y [B,T,D], the state for the call that goes on from here)."""
+    return (_native or _host()).conv_fwd(x, w, bias, state, bool(want_state), QD_SILU if silu else 0)
+
+
+def conv_bwd(x, w, bias, state, dy, dstate=None, silu=False, want_dstate=None):
+    """Backward of conv_fwd: `dstate` is the gradient of the state that it returned.  Returns dict(dx, dw, dbias, dstate), the last
+    of the state that it was given (want_dstate: default, if there was one)."""
+    want = state is not None if want_dstate is None else bool(want_dstate)
+    return (_native or _host()).conv_bwd(x, w, bias, state, dy, dstate, want, QD_SILU if silu else 0)
+
+
+def conv_steps(x, w, bias, state, y=None, silu=False):
+    """S tokens of every sequence, x [B,S,D]: single tokens, and draft tokens.  `state` [B,W-1,D] is updated in place.  Returns y."""
+    return (_native or _host()).conv_steps(x, w, bias, state, y, QD_SILU if silu else 0)
+
+
+def scan_fwd(u, dt, A, Bm, Cm, D=None, z=None, dt_bias=None, h0=None, softplus=False, save_for_bwd=False, workspace=None, want_hT=True):
+    """Selective state space scan: h_t = exp(dt_t A) h_{t-1} + dt_t u_t Bm_t, y_t = (<Cm_t, h_t> + D u_t) SiLU(z_t).
+    u, dt, z [B,T,D]; A [D,N] (N up to 64), D, dt_bias [D] and h0 [B,D,N] fp32; Bm, Cm [B,T,G,N] serve D / G channels each.
+    softplus=True: the step is softplus(dt + dt_bias).  Returns (y, hT [B,D,N] fp32, workspace)."""
+    flags = (QD_SOFTPLUS if softplus else 0) | (QD_FWD_SAVE_FOR_BWD if save_for_bwd else 0)
+    return (_native or _host()).scan_fwd(u, dt, A, Bm, Cm, D, z, dt_bias, h0, workspace, bool(want_hT), flags)
+
+
+def scan_bwd(u, dt, A, Bm, Cm, D, z, dt_bias, h0, dy, dhT=None, workspace=None, reuse_fwd=False, softplus=False, want_dh0=None):
+    """Backward of scan_fwd; reuse_fwd=True: `workspace` is that of a saving forward of the same inputs.
+    Returns dict(du, ddt, dA, dBm, dCm, dD, dz, ddt_bias, dh0); None for those of absent inputs."""
+    if workspace is None and reuse_fwd:
+        raise QdeltaError("reuse_fwd needs the workspace of the forward call")
+    flags = (QD_SOFTPLUS if softplus else 0) | (QD_BWD_REUSE_FWD if reuse_fwd else 0)
+    want = h0 is not None if want_dh0 is None else bool(want_dh0)
+    return (_native or _host()).scan_bwd(u, dt, A, Bm, Cm, D, z, dt_bias, h0, dy, dhT, workspace, want, flags)
+
+
+def scan_steps(u, dt, A, Bm, Cm, D, z, dt_bias, state, y=None, softplus=False):
+    """S tokens of every sequence, u, dt, z [B,S,D], Bm, Cm [B,S,G,N]: single tokens, and draft tokens.  `state` [B,D,N] fp32 is
+    updated in place.  Returns y."""
+    return (_native or _host()).scan_steps(u, dt, A, Bm, Cm, D, z, dt_bias, state, y, QD_SOFTPLUS if softplus else 0)
+
+
+def norm_fwd(x, weight=None, bias=None, eps=1e-5, rms=False, want_stats=True):
+    """Layer norm over the last dimension (up to 16384), weight, bias of x's type; rms=True: without the mean.
+    Returns (y, stats [2, rows] fp32: mean and reciprocal deviation of every row)."""
+    return (_native or _host()).norm_fwd(x, weight, bias, eps, bool(want_stats), QD_RMS if rms else 0)
+
+
+def norm_bwd(x, weight, dy, stats, rms=False, want_dweight=None, want_dbias=True):
+    """Backward of norm_fwd with the `stats` that it returned.  Returns dict(dx, dweight, dbias); None for unwanted ones (dweight:
+    wanted if there is a weight)."""
+    want = weight is not None if want_dweight is None else bool(want_dweight)
+    return (_native or _host()).norm_bwd(x, weight, dy, stats, want, bool(want_dbias), QD_RMS if rms else 0)

@@ -1,8 +1,8 @@
 """Build ``libqdelta.so`` (sm_100a only) with nvcc and ``_qdelta_host.so`` with g++, in-tree.
 
 Every ``csrc/*.cu`` is compiled to an object under ``build/`` (in parallel, only when its
-source or a header is newer) and linked into ``paper_2606_08804_b200/libqdelta.so``.  ``host/host.cpp``
-becomes the extension module ``paper_2606_08804_b200/_qdelta_host.so``, which calls into that library.
+source or a header is newer) and linked into ``paper_2606_08804_b200/libqdelta.so``.  ``host/*.cpp``
+become the extension module ``paper_2606_08804_b200/_qdelta_host.so``, which calls into that library.
 """
 import concurrent.futures as cf
 import glob
@@ -15,7 +15,7 @@ _ROOT = os.path.dirname(_HERE)
 CSRC = os.path.join(_HERE, "csrc")
 OBJ_DIR = os.path.join(_ROOT, "build", "obj")
 LIB = os.path.join(_HERE, "libqdelta.so")
-HOST_SRC = os.path.join(_HERE, "host", "host.cpp")
+HOST = os.path.join(_HERE, "host")
 HOST_LIB = os.path.join(_HERE, "_qdelta_host.so")
 
 NVCC_FLAGS = [
@@ -44,9 +44,10 @@ def _compile(src, obj, log):
 
 def _build_host(force):
     """The native side of binding.py, against the headers of the installed torch."""
-    header = os.path.join(_ROOT, "include", "qdelta.h")
+    srcs = sorted(glob.glob(os.path.join(HOST, "*.cpp")))
+    hdrs = glob.glob(os.path.join(HOST, "*.h")) + [os.path.join(_ROOT, "include", "qdelta.h"), os.path.abspath(__file__)]
     if not force and os.path.exists(HOST_LIB) and \
-            os.path.getmtime(HOST_LIB) >= max(os.path.getmtime(f) for f in (HOST_SRC, header, os.path.abspath(__file__))):
+            os.path.getmtime(HOST_LIB) >= max(os.path.getmtime(f) for f in srcs + hdrs):
         return
     import sysconfig
 
@@ -55,13 +56,20 @@ def _build_host(force):
     tmp = HOST_LIB + ".tmp.%d" % os.getpid()
     inc = cpp_extension.include_paths() + [sysconfig.get_paths()["include"], "/usr/local/cuda/include"]
     libdir = os.path.join(os.path.dirname(torch.__file__), "lib")
-    cmd = ["g++", "-O2", "-std=c++17", "-shared", "-fPIC", "-w", HOST_SRC, "-o", tmp,
-           "-D_GLIBCXX_USE_CXX11_ABI=%d" % torch._C._GLIBCXX_USE_CXX11_ABI] + ["-I" + d for d in inc] + \
-          ["-L" + _HERE, "-lqdelta", "-L" + libdir, "-ltorch", "-ltorch_cpu", "-ltorch_cuda", "-lc10", "-lc10_cuda",
-           "-ltorch_python", "-Wl,-rpath,$ORIGIN"]
-    r = subprocess.run(cmd, capture_output=True, text=True)
-    if r.returncode != 0:
-        raise RuntimeError("g++ failed for %s:\n%s" % (HOST_SRC, r.stdout + r.stderr))
+    flags = ["-O2", "-std=c++17", "-fPIC", "-w", "-D_GLIBCXX_USE_CXX11_ABI=%d" % torch._C._GLIBCXX_USE_CXX11_ABI] + ["-I" + d for d in inc]
+
+    def run(cmd, what):
+        r = subprocess.run(cmd, capture_output=True, text=True)
+        if r.returncode != 0:
+            raise RuntimeError("g++ failed for %s:\n%s" % (what, r.stdout + r.stderr))
+
+    objs = [os.path.join(OBJ_DIR, os.path.basename(s)[:-4] + ".host.o") for s in srcs]
+    with cf.ThreadPoolExecutor(max_workers=len(srcs)) as ex:
+        for f in [ex.submit(run, ["g++", "-c", s, "-o", o] + flags, s) for s, o in zip(srcs, objs)]:
+            f.result()
+    run(["g++", "-shared", "-o", tmp] + objs +
+        ["-L" + _HERE, "-lqdelta", "-L" + libdir, "-ltorch", "-ltorch_cpu", "-ltorch_cuda", "-lc10", "-lc10_cuda",
+         "-ltorch_python", "-Wl,-rpath,$ORIGIN"], HOST_LIB)
     os.replace(tmp, HOST_LIB)
 
 

@@ -4,107 +4,13 @@
 // tensors through ctypes (attribute look-ups, shape tuples, pointer objects) took 13 of the 16.5 us of such a step; here it
 // is about 1 us, and what is left is the allocation of the output and the kernel launch.
 // The checks and the messages are those that binding.py documents; every number is computed by libqdelta.so.
-#include <Python.h>
+#include "marshal.h"
 
-#include <ATen/ATen.h>
-#include <ATen/cuda/EmptyTensor.h>
-#include <c10/cuda/CUDAGuard.h>
-#include <c10/cuda/CUDAStream.h>
-#include <torch/csrc/DynamicTypes.h>
-#include <torch/csrc/Exceptions.h>
-#include <torch/csrc/autograd/custom_function.h>
-#include <torch/csrc/Dtype.h>
-#include <torch/csrc/autograd/python_variable.h>
+PyObject* qdhost::g_error = nullptr;
 
-#include "../../include/qdelta.h"
+using namespace qdhost;
 
 namespace {
-
-PyObject* g_error = nullptr;                       // binding.QdeltaError
-
-struct Raised {};                                  // a Python exception is set
-
-[[noreturn]] void fail(const char* fmt, ...) {
-    va_list ap;
-    va_start(ap, fmt);
-    PyErr_FormatV(g_error ? g_error : PyExc_RuntimeError, fmt, ap);
-    va_end(ap);
-    throw Raised{};
-}
-void check(int rc, const char* what) {
-    if (rc != QD_OK) fail("%s failed: %s (%d)", what, qdelta_status_string(rc), rc);
-}
-
-// nullptr for None
-const at::Tensor* tensor(PyObject* o, const char* name) {
-    if (o == Py_None || o == nullptr) return nullptr;
-    if (!THPVariable_Check(o)) { PyErr_Format(PyExc_TypeError, "%s must be a tensor, got %s", name, Py_TYPE(o)->tp_name); throw Raised{}; }
-    return &THPVariable_Unpack(o);
-}
-const at::Tensor& needed(PyObject* o, const char* name) {
-    const at::Tensor* t = tensor(o, name);
-    if (!t) { PyErr_Format(PyExc_TypeError, "%s must be a tensor, got NoneType", name); throw Raised{}; }
-    return *t;
-}
-void want_dims(const at::Tensor& t, int n) {
-    if (t.dim() == n) return;
-    if (t.dim() > n) PyErr_Format(PyExc_ValueError, "too many values to unpack (expected %d)", n);
-    else PyErr_Format(PyExc_ValueError, "not enough values to unpack (expected %d, got %d)", n, (int)t.dim());
-    throw Raised{};
-}
-int dtype_code(const at::Tensor& t) {
-    if (t.scalar_type() == at::kFloat) return QD_F32;
-    if (t.scalar_type() == at::kBFloat16) return QD_BF16;
-    fail("unsupported dtype torch.%s", torch::getTHPDtype(t.scalar_type())->name);
-}
-std::string text(c10::IntArrayRef s) {
-    std::string r = "(";
-    for (size_t i = 0; i < s.size(); ++i) r += (i ? ", " : "") + std::to_string(s[i]);
-    return r + (s.size() == 1 ? ",)" : ")");
-}
-// what a kernel that is given this tensor's address would trip over; empty if nothing
-std::string complaint(const at::Tensor& t, at::ScalarType dt, c10::IntArrayRef shape, const char* name, bool any_dtype = false) {
-    if (!t.is_cuda() || !t.is_contiguous()) return name + std::string(" must be a contiguous CUDA tensor");
-    if (!any_dtype && t.scalar_type() != dt)
-        return name + std::string(" must have dtype torch.") + torch::getTHPDtype(dt)->name + ", got torch." + torch::getTHPDtype(t.scalar_type())->name;
-    if (t.sizes() != shape) return name + std::string(" must have shape ") + text(shape) + ", got " + text(t.sizes());
-    return {};
-}
-// device pointer of a contiguous CUDA tensor of the given type and shape; nullptr for an absent one
-void* ptr(const at::Tensor* t, at::ScalarType dt, c10::IntArrayRef shape, const char* name, bool any_dtype = false) {
-    if (!t) return nullptr;
-    const std::string c = complaint(*t, dt, shape, name, any_dtype);
-    if (!c.empty()) fail("%s", c.c_str());
-    return t->data_ptr();
-}
-at::Tensor empty(c10::IntArrayRef shape, at::ScalarType dt, c10::Device dev) {
-    if (!dev.is_cuda()) fail("the inputs must be contiguous CUDA tensors");
-    return at::Tensor(at::detail::empty_cuda(shape, dt, dev, std::nullopt));
-}
-qd_stream stream() { return reinterpret_cast<qd_stream>(c10::cuda::getCurrentCUDAStream().stream()); }
-
-struct NoGil {                                     // other threads may run while kernels are enqueued
-    PyThreadState* s = PyEval_SaveThread();
-    ~NoGil() { PyEval_RestoreThread(s); }
-};
-
-// What torch throws keeps its Python type: torch.OutOfMemoryError of an allocation, IndexError, TypeError, or the exception that
-// a saved-tensor hook raised (non-reentrant checkpointing ends its recomputation with one).
-template <class F> PyObject* guarded(F f) {
-    try {
-        return f();
-    } catch (const Raised&) {
-    } catch (...) {
-        torch::translate_exception_to_python(std::current_exception());
-    }
-    return nullptr;
-}
-bool arity(Py_ssize_t n, Py_ssize_t want) {
-    if (n == want) return true;
-    PyErr_Format(PyExc_TypeError, "expected %zd arguments, got %zd", want, n);
-    return false;
-}
-PyObject* own(PyObject* o) { Py_INCREF(o); return o; }
 
 // recurrent_step(q, k, v, beta, alpha, lam, state, o)
 PyObject* recurrent_step(PyObject*, PyObject* const* a, Py_ssize_t n) {
@@ -200,11 +106,6 @@ struct Chunk {                                     // the inputs that forward an
         return empty({(int64_t)n}, at::kByte, dev);
     }
 };
-int to_int(PyObject* o) {
-    const long v = PyLong_AsLong(o);
-    if (v == -1 && PyErr_Occurred()) throw Raised{};
-    return (int)v;
-}
 
 // chunk_fwd(q, k, v, beta, alpha, lam, h0, chunk, workspace, o, hT, want_hT, flags) -> (o, hT, workspace)
 PyObject* chunk_fwd(PyObject*, PyObject* const* a, Py_ssize_t n) {
@@ -280,12 +181,7 @@ PyObject* chunk_bwd(PyObject*, PyObject* const* a, Py_ssize_t n) {
 
 // ---- autograd: the pair forward / backward as one node, without Python on the way ------------------------------------
 // (a Python-level Function spent 120 us per pair in the interpreter, more than the kernels of a short sequence take)
-using torch::autograd::AutogradContext;
-using torch::autograd::variable_list;
 constexpr int kChunk = 64;
-
-using MaybeTensor = std::optional<at::Tensor>;
-const at::Tensor* maybe(const MaybeTensor& t) { return t ? &*t : nullptr; }
 
 struct ChunkNode : torch::autograd::Function<ChunkNode> {
     static variable_list forward(AutogradContext* ctx, const at::Tensor& q, const at::Tensor& k, const at::Tensor& v,
@@ -304,14 +200,6 @@ struct ChunkNode : torch::autograd::Function<ChunkNode> {
             ctx->saved_data["flags"] = flags;
         }
         return {o, hT};
-    }
-    // a QdeltaError from a thread of the autograd engine, which does not hold the interpreter
-    [[noreturn]] static void raise(const std::string& what) {
-        pybind11::gil_scoped_acquire gil;
-        PyErr_SetString(g_error, what.c_str());
-        python_error e;
-        e.persist();
-        throw std::move(e);
     }
     static variable_list backward(AutogradContext* ctx, variable_list g) {
         const variable_list in = ctx->get_saved_variables();
@@ -398,4 +286,8 @@ PyModuleDef module_def = {PyModuleDef_HEAD_INIT, "_qdelta_host", nullptr, -1, me
 
 }  // namespace
 
-PyMODINIT_FUNC PyInit__qdelta_host(void) { return PyModule_Create(&module_def); }
+PyMODINIT_FUNC PyInit__qdelta_host(void) {
+    PyObject* m = PyModule_Create(&module_def);
+    if (m && PyModule_AddFunctions(m, qdhost::layer_methods)) { Py_DECREF(m); return nullptr; }
+    return m;
+}
