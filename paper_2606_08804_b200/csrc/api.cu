@@ -323,7 +323,7 @@ int qdelta_conv_steps(int B, int S, int D, int W, int dtype, const void* x, cons
 }
 
 size_t qdelta_conv_workspace_bytes(int B, int T, int D, int W, int dtype) {
-    return check_conv(B, T, D, W, dtype) == QD_OK ? conv_bwd_workspace(B, T, D, W, dtype) : 0;
+    return check_conv(B, T, D, W, dtype) == QD_OK ? conv_bwd_workspace(B, T, D, W) : 0;
 }
 
 int qdelta_conv_bwd(int B, int T, int D, int W, int dtype, const void* x, const void* w, const void* bias, const void* state,
@@ -334,7 +334,7 @@ int qdelta_conv_bwd(int B, int T, int D, int W, int dtype, const void* x, const 
     if (!x || !w || !dy || !dx || !dw || (bias && !dbias) || dx == x || dx == dy) return QD_ERR_INVALID_ARG;
     const void* const ptrs[] = {x, w, bias, state, dy, dlast, dx, dw, dbias, dstate, workspace};
     if (any_misaligned(ptrs) || (flags & ~(unsigned)QD_SILU)) return QD_ERR_INVALID_ARG;
-    if (!workspace || workspace_bytes < conv_bwd_workspace(B, T, D, W, dtype)) return QD_ERR_WORKSPACE;
+    if (!workspace || workspace_bytes < conv_bwd_workspace(B, T, D, W)) return QD_ERR_WORKSPACE;
     const cudaStream_t s = (cudaStream_t)stream;
     const cudaError_t e = timed(ST_CONV, s, [&] {
         return conv_bwd(B, T, D, W, dtype, x, w, bias, state, dy, dlast, dx, dw, dbias, dstate, (float*)workspace, (flags & QD_SILU) != 0, s);

@@ -5,184 +5,293 @@
 //   dx_s = sum_j w_j dpre_{s+W-1-j} (tokens and state rows alike, plus the gradient of the state afterwards),
 //   dw_j = sum_t dpre_t x_{t-W+1+j},   db = sum_t dpre_t.
 //
-// Bound by HBM: 4 + 2 W operations and one exponential per element read and written.  A thread owns a group of neighbouring channels
-// (16 bytes) and walks a run of tokens with the last W - 1 inputs (and, backward, the last W dpre) in registers, so an input is
-// read once but for the W - 1 tokens in front of a run (W - 1 on either side backward).  A warp reads 32 neighbouring groups of a token.
+// Bound by HBM.  A thread owns a group of neighbouring channels and walks a run of tokens with the last W - 1 inputs (and, backward, the
+// last W - 1 dpre) in registers, so an input is read once but for the W - 1 tokens in front of a run (W - 1 on either side backward); a
+// warp reads 32 neighbouring groups of a token.  So that the arithmetic stays below HBM's time, channels are taken two at a time in the
+// packed fp32 instructions of sm_100, an input is widened once, and bf16 gates use the special function unit directly.
+// Where rows are not whole groups, the channels of a thread are `cx` apart instead, so that a warp's single loads are neighbours.
 #include "rows.cuh"
 
 namespace qd {
 namespace {
 
+constexpr int kConvThreads = 128;
+
 struct ConvP {
-    int B, T, D, groups, cx, gx, run, runs;  // groups of channels; neighbouring groups per CTA, CTAs to cover them; tokens per run, runs per sequence
+    int B, T, D, cx, gx, run, runs;          // groups per row of a CTA's threads, CTAs across the channels; tokens per run, runs per sequence
     const void *x, *w, *bias, *state, *dy, *dlast;
     void *y, *last, *dx, *dstate;
     float* part;                             // backward: [gy][W + 1][D]
     bool silu, vec;
 };
 
-template <typename IO, int V, int W>
-__device__ __forceinline__ void load_taps(const ConvP& p, int c0, int left, float (&w)[W][V], float (&b)[V]) {
-    const IO* wp = static_cast<const IO*>(p.w) + (size_t)c0 * W;
-    const Pack<IO, V * W> t = load_pack<IO, V * W>(wp, left * W, p.vec);
+// The channels of a thread: c0, c0 + step, .. (V of them, those below D).
+template <int V> struct Cols {
+    int c0, step, left;
+    __device__ __forceinline__ Cols(const ConvP& p, int bx, int x) {
+        step = p.vec ? 1 : p.cx;
+        c0 = bx * p.cx * V + (p.vec ? x * V : x);
+        left = p.vec ? (c0 < p.D ? V : 0) : (p.D - c0 + step - 1) / step;
+    }
+};
+template <typename IO, int V>
+__device__ __forceinline__ Pack<IO, V> load_cols(const IO* p, const Cols<V>& c) {
+    if (c.step == 1) return load_pack<IO, V>(p, c.left, true);
+    Pack<IO, V> r = zero_pack<IO, V>();
 #pragma unroll
     for (int i = 0; i < V; ++i)
+        if (i < c.left) {
+            if constexpr (sizeof(IO) == 4) r.w[i] = __float_as_uint(p[(size_t)i * c.step]);
+            else r.w[i >> 1] |= (uint32_t)reinterpret_cast<const unsigned short*>(p)[(size_t)i * c.step] << (i & 1) * 16;
+        }
+    return r;
+}
+template <typename IO, int V>
+__device__ __forceinline__ void store_cols(IO* p, const Pack<IO, V>& r, const Cols<V>& c) {
+    if (c.step == 1) return store_pack(p, r, c.left, true);
 #pragma unroll
-        for (int j = 0; j < W; ++j) w[j][i] = pick(t, i * W + j);
-    if (p.bias) widen(load_pack<IO, V>(static_cast<const IO*>(p.bias) + c0, left, p.vec), b);
-    else
+    for (int i = 0; i < V; ++i)
+        if (i < c.left) {
+            if constexpr (sizeof(IO) == 4) p[(size_t)i * c.step] = __uint_as_float(r.w[i]);
+            else reinterpret_cast<unsigned short*>(p)[(size_t)i * c.step] = (unsigned short)(i & 1 ? r.w[i >> 1] >> 16 : r.w[i >> 1]);
+        }
+}
+template <typename IO, int V>
+__device__ __forceinline__ void widen2(const Pack<IO, V>& r, f2 (&f)[V / 2]) {
 #pragma unroll
-        for (float& f : b) f = 0.f;
+    for (int i = 0; i < V / 2; ++i) f[i] = pack2(pick(r, 2 * i), pick(r, 2 * i + 1));
+}
+template <typename IO, int V>
+__device__ __forceinline__ Pack<IO, V> narrow2(const f2 (&f)[V / 2]) {
+    float o[V];
+#pragma unroll
+    for (int i = 0; i < V / 2; ++i) {
+        const float2 t = unpack2(f[i]);
+        o[2 * i] = t.x;
+        o[2 * i + 1] = t.y;
+    }
+    return narrow<IO, V>(o);
 }
 
-// Row of token t of sequence b, or of the state for t < 0; zeros where there is none.
 template <typename IO, int V, int W>
-__device__ __forceinline__ Pack<IO, V> load_row(const ConvP& p, const IO* x, const IO* state, int t, int left) {
-    if (t >= 0) return load_pack<IO, V>(x + (size_t)t * p.D, left, p.vec);
-    if (state) return load_pack<IO, V>(state + (size_t)(t + W - 1) * p.D, left, p.vec);
-    return zero_pack<IO, V>();
+__device__ __forceinline__ void load_taps(const ConvP& p, const Cols<V>& c, f2 (&w)[W][V / 2], f2 (&b)[V / 2]) {
+    const IO* wp = static_cast<const IO*>(p.w) + (size_t)c.c0 * W;
+    float f[V][W];
+    if (c.step == 1) {
+        const Pack<IO, V * W> t = load_pack<IO, V * W>(wp, c.left * W, true);
+#pragma unroll
+        for (int i = 0; i < V; ++i)
+#pragma unroll
+            for (int j = 0; j < W; ++j) f[i][j] = pick(t, i * W + j);
+    } else {
+#pragma unroll
+        for (int i = 0; i < V; ++i)
+#pragma unroll
+            for (int j = 0; j < W; ++j) f[i][j] = i < c.left ? ld(wp, (size_t)i * c.step * W + j) : 0.f;
+    }
+#pragma unroll
+    for (int i = 0; i < V / 2; ++i) {
+        b[i] = 0;
+#pragma unroll
+        for (int j = 0; j < W; ++j) w[j][i] = pack2(f[2 * i][j], f[2 * i + 1][j]);
+    }
+    if (p.bias) widen2(load_cols(static_cast<const IO*>(p.bias) + c.c0, c), b);
 }
 
-// Forward and decode steps (one run for each sequence: the state may then be the one that is written).
+// sigmoid of two numbers.  bf16 results are rounded to 2^-9, so that e^-x may have a relative error of 2^-24 |x|.
+template <typename IO>
+__device__ __forceinline__ f2 sigmoid2(f2 v) {
+    const float2 t = unpack2(v);
+    if constexpr (sizeof(IO) == 2) return pack2(gate_sigmoid(t.x), gate_sigmoid(t.y));
+    else return pack2(sigmoid(t.x), sigmoid(t.y));
+}
+// The last rows in a ring of four: a token's row goes where its number mod 4 says, which unrolled by four is a register, and nothing moves.
+constexpr int kRing = 4;
+template <int V, int W>
+__device__ __forceinline__ void convolve(const f2 (&w)[W][V / 2], const f2 (&b)[V / 2], const f2 (&win)[kRing][V / 2], int u, f2 (&pre)[V / 2]) {
+#pragma unroll
+    for (int i = 0; i < V / 2; ++i) {
+        f2 s = b[i];
+#pragma unroll
+        for (int j = 0; j < W; ++j) s = fma2(w[j][i], win[(u + kRing - (W - 1) + j) % kRing][i], s);
+        pre[i] = s;
+    }
+}
+template <typename IO, int V>
+__device__ __forceinline__ Pack<IO, V> finish(const f2 (&pre)[V / 2], bool silu) {
+    f2 o[V / 2];
+#pragma unroll
+    for (int i = 0; i < V / 2; ++i) o[i] = silu ? mul2(pre[i], sigmoid2<IO>(pre[i])) : pre[i];
+    return narrow2<IO, V>(o);
+}
+// The W - 1 rows before token t0 of a sequence, from its tokens or its state; t0 is number 0 of the ring.
 template <typename IO, int V, int W>
-__global__ void __launch_bounds__(256) k_conv_fwd(const ConvP p) {
-    constexpr int U = 4;                                   // tokens on their way at a time
+__device__ __forceinline__ void load_window(const ConvP& p, const Cols<V>& c, const IO* x, const IO* state, int t0, f2 (&win)[kRing][V / 2]) {
+#pragma unroll
+    for (int j = 1; j < W; ++j) {
+        const int t = t0 - j;
+        widen2(t >= 0 ? load_cols(x + (size_t)t * p.D, c) : state ? load_cols(state + (size_t)(t + W - 1) * p.D, c) : zero_pack<IO, V>(), win[kRing - j]);
+    }
+}
+// The W - 1 rows up to the one whose number is u.
+template <typename IO, int V, int W>
+__device__ __forceinline__ void store_window(const ConvP& p, const Cols<V>& c, int b, const f2 (&win)[kRing][V / 2], int u) {
+    IO* last = static_cast<IO*>(p.last) + (size_t)b * (W - 1) * p.D + c.c0;
+#pragma unroll
+    for (int j = 0; j < W - 1; ++j) store_cols(last + (size_t)j * p.D, narrow2<IO, V>(win[(u + kRing - (W - 2) + j) % kRing]), c);
+}
+
+template <typename IO, int V, int W>
+__global__ void __launch_bounds__(kConvThreads, 4) k_conv_fwd(const ConvP p) {
     sm100::grid_dep_wait();
     sm100::grid_dep_launch();
-    const int bx = blockIdx.x % p.gx, by = blockIdx.x / p.gx;
-    const int g = bx * p.cx + threadIdx.x % p.cx;
-    const long long item = (long long)by * (256 / p.cx) + threadIdx.x / p.cx;
-    if (g >= p.groups || item >= (long long)p.B * p.runs) return;
+    const int bx = blockIdx.x % p.gx;
+    const long long item = (long long)(blockIdx.x / p.gx) * (kConvThreads / p.cx) + threadIdx.x / p.cx;
+    const Cols<V> c(p, bx, threadIdx.x % p.cx);
+    if (c.left <= 0 || item >= (long long)p.B * p.runs) return;
     const int b = (int)(item / p.runs), t0 = (int)(item % p.runs) * p.run, t1 = min(p.T, t0 + p.run);
-    const int c0 = g * V, left = p.D - c0;
-    const IO* x = static_cast<const IO*>(p.x) + (size_t)b * p.T * p.D + c0;
-    const IO* state = p.state ? static_cast<const IO*>(p.state) + (size_t)b * (W - 1) * p.D + c0 : nullptr;
-    IO* y = static_cast<IO*>(p.y) + (size_t)b * p.T * p.D + c0;
-    float w[W][V], bias[V];
-    Pack<IO, V> win[W];                                    // the last W - 1 rows and the present one
+    const IO* x = static_cast<const IO*>(p.x) + (size_t)b * p.T * p.D + c.c0;
+    const IO* state = p.state ? static_cast<const IO*>(p.state) + (size_t)b * (W - 1) * p.D + c.c0 : nullptr;
+    IO* y = static_cast<IO*>(p.y) + (size_t)b * p.T * p.D + c.c0;
+    Pack<IO, V> next[kRing];                               // tokens on their way
 #pragma unroll
-    for (int j = 0; j < W - 1; ++j) win[j] = load_row<IO, V, W>(p, x, state, t0 - (W - 1) + j, left);
-    Pack<IO, V> next[U];
+    for (int u = 0; u < kRing; ++u) next[u] = t0 + u < t1 ? load_cols(x + (size_t)(t0 + u) * p.D, c) : zero_pack<IO, V>();
+    f2 w[W][V / 2], bias[V / 2], win[kRing][V / 2];
+    load_window<IO, V, W>(p, c, x, state, t0, win);
+    load_taps<IO, V, W>(p, c, w, bias);
+    for (int t = t0; t < t1; t += kRing) {
 #pragma unroll
-    for (int i = 0; i < U; ++i) next[i] = t0 + i < t1 ? load_pack<IO, V>(x + (size_t)(t0 + i) * p.D, left, p.vec) : zero_pack<IO, V>();
-    load_taps<IO, V, W>(p, c0, left, w, bias);
-    for (int t = t0; t < t1; t += U) {
-        Pack<IO, V> cur[U];
-#pragma unroll
-        for (int i = 0; i < U; ++i) cur[i] = next[i];
-#pragma unroll
-        for (int i = 0; i < U; ++i)
-            if (t + U + i < t1) next[i] = load_pack<IO, V>(x + (size_t)(t + U + i) * p.D, left, p.vec);
-#pragma unroll
-        for (int i = 0; i < U; ++i) {
-            if (t + i >= t1) break;
-            win[W - 1] = cur[i];
-            float o[V];
-#pragma unroll
-            for (int c = 0; c < V; ++c) {
-                float s = bias[c];
-#pragma unroll
-                for (int j = 0; j < W; ++j) s = fmaf(w[j][c], pick(win[j], c), s);
-                o[c] = p.silu ? s * sigmoid(s) : s;
-            }
-            store_pack(y + (size_t)(t + i) * p.D, narrow<IO, V>(o), left, p.vec);
-#pragma unroll
-            for (int j = 0; j < W - 1; ++j) win[j] = win[j + 1];
+        for (int u = 0; u < kRing; ++u) {
+            if (t + u >= t1) break;
+            f2 pre[V / 2];
+            widen2(next[u], win[u]);
+            if (t + u + kRing < t1) next[u] = load_cols(x + (size_t)(t + u + kRing) * p.D, c);
+            convolve<V, W>(w, bias, win, u, pre);
+            store_cols(y + (size_t)(t + u) * p.D, finish<IO, V>(pre, p.silu), c);
+            // what this thread holds at the end are the last W - 1 rows
+            if (t + u + 1 == p.T && p.last) store_window<IO, V, W>(p, c, b, win, u);
         }
     }
-    if (p.last && t1 == p.T) {                             // what this thread holds are the last W - 1 rows
-        IO* last = static_cast<IO*>(p.last) + (size_t)b * (W - 1) * p.D + c0;
+}
+
+// Decode steps: every sequence in one run, the state written where it was read.
+template <typename IO, int V, int W>
+__global__ void __launch_bounds__(kConvThreads) k_conv_steps(const ConvP p) {
+    sm100::grid_dep_wait();
+    sm100::grid_dep_launch();
+    const int bx = blockIdx.x % p.gx;
+    const long long b = (long long)(blockIdx.x / p.gx) * (kConvThreads / p.cx) + threadIdx.x / p.cx;
+    const Cols<V> c(p, bx, threadIdx.x % p.cx);
+    if (c.left <= 0 || b >= p.B) return;
+    const IO* x = static_cast<const IO*>(p.x) + (size_t)b * p.T * p.D + c.c0;
+    const IO* state = static_cast<const IO*>(p.state) + (size_t)b * (W - 1) * p.D + c.c0;
+    IO* y = static_cast<IO*>(p.y) + (size_t)b * p.T * p.D + c.c0;
+    Pack<IO, V> next = load_cols(x, c);
+    f2 w[W][V / 2], bias[V / 2], win[kRing][V / 2];
+    load_window<IO, V, W>(p, c, x, state, 0, win);
+    load_taps<IO, V, W>(p, c, w, bias);
+    for (int t = 0; t < p.T; t += kRing) {
 #pragma unroll
-        for (int j = 0; j < W - 1; ++j) store_pack(last + (size_t)j * p.D, win[j], left, p.vec);
+        for (int u = 0; u < kRing; ++u) {
+            if (t + u >= p.T) break;
+            f2 pre[V / 2];
+            widen2(next, win[u]);
+            if (t + u + 1 < p.T) next = load_cols(x + (size_t)(t + u + 1) * p.D, c);
+            convolve<V, W>(w, bias, win, u, pre);
+            store_cols(y + (size_t)(t + u) * p.D, finish<IO, V>(pre, p.silu), c);
+            if (t + u + 1 == p.T) store_window<IO, V, W>(p, c, (int)b, win, u);
+        }
     }
 }
 
 // Backward of a run [t0, t1): dpre of its tokens and of the W - 1 behind them.  Token s emits dx of token s - W + 1.
 template <typename IO, int V, int W>
-__global__ void __launch_bounds__(256) k_conv_bwd(const ConvP p) {
-    __shared__ float red[256][V + 1];
+__global__ void __launch_bounds__(kConvThreads, 4) k_conv_bwd(const ConvP p) {
+    __shared__ float red[kConvThreads][V + 1];
     sm100::grid_dep_wait();
     sm100::grid_dep_launch();
-    const int bx = blockIdx.x % p.gx, by = blockIdx.x / p.gx;
-    const int g = bx * p.cx + threadIdx.x % p.cx;
-    const long long item = (long long)by * (256 / p.cx) + threadIdx.x / p.cx;
-    const bool live = g < p.groups && item < (long long)p.B * p.runs;
-    const int c0 = g * V, left = p.D - c0;
-    float dw[W][V], db[V];
+    const int bx = blockIdx.x % p.gx;
+    const long long by = blockIdx.x / p.gx, item = by * (kConvThreads / p.cx) + threadIdx.x / p.cx;
+    const Cols<V> c(p, bx, threadIdx.x % p.cx);
+    f2 dw[W][V / 2], db[V / 2];
 #pragma unroll
-    for (int c = 0; c < V; ++c) {
-        db[c] = 0.f;
+    for (int i = 0; i < V / 2; ++i) {
+        db[i] = 0;
 #pragma unroll
-        for (int j = 0; j < W; ++j) dw[j][c] = 0.f;
+        for (int j = 0; j < W; ++j) dw[j][i] = 0;
     }
-    if (live) {
+    if (c.left > 0 && item < (long long)p.B * p.runs) {
         const int b = (int)(item / p.runs), t0 = (int)(item % p.runs) * p.run, t1 = min(p.T, t0 + p.run);
-        const size_t base = (size_t)b * p.T * p.D + c0, sbase = (size_t)b * (W - 1) * p.D + c0;
+        const size_t base = (size_t)b * p.T * p.D + c.c0, sbase = (size_t)b * (W - 1) * p.D + c.c0;
         const IO *x = static_cast<const IO*>(p.x) + base, *dy = static_cast<const IO*>(p.dy) + base;
         const IO* state = p.state ? static_cast<const IO*>(p.state) + sbase : nullptr;
         const IO* dlast = p.dlast ? static_cast<const IO*>(p.dlast) + sbase : nullptr;
         IO* dx = static_cast<IO*>(p.dx) + base;
         IO* dstate = p.dstate ? static_cast<IO*>(p.dstate) + sbase : nullptr;
-        float w[W][V], bias[V], dp[W][V];
-        Pack<IO, V> win[W];
-#pragma unroll
-        for (int j = 0; j < W - 1; ++j) win[j] = load_row<IO, V, W>(p, x, state, t0 - (W - 1) + j, left);
-#pragma unroll
-        for (int j = 0; j < W; ++j)
-#pragma unroll
-            for (int c = 0; c < V; ++c) dp[j][c] = 0.f;
-        load_taps<IO, V, W>(p, c0, left, w, bias);
-        auto xrow = [&](int t) { return t < p.T ? load_pack<IO, V>(x + (size_t)t * p.D, left, p.vec) : zero_pack<IO, V>(); };
-        auto yrow = [&](int t) { return t < p.T ? load_pack<IO, V>(dy + (size_t)t * p.D, left, p.vec) : zero_pack<IO, V>(); };
         const int end = t1 + W - 1;
-        Pack<IO, V> nx = xrow(t0), ny = yrow(t0);
-#pragma unroll 2
-        for (int s = t0; s < end; ++s) {
-            win[W - 1] = nx;
-            float gy[V];
-            widen(ny, gy);
-            if (s + 1 < end) { nx = xrow(s + 1); ny = yrow(s + 1); }
-            const bool own = s < t1;
+        Pack<IO, V> nx[kRing], ny[kRing];
+        auto fetch = [&](int i, int s) {
+            const bool in = s < end && s < p.T;
+            nx[i] = in ? load_cols(x + (size_t)s * p.D, c) : zero_pack<IO, V>();
+            ny[i] = in ? load_cols(dy + (size_t)s * p.D, c) : zero_pack<IO, V>();
+        };
 #pragma unroll
-            for (int c = 0; c < V; ++c) {
-                float d = gy[c];
-                if (p.silu) {
-                    float a = bias[c];
+        for (int u = 0; u < kRing; ++u) fetch(u, t0 + u);
+        f2 w[W][V / 2], bias[V / 2], win[kRing][V / 2], dp[kRing][V / 2];
+        load_window<IO, V, W>(p, c, x, state, t0, win);
+        load_taps<IO, V, W>(p, c, w, bias);
 #pragma unroll
-                    for (int j = 0; j < W; ++j) a = fmaf(w[j][c], pick(win[j], c), a);
-                    const float sg = sigmoid(a);
-                    d *= sg * fmaf(a, 1.f - sg, 1.f);
+        for (int j = 0; j < kRing; ++j)
+#pragma unroll
+            for (int i = 0; i < V / 2; ++i) dp[j][i] = 0;
+        for (int s0 = t0; s0 < end; s0 += kRing) {
+#pragma unroll
+            for (int u = 0; u < kRing; ++u) {
+                const int s = s0 + u;
+                if (s >= end) break;
+                f2 (&d)[V / 2] = dp[u];
+                widen2(nx[u], win[u]);
+                widen2(ny[u], d);
+                fetch(u, s + kRing);
+                if (s >= p.T) {                            // behind the last token: nothing, whatever the window holds
+#pragma unroll
+                    for (f2& v : d) v = 0;
+                } else if (p.silu) {
+                    f2 pre[V / 2];
+                    convolve<V, W>(w, bias, win, u, pre);
+#pragma unroll
+                    for (int i = 0; i < V / 2; ++i) {
+                        const f2 sg = sigmoid2<IO>(pre[i]), rest = fma2(sg, both(-1.f), both(1.f));
+                        d[i] = mul2(d[i], mul2(sg, fma2(pre[i], rest, both(1.f))));
+                    }
                 }
-                if (s >= p.T) d = 0.f;                     // behind the last token: nothing, whatever the window holds
+                if (s < t1) {
 #pragma unroll
-                for (int j = 0; j < W - 1; ++j) dp[j][c] = dp[j + 1][c];
-                dp[W - 1][c] = d;
-                if (own) {
-                    db[c] += d;
+                    for (int i = 0; i < V / 2; ++i) {
+                        db[i] = add2(db[i], d[i]);
 #pragma unroll
-                    for (int j = 0; j < W; ++j) dw[j][c] = fmaf(d, pick(win[j], c), dw[j][c]);
+                        for (int j = 0; j < W; ++j) dw[j][i] = fma2(d[i], win[(u + kRing - (W - 1) + j) % kRing][i], dw[j][i]);
+                    }
+                }
+                const int t = s - (W - 1);                 // its gradient is complete
+                if (t >= t0 || (t < 0 && dstate)) {        // t < 0 in a sequence's first run only
+                    f2 o[V / 2];
+#pragma unroll
+                    for (int i = 0; i < V / 2; ++i) {
+                        f2 v = mul2(w[0][i], d[i]);
+#pragma unroll
+                        for (int j = 1; j < W; ++j) v = fma2(w[j][i], dp[(u + kRing - j) % kRing][i], v);
+                        o[i] = v;
+                    }
+                    if (dlast && t >= p.T - (W - 1)) {
+                        f2 e[V / 2];
+                        widen2(load_cols(dlast + (size_t)(t - (p.T - (W - 1))) * p.D, c), e);
+#pragma unroll
+                        for (int i = 0; i < V / 2; ++i) o[i] = add2(o[i], e[i]);
+                    }
+                    store_cols(t >= 0 ? dx + (size_t)t * p.D : dstate + (size_t)(t + W - 1) * p.D, narrow2<IO, V>(o), c);
                 }
             }
-            const int t = s - (W - 1);                     // its gradient is complete
-            if (t >= t0 || (t < 0 && dstate)) {            // t < 0 in a sequence's first run only
-                float o[V];
-#pragma unroll
-                for (int c = 0; c < V; ++c) {
-                    o[c] = 0.f;
-#pragma unroll
-                    for (int j = 0; j < W; ++j) o[c] = fmaf(w[W - 1 - j][c], dp[j][c], o[c]);
-                }
-                if (dlast && t >= p.T - (W - 1)) {
-                    float e[V];
-                    widen(load_pack<IO, V>(dlast + (size_t)(t - (p.T - (W - 1))) * p.D, left, p.vec), e);
-#pragma unroll
-                    for (int c = 0; c < V; ++c) o[c] += e[c];
-                }
-                IO* to = t >= 0 ? dx + (size_t)t * p.D : dstate + (size_t)(t + W - 1) * p.D;
-                store_pack(to, narrow<IO, V>(o), left, p.vec);
-            }
-#pragma unroll
-            for (int j = 0; j < W - 1; ++j) win[j] = win[j + 1];
         }
     }
     // one partial of dw and db for the CTA: the threads of a group of channels in order
@@ -190,81 +299,84 @@ __global__ void __launch_bounds__(256) k_conv_bwd(const ConvP p) {
     for (int j = 0; j <= W; ++j) {
         __syncthreads();
 #pragma unroll
-        for (int c = 0; c < V; ++c) red[threadIdx.x][c] = j < W ? dw[j < W ? j : 0][c] : db[c];
+        for (int i = 0; i < V / 2; ++i) {
+            const float2 t = unpack2(j < W ? dw[j < W ? j : 0][i] : db[i]);
+            red[threadIdx.x][2 * i] = t.x;
+            red[threadIdx.x][2 * i + 1] = t.y;
+        }
         __syncthreads();
-        for (int i = threadIdx.x; i < p.cx * V; i += 256) {
-            const int x = i / V, c = i % V, ch = (bx * p.cx + x) * V + c;
+        for (int e = threadIdx.x; e < p.cx * V; e += kConvThreads) {
+            const int gr = p.vec ? e / V : e % p.cx, i = p.vec ? e % V : e / p.cx, ch = bx * p.cx * V + e;      // channels in order
             if (ch >= p.D) continue;
             float t = 0.f;
-            for (int r = x; r < 256; r += p.cx) t += red[r][c];
+            for (int r = gr; r < kConvThreads; r += p.cx) t += red[r][i];
             p.part[((size_t)by * (W + 1) + j) * p.D + ch] = t;
         }
     }
 }
 
-struct ConvPlan { int V, groups, cx, run, runs, gx; long long gy; };
-// Runs as long as leaves `threads` of them: a run reads W - 1 tokens again.  Neighbouring groups per CTA: a warp's worth, fewer where
-// there are fewer channels.
-ConvPlan conv_plan(int B, int T, int D, int V, long long threads, int shortest, bool whole) {
+struct ConvPlan { int cx, gx, run, runs; long long gy; };
+// Runs of `longest` tokens where that leaves `threads` of them, shorter ones down to `shortest` where it does not: a run reads W - 1
+// tokens again.  Neighbouring groups in a row of threads: a warp's worth, fewer where there are fewer channels.
+ConvPlan conv_plan(int B, int T, int D, int V, long long threads, int shortest, int longest) {
     ConvPlan q{};
-    q.V = V;
-    q.groups = (D + V - 1) / V;
+    const int groups = (D + V - 1) / V;
     q.cx = 32;
-    while (q.cx > 1 && q.cx / 2 >= q.groups) q.cx /= 2;
-    const long long rows = (threads + q.groups - 1) / q.groups;             // runs wanted
-    const long long per = (rows + B - 1) / B;
-    long long run = whole ? T : ((long long)T + per - 1) / per;
+    while (q.cx > 1 && q.cx / 2 >= groups) q.cx /= 2;
+    const long long per = ((threads + groups - 1) / groups + B - 1) / B;    // runs wanted of a sequence
+    long long run = ((long long)T + per - 1) / per;
+    if (run > longest) run = longest;
     if (run < shortest) run = shortest;
     if (run > T) run = T;
     q.run = (int)run;
     q.runs = (int)(((long long)T + run - 1) / run);
-    q.gx = (q.groups + q.cx - 1) / q.cx;
-    const long long per_cta = 256 / q.cx;
+    q.gx = (groups + q.cx - 1) / q.cx;
+    const long long per_cta = kConvThreads / q.cx;
     q.gy = ((long long)B * q.runs + per_cta - 1) / per_cta;
     return q;
 }
-int vector_of(int dtype) { return dtype == QD_BF16 ? 8 : 4; }               // 16 bytes
-ConvPlan conv_fwd_plan(int B, int T, int D, int dtype, bool whole) {
-    return conv_plan(B, T, D, vector_of(dtype), (long long)kSMs * 2048, 4, whole);
-}
-ConvPlan conv_bwd_plan(int B, int T, int D, int dtype) { return conv_plan(B, T, D, vector_of(dtype), (long long)kSMs * 1024, 16, false); }
+int fwd_group(int dtype) { return dtype == QD_BF16 ? 8 : 4; }
+constexpr int kBwdGroup = 4;                               // half the registers of eight, so that more threads have loads on their way
+ConvPlan conv_bwd_plan(int B, int T, int D) { return conv_plan(B, T, D, kBwdGroup, (long long)kSMs * 512, 8, 64); }
 
-template <typename IO, int V>
-cudaError_t launch_fwd(int W, const ConvPlan& q, const ConvP& p, cudaStream_t stream) {
-    const auto k = W == 2 ? k_conv_fwd<IO, V, 2> : W == 3 ? k_conv_fwd<IO, V, 3> : k_conv_fwd<IO, V, 4>;
-    return launch_overlapped(k, dim3((unsigned)(q.gx * q.gy)), dim3(256), 0, stream, p);
+ConvP params(int B, int T, int D, const ConvPlan& q, bool silu, bool vec) {
+    ConvP p{};
+    p.B = B; p.T = T; p.D = D; p.cx = q.cx; p.gx = q.gx; p.run = q.run; p.runs = q.runs; p.silu = silu; p.vec = vec;
+    return p;
 }
 template <typename IO, int V>
+cudaError_t launch_fwd(int W, bool steps, const ConvPlan& q, const ConvP& p, cudaStream_t stream) {
+    const auto k = steps ? (W == 2 ? k_conv_steps<IO, V, 2> : W == 3 ? k_conv_steps<IO, V, 3> : k_conv_steps<IO, V, 4>)
+                         : (W == 2 ? k_conv_fwd<IO, V, 2> : W == 3 ? k_conv_fwd<IO, V, 3> : k_conv_fwd<IO, V, 4>);
+    return launch_overlapped(k, dim3((unsigned)(q.gx * q.gy)), dim3(kConvThreads), 0, stream, p);
+}
+template <typename IO>
 cudaError_t launch_bwd(int W, const ConvPlan& q, const ConvP& p, cudaStream_t stream) {
-    const auto k = W == 2 ? k_conv_bwd<IO, V, 2> : W == 3 ? k_conv_bwd<IO, V, 3> : k_conv_bwd<IO, V, 4>;
-    return launch_overlapped(k, dim3((unsigned)(q.gx * q.gy)), dim3(256), 0, stream, p);
+    const auto k = W == 2 ? k_conv_bwd<IO, kBwdGroup, 2> : W == 3 ? k_conv_bwd<IO, kBwdGroup, 3> : k_conv_bwd<IO, kBwdGroup, 4>;
+    return launch_overlapped(k, dim3((unsigned)(q.gx * q.gy)), dim3(kConvThreads), 0, stream, p);
 }
 
 }  // namespace
 
-size_t conv_bwd_workspace(int B, int T, int D, int W, int dtype) {
-    return (size_t)conv_bwd_plan(B, T, D, dtype).gy * (W + 1) * D * sizeof(float);
-}
+size_t conv_bwd_workspace(int B, int T, int D, int W) { return (size_t)conv_bwd_plan(B, T, D).gy * (W + 1) * D * sizeof(float); }
 
 cudaError_t conv_fwd(int B, int T, int D, int W, int dtype, const void* x, const void* w, const void* bias, const void* state, void* y,
                      void* last, bool silu, cudaStream_t stream) {
-    const ConvPlan q = conv_fwd_plan(B, T, D, dtype, state && state == last);
-    ConvP p{};
-    p.B = B; p.T = T; p.D = D; p.groups = q.groups; p.cx = q.cx; p.gx = q.gx; p.run = q.run; p.runs = q.runs;
+    const int V = fwd_group(dtype);
+    const bool steps = state && state == last;
+    const ConvPlan q = steps ? conv_plan(B, T, D, V, 1, T, T) : conv_plan(B, T, D, V, (long long)kSMs * 1024, 4, 32);
+    ConvP p = params(B, T, D, q, silu, D % V == 0);
     p.x = x; p.w = w; p.bias = bias; p.state = state; p.y = y; p.last = last;
-    p.silu = silu; p.vec = D % q.V == 0;
-    return dtype == QD_BF16 ? launch_fwd<__nv_bfloat16, 8>(W, q, p, stream) : launch_fwd<float, 4>(W, q, p, stream);
+    return dtype == QD_BF16 ? launch_fwd<__nv_bfloat16, 8>(W, steps, q, p, stream) : launch_fwd<float, 4>(W, steps, q, p, stream);
 }
 
 cudaError_t conv_bwd(int B, int T, int D, int W, int dtype, const void* x, const void* w, const void* bias, const void* state,
                      const void* dy, const void* dlast, void* dx, float* dw, float* dbias, void* dstate, float* part, bool silu,
                      cudaStream_t stream) {
-    const ConvPlan q = conv_bwd_plan(B, T, D, dtype);
-    ConvP p{};
-    p.B = B; p.T = T; p.D = D; p.groups = q.groups; p.cx = q.cx; p.gx = q.gx; p.run = q.run; p.runs = q.runs;
-    p.x = x; p.w = w; p.bias = bias; p.state = state; p.dy = dy; p.dlast = dlast; p.dx = dx; p.dstate = dstate;
-    p.part = part; p.silu = silu; p.vec = D % q.V == 0;
-    const cudaError_t e = dtype == QD_BF16 ? launch_bwd<__nv_bfloat16, 8>(W, q, p, stream) : launch_bwd<float, 4>(W, q, p, stream);
+    const ConvPlan q = conv_bwd_plan(B, T, D);
+    ConvP p = params(B, T, D, q, silu, D % kBwdGroup == 0);
+    p.x = x; p.w = w; p.bias = bias; p.state = state; p.dy = dy; p.dlast = dlast; p.dx = dx; p.dstate = dstate; p.part = part;
+    const cudaError_t e = dtype == QD_BF16 ? launch_bwd<__nv_bfloat16>(W, q, p, stream) : launch_bwd<float>(W, q, p, stream);
     if (e != cudaSuccess) return e;
     return sum_parts(part, (int)q.gy, (long long)(W + 1) * D, (long long)W * D, D, W, dw, dbias, stream);
 }

@@ -133,7 +133,7 @@ cudaError_t decode_steps(int B, int S, int H, int dk, int dv, int dtype, const v
 // short causal convolution (conv.cu); state == last: decode steps in place
 cudaError_t conv_fwd(int B, int T, int D, int W, int dtype, const void* x, const void* w, const void* bias, const void* state, void* y,
                      void* last, bool silu, cudaStream_t stream);
-size_t conv_bwd_workspace(int B, int T, int D, int W, int dtype);
+size_t conv_bwd_workspace(int B, int T, int D, int W);
 cudaError_t conv_bwd(int B, int T, int D, int W, int dtype, const void* x, const void* w, const void* bias, const void* state,
                      const void* dy, const void* dlast, void* dx, float* dw, float* dbias, void* dstate, float* part, bool silu,
                      cudaStream_t stream);

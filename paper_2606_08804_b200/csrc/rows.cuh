@@ -107,36 +107,76 @@ __device__ __forceinline__ float exp2_unit(float x) {
     return y;
 }
 
+constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
+__device__ __forceinline__ float reciprocal(float x) {
+    float y;
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+// the logistic function, with the relative error of e^-x: 2^-24 |x|
+__device__ __forceinline__ float gate_sigmoid(float x) { return reciprocal(1.f + exp2_unit(x * -kLog2e)); }
+
+// ---- the packed fp32 instructions of sm_100: one issue for two (the pipe takes as long as for two) ----
+typedef unsigned long long f2;               // two fp32 in a register pair
+__device__ __forceinline__ f2 pack2(float lo, float hi) {
+    f2 r;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(lo), "f"(hi));
+    return r;
+}
+__device__ __forceinline__ float2 unpack2(f2 v) {
+    float2 r;
+    asm("mov.b64 {%0, %1}, %2;" : "=f"(r.x), "=f"(r.y) : "l"(v));
+    return r;
+}
+__device__ __forceinline__ f2 mul2(f2 a, f2 b) {
+    f2 r;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+    return r;
+}
+__device__ __forceinline__ f2 add2(f2 a, f2 b) {
+    f2 r;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+    return r;
+}
+__device__ __forceinline__ f2 fma2(f2 a, f2 b, f2 c) {
+    f2 r;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+    return r;
+}
+__device__ __forceinline__ f2 both(float x) { return pack2(x, x); }
+__device__ __forceinline__ f2 exp2_pair(f2 x) {
+    const float2 t = unpack2(x);
+    return pack2(exp2_unit(t.x), exp2_unit(t.y));
+}
+
 // out[col] = sum over p of part[p][col], col < cols, fp32, p in an order that depends on nothing but `parts`.  Column c of the
 // partials is written to out0[c % inner * step0 + c / inner] while c < split, to out1[c - split] behind that.
-__global__ void __launch_bounds__(256) k_sum_parts(const float* part, int parts, long long cols, long long split, long long inner,
-                                                    int step0, float* out0, float* out1) {
-    __shared__ float s[8][33];
+constexpr int kSumRows = 32;                 // threads that share a column: many, since it is their loads' latency that counts
+__global__ void __launch_bounds__(32 * kSumRows) k_sum_parts(const float* part, int parts, long long cols, long long split, long long inner,
+                                                             int step0, float* out0, float* out1) {
+    __shared__ float s[kSumRows][33];
     sm100::grid_dep_wait();
     sm100::grid_dep_launch();
     const int x = threadIdx.x & 31, y = threadIdx.x >> 5;
     const long long c = (long long)blockIdx.x * 32 + x;
-    float a[4] = {0.f, 0.f, 0.f, 0.f};
-    if (c < cols) {
-        int p = y;
-        for (; p + 24 < parts; p += 32)
-#pragma unroll
-            for (int i = 0; i < 4; ++i) a[i] += part[(long long)(p + 8 * i) * cols + c];
-        for (; p < parts; p += 8) a[0] += part[(long long)p * cols + c];
-    }
-    s[y][x] = (a[0] + a[1]) + (a[2] + a[3]);
+    float a = 0.f;
+    if (c < cols)
+#pragma unroll 8
+        for (int p = y; p < parts; p += kSumRows) a += part[(long long)p * cols + c];
+    s[y][x] = a;
     __syncthreads();
-    if (y == 0 && c < cols) {
-        float t = 0.f;
+    a = s[x][y];                                            // a warp a column
 #pragma unroll
-        for (int i = 0; i < 8; ++i) t += s[i][x];
-        if (c < split) { if (out0) out0[c % inner * step0 + c / inner] = t; }
-        else if (out1) out1[c - split] = t;
+    for (int w = 16; w > 0; w >>= 1) a += __shfl_xor_sync(0xffffffffu, a, w);
+    const long long o = (long long)blockIdx.x * 32 + y;
+    if (x == 0 && o < cols) {
+        if (o < split) { if (out0) out0[o % inner * step0 + o / inner] = a; }
+        else if (out1) out1[o - split] = a;
     }
 }
 inline cudaError_t sum_parts(const float* part, int parts, long long cols, long long split, long long inner, int step0, float* out0,
                              float* out1, cudaStream_t stream) {
-    return launch_overlapped(k_sum_parts, dim3((unsigned)((cols + 31) / 32)), dim3(256), 0, stream, part, parts, cols, split, inner,
+    return launch_overlapped(k_sum_parts, dim3((unsigned)((cols + 31) / 32)), dim3(32 * kSumRows), 0, stream, part, parts, cols, split, inner,
                              step0, out0, out1);
 }
 

@@ -4,15 +4,21 @@
 //   y_t = (<C_t, h_t> + D u_t) SiLU(z_t)     (the factor only with z).
 //
 // Tiling.  A warp owns 16 channels x 16 states: lane = 4 c + q has channels 2c, 2c + 1 and states 4q .. 4q + 3, its eight states in
-// registers from token to token, neighbouring channels side by side in the packed fp32 pairs of sm_100 (the pipe is not faster for them,
-// but an instruction is issued for two).  Sums over the states (y, du, ddt) then are over 4 lanes, sums over the channels (dB, dC) over 8,
-// and B_t, C_t, dt_t, u_t come from shared memory, where a CTA stages them for a tile of tokens in fp32.  N > 16 takes more warps for the
-// same channels; states past N have A = B = C = 0 and channels past the group's last dt = u = 0, which leaves them at 0.  Tokens past T
-// have dt = 0: the state passes through.
+// registers from token to token, the two channels side by side in the packed fp32 pairs of sm_100 (the pipe is not faster for them,
+// but an instruction is issued for two).  Sums over the states (y, du, ddt) are then over 4 lanes, sums over the channels (dB, dC) over 8.
+// In such a sum a lane keeps a part and hands the rest on; so that it keeps the part that it has in the same register whichever lane it
+// is, the pair of channels is swapped where q is odd and the pairs of states where c & 2 (Map).
+//
+// Roles.  Half of a CTA's warps walk the tokens.  The other half reads a tile of tokens ahead of them, turns dt, u, z, dy into what the
+// walk needs (softplus, products, gates) in shared memory, in fp32, and writes out what the tile before left there.  One barrier a tile;
+// the two halves share the issue slots of the four sub-partitions, of which the walk alone, a chain of few wide steps, leaves many unused.
 //
 // Segments.  Where there are too few channels to fill the GPU, a sequence is cut into segments: each is first walked from a zero state
 // (the first from h0) without outputs, the states at the segments' ends are joined (h = exp(A sum dt) h + local end), and then all
 // segments run at once from their true states.  That walks all but the last twice, so one segment where channels suffice.
+//
+// States past N have A = B = C = 0 and channels past the group's last dt = u = 0, which leaves them at 0.  Tokens past T have dt = 0: the
+// state passes through.
 #pragma once
 #include "rows.cuh"
 
@@ -20,27 +26,26 @@ namespace qd {
 namespace scan {
 
 constexpr int kWarpChannels = 16, kWarpStates = 16;
-constexpr int kSave = 8;                     // tokens from one saved state to the next
-constexpr int kTile = 16;                    // tokens that a CTA stages at a time, forward
+constexpr int kWalkers = 4;                  // warps of a CTA that walk; as many prepare
+constexpr int kThreads = 2 * 32 * kWalkers;
+constexpr int kSave = 8;                     // tokens from one saved state to the next, and of a tile, backward
+constexpr int kTile = 16;                    // tokens of a tile, forward
 constexpr size_t kWarpTile = kWarpChannels * kWarpStates;          // states of a warp, in the order [lane][state][channel of the pair]
 
 // What both directions derive from the shape.
 struct Dims {
     int B, T, D, N, G, K;                    // K = D / G channels of a group
-    int nb;                                  // blocks of 16 states
-    int cw;                                  // warps side by side in the channels of a CTA
-    int tiles;                               // groups of 16 channels in a group
-    int ctas;                                // CTAs to cover a group
+    int nb;                                  // blocks of 16 states: 1, 2 or 4, side by side in a CTA
+    int ctas;                                // CTAs to cover a group's channels
     size_t states;                           // fp32 values of one state of one sequence in warp order
 };
 inline Dims dims(const qd_scan_shape& s) {
     Dims d{};
     d.B = s.B; d.T = s.T; d.D = s.D; d.N = s.N; d.G = s.G; d.K = s.D / s.G;
-    d.nb = (s.N + kWarpStates - 1) / kWarpStates;
-    d.cw = d.nb == 1 ? 4 : 2;
-    d.tiles = (d.K + kWarpChannels - 1) / kWarpChannels;
-    d.ctas = (d.tiles + d.cw - 1) / d.cw;
-    d.states = (size_t)d.G * d.ctas * d.cw * d.nb * kWarpTile;
+    d.nb = s.N <= 16 ? 1 : s.N <= 32 ? 2 : 4;
+    const int cc = kWalkers / d.nb * kWarpChannels;
+    d.ctas = (d.K + cc - 1) / cc;
+    d.states = (size_t)d.G * d.ctas * kWalkers * kWarpTile;
     return d;
 }
 
@@ -56,56 +61,119 @@ struct P {
     float *pA, *pD;                          // partial gradients of A [segs][B][D N], of D and dt_bias [segs][B][2][D]
     float *pBC;                              // of B and C [ctas][2][B T G N]
     bool softplus, vec, vecn;                // rows are read 16 bytes at a time; so are those of B, C
+    bool joined;                             // the ends are those of the true states already
 };
 
+// Segments of a sequence and tokens of one, a multiple of kTile.
+struct Cut { int segs, len; };
+Cut cut(const Dims& d);
+// True states at the segments' ends from those of each walked alone, which they overwrite, where the walk does not join them itself.
+constexpr int kMostJoined = 32;              // segments before one's own whose ends a CTA joins by itself
+cudaError_t join(float* ends, const float* decays, int n, int from, int step, size_t count, cudaStream_t stream);
+
 #ifdef __CUDACC__
-typedef unsigned long long f2;               // two fp32 in a register pair: channels 2c (low) and 2c + 1
-__device__ __forceinline__ f2 pack2(float lo, float hi) {
-    f2 r;
-    asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(lo), "f"(hi));
-    return r;
-}
-__device__ __forceinline__ float2 unpack2(f2 v) {
-    float2 r;
-    asm("mov.b64 {%0, %1}, %2;" : "=f"(r.x), "=f"(r.y) : "l"(v));
-    return r;
-}
-__device__ __forceinline__ f2 mul2(f2 a, f2 b) {
-    f2 r;
-    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
-    return r;
-}
-__device__ __forceinline__ f2 fma2(f2 a, f2 b, f2 c) {
-    f2 r;
-    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
-    return r;
-}
-__device__ __forceinline__ f2 exp2_pair(f2 x) {
-    const float2 t = unpack2(x);
-    return pack2(exp2_unit(t.x), exp2_unit(t.y));
-}
 struct alignas(16) f2x2 { f2 a, b; };
 
 // softplus(x) = max(x, 0) + log1p(e), e = exp(-|x|) in (0, 1].  log1p(e) = 2 artanh(s), s = e / (2 + e) <= 1/3, by the series
-// s + s^3 / 3 + s^5 / 5 + ..., whose first dropped term is below 1e-8 of the sum: the relative error stays at a few 2^-24 where e is small.
-__device__ __forceinline__ float softplus(float x) {
-    const float e = expf(-fabsf(x)), s = __fdividef(e, 2.f + e), w = s * s;
-    float t = fmaf(w, 1.f / 15, 1.f / 13);
-    t = fmaf(w, t, 1.f / 11);
-    t = fmaf(w, t, 1.f / 9);
-    t = fmaf(w, t, 1.f / 7);
-    t = fmaf(w, t, 1.f / 5);
-    t = fmaf(w, t, 1.f / 3);
-    const float l = 2.f * fmaf(s * w, t, s);
-    return fmaxf(x, 0.f) + (x != x ? x : l);
+// s + s^3 / 3 + s^5 / 5 + ..., whose first dropped term is below 1e-8 of the sum: the relative error stays at a few 2^-24 where e is
+// small, but for that of e, 2^-24 |x|.
+__device__ __forceinline__ float2 softplus(float x, float y) {
+    const float e = exp2_unit(fabsf(x) * -kLog2e), f = exp2_unit(fabsf(y) * -kLog2e);
+    const f2 ef = pack2(e, f), s = mul2(ef, pack2(reciprocal(2.f + e), reciprocal(2.f + f))), w = mul2(s, s), s2 = add2(s, s);
+    f2 t = fma2(w, both(1.f / 15), both(1.f / 13));
+    t = fma2(w, t, both(1.f / 11));
+    t = fma2(w, t, both(1.f / 9));
+    t = fma2(w, t, both(1.f / 7));
+    t = fma2(w, t, both(1.f / 5));
+    t = fma2(w, t, both(1.f / 3));
+    return unpack2(add2(fma2(mul2(s2, w), t, s2), pack2(fmaxf(x, 0.f), fmaxf(y, 0.f))));
 }
-
-constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
+// What a walking lane owns.
+struct Map {
+    int q, c, lo, hi;                        // lo, hi: its channels in the warp's 16, in the order of its register pairs
+    int pair[2];                             // its pairs of states in the warp's 16: registers 0, 1 and 2, 3
+    int at;                                  // where the pair of channels stands in a row [8][2] of f2, both orders of each pair
+    __device__ __forceinline__ explicit Map(int lane) {
+        q = lane & 3;
+        c = lane >> 2;
+        lo = 2 * c + (q & 1);
+        hi = 2 * c + 1 - (q & 1);
+        const int swap = c >> 1 & 1;
+        pair[0] = 2 * q + swap;
+        pair[1] = 2 * q + 1 - swap;
+        at = 2 * c + (q & 1);
+    }
+    __device__ __forceinline__ int state(int j) const { return 2 * pair[j >> 1] + (j & 1); }
+};
+// its four A times log2 e; 0 where there is none
+__device__ __forceinline__ void load_decay(const P& p, const Map& m, int g, int ch, int n0, f2 (&A2)[4]) {
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        const int n = n0 + m.state(j);
+        const float* row = p.A + (size_t)g * p.d.K * p.d.N + n;
+        A2[j] = pack2(n < p.d.N && ch + m.lo < p.d.K ? row[(size_t)(ch + m.lo) * p.d.N] * kLog2e : 0.f,
+                      n < p.d.N && ch + m.hi < p.d.K ? row[(size_t)(ch + m.hi) * p.d.N] * kLog2e : 0.f);
+    }
+}
+// its states of a tensor [B, D, N]
+__device__ __forceinline__ void load_state(const P& p, const Map& m, const float* s, int b, int g, int ch, int n0, f2 (&h)[4]) {
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        const int n = n0 + m.state(j);
+        const float* row = s + ((size_t)b * p.d.D + (size_t)g * p.d.K) * p.d.N + n;
+        h[j] = pack2(n < p.d.N && ch + m.lo < p.d.K ? row[(size_t)(ch + m.lo) * p.d.N] : 0.f,
+                     n < p.d.N && ch + m.hi < p.d.K ? row[(size_t)(ch + m.hi) * p.d.N] : 0.f);
+    }
+}
+__device__ __forceinline__ void store_state(const P& p, const Map& m, float* s, int b, int g, int ch, int n0, const f2 (&h)[4]) {
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        const int n = n0 + m.state(j);
+        float* row = s + ((size_t)b * p.d.D + (size_t)g * p.d.K) * p.d.N + n;
+        const float2 v = unpack2(h[j]);
+        if (n < p.d.N && ch + m.lo < p.d.K) row[(size_t)(ch + m.lo) * p.d.N] = v.x;
+        if (n < p.d.N && ch + m.hi < p.d.K) row[(size_t)(ch + m.hi) * p.d.N] = v.y;
+    }
+}
+// the same in warp order
+__device__ __forceinline__ void load_tile(const float* s, f2 (&h)[4]) {
+    const f2x2 *v = reinterpret_cast<const f2x2*>(s), a = v[0], b = v[1];
+    h[0] = a.a; h[1] = a.b; h[2] = b.a; h[3] = b.b;
+}
+__device__ __forceinline__ void store_tile(float* s, const f2 (&h)[4]) {
+    f2x2* v = reinterpret_cast<f2x2*>(s);
+    v[0] = {h[0], h[1]};
+    v[1] = {h[2], h[3]};
+}
+// end of a segment walked alone: what it adds, and the decay of what was before it
+__device__ __forceinline__ void store_end(const P& p, int k, int b, size_t lane, const f2 (&h)[4], const f2 (&A2)[4], f2 sum) {
+    const size_t at = ((size_t)k * p.d.B + b) * p.d.states + lane;
+    f2 a[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) a[j] = exp2_pair(mul2(sum, A2[j]));
+    store_tile(p.ends + at, h);
+    store_tile(p.decays + at, a);
+}
+// the state behind segment ends[n - 1] of `from, from + step, ..`
+__device__ __forceinline__ void load_end(const P& p, int from, int step, int n, int b, size_t lane, f2 (&h)[4]) {
+    const size_t stride = (size_t)p.d.B * p.d.states, base = (size_t)b * p.d.states + lane;
+    if (p.joined) return load_tile(p.ends + (size_t)(from + (n - 1) * step) * stride + base, h);
+    load_tile(p.ends + (size_t)from * stride + base, h);
+#pragma unroll 4
+    for (int k = 1; k < n; ++k) {
+        f2 a[4], e[4];
+        load_tile(p.decays + (size_t)(from + k * step) * stride + base, a);
+        load_tile(p.ends + (size_t)(from + k * step) * stride + base, e);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) h[j] = fma2(a[j], h[j], e[j]);
+    }
+}
+// two channel pairs of a row, both orders of each: {x0, x1, x1, x0}
+__device__ __forceinline__ void store_pairs(float4* to, float x0, float x1, float x2, float x3) {
+    to[0] = make_float4(x0, x1, x1, x0);
+    to[1] = make_float4(x2, x3, x3, x2);
+}
 #endif
-
-cudaError_t join(float* ends, const float* decays, int n, int from, int step, size_t count, cudaStream_t stream);
-int segments(const Dims& d, int slots, int shortest);
-int segment_tokens(int T, int segs);
 
 }  // namespace scan
 }  // namespace qd
