@@ -28,6 +28,9 @@ __device__ __forceinline__ Pack<IO, N> load_pack(const IO* p, int left, bool vec
             const uint2 t = *reinterpret_cast<const uint2*>(p);
             r.w[0] = t.x; r.w[1] = t.y;
             return r;
+        } else if constexpr (N * sizeof(IO) == 4) {
+            r.w[0] = *reinterpret_cast<const uint32_t*>(p);
+            return r;
         }
     }
 #pragma unroll
@@ -85,6 +88,9 @@ __device__ __forceinline__ void store_pack(IO* p, const Pack<IO, N>& r, int left
             return;
         } else if constexpr (W == 2) {
             *reinterpret_cast<uint2*>(p) = make_uint2(r.w[0], r.w[1]);
+            return;
+        } else if constexpr (N * sizeof(IO) == 4) {
+            *reinterpret_cast<uint32_t*>(p) = r.w[0];
             return;
         }
     }

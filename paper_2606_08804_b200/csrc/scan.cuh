@@ -4,14 +4,18 @@
 //   y_t = (<C_t, h_t> + D u_t) SiLU(z_t)     (the factor only with z).
 //
 // Tiling.  A warp owns 16 channels x 16 states: lane = 4 c + q has channels 2c, 2c + 1 and states 4q .. 4q + 3, its eight states in
-// registers from token to token, the two channels side by side in the packed fp32 pairs of sm_100 (the pipe is not faster for them,
-// but an instruction is issued for two).  Sums over the states (y, du, ddt) are then over 4 lanes, sums over the channels (dB, dC) over 8.
-// In such a sum a lane keeps a part and hands the rest on; so that it keeps the part that it has in the same register whichever lane it
-// is, the pair of channels is swapped where q is odd and the pairs of states where c & 2 (Map).
+// registers from token to token, neighbouring states side by side in the packed fp32 pairs of sm_100 (the pipe is not faster for them,
+// but an instruction is issued for two).  dt, u, B, C of a token come from shared memory; that returns 128 bytes a clock and SM, however
+// many lanes share a value, so a token costs a warp 12 clocks of it forward (B and C as pairs of equal values, with the channels packed
+// instead of the states: 20, which alone bounded the kernel).
+// Sums over the states (y, du, ddt) are over 4 lanes, sums over the channels (dB, dC) over 8.  In such a sum a lane keeps a part and hands
+// the rest on; so that it keeps the part that it has in the same register whichever lane it is, the channels of a pair are swapped where q
+// is odd and the pairs of states where c & 2 (Map), and shared memory holds both orders.
 //
-// Roles.  Half of a CTA's warps walk the tokens.  The other half reads a tile of tokens ahead of them, turns dt, u, z, dy into what the
-// walk needs (softplus, products, gates) in shared memory, in fp32, and writes out what the tile before left there.  One barrier a tile;
-// the two halves share the issue slots of the four sub-partitions, of which the walk alone, a chain of few wide steps, leaves many unused.
+// Roles.  Half of a CTA's warps walk the tokens.  The other half turns dt, u, z, dy of the tile after theirs into what the walk needs
+// (softplus, products, gates) in shared memory, in fp32, and writes out what the tile before left there; what it reads is copied to shared
+// memory two or three tiles ahead of that.
+// One barrier a tile; the two halves share the issue slots of the four sub-partitions, of which the walk alone leaves many unused.
 //
 // Segments.  Where there are too few channels to fill the GPU, a sequence is cut into segments: each is first walked from a zero state
 // (the first from h0) without outputs, the states at the segments' ends are joined (h = exp(A sum dt) h + local end), and then all
@@ -60,9 +64,14 @@ struct P {
     float *ends, *decays;                    // [segs - 1][B][states]: states (gradients) at segments' ends, exp(A sum dt) of segments
     float *pA, *pD;                          // partial gradients of A [segs][B][D N], of D and dt_bias [segs][B][2][D]
     float *pBC;                              // of B and C [ctas][2][B T G N]
-    bool softplus, vec, vecn;                // rows are read 16 bytes at a time; so are those of B, C
+    bool softplus;
+    int rows, bc;                            // how rows and those of B, C are copied (Copy)
     bool joined;                             // the ends are those of the true states already
 };
+
+// How groups of a row are copied: whole and aligned; in words of 4 bytes (bf16: an even number of elements); one by one.
+enum Copy { kSingle = 0, kWords = 1, kWhole = 2 };
+inline int copy_of(int width, int group, int dtype) { return width % group == 0 ? kWhole : dtype == QD_F32 || width % 2 == 0 ? kWords : kSingle; }
 
 // Segments of a sequence and tokens of one, a multiple of kTile.
 struct Cut { int segs, len; };
@@ -88,52 +97,43 @@ __device__ __forceinline__ float2 softplus(float x, float y) {
     t = fma2(w, t, both(1.f / 3));
     return unpack2(add2(fma2(mul2(s2, w), t, s2), pack2(fmaxf(x, 0.f), fmaxf(y, 0.f))));
 }
-// What a walking lane owns.
+// What a walking lane owns.  Registers [channel][pair of states], flat.
 struct Map {
-    int q, c, lo, hi;                        // lo, hi: its channels in the warp's 16, in the order of its register pairs
-    int pair[2];                             // its pairs of states in the warp's 16: registers 0, 1 and 2, 3
-    int at;                                  // where the pair of channels stands in a row [8][2] of f2, both orders of each pair
+    int q, ch[2], order, swap;               // its channels in the warp's 16; which order of a record it reads, of channels and of pairs of states
     __device__ __forceinline__ explicit Map(int lane) {
         q = lane & 3;
-        c = lane >> 2;
-        lo = 2 * c + (q & 1);
-        hi = 2 * c + 1 - (q & 1);
-        const int swap = c >> 1 & 1;
-        pair[0] = 2 * q + swap;
-        pair[1] = 2 * q + 1 - swap;
-        at = 2 * c + (q & 1);
+        const int c = lane >> 2;
+        order = q & 1;
+        ch[0] = 2 * c + order;
+        ch[1] = 2 * c + 1 - order;
+        swap = c >> 1 & 1;
     }
-    __device__ __forceinline__ int state(int j) const { return 2 * pair[j >> 1] + (j & 1); }
+    __device__ __forceinline__ int state(int pair, int e) const { return 4 * q + 2 * (pair ^ swap) + e; }       // in the warp's 16
 };
-// its four A times log2 e; 0 where there is none
-__device__ __forceinline__ void load_decay(const P& p, const Map& m, int g, int ch, int n0, f2 (&A2)[4]) {
+// f(register, low half or high, offset in a [D, N] state, whether there is such a state)
+template <class F>
+__device__ __forceinline__ void each_state(const P& p, const Map& m, int g, int ch, int n0, F f) {
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-        const int n = n0 + m.state(j);
-        const float* row = p.A + (size_t)g * p.d.K * p.d.N + n;
-        A2[j] = pack2(n < p.d.N && ch + m.lo < p.d.K ? row[(size_t)(ch + m.lo) * p.d.N] * kLog2e : 0.f,
-                      n < p.d.N && ch + m.hi < p.d.K ? row[(size_t)(ch + m.hi) * p.d.N] * kLog2e : 0.f);
-    }
+    for (int c = 0; c < 2; ++c)
+#pragma unroll
+        for (int pr = 0; pr < 2; ++pr)
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+                const int k = ch + m.ch[c], n = n0 + m.state(pr, e);
+                f(2 * c + pr, e, ((size_t)g * p.d.K + k) * p.d.N + n, k < p.d.K && n < p.d.N);
+            }
 }
-// its states of a tensor [B, D, N]
-__device__ __forceinline__ void load_state(const P& p, const Map& m, const float* s, int b, int g, int ch, int n0, f2 (&h)[4]) {
+__device__ __forceinline__ void load_state(const P& p, const Map& m, const float* s, int g, int ch, int n0, float scale, f2 (&h)[4]) {
+    float v[4][2];
+    each_state(p, m, g, ch, n0, [&](int r, int e, size_t at, bool in) { v[r][e] = in ? s[at] * scale : 0.f; });
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-        const int n = n0 + m.state(j);
-        const float* row = s + ((size_t)b * p.d.D + (size_t)g * p.d.K) * p.d.N + n;
-        h[j] = pack2(n < p.d.N && ch + m.lo < p.d.K ? row[(size_t)(ch + m.lo) * p.d.N] : 0.f,
-                     n < p.d.N && ch + m.hi < p.d.K ? row[(size_t)(ch + m.hi) * p.d.N] : 0.f);
-    }
+    for (int r = 0; r < 4; ++r) h[r] = pack2(v[r][0], v[r][1]);
 }
-__device__ __forceinline__ void store_state(const P& p, const Map& m, float* s, int b, int g, int ch, int n0, const f2 (&h)[4]) {
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-        const int n = n0 + m.state(j);
-        float* row = s + ((size_t)b * p.d.D + (size_t)g * p.d.K) * p.d.N + n;
-        const float2 v = unpack2(h[j]);
-        if (n < p.d.N && ch + m.lo < p.d.K) row[(size_t)(ch + m.lo) * p.d.N] = v.x;
-        if (n < p.d.N && ch + m.hi < p.d.K) row[(size_t)(ch + m.hi) * p.d.N] = v.y;
-    }
+__device__ __forceinline__ void store_state(const P& p, const Map& m, float* s, int g, int ch, int n0, const f2 (&h)[4]) {
+    each_state(p, m, g, ch, n0, [&](int r, int e, size_t at, bool in) {
+        const float2 v = unpack2(h[r]);
+        if (in) s[at] = e ? v.y : v.x;
+    });
 }
 // the same in warp order
 __device__ __forceinline__ void load_tile(const float* s, f2 (&h)[4]) {
@@ -145,12 +145,12 @@ __device__ __forceinline__ void store_tile(float* s, const f2 (&h)[4]) {
     v[0] = {h[0], h[1]};
     v[1] = {h[2], h[3]};
 }
-// end of a segment walked alone: what it adds, and the decay of what was before it
-__device__ __forceinline__ void store_end(const P& p, int k, int b, size_t lane, const f2 (&h)[4], const f2 (&A2)[4], f2 sum) {
+// end of a segment walked alone: what it adds, and the decay of what was before it; sum: of dt, of both channels
+__device__ __forceinline__ void store_end(const P& p, int k, int b, size_t lane, const f2 (&h)[4], const f2 (&A2)[4], const float (&sum)[2]) {
     const size_t at = ((size_t)k * p.d.B + b) * p.d.states + lane;
     f2 a[4];
 #pragma unroll
-    for (int j = 0; j < 4; ++j) a[j] = exp2_pair(mul2(sum, A2[j]));
+    for (int j = 0; j < 4; ++j) a[j] = exp2_pair(mul2(both(sum[j >> 1]), A2[j]));
     store_tile(p.ends + at, h);
     store_tile(p.decays + at, a);
 }
@@ -168,10 +168,45 @@ __device__ __forceinline__ void load_end(const P& p, int from, int step, int n, 
         for (int j = 0; j < 4; ++j) h[j] = fma2(a[j], h[j], e[j]);
     }
 }
-// two channel pairs of a row, both orders of each: {x0, x1, x1, x0}
-__device__ __forceinline__ void store_pairs(float4* to, float x0, float x1, float x2, float x3) {
-    to[0] = make_float4(x0, x1, x1, x0);
-    to[1] = make_float4(x2, x3, x3, x2);
+// N neighbouring elements on their way to shared memory: those from `left` on are 0.  kSingle waits for them.
+template <int BYTES>
+__device__ __forceinline__ void copy_bytes(void* dst, const void* src, int bytes) {
+    const uint32_t d = sm100::smem_u32(dst);
+    if constexpr (BYTES == 16) asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(d), "l"(src), "r"(bytes) : "memory");
+    else asm volatile("cp.async.ca.shared.global [%0], [%1], %2, %3;" ::"r"(d), "l"(src), "n"(BYTES), "r"(bytes) : "memory");
+}
+template <int N, typename IO>
+__device__ __forceinline__ void copy_group(IO* dst, const IO* src, int left, int how) {
+    constexpr int BYTES = N * sizeof(IO);
+    if (how == kWhole) copy_bytes<BYTES>(dst, src, left > 0 ? BYTES : 0);
+    else if (how == kWords) {
+        constexpr int E = 4 / sizeof(IO);
+#pragma unroll
+        for (int o = 0; o < N; o += E) copy_bytes<4>(dst + o, src + (o < left ? o : 0), o < left ? 4 : 0);
+    } else {
+#pragma unroll
+        for (int o = 0; o < N; ++o) st(dst, o, o < left ? ld(src, o) : 0.f);
+    }
+}
+// Tile of TT tokens (from tt, below `end`) x CC channels (from col, `left` of them) of a tensor [T, D], by 128 threads; row major.
+template <int TT, int CC, typename IO>
+__device__ __forceinline__ void copy_tile(IO* dst, const void* src, size_t row0, int D, int tt, int end, size_t col, int left, int how, int tid) {
+    constexpr int E = 16 / sizeof(IO), CH = TT * CC / E;
+#pragma unroll
+    for (int j = 0; j < (CH + 127) / 128; ++j) {
+        const int x = tid + j * 128, t = tt + x / (CC / E), c = x % (CC / E) * E;
+        if (CH % 128 != 0 && x >= CH) break;
+        const int have = t < end ? left - c : 0;
+        copy_group<E>(dst + x * E, static_cast<const IO*>(src) + (have > 0 ? (row0 + t) * D + col + c : 0), have, how);
+    }
+}
+__device__ __forceinline__ void copy_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N> __device__ __forceinline__ void copy_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
+
+__device__ __forceinline__ void prepare_barrier() { asm volatile("bar.sync 1, 128;" ::: "memory"); }     // the half that prepares
+__device__ __forceinline__ float sum_pair(f2 v) {
+    const float2 t = unpack2(v);
+    return t.x + t.y;
 }
 #endif
 

@@ -31,7 +31,7 @@ __global__ void __launch_bounds__(kThreads, 2) k_scan_bwd(const P p) {
     sm100::grid_dep_wait();
     sm100::grid_dep_launch();
     const Dims& d = p.d;
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int warp = sm100::warp_index(), lane = threadIdx.x & 31;
     int idx = blockIdx.x;
     const int ct = idx % d.ctas; idx /= d.ctas;
     const int g = idx % d.G; idx /= d.G;

@@ -7,24 +7,27 @@ namespace qd {
 namespace {
 using namespace scan;
 
-template <int NB> struct FwdSmem {
+template <typename IO, int NB> struct FwdSmem {
     static constexpr int CC = kWalkers / NB * kWarpChannels, NS = NB * kWarpStates;
-    float4 dt[2][kTile][CC / 2], x[2][kTile][CC / 2];      // dt, dt u: every pair of channels in both orders
-    f2x2 B[2][kTile][NS / 2], C[2][kTile][NS / 2];         // each state's value twice, for both channels of a pair
+    static constexpr int PAIRS = CC / 2, ROWS = 128 / PAIRS, PASSES = kTile / ROWS;      // of a thread that prepares: a pair of channels, PASSES tokens
+    static constexpr int RING = sizeof(IO) == 2 ? 5 : 4;   // tiles of what is copied: i - 1 (for y), i, i + 1 (prepared now), i + 2 (has come), fp32 no more
+    float4 step[2][kTile][2][PAIRS];                       // dt, dt, dt u, dt u of a pair of channels, in both orders
+    float4 B[2][kTile][2][NS / 4], C[2][kTile][2][NS / 4]; // four states, the pairs in both orders
     float y[2][NB][kTile][CC];
-    float bias[CC], skip[CC];
+    alignas(16) IO u[RING][kTile * CC], dt[RING][kTile * CC], z[RING][kTile * CC];
+    Pack<IO, 4> bc[RING][NB][128];
 };
 
 template <typename IO, int NB, bool LOCAL>
 __global__ void __launch_bounds__(kThreads, 2) k_scan_fwd(const P p) {
-    using S = FwdSmem<NB>;
+    using S = FwdSmem<IO, NB>;
     constexpr int CW = kWalkers / NB, CC = S::CC, NS = S::NS;
     extern __shared__ __align__(16) unsigned char raw_smem[];
     S& sm = *reinterpret_cast<S*>(raw_smem);
     sm100::grid_dep_wait();
     sm100::grid_dep_launch();
     const Dims& d = p.d;
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int warp = sm100::warp_index(), lane = threadIdx.x & 31;
     int idx = blockIdx.x;
     const int ct = idx % d.ctas; idx /= d.ctas;
     const int g = idx % d.G; idx /= d.G;
@@ -35,147 +38,145 @@ __global__ void __launch_bounds__(kThreads, 2) k_scan_fwd(const P p) {
     if (warp < kWalkers) {
         // ---- walk ----------------------------------------------------------------------------------------------------------
         const Map m(lane);
-        const int wc = warp % CW, n0 = warp / CW * kWarpStates, ch = ct * CC + wc * kWarpChannels;
-        const size_t mine = (((size_t)g * d.ctas + ct) * kWalkers + warp) * kWarpTile + lane * 8;
-        f2 A2[4], h[4] = {0, 0, 0, 0}, sum = 0;
-        load_decay(p, m, g, ch, n0, A2);
+        const int wc = warp % CW, wb = warp / CW, n0 = wb * kWarpStates, ch = ct * CC + wc * kWarpChannels;
+        const size_t mine = (((size_t)g * d.ctas + ct) * kWalkers + warp) * kWarpTile + lane * 8, state = (size_t)b * d.D * d.N;
+        f2 A2[4], h[4] = {0, 0, 0, 0};
+        float sum[2] = {0.f, 0.f};
+        load_state(p, m, p.A, g, ch, n0, kLog2e, A2);
         if (seg == 0) {
-            if (p.h0) load_state(p, m, p.h0, b, g, ch, n0, h);
+            if (p.h0) load_state(p, m, p.h0 + state, g, ch, n0, 1.f, h);
         } else if (!LOCAL) load_end(p, 0, 1, seg, b, mine, h);
         float* saved = p.saved ? p.saved + ((size_t)b * ((d.T + kSave - 1) / kSave) + t0 / kSave) * d.states + mine : nullptr;
+        const int pair = wc * (kWarpChannels / 2) + (lane >> 2), quad = n0 / 4 + m.q;
         __syncthreads();
         for (int i = 0; i < n; ++i) {
             const int k = i & 1;
-            const f2 *dt = reinterpret_cast<const f2*>(sm.dt[k]) + wc * kWarpChannels + m.at, *x = reinterpret_cast<const f2*>(sm.x[k]) + wc * kWarpChannels + m.at;
-            const f2x2 *B = &sm.B[k][0][n0 / 2], *C = &sm.C[k][0][n0 / 2];
-            float out[kTile / 2];                          // stored when the tile is done: nothing stands in the way of the loads till then
+            const float4 *step = &sm.step[k][0][m.order][pair], *B = &sm.B[k][0][m.swap][quad], *C = &sm.C[k][0][m.swap][quad];
+            float out[kTile / 2], held[2];                 // stored when the tile is done: nothing stands in the way of the loads till then
 #pragma unroll
-            for (int t = 0; t < kTile; t += 2) {
+            for (int t = 0; t < kTile; ++t) {
                 if (!LOCAL && saved && t % kSave == 0 && t0 + i * kTile + t < t1) {
                     store_tile(saved, h);
                     saved += d.states;
                 }
-                f2 y[2];
+                const float4 v = step[t * 2 * S::PAIRS], vb = B[t * 2 * (NS / 4)];
+                const f2 dt[2] = {both(v.x), both(v.y)}, x[2] = {both(v.z), both(v.w)}, bp[2] = {pack2(vb.x, vb.y), pack2(vb.z, vb.w)};
 #pragma unroll
-                for (int s = 0; s < 2; ++s) {
-                    const f2 vd = dt[(t + s) * CC], vx = x[(t + s) * CC];
-                    const f2x2 b0 = B[(t + s) * (NS / 2) + m.pair[0]], b1 = B[(t + s) * (NS / 2) + m.pair[1]];
-                    const f2 vb[4] = {b0.a, b0.b, b1.a, b1.b};
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) h[j] = fma2(exp2_pair(mul2(vd, A2[j])), h[j], mul2(vx, vb[j]));
-                    if (LOCAL) sum = add2(sum, vd);
-                    else {
-                        const f2x2 c0 = C[(t + s) * (NS / 2) + m.pair[0]], c1 = C[(t + s) * (NS / 2) + m.pair[1]];
-                        y[s] = fma2(h[3], c1.b, fma2(h[2], c1.a, fma2(h[1], c0.b, mul2(h[0], c0.a))));
+                for (int j = 0; j < 4; ++j) h[j] = fma2(exp2_pair(mul2(dt[j >> 1], A2[j])), h[j], mul2(x[j >> 1], bp[j & 1]));
+                if (LOCAL) {
+                    sum[0] += v.x;
+                    sum[1] += v.y;
+                } else {
+                    const float4 vc = C[t * 2 * (NS / 4)];
+                    const f2 cp[2] = {pack2(vc.x, vc.y), pack2(vc.z, vc.w)};
+                    const float y0 = sum_pair(fma2(h[1], cp[1], mul2(h[0], cp[0]))), y1 = sum_pair(fma2(h[3], cp[1], mul2(h[2], cp[0])));
+                    // over the four lanes: a lane keeps its first channel, then of two tokens that of its q / 2
+                    held[t & 1] = y0 + __shfl_xor_sync(0xffffffffu, y1, 1);
+                    if (t & 1) {
+                        const bool second = m.q & 2;
+                        out[t / 2] = (second ? held[1] : held[0]) + __shfl_xor_sync(0xffffffffu, second ? held[0] : held[1], 2);
                     }
-                }
-                if (!LOCAL) {
-                    // over the four lanes: a lane keeps its first channel, then of the two tokens that of its q / 2
-                    const float2 e0 = unpack2(y[0]), e1 = unpack2(y[1]);
-                    const float k0 = e0.x + __shfl_xor_sync(0xffffffffu, e0.y, 1), k1 = e1.x + __shfl_xor_sync(0xffffffffu, e1.y, 1);
-                    const bool second = m.q & 2;
-                    out[t / 2] = (second ? k1 : k0) + __shfl_xor_sync(0xffffffffu, second ? k0 : k1, 2);
                 }
             }
             if (!LOCAL)
 #pragma unroll
-                for (int t = 0; t < kTile; t += 2) sm.y[k][warp / CW][t + (m.q >> 1)][wc * kWarpChannels + m.lo] = out[t / 2];
+                for (int t = 0; t < kTile; t += 2) sm.y[k][wb][t + (m.q >> 1)][wc * kWarpChannels + m.ch[0]] = out[t / 2];
             __syncthreads();
         }
         if (LOCAL) store_end(p, seg, b, mine, h, A2, sum);
-        else if (p.hT && t1 == d.T) store_state(p, m, p.hT, b, g, ch, n0, h);
+        else if (p.hT && t1 == d.T) store_state(p, m, p.hT + state, g, ch, n0, h);
         return;
     }
     // ---- prepare tiles, write y ------------------------------------------------------------------------------------------------
     const int tid = threadIdx.x - 32 * kWalkers;
-    const int it = tid / (CC / 8), ic = tid % (CC / 8) * 8;                // a token of the tile, eight channels of the CTA's
-    const int left = it < kTile ? d.K - ct * CC - ic : 0;                  // with NB > 1 some threads have none
-    const size_t col = (size_t)g * d.K + ct * CC + ic;
-    if (tid < CC) {                                        // read by this half of the CTA only
-        const bool in = ct * CC + tid < d.K;
-        sm.bias[tid] = p.dt_bias && in ? p.dt_bias[(size_t)g * d.K + ct * CC + tid] : 0.f;
-        sm.skip[tid] = p.D && in ? p.D[(size_t)g * d.K + ct * CC + tid] : 0.f;
-    }
-    asm volatile("bar.sync 1, %0;" ::"n"(kThreads / 2) : "memory");
-    struct Raw { Pack<IO, 8> u, dt, z; Pack<IO, 4> bc[NB]; } next;
-    struct Held { Pack<IO, 8> u, z; } held[2];                             // of the tiles i, i - 1
-    next.u = next.dt = next.z = zero_pack<IO, 8>();
-    auto fetch = [&](int tt) {
-        const int t = tt + it;
-        if (left > 0 && t < t1) {
-            const size_t at = ((size_t)b * d.T + t) * d.D + col;
-            next.u = load_pack<IO, 8>(static_cast<const IO*>(p.u) + at, left, p.vec);
-            next.dt = load_pack<IO, 8>(static_cast<const IO*>(p.dt) + at, left, p.vec);
-            if (!LOCAL && p.z) next.z = load_pack<IO, 8>(static_cast<const IO*>(p.z) + at, left, p.vec);
-        }
+    const size_t rows = (size_t)b * d.T, col = (size_t)g * d.K + ct * CC;
+    const int left = d.K - ct * CC;
+    // a tile is prepared by pairs of channels and written out by groups of eight (where NB > 1 some threads have none)
+    const int pr = tid % S::PAIRS, first = tid / S::PAIRS, it = tid / (CC / 8), ic = tid % (CC / 8) * 8;
+    float bias[2], skip[8];
 #pragma unroll
-        for (int i = 0; i < NB; ++i) {                                     // four states of B or C of a token
-            const int x = tid + i * 128, bt = x / (NS / 2), r = x % (NS / 2), s = r % (NS / 4) * 4;
-            next.bc[i] = zero_pack<IO, 4>();
-            if (tt + bt < t1 && s < d.N && !(LOCAL && r >= NS / 4))
-                next.bc[i] = load_pack<IO, 4>(static_cast<const IO*>(r < NS / 4 ? p.Bm : p.Cm) + (((size_t)b * d.T + tt + bt) * d.G + g) * d.N + s,
-                                              d.N - s, p.vecn);
-        }
-    };
-    auto turn = [&](int tt, int k) {
-        if (it < kTile) {
-            const bool live = tt + it < t1;
-            float fd[8], fx[8];
+    for (int e = 0; e < 2; ++e) bias[e] = p.dt_bias && 2 * pr + e < left ? p.dt_bias[col + 2 * pr + e] : 0.f;
 #pragma unroll
-            for (int i = 0; i < 8; i += 2) {
-                const float2 e = *reinterpret_cast<const float2*>(&sm.bias[ic + i]);
-                float2 v = make_float2(pick(next.dt, i) + e.x, pick(next.dt, i + 1) + e.y);
-                if (p.softplus) v = softplus(v.x, v.y);
-                fd[i] = live && i < left ? v.x : 0.f;
-                fd[i + 1] = live && i + 1 < left ? v.y : 0.f;
-                fx[i] = live && i < left ? v.x * pick(next.u, i) : 0.f;
-                fx[i + 1] = live && i + 1 < left ? v.y * pick(next.u, i + 1) : 0.f;
-            }
+    for (int e = 0; e < 8; ++e) skip[e] = !LOCAL && p.D && ic + e < left ? p.D[col + ic + e] : 0.f;
+    auto fetch = [&](int i) {
+        if (i < n) {
+            const int tt = t0 + i * kTile, slot = i % S::RING;
+            copy_tile<kTile, CC>(sm.u[slot], p.u, rows, d.D, tt, t1, col, left, p.rows, tid);
+            copy_tile<kTile, CC>(sm.dt[slot], p.dt, rows, d.D, tt, t1, col, left, p.rows, tid);
+            if (!LOCAL && p.z) copy_tile<kTile, CC>(sm.z[slot], p.z, rows, d.D, tt, t1, col, left, p.rows, tid);
 #pragma unroll
-            for (int i = 0; i < 8; i += 4) {
-                store_pairs(&sm.dt[k][it][(ic + i) / 2], fd[i], fd[i + 1], fd[i + 2], fd[i + 3]);
-                store_pairs(&sm.x[k][it][(ic + i) / 2], fx[i], fx[i + 1], fx[i + 2], fx[i + 3]);
+            for (int j = 0; j < NB; ++j) {                                 // four states of B or C of a token, which this thread prepares too
+                const int x = tid + j * 128, bt = x / (NS / 2), r = x % (NS / 2), s = r % (NS / 4) * 4;
+                const int have = tt + bt < t1 && !(LOCAL && r >= NS / 4) ? d.N - s : 0;
+                copy_group<4>(reinterpret_cast<IO*>(&sm.bc[slot][j][tid]),
+                              static_cast<const IO*>(r < NS / 4 ? p.Bm : p.Cm) + (have > 0 ? ((rows + tt + bt) * d.G + g) * d.N + s : 0), have, p.bc);
             }
         }
+        copy_commit();
+    };
+    // Channels past the last have u = 0 and any step; tokens past the last a step of 0.
+    auto turn = [&](int i) {
+        const int k = i & 1, slot = i % S::RING;
 #pragma unroll
-        for (int i = 0; i < NB; ++i) {
-            const int x = tid + i * 128, bt = x / (NS / 2), r = x % (NS / 2), s = r % (NS / 4) * 4;
-            f2x2* to = r < NS / 4 ? &sm.B[k][bt][s / 2] : &sm.C[k][bt][s / 2];
-            to[0] = {both(pick(next.bc[i], 0)), both(pick(next.bc[i], 1))};
-            to[1] = {both(pick(next.bc[i], 2)), both(pick(next.bc[i], 3))};
+        for (int r = 0; r < S::PASSES; ++r) {
+            const int row = first + r * S::ROWS;
+            const Pack<IO, 2> dt = load_pack<IO, 2>(&sm.dt[slot][row * CC + 2 * pr], 2, true), u = load_pack<IO, 2>(&sm.u[slot][row * CC + 2 * pr], 2, true);
+            float2 v = make_float2(pick(dt, 0) + bias[0], pick(dt, 1) + bias[1]);
+            if (p.softplus) v = softplus(v.x, v.y);
+            if (t0 + i * kTile + row >= t1) v.x = v.y = 0.f;
+            const float x0 = v.x * pick(u, 0), x1 = v.y * pick(u, 1);
+            sm.step[k][row][0][pr] = make_float4(v.x, v.y, x0, x1);
+            sm.step[k][row][1][pr] = make_float4(v.y, v.x, x1, x0);
+        }
+#pragma unroll
+        for (int j = 0; j < NB; ++j) {
+            const int x = tid + j * 128, bt = x / (NS / 2), r = x % (NS / 2), s = r % (NS / 4);
+            const Pack<IO, 4> v = sm.bc[slot][j][tid];
+            float4(&to)[2][NS / 4] = r < NS / 4 ? sm.B[k][bt] : sm.C[k][bt];
+            to[0][s] = make_float4(pick(v, 0), pick(v, 1), pick(v, 2), pick(v, 3));
+            to[1][s] = make_float4(pick(v, 2), pick(v, 3), pick(v, 0), pick(v, 1));
         }
     };
-    auto finish = [&](int tt, int k) {
-        if (!p.y || left <= 0 || tt + it >= t1) return;
+    auto finish = [&](int i) {
+        const int t = t0 + i * kTile + it, k = i & 1, slot = i % S::RING;
+        if (!p.y || it >= kTile || ic >= left || t >= t1) return;
+        const Pack<IO, 8> u = load_pack<IO, 8>(&sm.u[slot][it * CC + ic], 8, true), z = load_pack<IO, 8>(&sm.z[slot][it * CC + ic], 8, true);
         float o[8];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            float s = sm.y[k][0][it][ic + i];
+        for (int e = 0; e < 8; ++e) {
+            o[e] = sm.y[k][0][it][ic + e];
 #pragma unroll
-            for (int w = 1; w < NB; ++w) s += sm.y[k][w][it][ic + i];
-            if (p.D) s = fmaf(sm.skip[ic + i], pick(held[1].u, i), s);
-            const float zz = pick(held[1].z, i);
-            o[i] = p.z ? s * (zz * gate_sigmoid(zz)) : s;
+            for (int w = 1; w < NB; ++w) o[e] += sm.y[k][w][it][ic + e];
         }
-        store_pack(static_cast<IO*>(p.y) + ((size_t)b * d.T + tt + it) * d.D + col, narrow<IO, 8>(o), left, p.vec);
+#pragma unroll
+        for (int e = 0; e < 8; e += 2) {
+            f2 v = pack2(o[e], o[e + 1]);
+            if (p.D) v = fma2(pack2(skip[e], skip[e + 1]), pack2(pick(u, e), pick(u, e + 1)), v);
+            if (p.z) {
+                const f2 zz = pack2(pick(z, e), pick(z, e + 1));
+                const float2 den = unpack2(add2(exp2_pair(mul2(zz, both(-kLog2e))), both(1.f)));
+                v = mul2(v, mul2(zz, pack2(reciprocal(den.x), reciprocal(den.y))));
+            }
+            const float2 r = unpack2(v);
+            o[e] = r.x;
+            o[e + 1] = r.y;
+        }
+        store_pack(static_cast<IO*>(p.y) + (rows + t) * d.D + col + ic, narrow<IO, 8>(o), left - ic, p.rows == kWhole && left - ic >= 8 && (d.K * sizeof(IO)) % 16 == 0);
     };
-    fetch(t0);
-    turn(t0, 0);
-    held[0] = {next.u, next.z};
-    if (n > 1) fetch(t0 + kTile);
+#pragma unroll
+    for (int i = 0; i < S::RING - 2; ++i) fetch(i);
+    copy_wait<S::RING - 4>();                                              // tiles 0 and 1
+    prepare_barrier();
+    turn(0);
     __syncthreads();
     for (int i = 0; i < n; ++i) {
-        const int tt = t0 + i * kTile;
-        if (!LOCAL && i > 0) finish(tt - kTile, (i - 1) & 1);
-        held[1] = held[0];
-        if (i + 1 < n) {
-            turn(tt + kTile, (i + 1) & 1);
-            held[0] = {next.u, next.z};
-            if (i + 2 < n) fetch(tt + 2 * kTile);
-        }
+        if (!LOCAL && i > 0) finish(i - 1);
+        fetch(i + S::RING - 2);                                            // where a tile stood that was finished before the last barrier
+        if (i + 1 < n) turn(i + 1);
+        copy_wait<S::RING - 4>();                                          // tile i + 2, for all after the barrier
         __syncthreads();
     }
-    if (!LOCAL) finish(t0 + (n - 1) * kTile, (n - 1) & 1);
+    if (!LOCAL) finish(n - 1);
 }
 
 }  // namespace
@@ -234,7 +235,7 @@ FwdPlan fwd_plan(const qd_scan_shape& s, bool save) {
 template <typename IO, int NB>
 cudaError_t launch(P p, cudaStream_t stream) {
     const long long per = (long long)p.d.ctas * p.d.G * p.d.B;
-    constexpr size_t smem = sizeof(FwdSmem<NB>);
+    constexpr size_t smem = sizeof(FwdSmem<IO, NB>);
     cudaError_t e;
     if (p.segs > 1) {
         e = set_max_smem_once((const void*)k_scan_fwd<IO, NB, true>, smem);
@@ -264,7 +265,7 @@ cudaError_t scan_fwd(const ScanArgs& a) {
     p.saved = a.save ? reinterpret_cast<float*>(a.ws) : nullptr;
     p.ends = reinterpret_cast<float*>(a.ws + q.saved);
     p.decays = reinterpret_cast<float*>(a.ws + q.saved + q.ends);
-    p.softplus = a.softplus; p.vec = q.d.K % 8 == 0; p.vecn = a.s.N % 4 == 0;
+    p.softplus = a.softplus; p.rows = copy_of(q.d.K, a.s.dtype == QD_BF16 ? 8 : 4, a.s.dtype); p.bc = copy_of(a.s.N, 4, a.s.dtype);
     p.joined = p.segs - 1 > kMostJoined;
     return a.s.dtype == QD_BF16 ? launch<__nv_bfloat16>(p, a.stream) : launch<float>(p, a.stream);
 }
