@@ -2,8 +2,9 @@
 //   dC_t = sum_channels dy_t h_t        dB_t = sum_channels dt_t u_t g_t        du = dt <g, B> + D dy
 //   ddt = u <g, B> + <g p, A>           dA = sum_t dt g p                       dh0 = a_1 g_1,   dz = dy y_raw SiLU'(z).
 // The forward saved the state before every kSave-th token; from the last such tile to the first the states of its tokens are walked anew,
-// a_t and p_t of all of them kept in registers (p, not h - dt u B, so that a small p keeps its precision), and then g is walked back.
-// Per token, channel and state one exponential and 13 operations of the fp32 pipe: bound by that pipe and by what is issued beside it.
+// a_t and h_{t-1} kept in registers, and then g is walked back, (a g) h_{t-1} being g p.  The registers hold half a tile; the first half is
+// walked once more ahead, to the state in the middle (a state saved every fourth token would be 134 MB more for each 8192 x 2048 x 16).
+// Per token, channel and state 1.5 exponentials and 13 operations of the fp32 pipe: bound by what is issued.
 #include "scan.cuh"
 
 namespace qd {
@@ -11,21 +12,28 @@ namespace {
 using namespace scan;
 
 constexpr unsigned kAll = 0xffffffffu;
-constexpr int kWalkRegs = 184, kPrepareRegs = 72;          // of 2 x 128: what the launch gives a pair of threads, one of each role
+constexpr int kHalf = kSave / 2;             // tokens whose a_t, h_{t-1} are in registers at a time
 
-template <int NB> struct BwdSmem {
+template <typename IO, int NB> struct BwdSmem {
     static constexpr int CC = kWalkers / NB * kWarpChannels, NS = NB * kWarpStates;
-    float4 dt[2][kSave][CC / 2], x[2][kSave][CC / 2], dy[2][kSave][CC / 2];      // every pair of channels in both orders
-    f2x2 B[2][kSave][NS / 2], C[2][kSave][NS / 2];         // each state's value twice
+    static constexpr int PAIRS = CC / 2, ROWS = 128 / PAIRS, PASSES = ROWS < kSave ? kSave / ROWS : 1;     // who prepares: a pair of channels, PASSES tokens
+    static constexpr int RING = sizeof(IO) == 2 ? 5 : 4;   // tiles of what is copied: the one walked before, this, the next two, bf16 one more
+    static constexpr int SAVED = 4;
+    static constexpr int BC = kSave * 2 * NS / 4, BCT = (BC + 127) / 128;         // groups of four states of B and C of a tile; of a thread
+    float4 step[2][kSave][2][PAIRS];                       // dt, dt, dt u, dt u of a pair of channels, in both orders
+    float4 dy[2][kSave][PAIRS];                            // dy of a pair of channels in both orders
+    float4 B[2][kSave][2][NS / 4], C[2][kSave][2][NS / 4]; // four states, the pairs in both orders
     float gB[2][NB][kSave][CC], gpA[2][NB][kSave][CC], y[2][NB][kSave][CC];
     float bc[2][kWalkers][kSave][32];                      // dB, dC summed over a warp's channels
-    float bias[CC], skip[CC];
+    f2x2 saved[SAVED][2][128];                             // of a thread that walks
+    alignas(16) IO u[RING][kSave * CC], dt[RING][kSave * CC], z[RING][kSave * CC], gy[RING][kSave * CC];
+    Pack<IO, 4> rbc[RING][BCT][128];
 };
 
 template <typename IO, int NB, bool LOCAL>
 __global__ void __launch_bounds__(kThreads, 2) k_scan_bwd(const P p) {
-    using S = BwdSmem<NB>;
-    constexpr int CW = kWalkers / NB, CC = S::CC, NS = S::NS, K = kSave;
+    using S = BwdSmem<IO, NB>;
+    constexpr int CW = kWalkers / NB, CC = S::CC, NS = S::NS, K = kSave, H = kHalf;
     extern __shared__ __align__(16) unsigned char raw_smem[];
     S& sm = *reinterpret_cast<S*>(raw_smem);
     sm100::grid_dep_wait();
@@ -41,256 +49,276 @@ __global__ void __launch_bounds__(kThreads, 2) k_scan_bwd(const P p) {
     const size_t part = (size_t)seg * d.B + b;
 
     if (warp < kWalkers) {
-        // ---- walk ----------------------------------------------------------------------------------------------------------
-        if constexpr (!LOCAL) asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kWalkRegs));
+        // ---- walk, from the last tile to the first ----------------------------------------------------------------------------
         const Map m(lane);
         const int wc = warp % CW, wb = warp / CW, n0 = wb * kWarpStates, ch = ct * CC + wc * kWarpChannels;
-        const size_t mine = (((size_t)g * d.ctas + ct) * kWalkers + warp) * kWarpTile + lane * 8;
-        f2 A2[4], ga[4] = {0, 0, 0, 0}, dA[4] = {0, 0, 0, 0}, sum = 0;     // ga = a_{t+1} g_{t+1}
-        load_decay(p, m, g, ch, n0, A2);
+        const size_t mine = (((size_t)g * d.ctas + ct) * kWalkers + warp) * kWarpTile + lane * 8, state = (size_t)b * d.D * d.N;
+        f2 A2[4], ga[4] = {0, 0, 0, 0}, dA[4] = {0, 0, 0, 0};              // ga = a_{t+1} g_{t+1}
+        float sum[2] = {0.f, 0.f};
+        load_state(p, m, p.A, g, ch, n0, kLog2e, A2);
         if (seg == p.segs - 1) {
-            if (p.dhT) load_state(p, m, p.dhT, b, g, ch, n0, ga);
+            if (p.dhT) load_state(p, m, p.dhT + state, g, ch, n0, 1.f, ga);
         } else if (!LOCAL) load_end(p, p.segs - 2, -1, p.segs - 1 - seg, b, mine, ga);
         const float* saved = LOCAL ? nullptr : p.saved + ((size_t)b * ((d.T + K - 1) / K) + t0 / K) * d.states + mine;
-        f2 h[4];
-        if (!LOCAL) load_tile(saved + (size_t)(n - 1) * d.states, h);
+        auto fetch = [&](int i) {                          // the state before tile i, three tiles ahead
+            if (i >= 0)
+#pragma unroll
+                for (int e = 0; e < 2; ++e) copy_bytes<16>(&sm.saved[i % S::SAVED][e][threadIdx.x], saved + (size_t)i * d.states + 4 * e, 16);
+            copy_commit();
+        };
+        if (!LOCAL)
+#pragma unroll
+            for (int e = 1; e < S::SAVED; ++e) fetch(n - e);
+        const int pair = wc * (kWarpChannels / 2) + (lane >> 2), quad = n0 / 4 + m.q;
+        const bool odd = lane & 4, up = lane & 16, second = m.q & 2;
         __syncthreads();
         for (int i = n - 1; i >= 0; --i) {
             const int k = i & 1;
-            const f2 *dt = reinterpret_cast<const f2*>(sm.dt[k]) + wc * kWarpChannels + m.at, *x = reinterpret_cast<const f2*>(sm.x[k]) + wc * kWarpChannels + m.at;
-            const f2* dy = reinterpret_cast<const f2*>(sm.dy[k]) + wc * kWarpChannels + m.at;
-            const f2x2 *B = &sm.B[k][0][n0 / 2], *C = &sm.C[k][0][n0 / 2];
+            const float4 *step = &sm.step[k][0][m.order][pair], *B = &sm.B[k][0][m.swap][quad], *C = &sm.C[k][0][m.swap][quad];
+            const float2* dy = reinterpret_cast<const float2*>(&sm.dy[k][0][pair]) + m.order;
             if constexpr (LOCAL) {
 #pragma unroll
                 for (int t = K - 1; t >= 0; --t) {
-                    const f2 vd = dt[t * CC], vy = dy[t * CC];
-                    const f2x2 c0 = C[t * (NS / 2) + m.pair[0]], c1 = C[t * (NS / 2) + m.pair[1]];
-                    const f2 vc[4] = {c0.a, c0.b, c1.a, c1.b};
+                    const float4 v = step[t * 2 * S::PAIRS], c4 = C[t * 2 * (NS / 4)];
+                    const float2 vy = dy[t * 2 * S::PAIRS];
+                    const f2 dt[2] = {both(v.x), both(v.y)}, gy[2] = {both(vy.x), both(vy.y)}, vc[2] = {pack2(c4.x, c4.y), pack2(c4.z, c4.w)};
 #pragma unroll
-                    for (int j = 0; j < 4; ++j) ga[j] = mul2(exp2_pair(mul2(vd, A2[j])), fma2(vy, vc[j], ga[j]));
-                    sum = add2(sum, vd);
+                    for (int j = 0; j < 4; ++j) ga[j] = mul2(exp2_pair(mul2(dt[j >> 1], A2[j])), fma2(gy[j >> 1], vc[j & 1], ga[j]));
+                    sum[0] += v.x;
+                    sum[1] += v.y;
                 }
             } else {
-                f2 a[K][4], pr[K][4], tA[4];
+                copy_wait<S::SAVED - 2>();
+                const f2x2 s0 = sm.saved[i % S::SAVED][0][threadIdx.x], s1 = sm.saved[i % S::SAVED][1][threadIdx.x];
+                f2 hs[4] = {s0.a, s0.b, s1.a, s1.b}, hm[4] = {s0.a, s0.b, s1.a, s1.b}, tA[4] = {0, 0, 0, 0};
+                fetch(i - (S::SAVED - 1));
 #pragma unroll
-                for (int t = 0; t < K; ++t) {
-                    const f2 vd = dt[t * CC], vx = x[t * CC];
-                    const f2x2 b0 = B[t * (NS / 2) + m.pair[0]], b1 = B[t * (NS / 2) + m.pair[1]];
-                    const f2 vb[4] = {b0.a, b0.b, b1.a, b1.b};
+                for (int t = 0; t < H; ++t) {              // the state in the middle of the tile
+                    const float4 v = step[t * 2 * S::PAIRS], b4 = B[t * 2 * (NS / 4)];
+                    const f2 dt[2] = {both(v.x), both(v.y)}, x[2] = {both(v.z), both(v.w)}, vb[2] = {pack2(b4.x, b4.y), pack2(b4.z, b4.w)};
 #pragma unroll
-                    for (int j = 0; j < 4; ++j) {
-                        a[t][j] = exp2_pair(mul2(vd, A2[j]));
-                        pr[t][j] = mul2(a[t][j], h[j]);
-                        h[j] = fma2(vx, vb[j], pr[t][j]);
+                    for (int j = 0; j < 4; ++j) hm[j] = fma2(exp2_pair(mul2(dt[j >> 1], A2[j])), hm[j], mul2(x[j >> 1], vb[j & 1]));
+                }
+                auto half = [&](int base, f2(&h)[4]) {
+                    f2 a[H][4], hp[H][4];
+#pragma unroll
+                    for (int t = 0; t < H; ++t) {
+                        const float4 v = step[(base + t) * 2 * S::PAIRS], b4 = B[(base + t) * 2 * (NS / 4)];
+                        const f2 dt[2] = {both(v.x), both(v.y)}, x[2] = {both(v.z), both(v.w)}, vb[2] = {pack2(b4.x, b4.y), pack2(b4.z, b4.w)};
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) {
+                            a[t][j] = exp2_pair(mul2(dt[j >> 1], A2[j]));
+                            hp[t][j] = h[j];
+                            h[j] = fma2(a[t][j], h[j], mul2(x[j >> 1], vb[j & 1]));
+                        }
                     }
-                }
-                // stored when the tile is done: nothing stands in the way of the loads till then
-                float held = 0.f, out_bc[K], out_g[K], out_y[K / 2];
-                const bool odd = lane & 4, up = lane & 16, second = m.q & 2;
+                    // stored when the half is done: nothing stands in the way of the loads till then
+                    float held = 0.f, out_bc[H], out_g[H], out_y[H / 2];
 #pragma unroll
-                for (int t = K - 1; t >= 0; --t) {
-                    const f2 vd = dt[t * CC], vx = x[t * CC], vy = dy[t * CC];
-                    const f2x2 b0 = B[t * (NS / 2) + m.pair[0]], b1 = B[t * (NS / 2) + m.pair[1]];
-                    const f2x2 c0 = C[t * (NS / 2) + m.pair[0]], c1 = C[t * (NS / 2) + m.pair[1]];
-                    const f2 vb[4] = {b0.a, b0.b, b1.a, b1.b}, vc[4] = {c0.a, c0.b, c1.a, c1.b};
-                    const float2 xs = unpack2(vx), ys = unpack2(vy);
-                    f2 r1 = 0, r2 = 0, r3 = 0;
-                    float vB[4], vC[4];
+                    for (int t = H - 1; t >= 0; --t) {
+                        const int tt = base + t;
+                        const float4 v = step[tt * 2 * S::PAIRS], b4 = B[tt * 2 * (NS / 4)], c4 = C[tt * 2 * (NS / 4)];
+                        const float2 vy = dy[tt * 2 * S::PAIRS];
+                        const f2 dt[2] = {both(v.x), both(v.y)}, x[2] = {both(v.z), both(v.w)}, gy[2] = {both(vy.x), both(vy.y)};
+                        const f2 vb[2] = {pack2(b4.x, b4.y), pack2(b4.z, b4.w)}, vc[2] = {pack2(c4.x, c4.y), pack2(c4.z, c4.w)};
+                        f2 gB[2], gC[2], r1[2], r2[2], r3[2];
 #pragma unroll
-                    for (int j = 0; j < 4; ++j) {
-                        const f2 ht = fma2(vx, vb[j], pr[t][j]), gt = fma2(vy, vc[j], ga[j]), gp = mul2(gt, pr[t][j]);
-                        const float2 hs = unpack2(ht), gs = unpack2(gt);
-                        vB[j] = fmaf(gs.y, xs.y, gs.x * xs.x);
-                        vC[j] = fmaf(hs.y, ys.y, hs.x * ys.x);
-                        r1 = j ? fma2(gt, vb[j], r1) : mul2(gt, vb[j]);
-                        r2 = j ? fma2(gp, A2[j], r2) : mul2(gp, A2[j]);
-                        r3 = j ? fma2(ht, vc[j], r3) : mul2(ht, vc[j]);
-                        tA[j] = t == K - 1 ? mul2(gp, vd) : fma2(gp, vd, tA[j]);
-                        ga[j] = mul2(gt, a[t][j]);
+                        for (int c = 0; c < 2; ++c)
+#pragma unroll
+                            for (int e = 0; e < 2; ++e) {
+                                const int j = 2 * c + e;
+                                const f2 ht = t == H - 1 ? h[j] : hp[t + 1 < H ? t + 1 : 0][j], gt = fma2(gy[c], vc[e], ga[j]);
+                                ga[j] = mul2(gt, a[t][j]);
+                                const f2 gp = mul2(ga[j], hp[t][j]);
+                                gB[e] = c ? fma2(gt, x[c], gB[e]) : mul2(gt, x[c]);
+                                gC[e] = c ? fma2(ht, gy[c], gC[e]) : mul2(ht, gy[c]);
+                                r1[c] = e ? fma2(gt, vb[e], r1[c]) : mul2(gt, vb[e]);
+                                r2[c] = e ? fma2(gp, A2[j], r2[c]) : mul2(gp, A2[j]);
+                                r3[c] = e ? fma2(ht, vc[e], r3[c]) : mul2(ht, vc[e]);
+                                tA[j] = fma2(gp, dt[c], tA[j]);
+                            }
+                        // dB, dC over the eight lanes of equal q: a lane keeps its first pair of states, of that the state c & 1, of dB and
+                        // dC that of c / 4
+                        const float2 B0 = unpack2(gB[0]), B1 = unpack2(gB[1]), C0 = unpack2(gC[0]), C1 = unpack2(gC[1]);
+                        float w0 = B0.x + __shfl_xor_sync(kAll, B1.x, 8), w1 = B0.y + __shfl_xor_sync(kAll, B1.y, 8);
+                        const float kB = (odd ? w1 : w0) + __shfl_xor_sync(kAll, odd ? w0 : w1, 4);
+                        w0 = C0.x + __shfl_xor_sync(kAll, C1.x, 8);
+                        w1 = C0.y + __shfl_xor_sync(kAll, C1.y, 8);
+                        const float kC = (odd ? w1 : w0) + __shfl_xor_sync(kAll, odd ? w0 : w1, 4);
+                        out_bc[t] = (up ? kC : kB) + __shfl_xor_sync(kAll, up ? kB : kC, 16);
+                        // <g, B>, <g p, A>, <C, h> over the four lanes of equal c: a lane keeps its first channel, of the first two that of
+                        // q / 2; of the third it keeps one of two tokens
+                        const float k1 = sum_pair(r1[0]) + __shfl_xor_sync(kAll, sum_pair(r1[1]), 1);
+                        const float k2 = sum_pair(r2[0]) + __shfl_xor_sync(kAll, sum_pair(r2[1]), 1);
+                        const float k3 = sum_pair(r3[0]) + __shfl_xor_sync(kAll, sum_pair(r3[1]), 1);
+                        out_g[t] = (second ? k2 : k1) + __shfl_xor_sync(kAll, second ? k1 : k2, 2);
+                        if (t & 1) held = k3;
+                        else out_y[t / 2] = (second ? held : k3) + __shfl_xor_sync(kAll, second ? k3 : held, 2);
                     }
-                    // dB, dC over the eight lanes of equal q: a lane keeps its first pair of states, of that the state c & 1, of dB and dC
-                    // that of c / 4
-                    float w0 = vB[0] + __shfl_xor_sync(kAll, vB[2], 8), w1 = vB[1] + __shfl_xor_sync(kAll, vB[3], 8);
-                    const float kB = (odd ? w1 : w0) + __shfl_xor_sync(kAll, odd ? w0 : w1, 4);
-                    w0 = vC[0] + __shfl_xor_sync(kAll, vC[2], 8);
-                    w1 = vC[1] + __shfl_xor_sync(kAll, vC[3], 8);
-                    const float kC = (odd ? w1 : w0) + __shfl_xor_sync(kAll, odd ? w0 : w1, 4);
-                    out_bc[t] = (up ? kC : kB) + __shfl_xor_sync(kAll, up ? kB : kC, 16);
-                    // <g, B>, <g p, A>, <C, h> over the four lanes of equal c: a lane keeps its first channel, of the first two that of q / 2;
-                    // of the third it keeps one of two tokens
-                    const float2 e1 = unpack2(r1), e2 = unpack2(r2), e3 = unpack2(r3);
-                    const float k1 = e1.x + __shfl_xor_sync(kAll, e1.y, 1), k2 = e2.x + __shfl_xor_sync(kAll, e2.y, 1);
-                    const float k3 = e3.x + __shfl_xor_sync(kAll, e3.y, 1);
-                    out_g[t] = (second ? k2 : k1) + __shfl_xor_sync(kAll, second ? k1 : k2, 2);
-                    if (t & 1) held = k3;
-                    else out_y[t / 2] = (second ? held : k3) + __shfl_xor_sync(kAll, second ? k3 : held, 2);
-                    // the tile before: its state, in the registers of tokens that are done
-                    if (t == K / 2 && i > 0) load_tile(saved + (size_t)(i - 1) * d.states, h);
-                }
-                float* g_to = &(second ? sm.gpA : sm.gB)[k][wb][0][wc * kWarpChannels + m.lo];
-                float* bc_to = &sm.bc[k][warp][0][(up ? 16 : 0) + 2 * m.pair[0] + (odd ? 1 : 0)];
+                    float* g_to = &(second ? sm.gpA : sm.gB)[k][wb][base][wc * kWarpChannels + m.ch[0]];
+                    float* bc_to = &sm.bc[k][warp][base][(up ? 16 : 0) + m.state(0, odd ? 1 : 0)];
 #pragma unroll
-                for (int t = 0; t < K; ++t) {
-                    bc_to[t * 32] = out_bc[t];
-                    g_to[t * CC] = out_g[t];
-                    if (!(t & 1)) sm.y[k][wb][t + (m.q >> 1)][wc * kWarpChannels + m.lo] = out_y[t / 2];
-                }
+                    for (int t = 0; t < H; ++t) {
+                        bc_to[t * 32] = out_bc[t];
+                        g_to[t * CC] = out_g[t];
+                        if (!(t & 1)) sm.y[k][wb][base + t + (m.q >> 1)][wc * kWarpChannels + m.ch[0]] = out_y[t / 2];
+                    }
+                };
+                half(H, hm);
+                half(0, hs);
 #pragma unroll
                 for (int j = 0; j < 4; ++j) dA[j] = add2(dA[j], tA[j]);    // a tile's sum first: 2000 tokens one by one lose two digits
             }
             __syncthreads();
         }
-        if (LOCAL) store_end(p, seg - 1, b, mine, ga, A2, sum);
-        else {
-            // [part][D][N]: the state of sequence `part`
-            store_state(p, m, p.pA + (part - b) * d.D * d.N, b, g, ch, n0, dA);
-            if (seg == 0 && p.dh0) store_state(p, m, p.dh0, b, g, ch, n0, ga);
+        if (LOCAL) {
+            store_end(p, seg - 1, b, mine, ga, A2, sum);
+            return;
         }
-        if (!LOCAL) {
-            __syncthreads();
-            __syncthreads();
-        }
+        store_state(p, m, p.pA + part * d.D * d.N, g, ch, n0, dA);
+        if (seg == 0 && p.dh0) store_state(p, m, p.dh0 + state, g, ch, n0, ga);
         return;
     }
     // ---- prepare tiles, write gradients ---------------------------------------------------------------------------------------
-    if constexpr (!LOCAL) asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kPrepareRegs));
-    constexpr int BCT = (NB + 1) / 2;                                      // groups of four states of B and C that a thread stages
     const int tid = threadIdx.x - 32 * kWalkers;
-    const int it = tid / (CC / 4), ic = tid % (CC / 4) * 4;                // a token of the tile, four channels of the CTA's
-    const int left = it < K ? d.K - ct * CC - ic : 0;
-    const size_t col = (size_t)g * d.K + ct * CC + ic;
-    if (tid < CC) {                                        // read by this half of the CTA only
-        const bool in = ct * CC + tid < d.K;
-        sm.bias[tid] = p.dt_bias && in ? p.dt_bias[(size_t)g * d.K + ct * CC + tid] : 0.f;
-        sm.skip[tid] = p.D && in ? p.D[(size_t)g * d.K + ct * CC + tid] : 0.f;
+    const size_t rows = (size_t)b * d.T, col = (size_t)g * d.K + ct * CC;
+    const int left = d.K - ct * CC;
+    // a tile is prepared by pairs of channels and written out by groups of four (where NB > 1 some threads have none)
+    const int pr = tid % S::PAIRS, first = tid / S::PAIRS, it = tid / (CC / 4), ic = tid % (CC / 4) * 4;
+    float bias2[2], bias[4], skip[4], sumD[4] = {0.f, 0.f, 0.f, 0.f}, sumb[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int e = 0; e < 2; ++e) bias2[e] = p.dt_bias && 2 * pr + e < left ? p.dt_bias[col + 2 * pr + e] : 0.f;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+        bias[e] = p.dt_bias && ic + e < left ? p.dt_bias[col + ic + e] : 0.f;
+        skip[e] = !LOCAL && p.D && ic + e < left ? p.D[col + ic + e] : 0.f;
     }
-    asm volatile("bar.sync 1, %0;" ::"n"(kThreads / 2) : "memory");
-    struct Raw { Pack<IO, 4> u, dt, z, y; } next, held[2];                 // held: of the tiles i, i + 1
-    Pack<IO, 4> bc[BCT];
-    float sumD[4] = {0.f, 0.f, 0.f, 0.f}, sumb[4] = {0.f, 0.f, 0.f, 0.f};
-    next.u = next.dt = next.z = next.y = zero_pack<IO, 4>();
-    auto fetch = [&](int tt) {
-        const int t = tt + it;
-        if (left > 0 && t < t1) {
-            const size_t at = ((size_t)b * d.T + t) * d.D + col;
-            if (!LOCAL) next.u = load_pack<IO, 4>(static_cast<const IO*>(p.u) + at, left, p.vec);
-            next.dt = load_pack<IO, 4>(static_cast<const IO*>(p.dt) + at, left, p.vec);
-            next.y = load_pack<IO, 4>(static_cast<const IO*>(p.dy) + at, left, p.vec);
-            if (p.z) next.z = load_pack<IO, 4>(static_cast<const IO*>(p.z) + at, left, p.vec);
-        }
+    auto fetch = [&](int i) {
+        if (i >= 0) {
+            const int tt = t0 + i * K, slot = i % S::RING;
+            if (!LOCAL) copy_tile<K, CC>(sm.u[slot], p.u, rows, d.D, tt, t1, col, left, p.rows, tid);
+            copy_tile<K, CC>(sm.dt[slot], p.dt, rows, d.D, tt, t1, col, left, p.rows, tid);
+            copy_tile<K, CC>(sm.gy[slot], p.dy, rows, d.D, tt, t1, col, left, p.rows, tid);
+            if (p.z) copy_tile<K, CC>(sm.z[slot], p.z, rows, d.D, tt, t1, col, left, p.rows, tid);
 #pragma unroll
-        for (int i = 0; i < BCT; ++i) {
-            const int x = tid + i * 128, bt = x / (NS / 2), r = x % (NS / 2), s = r % (NS / 4) * 4;
-            bc[i] = zero_pack<IO, 4>();
-            if (bt < K && tt + bt < t1 && s < d.N && !(LOCAL && r < NS / 4))
-                bc[i] = load_pack<IO, 4>(static_cast<const IO*>(r < NS / 4 ? p.Bm : p.Cm) + (((size_t)b * d.T + tt + bt) * d.G + g) * d.N + s,
-                                         d.N - s, p.vecn);
-        }
-    };
-    auto turn = [&](int tt, int k) {
-        if (it < K) {
-            const bool live = tt + it < t1;
-            float fd[4], fx[4], fy[4];
-#pragma unroll
-            for (int i = 0; i < 4; i += 2) {
-                const float2 bi = *reinterpret_cast<const float2*>(&sm.bias[ic + i]);
-                float2 v = make_float2(pick(next.dt, i) + bi.x, pick(next.dt, i + 1) + bi.y);
-                if (p.softplus) v = softplus(v.x, v.y);
-                const float e[2] = {v.x, v.y};
-#pragma unroll
-                for (int o = 0; o < 2; ++o) {
-                    const bool on = live && i + o < left;
-                    const float z = pick(next.z, i + o), y = pick(next.y, i + o);
-                    fd[i + o] = on ? e[o] : 0.f;
-                    fx[i + o] = on && !LOCAL ? e[o] * pick(next.u, i + o) : 0.f;
-                    fy[i + o] = on ? (p.z ? y * (z * gate_sigmoid(z)) : y) : 0.f;
-                }
+            for (int j = 0; j < S::BCT; ++j) {                             // four states of B or C of a token, which this thread prepares too
+                const int x = tid + j * 128, bt = x / (NS / 2), r = x % (NS / 2), s = r % (NS / 4) * 4;
+                if (bt >= K) break;
+                const int have = tt + bt < t1 && !(LOCAL && r < NS / 4) ? d.N - s : 0;
+                copy_group<4>(reinterpret_cast<IO*>(&sm.rbc[slot][j][tid]),
+                              static_cast<const IO*>(r < NS / 4 ? p.Bm : p.Cm) + (have > 0 ? ((rows + tt + bt) * d.G + g) * d.N + s : 0), have, p.bc);
             }
-            store_pairs(&sm.dt[k][it][ic / 2], fd[0], fd[1], fd[2], fd[3]);
-            if (!LOCAL) store_pairs(&sm.x[k][it][ic / 2], fx[0], fx[1], fx[2], fx[3]);
-            store_pairs(&sm.dy[k][it][ic / 2], fy[0], fy[1], fy[2], fy[3]);
+        }
+        copy_commit();
+    };
+    // Channels past the last have u = dy = 0 and any step; tokens past the last a step of 0.
+    auto turn = [&](int i) {
+        const int k = i & 1, slot = i % S::RING;
+#pragma unroll
+        for (int r = 0; r < S::PASSES; ++r) {
+            const int row = first + r * S::ROWS, at = row * CC + 2 * pr;
+            if (S::ROWS > K && row >= K) break;
+            const Pack<IO, 2> dt = load_pack<IO, 2>(&sm.dt[slot][at], 2, true), gy = load_pack<IO, 2>(&sm.gy[slot][at], 2, true);
+            const Pack<IO, 2> u = LOCAL ? dt : load_pack<IO, 2>(&sm.u[slot][at], 2, true);
+            float2 v = make_float2(pick(dt, 0) + bias2[0], pick(dt, 1) + bias2[1]), y = make_float2(pick(gy, 0), pick(gy, 1));
+            if (p.softplus) v = softplus(v.x, v.y);
+            if (t0 + i * K + row >= t1) v.x = v.y = 0.f;
+            if (p.z) {
+                const Pack<IO, 2> z = load_pack<IO, 2>(&sm.z[slot][at], 2, true);
+                const float z0 = pick(z, 0), z1 = pick(z, 1);
+                y.x *= z0 * gate_sigmoid(z0);
+                y.y *= z1 * gate_sigmoid(z1);
+            }
+            const float x0 = v.x * pick(u, 0), x1 = v.y * pick(u, 1);
+            sm.step[k][row][0][pr] = make_float4(v.x, v.y, x0, x1);
+            sm.step[k][row][1][pr] = make_float4(v.y, v.x, x1, x0);
+            sm.dy[k][row][pr] = make_float4(y.x, y.y, y.y, y.x);
         }
 #pragma unroll
-        for (int i = 0; i < BCT; ++i) {
-            const int x = tid + i * 128, bt = x / (NS / 2), r = x % (NS / 2), s = r % (NS / 4) * 4;
-            if (bt >= K) continue;
-            f2x2* to = r < NS / 4 ? &sm.B[k][bt][s / 2] : &sm.C[k][bt][s / 2];
-            to[0] = {both(pick(bc[i], 0)), both(pick(bc[i], 1))};
-            to[1] = {both(pick(bc[i], 2)), both(pick(bc[i], 3))};
+        for (int j = 0; j < S::BCT; ++j) {
+            const int x = tid + j * 128, bt = x / (NS / 2), r = x % (NS / 2), s = r % (NS / 4);
+            if (bt >= K) break;
+            const Pack<IO, 4> v = sm.rbc[slot][j][tid];
+            float4(&to)[2][NS / 4] = r < NS / 4 ? sm.B[k][bt] : sm.C[k][bt];
+            to[0][s] = make_float4(pick(v, 0), pick(v, 1), pick(v, 2), pick(v, 3));
+            to[1][s] = make_float4(pick(v, 2), pick(v, 3), pick(v, 0), pick(v, 1));
         }
     };
-    // of a tile that has been walked; it is prepared over only afterwards, and a thread reads what it wrote there itself
-    auto finish = [&](int tt, int k) {
-        if (left > 0 && tt + it < t1) {
-            const Raw& r = held[1];
-            const float4 d0 = sm.dt[k][it][ic / 2], d1 = sm.dt[k][it][ic / 2 + 1], y0 = sm.dy[k][it][ic / 2], y1 = sm.dy[k][it][ic / 2 + 1];
-            const float vdt[4] = {d0.x, d0.y, d1.x, d1.y}, vdy[4] = {y0.x, y0.y, y1.x, y1.y};
+    auto finish = [&](int i) {                             // of a tile that has been walked
+        const int t = t0 + i * K + it, k = i & 1, slot = i % S::RING;
+        if (it < K && ic < left && t < t1) {
+            const int at = it * CC + ic;
+            const Pack<IO, 4> u = load_pack<IO, 4>(&sm.u[slot][at], 4, true), gy = load_pack<IO, 4>(&sm.gy[slot][at], 4, true);
+            const Pack<IO, 4> dt = load_pack<IO, 4>(&sm.dt[slot][at], 4, true), z = load_pack<IO, 4>(&sm.z[slot][at], 4, true);
+            const float4 s0 = sm.step[k][it][0][ic / 2], s1 = sm.step[k][it][0][ic / 2 + 1], y0 = sm.dy[k][it][ic / 2], y1 = sm.dy[k][it][ic / 2 + 1];
+            const float vdt[4] = {s0.x, s0.y, s1.x, s1.y}, vdy[4] = {y0.x, y0.y, y1.x, y1.y};
             float odu[4], odt[4], odz[4];
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
+            for (int e = 0; e < 4; ++e) {
                 float e1 = 0.f, e2 = 0.f, ey = 0.f;
 #pragma unroll
-                for (int w = 0; w < NB; ++w) { e1 += sm.gB[k][w][it][ic + i]; e2 += sm.gpA[k][w][it][ic + i]; ey += sm.y[k][w][it][ic + i]; }
-                const float uu = pick(r.u, i), sk = sm.skip[ic + i];
-                odu[i] = fmaf(e1, vdt[i], sk * vdy[i]);
-                odt[i] = fmaf(e1, uu, e2 * kLn2);
-                if (p.softplus) odt[i] *= gate_sigmoid(pick(r.dt, i) + sm.bias[ic + i]);
-                sumD[i] = fmaf(vdy[i], uu, sumD[i]);
-                sumb[i] += odt[i];
-                const float zz = pick(r.z, i), sg = gate_sigmoid(zz);
-                odz[i] = pick(r.y, i) * fmaf(sk, uu, ey) * (sg * fmaf(zz, 1.f - sg, 1.f));
+                for (int w = 0; w < NB; ++w) { e1 += sm.gB[k][w][it][ic + e]; e2 += sm.gpA[k][w][it][ic + e]; ey += sm.y[k][w][it][ic + e]; }
+                const float uu = pick(u, e);
+                odu[e] = fmaf(e1, vdt[e], skip[e] * vdy[e]);
+                odt[e] = fmaf(e1, uu, e2 * kLn2);
+                if (p.softplus) odt[e] *= gate_sigmoid(pick(dt, e) + bias[e]);
+                sumD[e] = fmaf(vdy[e], uu, sumD[e]);
+                sumb[e] += odt[e];
+                if (p.z) {
+                    const float zz = pick(z, e), sg = gate_sigmoid(zz);
+                    odz[e] = pick(gy, e) * fmaf(skip[e], uu, ey) * (sg * fmaf(zz, 1.f - sg, 1.f));
+                }
             }
-            const size_t at = ((size_t)b * d.T + tt + it) * d.D + col;
-            store_pack(static_cast<IO*>(p.du) + at, narrow<IO, 4>(odu), left, p.vec);
-            store_pack(static_cast<IO*>(p.ddt) + at, narrow<IO, 4>(odt), left, p.vec);
-            if (p.z) store_pack(static_cast<IO*>(p.dz) + at, narrow<IO, 4>(odz), left, p.vec);
+            const size_t to = (rows + t) * d.D + col + ic;
+            const bool whole = p.rows == kWhole;
+            store_pack(static_cast<IO*>(p.du) + to, narrow<IO, 4>(odu), left - ic, whole);
+            store_pack(static_cast<IO*>(p.ddt) + to, narrow<IO, 4>(odt), left - ic, whole);
+            if (p.z) store_pack(static_cast<IO*>(p.dz) + to, narrow<IO, 4>(odz), left - ic, whole);
         }
-        const size_t rows = (size_t)d.B * d.T * d.G * d.N;
+        const size_t all = (size_t)d.B * d.T * d.G * d.N;
 #pragma unroll
         for (int x = tid; x < K * 2 * NS; x += 128) {
-            const int t = x / (2 * NS), which = x / NS % 2, s = x % NS;
-            if (tt + t >= t1 || s >= d.N) continue;
+            const int tk = x / (2 * NS), which = x / NS % 2, s = x % NS, tt = t0 + i * K + tk;
+            if (tt >= t1 || s >= d.N) continue;
             float v = 0.f;
 #pragma unroll
-            for (int w = 0; w < CW; ++w) v += sm.bc[k][s / kWarpStates * CW + w][t][which * 16 + s % kWarpStates];
-            p.pBC[((size_t)ct * 2 + which) * rows + (((size_t)b * d.T + tt + t) * d.G + g) * d.N + s] = v;
+            for (int w = 0; w < CW; ++w) v += sm.bc[k][s / kWarpStates * CW + w][tk][which * 16 + s % kWarpStates];
+            p.pBC[((size_t)ct * 2 + which) * all + ((rows + tt) * d.G + g) * d.N + s] = v;
         }
     };
-    fetch(t0 + (n - 1) * K);
-    turn(t0 + (n - 1) * K, (n - 1) & 1);
-    held[0] = next;
-    if (n > 1) fetch(t0 + (n - 2) * K);
+#pragma unroll
+    for (int e = 1; e <= S::RING - 2; ++e) fetch(n - e);
+    copy_wait<S::RING - 4>();                                              // the first two tiles
+    prepare_barrier();
+    turn(n - 1);
     __syncthreads();
     for (int i = n - 1; i >= 0; --i) {
-        const int tt = t0 + i * K;
-        if (!LOCAL && i < n - 1) finish(tt + K, (i + 1) & 1);
-        held[1] = held[0];
-        if (i > 0) {
-            turn(tt - K, (i - 1) & 1);
-            held[0] = next;
-            if (i > 1) fetch(tt - 2 * K);
-        }
+        if (!LOCAL && i < n - 1) finish(i + 1);
+        fetch(i - (S::RING - 2));                                          // where a tile stood that was finished before the last barrier
+        prepare_barrier();                                                 // the next tile takes the place of the one that is finished now
+        if (i > 0) turn(i - 1);
+        copy_wait<S::RING - 4>();                                          // tile i - 2, for all after the barrier
         __syncthreads();
     }
     if (LOCAL) return;
-    finish(t0, 0);
-    // sums over the tokens of a channel: the rows of a tile in order (the walkers are at the same barriers)
-    float* cols = reinterpret_cast<float*>(sm.x);
-    __syncthreads();
+    finish(0);
+    // sums over the tokens of a channel: the rows of a tile in order
+    float* cols = reinterpret_cast<float*>(sm.step);
+    prepare_barrier();
     if (it < K)
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            cols[it * CC + ic + i] = sumD[i];
-            cols[(K + it) * CC + ic + i] = sumb[i];
+        for (int e = 0; e < 4; ++e) {
+            cols[it * CC + ic + e] = sumD[e];
+            cols[(K + it) * CC + ic + e] = sumb[e];
         }
-    __syncthreads();
+    prepare_barrier();
     for (int x = tid; x < 2 * CC; x += 128) {
         const int which = x / CC, c = x % CC;
-        if (ct * CC + c >= d.K) continue;
+        if (c >= left) continue;
         float v = 0.f;
 #pragma unroll
         for (int r = 0; r < K; ++r) v += cols[(which * K + r) * CC + c];
-        p.pD[(part * 2 + which) * d.D + (size_t)g * d.K + ct * CC + c] = v;
+        p.pD[(part * 2 + which) * d.D + col + c] = v;
     }
 }
 
@@ -325,7 +353,7 @@ BwdPlan bwd_plan(const qd_scan_shape& s) {
 template <typename IO, int NB>
 cudaError_t launch(const P& p, cudaStream_t stream) {
     const long long per = (long long)p.d.ctas * p.d.G * p.d.B;
-    constexpr size_t smem = sizeof(BwdSmem<NB>);
+    constexpr size_t smem = sizeof(BwdSmem<IO, NB>);
     cudaError_t e;
     if (p.segs > 1) {
         e = set_max_smem_once((const void*)k_scan_bwd<IO, NB, true>, smem);
@@ -363,7 +391,7 @@ cudaError_t scan_bwd(const ScanArgs& a) {
     p.pA = reinterpret_cast<float*>(w); w += q.pA;
     p.pD = reinterpret_cast<float*>(w); w += q.pD;
     p.pBC = reinterpret_cast<float*>(w);
-    p.softplus = a.softplus; p.vec = q.d.K % 4 == 0; p.vecn = a.s.N % 4 == 0;
+    p.softplus = a.softplus; p.rows = copy_of(q.d.K, a.s.dtype == QD_BF16 ? 8 : 4, a.s.dtype); p.bc = copy_of(a.s.N, 4, a.s.dtype);
     p.joined = p.segs - 1 > kMostJoined;
     cudaError_t e = a.s.dtype == QD_BF16 ? launch<__nv_bfloat16>(p, a) : launch<float>(p, a);
     if (e != cudaSuccess) return e;
