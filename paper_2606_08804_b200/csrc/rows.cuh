@@ -113,6 +113,16 @@ __device__ __forceinline__ float exp2_unit(float x) {
     return y;
 }
 
+// BYTES on their way to shared memory, zeros where `bytes` is 0; committed in groups, of which all but the last N have come after a wait.
+template <int BYTES>
+__device__ __forceinline__ void copy_bytes(void* dst, const void* src, int bytes) {
+    const uint32_t d = sm100::smem_u32(dst);
+    if constexpr (BYTES == 16) asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(d), "l"(src), "r"(bytes) : "memory");
+    else asm volatile("cp.async.ca.shared.global [%0], [%1], %2, %3;" ::"r"(d), "l"(src), "n"(BYTES), "r"(bytes) : "memory");
+}
+__device__ __forceinline__ void copy_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N> __device__ __forceinline__ void copy_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
+
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 __device__ __forceinline__ float reciprocal(float x) {
     float y;

@@ -169,12 +169,6 @@ __device__ __forceinline__ void load_end(const P& p, int from, int step, int n, 
     }
 }
 // N neighbouring elements on their way to shared memory: those from `left` on are 0.  kSingle waits for them.
-template <int BYTES>
-__device__ __forceinline__ void copy_bytes(void* dst, const void* src, int bytes) {
-    const uint32_t d = sm100::smem_u32(dst);
-    if constexpr (BYTES == 16) asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(d), "l"(src), "r"(bytes) : "memory");
-    else asm volatile("cp.async.ca.shared.global [%0], [%1], %2, %3;" ::"r"(d), "l"(src), "n"(BYTES), "r"(bytes) : "memory");
-}
 template <int N, typename IO>
 __device__ __forceinline__ void copy_group(IO* dst, const IO* src, int left, int how) {
     constexpr int BYTES = N * sizeof(IO);
@@ -200,9 +194,6 @@ __device__ __forceinline__ void copy_tile(IO* dst, const void* src, size_t row0,
         copy_group<E>(dst + x * E, static_cast<const IO*>(src) + (have > 0 ? (row0 + t) * D + col + c : 0), have, how);
     }
 }
-__device__ __forceinline__ void copy_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
-template <int N> __device__ __forceinline__ void copy_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
-
 __device__ __forceinline__ void prepare_barrier() { asm volatile("bar.sync 1, 128;" ::: "memory"); }     // the half that prepares
 __device__ __forceinline__ float sum_pair(f2 v) {
     const float2 t = unpack2(v);
