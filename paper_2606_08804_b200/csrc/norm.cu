@@ -26,7 +26,7 @@ struct NormP {
 constexpr __host__ __device__ int norm_threads(int tpr) { return tpr > 256 ? tpr : 256; }
 // CTAs to an SM that the register budget is made for, for K groups of V columns to a thread
 constexpr __host__ __device__ int norm_resident(int k, int v, int tpr, bool bwd) {
-    return tpr > 256 ? 1 : bwd ? (k * v <= 8 ? 3 : k * v <= 16 ? 2 : 1) : (k * v <= 8 ? 4 : k * v <= 32 ? 3 : 2);
+    return tpr > 256 ? 1 : bwd ? (k * v < 8 ? 3 : k * v <= 16 ? 2 : 1) : (k * v <= 8 ? 4 : k * v <= 16 ? 3 : 2);
 }
 
 // Sums of v[0 .. M) over the TPR threads of a row, the same bits in each of them.  One barrier: `turn` alternates between two halves of red,

@@ -19,7 +19,7 @@ struct StepsP {
 };
 
 template <typename IO, int LN, int R>
-__global__ void __launch_bounds__(256) k_scan_steps(const StepsP p) {
+__global__ void __launch_bounds__(256, 4) k_scan_steps(const StepsP p) {
     constexpr int M = R > LN ? R / LN : 1;                 // sequences whose channel a lane does alone: l, l + LN, ..
     sm100::grid_dep_wait();
     sm100::grid_dep_launch();
