@@ -63,7 +63,8 @@ struct P {
     float *saved;                            // [B][ceil(T / kSave)][states]: state before every kSave-th token
     float *ends, *decays;                    // [segs - 1][B][states]: states (gradients) at segments' ends, exp(A sum dt) of segments
     float *pA, *pD;                          // partial gradients of A [segs][B][D N], of D and dt_bias [segs][B][2][D]
-    float *pBC;                              // of B and C [ctas][2][B T G N]
+    float *pBC;                              // of B and C [ctas][2][bcs]
+    size_t bcs;                              // B T G N
     bool softplus;
     int rows, bc;                            // how rows and those of B, C are copied (Copy)
     bool joined;                             // the ends are those of the true states already
@@ -182,16 +183,20 @@ __device__ __forceinline__ void copy_group(IO* dst, const IO* src, int left, int
         for (int o = 0; o < N; ++o) st(dst, o, o < left ? ld(src, o) : 0.f);
     }
 }
-// Tile of TT tokens (from tt, below `end`) x CC channels (from col, `left` of them) of a tensor [T, D], by 128 threads; row major.
-template <int TT, int CC, typename IO>
-__device__ __forceinline__ void copy_tile(IO* dst, const void* src, size_t row0, int D, int tt, int end, size_t col, int left, int how, int tid) {
-    constexpr int E = 16 / sizeof(IO), CH = TT * CC / E;
+// Tiles of TT tokens (from tt, below `end`) x CC channels (from col, `left` of them) of NA tensors [T, D] (absent ones null), row major, by
+// 128 threads, which share out the tensors where a tile is fewer than 128 groups of 16 bytes.
+template <int TT, int CC, typename IO, int NA>
+__device__ __forceinline__ void copy_tiles(IO* const (&dst)[NA], const void* const (&src)[NA], size_t row0, int D, int tt, int end, size_t col, int left,
+                                           int how, int tid) {
+    constexpr int E = 16 / sizeof(IO), CH = TT * CC / E, SETS = CH < 128 ? 128 / CH : 1;
 #pragma unroll
     for (int j = 0; j < (CH + 127) / 128; ++j) {
-        const int x = tid + j * 128, t = tt + x / (CC / E), c = x % (CC / E) * E;
-        if (CH % 128 != 0 && x >= CH) break;
+        const int x = SETS > 1 ? tid % CH : tid + j * 128, t = tt + x / (CC / E), c = x % (CC / E) * E;
         const int have = t < end ? left - c : 0;
-        copy_group<E>(dst + x * E, static_cast<const IO*>(src) + (have > 0 ? (row0 + t) * D + col + c : 0), have, how);
+        const size_t at = have > 0 ? (row0 + t) * D + col + c : 0;
+#pragma unroll
+        for (int a = 0; a < NA; ++a)
+            if (src[a] && (SETS == 1 || a % SETS == tid / CH)) copy_group<E>(dst[a] + x * E, static_cast<const IO*>(src[a]) + at, have, how);
     }
 }
 __device__ __forceinline__ void prepare_barrier() { asm volatile("bar.sync 1, 128;" ::: "memory"); }     // the half that prepares

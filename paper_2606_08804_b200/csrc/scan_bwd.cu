@@ -12,6 +12,7 @@ namespace {
 using namespace scan;
 
 constexpr unsigned kAll = 0xffffffffu;
+constexpr int kWalkRegs = 152, kPrepareRegs = 104;         // of 2 x 128: what the launch gives a pair of threads, one of each half of the CTA
 constexpr int kHalf = kSave / 2;             // tokens whose a_t, h_{t-1} are in registers at a time
 
 template <typename IO, int NB> struct BwdSmem {
@@ -23,8 +24,8 @@ template <typename IO, int NB> struct BwdSmem {
     float4 step[2][kSave][2][PAIRS];                       // dt, dt, dt u, dt u of a pair of channels, in both orders
     float4 dy[2][kSave][PAIRS];                            // dy of a pair of channels in both orders
     float4 B[2][kSave][2][NS / 4], C[2][kSave][2][NS / 4]; // four states, the pairs in both orders
-    float gB[2][NB][kSave][CC], gpA[2][NB][kSave][CC], y[2][NB][kSave][CC];
-    float bc[2][kWalkers][kSave][32];                      // dB, dC summed over a warp's channels
+    alignas(16) float gB[2][NB][kSave][CC], gpA[2][NB][kSave][CC], y[2][NB][kSave][CC];
+    alignas(16) float bc[2][kWalkers][kSave][32];          // dB, dC summed over a warp's channels
     f2x2 saved[SAVED][2][128];                             // of a thread that walks
     alignas(16) IO u[RING][kSave * CC], dt[RING][kSave * CC], z[RING][kSave * CC], gy[RING][kSave * CC];
     Pack<IO, 4> rbc[RING][BCT][128];
@@ -50,6 +51,7 @@ __global__ void __launch_bounds__(kThreads, 2) k_scan_bwd(const P p) {
 
     if (warp < kWalkers) {
         // ---- walk, from the last tile to the first ----------------------------------------------------------------------------
+        if constexpr (!LOCAL) asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kWalkRegs));
         const Map m(lane);
         const int wc = warp % CW, wb = warp / CW, n0 = wb * kWarpStates, ch = ct * CC + wc * kWarpChannels;
         const size_t mine = (((size_t)g * d.ctas + ct) * kWalkers + warp) * kWarpTile + lane * 8, state = (size_t)b * d.D * d.N;
@@ -180,6 +182,7 @@ __global__ void __launch_bounds__(kThreads, 2) k_scan_bwd(const P p) {
         return;
     }
     // ---- prepare tiles, write gradients ---------------------------------------------------------------------------------------
+    if constexpr (!LOCAL) asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kPrepareRegs));
     const int tid = threadIdx.x - 32 * kWalkers;
     const size_t rows = (size_t)b * d.T, col = (size_t)g * d.K + ct * CC;
     const int left = d.K - ct * CC;
@@ -196,10 +199,8 @@ __global__ void __launch_bounds__(kThreads, 2) k_scan_bwd(const P p) {
     auto fetch = [&](int i) {
         if (i >= 0) {
             const int tt = t0 + i * K, slot = i % S::RING;
-            if (!LOCAL) copy_tile<K, CC>(sm.u[slot], p.u, rows, d.D, tt, t1, col, left, p.rows, tid);
-            copy_tile<K, CC>(sm.dt[slot], p.dt, rows, d.D, tt, t1, col, left, p.rows, tid);
-            copy_tile<K, CC>(sm.gy[slot], p.dy, rows, d.D, tt, t1, col, left, p.rows, tid);
-            if (p.z) copy_tile<K, CC>(sm.z[slot], p.z, rows, d.D, tt, t1, col, left, p.rows, tid);
+            copy_tiles<K, CC, IO, 4>({sm.u[slot], sm.dt[slot], sm.z[slot], sm.gy[slot]}, {LOCAL ? nullptr : p.u, p.dt, p.z, p.dy}, rows, d.D, tt, t1, col, left,
+                                     p.rows, tid);
 #pragma unroll
             for (int j = 0; j < S::BCT; ++j) {                             // four states of B or C of a token, which this thread prepares too
                 const int x = tid + j * 128, bt = x / (NS / 2), r = x % (NS / 2), s = r % (NS / 4) * 4;
@@ -252,21 +253,26 @@ __global__ void __launch_bounds__(kThreads, 2) k_scan_bwd(const P p) {
             const Pack<IO, 4> dt = load_pack<IO, 4>(&sm.dt[slot][at], 4, true), z = load_pack<IO, 4>(&sm.z[slot][at], 4, true);
             const float4 s0 = sm.step[k][it][0][ic / 2], s1 = sm.step[k][it][0][ic / 2 + 1], y0 = sm.dy[k][it][ic / 2], y1 = sm.dy[k][it][ic / 2 + 1];
             const float vdt[4] = {s0.x, s0.y, s1.x, s1.y}, vdy[4] = {y0.x, y0.y, y1.x, y1.y};
-            float odu[4], odt[4], odz[4];
+            float odu[4], odt[4], odz[4], g1[4] = {0.f, 0.f, 0.f, 0.f}, g2[4] = {0.f, 0.f, 0.f, 0.f}, gy4[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int w = 0; w < NB; ++w) {
+                const float4 a = *reinterpret_cast<const float4*>(&sm.gB[k][w][it][ic]), c = *reinterpret_cast<const float4*>(&sm.gpA[k][w][it][ic]);
+                const float4 f = *reinterpret_cast<const float4*>(&sm.y[k][w][it][ic]);
+                g1[0] += a.x; g1[1] += a.y; g1[2] += a.z; g1[3] += a.w;
+                g2[0] += c.x; g2[1] += c.y; g2[2] += c.z; g2[3] += c.w;
+                gy4[0] += f.x; gy4[1] += f.y; gy4[2] += f.z; gy4[3] += f.w;
+            }
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
-                float e1 = 0.f, e2 = 0.f, ey = 0.f;
-#pragma unroll
-                for (int w = 0; w < NB; ++w) { e1 += sm.gB[k][w][it][ic + e]; e2 += sm.gpA[k][w][it][ic + e]; ey += sm.y[k][w][it][ic + e]; }
                 const float uu = pick(u, e);
-                odu[e] = fmaf(e1, vdt[e], skip[e] * vdy[e]);
-                odt[e] = fmaf(e1, uu, e2 * kLn2);
+                odu[e] = fmaf(g1[e], vdt[e], skip[e] * vdy[e]);
+                odt[e] = fmaf(g1[e], uu, g2[e] * kLn2);
                 if (p.softplus) odt[e] *= gate_sigmoid(pick(dt, e) + bias[e]);
                 sumD[e] = fmaf(vdy[e], uu, sumD[e]);
                 sumb[e] += odt[e];
                 if (p.z) {
                     const float zz = pick(z, e), sg = gate_sigmoid(zz);
-                    odz[e] = pick(gy, e) * fmaf(skip[e], uu, ey) * (sg * fmaf(zz, 1.f - sg, 1.f));
+                    odz[e] = pick(gy, e) * fmaf(skip[e], uu, gy4[e]) * (sg * fmaf(zz, 1.f - sg, 1.f));
                 }
             }
             const size_t to = (rows + t) * d.D + col + ic;
@@ -275,15 +281,21 @@ __global__ void __launch_bounds__(kThreads, 2) k_scan_bwd(const P p) {
             store_pack(static_cast<IO*>(p.ddt) + to, narrow<IO, 4>(odt), left - ic, whole);
             if (p.z) store_pack(static_cast<IO*>(p.dz) + to, narrow<IO, 4>(odz), left - ic, whole);
         }
-        const size_t all = (size_t)d.B * d.T * d.G * d.N;
+        // dB, dC of the CTA's channels: four states of a token
 #pragma unroll
-        for (int x = tid; x < K * 2 * NS; x += 128) {
-            const int tk = x / (2 * NS), which = x / NS % 2, s = x % NS, tt = t0 + i * K + tk;
-            if (tt >= t1 || s >= d.N) continue;
-            float v = 0.f;
+        for (int j = 0; j < S::BCT; ++j) {
+            const int x = tid + j * 128, tk = x / (NS / 2), which = x / (NS / 4) % 2, s = x % (NS / 4) * 4, tt = t0 + i * K + tk;
+            if (tk >= K || tt >= t1 || s >= d.N) continue;
+            float v[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-            for (int w = 0; w < CW; ++w) v += sm.bc[k][s / kWarpStates * CW + w][tk][which * 16 + s % kWarpStates];
-            p.pBC[((size_t)ct * 2 + which) * all + ((rows + tt) * d.G + g) * d.N + s] = v;
+            for (int w = 0; w < CW; ++w) {
+                const float4 a = *reinterpret_cast<const float4*>(&sm.bc[k][s / kWarpStates * CW + w][tk][which * 16 + s % kWarpStates]);
+                v[0] += a.x; v[1] += a.y; v[2] += a.z; v[3] += a.w;
+            }
+            Pack<float, 4> o;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) o.w[e] = __float_as_uint(v[e]);
+            store_pack(p.pBC + ((size_t)ct * 2 + which) * p.bcs + ((rows + tt) * d.G + g) * d.N + s, o, d.N - s, p.bc == kWhole);
         }
     };
 #pragma unroll
@@ -391,6 +403,7 @@ cudaError_t scan_bwd(const ScanArgs& a) {
     p.pA = reinterpret_cast<float*>(w); w += q.pA;
     p.pD = reinterpret_cast<float*>(w); w += q.pD;
     p.pBC = reinterpret_cast<float*>(w);
+    p.bcs = (size_t)a.s.B * a.s.T * a.s.G * a.s.N;
     p.softplus = a.softplus; p.rows = copy_of(q.d.K, a.s.dtype == QD_BF16 ? 8 : 4, a.s.dtype); p.bc = copy_of(a.s.N, 4, a.s.dtype);
     p.joined = p.segs - 1 > kMostJoined;
     cudaError_t e = a.s.dtype == QD_BF16 ? launch<__nv_bfloat16>(p, a) : launch<float>(p, a);

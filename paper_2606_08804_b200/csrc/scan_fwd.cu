@@ -13,7 +13,7 @@ template <typename IO, int NB> struct FwdSmem {
     static constexpr int RING = sizeof(IO) == 2 ? 5 : 4;   // tiles of what is copied: i - 1 (for y), i, i + 1 (prepared now), i + 2 (has come), fp32 no more
     float4 step[2][kTile][2][PAIRS];                       // dt, dt, dt u, dt u of a pair of channels, in both orders
     float4 B[2][kTile][2][NS / 4], C[2][kTile][2][NS / 4]; // four states, the pairs in both orders
-    float y[2][NB][kTile][CC];
+    alignas(16) float y[2][NB][kTile][CC];
     alignas(16) IO u[RING][kTile * CC], dt[RING][kTile * CC], z[RING][kTile * CC];
     Pack<IO, 4> bc[RING][NB][128];
 };
@@ -101,9 +101,7 @@ __global__ void __launch_bounds__(kThreads, 2) k_scan_fwd(const P p) {
     auto fetch = [&](int i) {
         if (i < n) {
             const int tt = t0 + i * kTile, slot = i % S::RING;
-            copy_tile<kTile, CC>(sm.u[slot], p.u, rows, d.D, tt, t1, col, left, p.rows, tid);
-            copy_tile<kTile, CC>(sm.dt[slot], p.dt, rows, d.D, tt, t1, col, left, p.rows, tid);
-            if (!LOCAL && p.z) copy_tile<kTile, CC>(sm.z[slot], p.z, rows, d.D, tt, t1, col, left, p.rows, tid);
+            copy_tiles<kTile, CC, IO, 3>({sm.u[slot], sm.dt[slot], sm.z[slot]}, {p.u, p.dt, LOCAL ? nullptr : p.z}, rows, d.D, tt, t1, col, left, p.rows, tid);
 #pragma unroll
             for (int j = 0; j < NB; ++j) {                                 // four states of B or C of a token, which this thread prepares too
                 const int x = tid + j * 128, bt = x / (NS / 2), r = x % (NS / 2), s = r % (NS / 4) * 4;
@@ -141,13 +139,14 @@ __global__ void __launch_bounds__(kThreads, 2) k_scan_fwd(const P p) {
         const int t = t0 + i * kTile + it, k = i & 1, slot = i % S::RING;
         if (!p.y || it >= kTile || ic >= left || t >= t1) return;
         const Pack<IO, 8> u = load_pack<IO, 8>(&sm.u[slot][it * CC + ic], 8, true), z = load_pack<IO, 8>(&sm.z[slot][it * CC + ic], 8, true);
-        float o[8];
+        float o[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            o[e] = sm.y[k][0][it][ic + e];
+        for (int w = 0; w < NB; ++w)
 #pragma unroll
-            for (int w = 1; w < NB; ++w) o[e] += sm.y[k][w][it][ic + e];
-        }
+            for (int e = 0; e < 8; e += 4) {
+                const float4 v = *reinterpret_cast<const float4*>(&sm.y[k][w][it][ic + e]);
+                o[e] += v.x; o[e + 1] += v.y; o[e + 2] += v.z; o[e + 3] += v.w;
+            }
 #pragma unroll
         for (int e = 0; e < 8; e += 2) {
             f2 v = pack2(o[e], o[e + 1]);
