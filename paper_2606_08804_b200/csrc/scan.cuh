@@ -10,7 +10,7 @@
 // instead of the states: 20, which alone bounded the kernel).
 // Sums over the states (y, du, ddt) are over 4 lanes, sums over the channels (dB, dC) over 8.  In such a sum a lane keeps a part and hands
 // the rest on; so that it keeps the part that it has in the same register whichever lane it is, the channels of a pair are swapped where q
-// is odd and the pairs of states where c & 2 (Map), and shared memory holds both orders.
+// is odd and, backward, the pairs of states where c & 2 (Map), and shared memory holds both orders.
 //
 // Roles.  Half of a CTA's warps walk the tokens.  The other half turns dt, u, z, dy of the tile after theirs into what the walk needs
 // (softplus, products, gates) in shared memory, in fp32, and writes out what the tile before left there; what it reads is copied to shared
@@ -34,7 +34,7 @@ constexpr int kWalkers = 4;                  // warps of a CTA that walk; as man
 constexpr int kThreads = 2 * 32 * kWalkers;
 constexpr int kSave = 8;                     // tokens from one saved state to the next, and of a tile, backward
 constexpr int kTile = 16;                    // tokens of a tile, forward
-constexpr size_t kWarpTile = kWarpChannels * kWarpStates;          // states of a warp, in the order [lane][state][channel of the pair]
+constexpr size_t kWarpTile = kWarpChannels * kWarpStates;          // states of a warp, in the order [lane][channel][state]
 
 // What both directions derive from the shape.
 struct Dims {
@@ -101,13 +101,13 @@ __device__ __forceinline__ float2 softplus(float x, float y) {
 // What a walking lane owns.  Registers [channel][pair of states], flat.
 struct Map {
     int q, ch[2], order, swap;               // its channels in the warp's 16; which order of a record it reads, of channels and of pairs of states
-    __device__ __forceinline__ explicit Map(int lane) {
+    __device__ __forceinline__ Map(int lane, bool backward) {
         q = lane & 3;
         const int c = lane >> 2;
         order = q & 1;
         ch[0] = 2 * c + order;
         ch[1] = 2 * c + 1 - order;
-        swap = c >> 1 & 1;
+        swap = backward ? c >> 1 & 1 : 0;
     }
     __device__ __forceinline__ int state(int pair, int e) const { return 4 * q + 2 * (pair ^ swap) + e; }       // in the warp's 16
 };

@@ -52,7 +52,7 @@ __global__ void __launch_bounds__(kThreads, 2) k_scan_bwd(const P p) {
     if (warp < kWalkers) {
         // ---- walk, from the last tile to the first ----------------------------------------------------------------------------
         if constexpr (!LOCAL) asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kWalkRegs));
-        const Map m(lane);
+        const Map m(lane, true);
         const int wc = warp % CW, wb = warp / CW, n0 = wb * kWarpStates, ch = ct * CC + wc * kWarpChannels;
         const size_t mine = (((size_t)g * d.ctas + ct) * kWalkers + warp) * kWarpTile + lane * 8, state = (size_t)b * d.D * d.N;
         f2 A2[4], ga[4] = {0, 0, 0, 0}, dA[4] = {0, 0, 0, 0};              // ga = a_{t+1} g_{t+1}
@@ -91,8 +91,10 @@ __global__ void __launch_bounds__(kThreads, 2) k_scan_bwd(const P p) {
                 }
             } else {
                 copy_wait<S::SAVED - 2>();
-                const f2x2 s0 = sm.saved[i % S::SAVED][0][threadIdx.x], s1 = sm.saved[i % S::SAVED][1][threadIdx.x];
-                f2 hs[4] = {s0.a, s0.b, s1.a, s1.b}, hm[4] = {s0.a, s0.b, s1.a, s1.b}, tA[4] = {0, 0, 0, 0};
+                f2 hs[4], hm[4], tA[4] = {0, 0, 0, 0};
+#pragma unroll
+                for (int j = 0; j < 4; ++j)                // the forward has the pairs of states in their order
+                    hs[j] = hm[j] = reinterpret_cast<const f2*>(&sm.saved[i % S::SAVED][j >> 1][threadIdx.x])[(j & 1) ^ m.swap];
                 fetch(i - (S::SAVED - 1));
 #pragma unroll
                 for (int t = 0; t < H; ++t) {              // the state in the middle of the tile

@@ -7,18 +7,30 @@ namespace qd {
 namespace {
 using namespace scan;
 
+// 2^x of a pair, for |x| < 1/16 by the series of the exponential, whose rounding to nearest has no bias: what the special function unit gives
+// there is 5e-9 to 2e-8 too small on average, a decay of almost 1 is applied a thousand times, and the gradient of A grows with the
+// square of that (1.8e-6 of it off instead of 1.1e-6, fp32 sums of the definition 0.9e-6).
+__device__ __forceinline__ f2 exp2_pair_near(f2 x) {
+    f2 p = fma2(x, both(9.61812911e-3f), both(5.55041087e-2f));            // (ln 2)^k / k!
+    p = fma2(x, p, both(2.40226507e-1f));
+    p = fma2(x, p, both(6.93147181e-1f));
+    const float2 near = unpack2(fma2(x, p, both(1.f))), far = unpack2(exp2_pair(x)), t = unpack2(x);
+    return pack2(fabsf(t.x) < 0.0625f ? near.x : far.x, fabsf(t.y) < 0.0625f ? near.y : far.y);
+}
+
 template <typename IO, int NB> struct FwdSmem {
     static constexpr int CC = kWalkers / NB * kWarpChannels, NS = NB * kWarpStates;
     static constexpr int PAIRS = CC / 2, ROWS = 128 / PAIRS, PASSES = kTile / ROWS;      // of a thread that prepares: a pair of channels, PASSES tokens
     static constexpr int RING = sizeof(IO) == 2 ? 5 : 4;   // tiles of what is copied: i - 1 (for y), i, i + 1 (prepared now), i + 2 (has come), fp32 no more
     float4 step[2][kTile][2][PAIRS];                       // dt, dt, dt u, dt u of a pair of channels, in both orders
-    float4 B[2][kTile][2][NS / 4], C[2][kTile][2][NS / 4]; // four states, the pairs in both orders
+    float4 B[2][kTile][NS / 4], C[2][kTile][NS / 4];       // four states
     alignas(16) float y[2][NB][kTile][CC];
     alignas(16) IO u[RING][kTile * CC], dt[RING][kTile * CC], z[RING][kTile * CC];
     Pack<IO, 4> bc[RING][NB][128];
 };
 
-template <typename IO, int NB, bool LOCAL>
+// SAVE: for a backward; then the first two of a lane's states, which are the slow ones where A grows along a row, have the closer exponential.
+template <typename IO, int NB, bool LOCAL, bool SAVE>
 __global__ void __launch_bounds__(kThreads, 2) k_scan_fwd(const P p) {
     using S = FwdSmem<IO, NB>;
     constexpr int CW = kWalkers / NB, CC = S::CC, NS = S::NS;
@@ -37,7 +49,7 @@ __global__ void __launch_bounds__(kThreads, 2) k_scan_fwd(const P p) {
 
     if (warp < kWalkers) {
         // ---- walk ----------------------------------------------------------------------------------------------------------
-        const Map m(lane);
+        const Map m(lane, false);
         const int wc = warp % CW, wb = warp / CW, n0 = wb * kWarpStates, ch = ct * CC + wc * kWarpChannels;
         const size_t mine = (((size_t)g * d.ctas + ct) * kWalkers + warp) * kWarpTile + lane * 8, state = (size_t)b * d.D * d.N;
         f2 A2[4], h[4] = {0, 0, 0, 0};
@@ -46,28 +58,31 @@ __global__ void __launch_bounds__(kThreads, 2) k_scan_fwd(const P p) {
         if (seg == 0) {
             if (p.h0) load_state(p, m, p.h0 + state, g, ch, n0, 1.f, h);
         } else if (!LOCAL) load_end(p, 0, 1, seg, b, mine, h);
-        float* saved = p.saved ? p.saved + ((size_t)b * ((d.T + kSave - 1) / kSave) + t0 / kSave) * d.states + mine : nullptr;
+        float* saved = SAVE ? p.saved + ((size_t)b * ((d.T + kSave - 1) / kSave) + t0 / kSave) * d.states + mine : nullptr;
         const int pair = wc * (kWarpChannels / 2) + (lane >> 2), quad = n0 / 4 + m.q;
         __syncthreads();
         for (int i = 0; i < n; ++i) {
             const int k = i & 1;
-            const float4 *step = &sm.step[k][0][m.order][pair], *B = &sm.B[k][0][m.swap][quad], *C = &sm.C[k][0][m.swap][quad];
+            const float4 *step = &sm.step[k][0][m.order][pair], *B = &sm.B[k][0][quad], *C = &sm.C[k][0][quad];
             float out[kTile / 2], held[2];                 // stored when the tile is done: nothing stands in the way of the loads till then
 #pragma unroll
             for (int t = 0; t < kTile; ++t) {
-                if (!LOCAL && saved && t % kSave == 0 && t0 + i * kTile + t < t1) {
+                if (SAVE && !LOCAL && t % kSave == 0 && t0 + i * kTile + t < t1) {
                     store_tile(saved, h);
                     saved += d.states;
                 }
-                const float4 v = step[t * 2 * S::PAIRS], vb = B[t * 2 * (NS / 4)];
+                const float4 v = step[t * 2 * S::PAIRS], vb = B[t * (NS / 4)];
                 const f2 dt[2] = {both(v.x), both(v.y)}, x[2] = {both(v.z), both(v.w)}, bp[2] = {pack2(vb.x, vb.y), pack2(vb.z, vb.w)};
 #pragma unroll
-                for (int j = 0; j < 4; ++j) h[j] = fma2(exp2_pair(mul2(dt[j >> 1], A2[j])), h[j], mul2(x[j >> 1], bp[j & 1]));
+                for (int j = 0; j < 4; ++j) {
+                    const f2 arg = mul2(dt[j >> 1], A2[j]);
+                    h[j] = fma2(SAVE && !(j & 1) ? exp2_pair_near(arg) : exp2_pair(arg), h[j], mul2(x[j >> 1], bp[j & 1]));
+                }
                 if (LOCAL) {
                     sum[0] += v.x;
                     sum[1] += v.y;
                 } else {
-                    const float4 vc = C[t * 2 * (NS / 4)];
+                    const float4 vc = C[t * (NS / 4)];
                     const f2 cp[2] = {pack2(vc.x, vc.y), pack2(vc.z, vc.w)};
                     const float y0 = sum_pair(fma2(h[1], cp[1], mul2(h[0], cp[0]))), y1 = sum_pair(fma2(h[3], cp[1], mul2(h[2], cp[0])));
                     // over the four lanes: a lane keeps its first channel, then of two tokens that of its q / 2
@@ -130,9 +145,7 @@ __global__ void __launch_bounds__(kThreads, 2) k_scan_fwd(const P p) {
         for (int j = 0; j < NB; ++j) {
             const int x = tid + j * 128, bt = x / (NS / 2), r = x % (NS / 2), s = r % (NS / 4);
             const Pack<IO, 4> v = sm.bc[slot][j][tid];
-            float4(&to)[2][NS / 4] = r < NS / 4 ? sm.B[k][bt] : sm.C[k][bt];
-            to[0][s] = make_float4(pick(v, 0), pick(v, 1), pick(v, 2), pick(v, 3));
-            to[1][s] = make_float4(pick(v, 2), pick(v, 3), pick(v, 0), pick(v, 1));
+            (r < NS / 4 ? sm.B[k][bt] : sm.C[k][bt])[s] = make_float4(pick(v, 0), pick(v, 1), pick(v, 2), pick(v, 3));
         }
     };
     auto finish = [&](int i) {
@@ -231,21 +244,24 @@ FwdPlan fwd_plan(const qd_scan_shape& s, bool save) {
     return q;
 }
 
-template <typename IO, int NB>
-cudaError_t launch(P p, cudaStream_t stream) {
+template <typename IO, int NB, bool SAVE>
+cudaError_t launch(const P& p, cudaStream_t stream) {
     const long long per = (long long)p.d.ctas * p.d.G * p.d.B;
     constexpr size_t smem = sizeof(FwdSmem<IO, NB>);
+    const auto local = k_scan_fwd<IO, NB, true, SAVE>, all = k_scan_fwd<IO, NB, false, SAVE>;
     cudaError_t e;
     if (p.segs > 1) {
-        e = set_max_smem_once((const void*)k_scan_fwd<IO, NB, true>, smem);
-        if (e == cudaSuccess)
-            e = launch_overlapped(k_scan_fwd<IO, NB, true>, dim3((unsigned)(per * (p.segs - 1))), dim3(kThreads), smem, stream, p);
+        e = set_max_smem_once((const void*)local, smem);
+        if (e == cudaSuccess) e = launch_overlapped(local, dim3((unsigned)(per * (p.segs - 1))), dim3(kThreads), smem, stream, p);
         if (e == cudaSuccess && p.joined) e = join(p.ends, p.decays, p.segs - 1, 0, 1, (size_t)p.d.B * p.d.states, stream);
         if (e != cudaSuccess) return e;
     }
-    e = set_max_smem_once((const void*)k_scan_fwd<IO, NB, false>, smem);
-    if (e != cudaSuccess) return e;
-    return launch_overlapped(k_scan_fwd<IO, NB, false>, dim3((unsigned)(per * p.segs)), dim3(kThreads), smem, stream, p);
+    e = set_max_smem_once((const void*)all, smem);
+    return e != cudaSuccess ? e : launch_overlapped(all, dim3((unsigned)(per * p.segs)), dim3(kThreads), smem, stream, p);
+}
+template <typename IO, int NB>
+cudaError_t launch(const P& p, cudaStream_t stream) {
+    return p.saved ? launch<IO, NB, true>(p, stream) : launch<IO, NB, false>(p, stream);
 }
 template <typename IO>
 cudaError_t launch(const P& p, cudaStream_t stream) {
