@@ -3,6 +3,8 @@
 // tensors, in the current stream of that device, whichever device is current.
 #include "marshal.h"
 
+#include <torch/csrc/autograd/functions/basic_ops.h>
+
 #include <array>
 #include <climits>
 
@@ -49,6 +51,24 @@ struct On {
     at::Tensor make(c10::IntArrayRef shape, at::ScalarType dt) const { return at::Tensor(at::detail::empty_cuda(shape, dt, dev, std::nullopt)); }
 };
 
+// Gradients of parameters, fp32, side by side in one allocation: one conversion takes all of them to another type.
+struct Params {
+    at::Tensor all;
+    int64_t at = 0;
+    Params(const On& on, std::initializer_list<int64_t> sizes) {
+        int64_t n = 0;
+        for (const int64_t s : sizes) n += (s + 3) / 4 * 4;
+        all = on.make({n}, at::kFloat);
+    }
+    at::Tensor next(c10::IntArrayRef shape) {              // each 16-byte aligned
+        int64_t n = 1;
+        for (const int64_t s : shape) n *= s;
+        const at::Tensor t = all.narrow(0, at, n).view(shape);
+        at += (n + 3) / 4 * 4;
+        return t;
+    }
+};
+
 // ---- convolution --------------------------------------------------------------------------------------------------------
 struct Conv {
     On on;
@@ -80,7 +100,7 @@ std::pair<at::Tensor, at::Tensor> conv_forward(const at::Tensor& x, const at::Te
              "qdelta_conv_fwd");
     return {y, last};
 }
-struct ConvGrads { at::Tensor dx, dw, dbias, dstate; };
+struct ConvGrads { at::Tensor dx, dw, dbias, dstate, params; };
 ConvGrads conv_backward(const at::Tensor& x, const at::Tensor& w, const at::Tensor* bias, const at::Tensor* state, const at::Tensor& dy,
                         const at::Tensor* dlast, bool want_dstate, unsigned flags) {
     const Conv c(x, w, bias);
@@ -91,8 +111,10 @@ ConvGrads conv_backward(const at::Tensor& x, const at::Tensor& w, const at::Tens
     const at::Tensor ws = c.on.make({(int64_t)n}, at::kByte);
     ConvGrads g;
     g.dx = c.on.make({c.B, c.T, c.D}, c.dt);
-    g.dw = c.on.make({c.D, c.W}, at::kFloat);
-    if (bias) g.dbias = c.on.make({c.D}, at::kFloat);
+    Params params(c.on, {c.D * c.W, bias ? c.D : 0});
+    g.params = params.all;
+    g.dw = params.next({c.D, c.W});
+    if (bias) g.dbias = params.next({c.D});
     if (want_dstate) g.dstate = c.on.make(c.state(), c.dt);
     rc_check(qdelta_conv_bwd(c.b, c.t, c.d, c.w, c.code, c.xp, c.wp, c.bp, sp, gp, lp, g.dx.data_ptr(), g.dw.data_ptr<float>(),
                              bias ? g.dbias.data_ptr<float>() : nullptr, want_dstate ? g.dstate.data_ptr() : nullptr, ws.data_ptr(), n, flags,
@@ -203,7 +225,7 @@ std::pair<at::Tensor, at::Tensor> norm_forward(const at::Tensor& x, const at::Te
              "qdelta_norm_fwd");
     return {y, stats};
 }
-struct NormGrads { at::Tensor dx, dweight, dbias; };
+struct NormGrads { at::Tensor dx, dweight, dbias, params; };
 NormGrads norm_backward(const at::Tensor& x, const at::Tensor* weight, const at::Tensor& dy, const at::Tensor& stats, bool want_dweight,
                         bool want_dbias, unsigned flags) {
     const Norm c(x, weight);
@@ -217,8 +239,10 @@ NormGrads norm_backward(const at::Tensor& x, const at::Tensor* weight, const at:
         if (n == 0) bad("unsupported or invalid shape for the norm");
         ws = c.on.make({(int64_t)n}, at::kByte);
     }
-    if (want_dweight) g.dweight = c.on.make({c.width}, at::kFloat);
-    if (want_dbias) g.dbias = c.on.make({c.width}, at::kFloat);
+    Params params(c.on, {want_dweight ? c.width : 0, want_dbias ? c.width : 0});
+    g.params = params.all;
+    if (want_dweight) g.dweight = params.next({c.width});
+    if (want_dbias) g.dbias = params.next({c.width});
     rc_check(qdelta_norm_bwd(c.rows, c.w, c.code, c.xp, c.wp, gp, sp, g.dx.data_ptr(), want_dweight ? g.dweight.data_ptr<float>() : nullptr,
                              want_dbias ? g.dbias.data_ptr<float>() : nullptr, ws.defined() ? ws.data_ptr() : nullptr,
                              ws.defined() ? (size_t)ws.numel() : 0, flags, stream()),
@@ -398,15 +422,32 @@ at::Tensor upstream(const at::Tensor& g, at::ScalarType dt) { return g.defined()
 at::Tensor or_zeros(const at::Tensor& g, const at::Tensor& like) { return g.defined() ? g : at::zeros_like(like); }
 const at::Tensor* given(const at::Tensor& t) { return t.defined() ? &t : nullptr; }
 at::Tensor or_none(const MaybeTensor& t) { return t ? *t : at::Tensor(); }
-// a parameter's gradient in the parameter's type
-at::Tensor as(const at::Tensor& g, const at::Tensor& like) { return !g.defined() || g.scalar_type() == like.scalar_type() ? g : g.to(like.scalar_type()); }
+// a parameter's gradient in the type of `like`: the same place in the converted allocation
+at::Tensor as(const at::Tensor& g, const at::Tensor& like, const at::Tensor& all, at::Tensor& converted) {
+    if (!g.defined() || g.scalar_type() == like.scalar_type()) return g;
+    if (!converted.defined()) converted = all.to(like.scalar_type());
+    return converted.narrow(0, g.storage_offset() - all.storage_offset(), g.numel()).view(g.sizes());
+}
 
+// The kernels give first derivatives: with create_graph a second one is refused when it is asked for.
 template <class F> variable_list in_backward(F f) {
+    variable_list g;
     try {
-        return f();
+        at::NoGradGuard off;
+        g = f();
     } catch (const Bad& b) {
         raise(b.what);
     }
+    if (!at::GradMode::is_enabled()) return g;
+    variable_list have;
+    for (at::Tensor& t : g)
+        if (t.defined()) have.push_back(t.detach().set_requires_grad(true));
+    auto refuse = std::make_shared<torch::autograd::DelayedError>("second derivatives of this operator are not available", (int64_t)have.size());
+    have = (*refuse)(std::move(have));
+    size_t i = 0;
+    for (at::Tensor& t : g)
+        if (t.defined()) t = have[i++];
+    return g;
 }
 // saved tensors that hooks hand back may be others than were saved: the checks of the call see them again
 void present(const at::Tensor& t, const char* name) {
@@ -433,7 +474,8 @@ struct ConvNode : torch::autograd::Function<ConvNode> {
             const at::Tensor dy = or_zeros(upstream(g[0], x.scalar_type()), x), dlast = upstream(g[1], x.scalar_type());
             const ConvGrads r = conv_backward(x, w, given(bias), given(state), dy, given(dlast), state.defined(),
                                               (unsigned)ctx->saved_data["flags"].toInt());
-            return {r.dx, as(r.dw, w), bias.defined() ? as(r.dbias, bias) : at::Tensor(), r.dstate, at::Tensor(), at::Tensor()};
+            at::Tensor converted;
+            return {r.dx, as(r.dw, w, r.params, converted), as(r.dbias, w, r.params, converted), r.dstate, at::Tensor(), at::Tensor()};
         });
     }
 };
@@ -492,8 +534,8 @@ struct NormNode : torch::autograd::Function<NormNode> {
             const at::Tensor dy = or_zeros(upstream(g[0], x.scalar_type()), x);
             const NormGrads r = norm_backward(x, given(weight), dy, stats, weight.defined() && ctx->saved_data["dweight"].toBool(),
                                               bias.defined() && ctx->saved_data["dbias"].toBool(), (unsigned)ctx->saved_data["flags"].toInt());
-            return {r.dx, weight.defined() ? as(r.dweight, weight) : at::Tensor(), bias.defined() ? as(r.dbias, bias) : at::Tensor(),
-                    at::Tensor(), at::Tensor(), at::Tensor()};
+            at::Tensor converted;
+            return {r.dx, as(r.dweight, x, r.params, converted), as(r.dbias, x, r.params, converted), at::Tensor(), at::Tensor(), at::Tensor()};
         });
     }
 };

@@ -99,7 +99,8 @@ SCAN = [  # B, T, D, N, G, dtype, softplus, gate, skip, bias, state
     (1, 130, 66, 16, 2, F32, True, True, False, True, True), (2, 300, 100, 8, 1, BF, True, True, True, True, True),
     (1, 700, 8, 4, 1, F32, True, True, True, True, True), (1, 333, 24, 64, 3, F32, True, True, True, False, True),
     (2, 129, 130, 33, 1, BF, False, True, True, True, True), (1, 200, 36, 48, 2, BF, True, True, True, True, False),
-    (1, 64, 4, 16, 4, F32, True, True, True, True, True), (1, 1025, 32, 16, 1, F32, True, False, False, True, True)]
+    (1, 64, 4, 16, 4, F32, True, True, True, True, True), (1, 1025, 32, 16, 1, F32, True, False, False, True, True),
+    (1, 2500, 20, 16, 1, F32, True, True, True, True, True)]         # more segments than one joins by itself
 
 
 def _scan_inputs(B, T, D, N, G, dt, softplus, gate, skip, bias, state, seed=0):
