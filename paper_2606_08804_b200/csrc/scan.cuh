@@ -19,7 +19,7 @@
 //
 // Segments.  Where there are too few channels to fill the GPU, a sequence is cut into segments: each is first walked from a zero state
 // (the first from h0) without outputs, the states at the segments' ends are joined (h = exp(A sum dt) h + local end), and then all
-// segments run at once from their true states.  That walks all but the last twice, so one segment where channels suffice.
+// segments run at once from their true states.  That walks all but the last twice, so one segment where channels suffice (cut).
 //
 // States past N have A = B = C = 0 and channels past the group's last dt = u = 0, which leaves them at 0.  Tokens past T have dt = 0: the
 // state passes through.
@@ -35,6 +35,10 @@ constexpr int kThreads = 2 * 32 * kWalkers;
 constexpr int kSave = 8;                     // tokens from one saved state to the next, and of a tile, backward
 constexpr int kTile = 16;                    // tokens of a tile, forward
 constexpr size_t kWarpTile = kWarpChannels * kWarpStates;          // states of a warp, in the order [lane][channel][state]
+
+// Shared memory that two CTAs of an SM do not have: asked for where every CTA can have an SM for itself, which it would not get while the
+// kernel before still holds some of them (backward of 128 CTAs after another kernel: 680 us instead of 480).
+constexpr size_t kAloneSmem = 116 * 1024;
 
 // What both directions derive from the shape.
 struct Dims {
@@ -74,9 +78,12 @@ struct P {
 enum Copy { kSingle = 0, kWords = 1, kWhole = 2 };
 inline int copy_of(int width, int group, int dtype) { return width % group == 0 ? kWhole : dtype == QD_F32 || width % 2 == 0 ? kWords : kSingle; }
 
-// Segments of a sequence and tokens of one, a multiple of kTile.
+// Segments of a sequence and tokens of one, a multiple of kTile, two tiles at least: those that take least by what the two walks of a token
+// cost, a walk taking the time of kBegin tokens more to begin, a second one kLaunch ns to launch.  CTAs beyond two an SM wait for those
+// before.
 struct Cut { int segs, len; };
-Cut cut(const Dims& d);
+constexpr int kBegin = 24, kMostWaves = 5, kLaunch = 1500;
+Cut cut(const Dims& d, bool backward);
 // True states at the segments' ends from those of each walked alone, which they overwrite, where the walk does not join them itself.
 constexpr int kMostJoined = 32;              // segments before one's own whose ends a CTA joins by itself
 cudaError_t join(float* ends, const float* decays, int n, int from, int step, size_t count, cudaStream_t stream);

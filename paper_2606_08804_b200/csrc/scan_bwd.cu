@@ -353,14 +353,14 @@ struct BwdPlan { Dims d; Cut c; size_t saved, ends, pA, pD, pBC, bytes; };
 BwdPlan bwd_plan(const qd_scan_shape& s) {
     BwdPlan q{};
     q.d = dims(s);
-    q.c = cut(q.d);
+    q.c = cut(q.d, true);
     const auto up = [](size_t n) { return (n + 255) / 256 * 256; };
     q.saved = (size_t)s.B * ((s.T + kSave - 1) / kSave) * q.d.states * sizeof(float);
     q.ends = (size_t)(q.c.segs - 1) * s.B * q.d.states * sizeof(float);
     q.pA = up((size_t)q.c.segs * s.B * s.D * s.N * sizeof(float));
     q.pD = up((size_t)q.c.segs * s.B * 2 * s.D * sizeof(float));
     q.pBC = up((size_t)q.d.ctas * 2 * s.B * s.T * s.G * s.N * sizeof(float));
-    q.bytes = q.saved + 2 * q.ends + q.pA + q.pD + q.pBC;                  // more than a saving forward's
+    q.bytes = q.saved + 2 * q.ends + q.pA + q.pD + q.pBC;
     return q;
 }
 
@@ -368,17 +368,18 @@ template <typename IO, int NB>
 cudaError_t launch(const P& p, cudaStream_t stream) {
     const long long per = (long long)p.d.ctas * p.d.G * p.d.B;
     constexpr size_t smem = sizeof(BwdSmem<IO, NB>);
+    constexpr size_t most = smem > kAloneSmem ? smem : kAloneSmem;
     cudaError_t e;
     if (p.segs > 1) {
-        e = set_max_smem_once((const void*)k_scan_bwd<IO, NB, true>, smem);
+        e = set_max_smem_once((const void*)k_scan_bwd<IO, NB, true>, most);
         if (e == cudaSuccess)
-            e = launch_overlapped(k_scan_bwd<IO, NB, true>, dim3((unsigned)(per * (p.segs - 1))), dim3(kThreads), smem, stream, p);
+            e = launch_overlapped(k_scan_bwd<IO, NB, true>, dim3((unsigned)(per * (p.segs - 1))), dim3(kThreads), per * (p.segs - 1) > kSMs ? smem : most, stream, p);
         if (e == cudaSuccess && p.joined) e = join(p.ends, p.decays, p.segs - 1, p.segs - 2, -1, (size_t)p.d.B * p.d.states, stream);
         if (e != cudaSuccess) return e;
     }
-    e = set_max_smem_once((const void*)k_scan_bwd<IO, NB, false>, smem);
+    e = set_max_smem_once((const void*)k_scan_bwd<IO, NB, false>, most);
     if (e != cudaSuccess) return e;
-    return launch_overlapped(k_scan_bwd<IO, NB, false>, dim3((unsigned)(per * p.segs)), dim3(kThreads), smem, stream, p);
+    return launch_overlapped(k_scan_bwd<IO, NB, false>, dim3((unsigned)(per * p.segs)), dim3(kThreads), per * p.segs > kSMs ? smem : most, stream, p);
 }
 template <typename IO>
 cudaError_t launch(const P& p, const ScanArgs& a) {
@@ -390,7 +391,11 @@ cudaError_t launch(const P& p, const ScanArgs& a) {
 }
 }  // namespace
 
-size_t scan_bwd_workspace(const qd_scan_shape& s) { return bwd_plan(s).bytes; }
+// that of the forward that saves for it, too
+size_t scan_bwd_workspace(const qd_scan_shape& s) {
+    const size_t fwd = scan_fwd_workspace(s, true), bwd = bwd_plan(s).bytes;
+    return fwd > bwd ? fwd : bwd;
+}
 
 cudaError_t scan_bwd(const ScanArgs& a) {
     const BwdPlan q = bwd_plan(a.s);

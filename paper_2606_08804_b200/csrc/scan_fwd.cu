@@ -3,6 +3,8 @@
 // fp32 pipe, softplus and gate another 16: bound by the exponentials, not by HBM, when there are warps enough.
 #include "scan.cuh"
 
+#include <algorithm>
+
 namespace qd {
 namespace {
 using namespace scan;
@@ -215,19 +217,32 @@ cudaError_t join(float* ends, const float* decays, int n, int from, int step, si
     return launch_overlapped(k_join, dim3((unsigned)((count + 255) / 256)), dim3(256), 0, stream, ends, decays, n, from, step, count);
 }
 
-// As many segments as fill the GPU twice over, none where that would be fewer than three (walking all but the last twice costs what two
-// gain), each of four tiles at least.
-Cut cut(const Dims& d) {
+// What a walk of a token costs, in ns: without outputs and with them, by a CTA that has an SM for itself and by one of two (4096 x 16
+// channels of 16 states and of twice as many).
+struct Cost { int end_alone, end_paired, alone, paired; };
+constexpr Cost kForward{54, 85, 78, 128}, kBackward{88, 118, 228, 358};
+
+Cut cut(const Dims& d, bool backward) {
+    const Cost& w = backward ? kBackward : kForward;
     const long long units = (long long)d.B * d.G * d.ctas;
-    long long n = 2 * kSMs / units;
-    if (n < 3) n = 1;
-    const long long most = d.T / (2 * kTile);
-    if (n > most) n = most;
-    if (n < 1) n = 1;
-    const long long per = (d.T + n - 1) / n;
-    Cut c;
-    c.len = (int)((per + kTile - 1) / kTile * kTile);
-    c.segs = (int)(((long long)d.T + c.len - 1) / c.len);
+    auto waves = [](long long ctas, int alone, int paired) {
+        const long long rest = ctas % (2 * kSMs);
+        return ctas / (2 * kSMs) * paired + (rest == 0 ? 0 : rest <= kSMs ? alone : paired);
+    };
+    Cut c{1, (d.T + kTile - 1) / kTile * kTile};
+    long long least = waves(units, w.alone, w.paired) * (d.T + kBegin);
+    for (int k = 1; k <= 2 * kMostWaves; ++k) {            // of those that need as many waves of CTAs the largest number is the best
+        const long long n = std::min<long long>(k * kSMs / units, d.T / (2 * kTile));
+        if (n < 2) continue;
+        Cut x;
+        x.len = (int)(((d.T + n - 1) / n + kTile - 1) / kTile * kTile);
+        x.segs = (d.T + x.len - 1) / x.len;
+        const long long time = (waves(units * (x.segs - 1), w.end_alone, w.end_paired) + waves(units * x.segs, w.alone, w.paired)) * (x.len + kBegin) + kLaunch;
+        if (time < least) {
+            least = time;
+            c = x;
+        }
+    }
     return c;
 }
 }  // namespace scan
@@ -237,7 +252,7 @@ struct FwdPlan { Dims d; Cut c; size_t saved, ends, bytes; };
 FwdPlan fwd_plan(const qd_scan_shape& s, bool save) {
     FwdPlan q{};
     q.d = dims(s);
-    q.c = cut(q.d);
+    q.c = cut(q.d, false);
     q.saved = save ? (size_t)s.B * ((s.T + kSave - 1) / kSave) * q.d.states * sizeof(float) : 0;
     q.ends = (size_t)(q.c.segs - 1) * s.B * q.d.states * sizeof(float);
     q.bytes = q.saved + 2 * q.ends;
@@ -248,16 +263,17 @@ template <typename IO, int NB, bool SAVE>
 cudaError_t launch(const P& p, cudaStream_t stream) {
     const long long per = (long long)p.d.ctas * p.d.G * p.d.B;
     constexpr size_t smem = sizeof(FwdSmem<IO, NB>);
+    constexpr size_t most = smem > kAloneSmem ? smem : kAloneSmem;
     const auto local = k_scan_fwd<IO, NB, true, SAVE>, all = k_scan_fwd<IO, NB, false, SAVE>;
     cudaError_t e;
     if (p.segs > 1) {
-        e = set_max_smem_once((const void*)local, smem);
-        if (e == cudaSuccess) e = launch_overlapped(local, dim3((unsigned)(per * (p.segs - 1))), dim3(kThreads), smem, stream, p);
+        e = set_max_smem_once((const void*)local, most);
+        if (e == cudaSuccess) e = launch_overlapped(local, dim3((unsigned)(per * (p.segs - 1))), dim3(kThreads), per * (p.segs - 1) > kSMs ? smem : most, stream, p);
         if (e == cudaSuccess && p.joined) e = join(p.ends, p.decays, p.segs - 1, 0, 1, (size_t)p.d.B * p.d.states, stream);
         if (e != cudaSuccess) return e;
     }
-    e = set_max_smem_once((const void*)all, smem);
-    return e != cudaSuccess ? e : launch_overlapped(all, dim3((unsigned)(per * p.segs)), dim3(kThreads), smem, stream, p);
+    e = set_max_smem_once((const void*)all, most);
+    return e != cudaSuccess ? e : launch_overlapped(all, dim3((unsigned)(per * p.segs)), dim3(kThreads), per * p.segs > kSMs ? smem : most, stream, p);
 }
 template <typename IO, int NB>
 cudaError_t launch(const P& p, cudaStream_t stream) {
