@@ -59,7 +59,7 @@ inline Dims dims(const qd_scan_shape& s) {
 
 struct P {
     Dims d;
-    int segs, seglen;                        // segments of a sequence and tokens of one
+    int segs, first, seglen;                 // segments of a sequence, tokens of the first and of the others (Cut)
     const void *u, *dt, *Bm, *Cm, *z, *dy;
     const float *A, *D, *dt_bias, *h0, *dhT;
     void *y, *du, *ddt, *dz;
@@ -78,10 +78,11 @@ struct P {
 enum Copy { kSingle = 0, kWords = 1, kWhole = 2 };
 inline int copy_of(int width, int group, int dtype) { return width % group == 0 ? kWhole : dtype == QD_F32 || width % 2 == 0 ? kWords : kSingle; }
 
-// Segments of a sequence and tokens of one, a multiple of kTile, two tiles at least: those that take least by what the two walks of a token
-// cost, a walk taking the time of kBegin tokens more to begin, a second one kLaunch ns to launch.  CTAs beyond two an SM wait for those
-// before.
-struct Cut { int segs, len; };
+// Segments of a sequence; tokens of the first and of each other, multiples of kTile.  Taken are those that need least time by what the two
+// walks of a token cost, a walk taking the time of kBegin tokens more to begin, a second one kLaunch ns to launch.  CTAs beyond two an SM
+// wait for those before.  Where one segment leaves some SMs a single CTA, the segment that is walked first, to be joined to the other, is a
+// short one, for the places that are left over.
+struct Cut { int segs, first, len; };
 constexpr int kBegin = 24, kMostWaves = 5, kLaunch = 1500;
 Cut cut(const Dims& d, bool backward);
 // True states at the segments' ends from those of each walked alone, which they overwrite, where the walk does not join them itself.

@@ -44,9 +44,8 @@ __global__ void __launch_bounds__(kThreads, 2) k_scan_bwd(const P p) {
     int idx = blockIdx.x;
     const int ct = idx % d.ctas; idx /= d.ctas;
     const int g = idx % d.G; idx /= d.G;
-    const int walked = LOCAL ? p.segs - 1 : p.segs;        // LOCAL: the first segment is not launched
-    const int seg = idx % walked + (LOCAL ? 1 : 0), b = idx / walked;
-    const int t0 = seg * p.seglen, t1 = min(d.T, t0 + p.seglen), n = (t1 - t0 + K - 1) / K;
+    const int b = idx % d.B, seg = idx / d.B + (LOCAL ? 1 : 0);            // LOCAL: without the first; the last may be short
+    const int t0 = seg ? p.first + (seg - 1) * p.seglen : 0, t1 = min(d.T, p.first + seg * p.seglen), n = (t1 - t0 + K - 1) / K;
     const size_t part = (size_t)seg * d.B + b;
 
     if (warp < kWalkers) {
@@ -400,7 +399,7 @@ size_t scan_bwd_workspace(const qd_scan_shape& s) {
 cudaError_t scan_bwd(const ScanArgs& a) {
     const BwdPlan q = bwd_plan(a.s);
     P p{};
-    p.d = q.d; p.segs = q.c.segs; p.seglen = q.c.len;
+    p.d = q.d; p.segs = q.c.segs; p.first = q.c.first; p.seglen = q.c.len;
     p.u = a.u; p.dt = a.dt; p.Bm = a.Bm; p.Cm = a.Cm; p.z = a.z; p.A = a.A; p.D = a.D; p.dt_bias = a.dt_bias;
     p.dy = a.dy; p.dhT = a.dhT; p.du = a.du; p.ddt = a.ddt; p.dz = a.dz; p.dh0 = a.dh0;
     char* w = a.ws;

@@ -45,9 +45,8 @@ __global__ void __launch_bounds__(kThreads, 2) k_scan_fwd(const P p) {
     int idx = blockIdx.x;
     const int ct = idx % d.ctas; idx /= d.ctas;
     const int g = idx % d.G; idx /= d.G;
-    const int walked = LOCAL ? p.segs - 1 : p.segs;        // LOCAL: the last segment is not launched
-    const int seg = idx % walked, b = idx / walked;
-    const int t0 = seg * p.seglen, t1 = min(d.T, t0 + p.seglen), n = (t1 - t0 + kTile - 1) / kTile;
+    const int b = idx % d.B, seg = (LOCAL ? p.segs - 2 : p.segs - 1) - idx / d.B;       // LOCAL: without the last; the first, which may be short, last
+    const int t0 = seg ? p.first + (seg - 1) * p.seglen : 0, t1 = min(d.T, p.first + seg * p.seglen), n = (t1 - t0 + kTile - 1) / kTile;
 
     if (warp < kWalkers) {
         // ---- walk ----------------------------------------------------------------------------------------------------------
@@ -229,19 +228,26 @@ Cut cut(const Dims& d, bool backward) {
         const long long rest = ctas % (2 * kSMs);
         return ctas / (2 * kSMs) * paired + (rest == 0 ? 0 : rest <= kSMs ? alone : paired);
     };
-    Cut c{1, (d.T + kTile - 1) / kTile * kTile};
+    auto tiles = [](long long tokens) { return (int)((tokens + kTile - 1) / kTile * kTile); };
+    Cut c{1, tiles(d.T), tiles(d.T)};
     long long least = waves(units, w.alone, w.paired) * (d.T + kBegin);
     for (int k = 1; k <= 2 * kMostWaves; ++k) {            // of those that need as many waves of CTAs the largest number is the best
         const long long n = std::min<long long>(k * kSMs / units, d.T / (2 * kTile));
         if (n < 2) continue;
-        Cut x;
-        x.len = (int)(((d.T + n - 1) / n + kTile - 1) / kTile * kTile);
+        Cut x{0, 0, tiles((d.T + n - 1) / n)};
+        x.first = x.len;
         x.segs = (d.T + x.len - 1) / x.len;
         const long long time = (waves(units * (x.segs - 1), w.end_alone, w.end_paired) + waves(units * x.segs, w.alone, w.paired)) * (x.len + kBegin) + kLaunch;
         if (time < least) {
             least = time;
             c = x;
         }
+    }
+    if (units > kSMs && units < 2 * kSMs) {                // turns: short segments that a place left over takes; many of them even out
+        const long long places = 2 * kSMs, free = places - units, turns = (units + free - 1) / free;
+        const int shorter = (int)(turns > 3 ? d.T * free / places : d.T / (turns + 1)) / kTile * kTile, longer = tiles(d.T - shorter);
+        const long long time = w.end_paired * (shorter + kBegin) + w.paired * (longer + kBegin) + kLaunch;
+        if (shorter >= 2 * kTile && time * 13 < least * 12) c = backward ? Cut{2, longer, longer} : Cut{2, shorter, longer};
     }
     return c;
 }
@@ -290,7 +296,7 @@ size_t scan_fwd_workspace(const qd_scan_shape& s, bool save) { return fwd_plan(s
 cudaError_t scan_fwd(const ScanArgs& a) {
     const FwdPlan q = fwd_plan(a.s, a.save);
     P p{};
-    p.d = q.d; p.segs = q.c.segs; p.seglen = q.c.len;
+    p.d = q.d; p.segs = q.c.segs; p.first = q.c.first; p.seglen = q.c.len;
     p.u = a.u; p.dt = a.dt; p.Bm = a.Bm; p.Cm = a.Cm; p.z = a.z; p.A = a.A; p.D = a.D; p.dt_bias = a.dt_bias; p.h0 = a.h0;
     p.y = a.y; p.hT = a.hT;
     p.saved = a.save ? reinterpret_cast<float*>(a.ws) : nullptr;

@@ -100,7 +100,10 @@ SCAN = [  # B, T, D, N, G, dtype, softplus, gate, skip, bias, state
     (1, 700, 8, 4, 1, F32, True, True, True, True, True), (1, 333, 24, 64, 3, F32, True, True, True, False, True),
     (2, 129, 130, 33, 1, BF, False, True, True, True, True), (1, 200, 36, 48, 2, BF, True, True, True, True, False),
     (1, 64, 4, 16, 4, F32, True, True, True, True, True), (1, 1025, 32, 16, 1, F32, True, False, False, True, True),
-    (1, 2500, 20, 16, 1, F32, True, True, True, True, True)]         # more segments than one joins by itself
+    (1, 2500, 20, 16, 1, F32, True, True, True, True, True),         # more segments than one joins by itself
+    # segments of unequal lengths backward; in both directions; more CTAs than have room at once
+    (5, 303, 40, 4, 40, F32, True, True, True, True, True), (4, 1301, 43, 3, 43, BF, True, True, True, True, True),
+    (2, 606, 50, 2, 50, F32, True, True, True, True, True), (1, 1503, 64, 2, 64, BF, True, True, True, True, True)]
 
 
 def _scan_inputs(B, T, D, N, G, dt, softplus, gate, skip, bias, state, seed=0):
