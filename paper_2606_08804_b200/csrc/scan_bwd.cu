@@ -187,16 +187,18 @@ __global__ void __launch_bounds__(kThreads, 2) k_scan_bwd(const P p) {
     const int tid = threadIdx.x - 32 * kWalkers;
     const size_t rows = (size_t)b * d.T, col = (size_t)g * d.K + ct * CC;
     const int left = d.K - ct * CC;
-    // a tile is prepared by pairs of channels and written out by groups of four (where NB > 1 some threads have none)
-    const int pr = tid % S::PAIRS, first = tid / S::PAIRS, it = tid / (CC / 4), ic = tid % (CC / 4) * 4;
-    float bias2[2], bias[4], skip[4], sumD[4] = {0.f, 0.f, 0.f, 0.f}, sumb[4] = {0.f, 0.f, 0.f, 0.f};
+    // a thread prepares pairs of channels of PASSES tokens (where NB > 1 some threads none), keeps what it needs of them until the walk has
+    // been there two tiles later, and writes out their gradients
+    const int pr = tid % S::PAIRS, first = tid / S::PAIRS;
+    float bias[2], skips[2];
 #pragma unroll
-    for (int e = 0; e < 2; ++e) bias2[e] = p.dt_bias && 2 * pr + e < left ? p.dt_bias[col + 2 * pr + e] : 0.f;
-#pragma unroll
-    for (int e = 0; e < 4; ++e) {
-        bias[e] = p.dt_bias && ic + e < left ? p.dt_bias[col + ic + e] : 0.f;
-        skip[e] = !LOCAL && p.D && ic + e < left ? p.D[col + ic + e] : 0.f;
+    for (int e = 0; e < 2; ++e) {
+        bias[e] = p.dt_bias && 2 * pr + e < left ? p.dt_bias[col + 2 * pr + e] : 0.f;
+        skips[e] = !LOCAL && p.D && 2 * pr + e < left ? p.D[col + 2 * pr + e] : 0.f;
     }
+    const f2 skip = pack2(skips[0], skips[1]);
+    f2 sumD = 0, sumb = 0;
+    struct Kept { f2 u, dt, dy, slope, gate; };             // slope: of the softplus; gate: dy SiLU'(z), with dy as it came in
     auto fetch = [&](int i) {
         if (i >= 0) {
             const int tt = t0 + i * K, slot = i % S::RING;
@@ -214,7 +216,7 @@ __global__ void __launch_bounds__(kThreads, 2) k_scan_bwd(const P p) {
         copy_commit();
     };
     // Channels past the last have u = dy = 0 and any step; tokens past the last a step of 0.
-    auto turn = [&](int i) {
+    auto turn = [&](int i, Kept(&kept)[S::PASSES]) {
         const int k = i & 1, slot = i % S::RING;
 #pragma unroll
         for (int r = 0; r < S::PASSES; ++r) {
@@ -222,16 +224,25 @@ __global__ void __launch_bounds__(kThreads, 2) k_scan_bwd(const P p) {
             if (S::ROWS > K && row >= K) break;
             const Pack<IO, 2> dt = load_pack<IO, 2>(&sm.dt[slot][at], 2, true), gy = load_pack<IO, 2>(&sm.gy[slot][at], 2, true);
             const Pack<IO, 2> u = LOCAL ? dt : load_pack<IO, 2>(&sm.u[slot][at], 2, true);
-            float2 v = make_float2(pick(dt, 0) + bias2[0], pick(dt, 1) + bias2[1]), y = make_float2(pick(gy, 0), pick(gy, 1));
-            if (p.softplus) v = softplus(v.x, v.y);
+            float2 v = make_float2(pick(dt, 0) + bias[0], pick(dt, 1) + bias[1]), y = make_float2(pick(gy, 0), pick(gy, 1));
+            if (p.softplus) {
+                if (!LOCAL) kept[r].slope = pack2(gate_sigmoid(v.x), gate_sigmoid(v.y));
+                v = softplus(v.x, v.y);
+            }
             if (t0 + i * K + row >= t1) v.x = v.y = 0.f;
             if (p.z) {
                 const Pack<IO, 2> z = load_pack<IO, 2>(&sm.z[slot][at], 2, true);
-                const float z0 = pick(z, 0), z1 = pick(z, 1);
-                y.x *= z0 * gate_sigmoid(z0);
-                y.y *= z1 * gate_sigmoid(z1);
+                const float z0 = pick(z, 0), z1 = pick(z, 1), s0 = gate_sigmoid(z0), s1 = gate_sigmoid(z1);
+                if (!LOCAL) kept[r].gate = pack2(y.x * (s0 * fmaf(z0, 1.f - s0, 1.f)), y.y * (s1 * fmaf(z1, 1.f - s1, 1.f)));
+                y.x *= z0 * s0;
+                y.y *= z1 * s1;
             }
-            const float x0 = v.x * pick(u, 0), x1 = v.y * pick(u, 1);
+            const float u0 = pick(u, 0), u1 = pick(u, 1), x0 = v.x * u0, x1 = v.y * u1;
+            if (!LOCAL) {
+                kept[r].u = pack2(u0, u1);
+                kept[r].dt = pack2(v.x, v.y);
+                kept[r].dy = pack2(y.x, y.y);
+            }
             sm.step[k][row][0][pr] = make_float4(v.x, v.y, x0, x1);
             sm.step[k][row][1][pr] = make_float4(v.y, v.x, x1, x0);
             sm.dy[k][row][pr] = make_float4(y.x, y.y, y.y, y.x);
@@ -246,41 +257,36 @@ __global__ void __launch_bounds__(kThreads, 2) k_scan_bwd(const P p) {
             to[1][s] = make_float4(pick(v, 2), pick(v, 3), pick(v, 0), pick(v, 1));
         }
     };
-    auto finish = [&](int i) {                             // of a tile that has been walked
-        const int t = t0 + i * K + it, k = i & 1, slot = i % S::RING;
-        if (it < K && ic < left && t < t1) {
-            const int at = it * CC + ic;
-            const Pack<IO, 4> u = load_pack<IO, 4>(&sm.u[slot][at], 4, true), gy = load_pack<IO, 4>(&sm.gy[slot][at], 4, true);
-            const Pack<IO, 4> dt = load_pack<IO, 4>(&sm.dt[slot][at], 4, true), z = load_pack<IO, 4>(&sm.z[slot][at], 4, true);
-            const float4 s0 = sm.step[k][it][0][ic / 2], s1 = sm.step[k][it][0][ic / 2 + 1], y0 = sm.dy[k][it][ic / 2], y1 = sm.dy[k][it][ic / 2 + 1];
-            const float vdt[4] = {s0.x, s0.y, s1.x, s1.y}, vdy[4] = {y0.x, y0.y, y1.x, y1.y};
-            float odu[4], odt[4], odz[4], g1[4] = {0.f, 0.f, 0.f, 0.f}, g2[4] = {0.f, 0.f, 0.f, 0.f}, gy4[4] = {0.f, 0.f, 0.f, 0.f};
+    const bool pairs = sizeof(IO) == 2 ? p.rows != kSingle : p.rows == kWhole;             // of the gradients, aligned
+    auto finish = [&](int i, const Kept(&kept)[S::PASSES]) {                               // of a tile that has been walked
+        const int k = i & 1;
+#pragma unroll
+        for (int r = 0; r < S::PASSES; ++r) {
+            const int row = first + r * S::ROWS, t = t0 + i * K + row;
+            if (row >= K || 2 * pr >= left || t >= t1) break;
+            f2 gB = 0, gpA = 0, y = 0;
 #pragma unroll
             for (int w = 0; w < NB; ++w) {
-                const float4 a = *reinterpret_cast<const float4*>(&sm.gB[k][w][it][ic]), c = *reinterpret_cast<const float4*>(&sm.gpA[k][w][it][ic]);
-                const float4 f = *reinterpret_cast<const float4*>(&sm.y[k][w][it][ic]);
-                g1[0] += a.x; g1[1] += a.y; g1[2] += a.z; g1[3] += a.w;
-                g2[0] += c.x; g2[1] += c.y; g2[2] += c.z; g2[3] += c.w;
-                gy4[0] += f.x; gy4[1] += f.y; gy4[2] += f.z; gy4[3] += f.w;
+                const f2 a = *reinterpret_cast<const f2*>(&sm.gB[k][w][row][2 * pr]), c = *reinterpret_cast<const f2*>(&sm.gpA[k][w][row][2 * pr]);
+                const f2 f = *reinterpret_cast<const f2*>(&sm.y[k][w][row][2 * pr]);
+                gB = w ? add2(gB, a) : a;
+                gpA = w ? add2(gpA, c) : c;
+                y = w ? add2(y, f) : f;
             }
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                const float uu = pick(u, e);
-                odu[e] = fmaf(g1[e], vdt[e], skip[e] * vdy[e]);
-                odt[e] = fmaf(g1[e], uu, g2[e] * kLn2);
-                if (p.softplus) odt[e] *= gate_sigmoid(pick(dt, e) + bias[e]);
-                sumD[e] = fmaf(vdy[e], uu, sumD[e]);
-                sumb[e] += odt[e];
-                if (p.z) {
-                    const float zz = pick(z, e), sg = gate_sigmoid(zz);
-                    odz[e] = pick(gy, e) * fmaf(skip[e], uu, gy4[e]) * (sg * fmaf(zz, 1.f - sg, 1.f));
-                }
-            }
-            const size_t to = (rows + t) * d.D + col + ic;
-            const bool whole = p.rows == kWhole;
-            store_pack(static_cast<IO*>(p.du) + to, narrow<IO, 4>(odu), left - ic, whole);
-            store_pack(static_cast<IO*>(p.ddt) + to, narrow<IO, 4>(odt), left - ic, whole);
-            if (p.z) store_pack(static_cast<IO*>(p.dz) + to, narrow<IO, 4>(odz), left - ic, whole);
+            const Kept& x = kept[r];
+            f2 ddt = fma2(gB, x.u, mul2(gpA, both(kLn2)));
+            if (p.softplus) ddt = mul2(ddt, x.slope);
+            sumD = fma2(x.dy, x.u, sumD);
+            sumb = add2(sumb, ddt);
+            const size_t to = (rows + t) * d.D + col + 2 * pr;
+            auto put = [&](void* out, f2 v) {
+                const float2 o = unpack2(v);
+                const float w[2] = {o.x, o.y};
+                store_pack(static_cast<IO*>(out) + to, narrow<IO, 2>(w), left - 2 * pr, pairs);
+            };
+            put(p.du, fma2(gB, x.dt, mul2(skip, x.dy)));
+            put(p.ddt, ddt);
+            if (p.z) put(p.dz, mul2(x.gate, fma2(skip, x.u, y)));
         }
         // dB, dC of the CTA's channels: four states of a token
 #pragma unroll
@@ -303,34 +309,38 @@ __global__ void __launch_bounds__(kThreads, 2) k_scan_bwd(const P p) {
     for (int e = 1; e <= S::RING - 2; ++e) fetch(n - e);
     copy_wait<S::RING - 4>();                                              // the first two tiles
     prepare_barrier();
-    turn(n - 1);
+    Kept kept[2][S::PASSES];                                               // of the next tile to be finished, of the one after it
+    turn(n - 1, kept[1]);
     __syncthreads();
     for (int i = n - 1; i >= 0; --i) {
-        if (!LOCAL && i < n - 1) finish(i + 1);
+        if (!LOCAL) {
+            if (i < n - 1) finish(i + 1, kept[0]);
+#pragma unroll
+            for (int r = 0; r < S::PASSES; ++r) kept[0][r] = kept[1][r];
+        }
         fetch(i - (S::RING - 2));                                          // where a tile stood that was finished before the last barrier
         prepare_barrier();                                                 // the next tile takes the place of the one that is finished now
-        if (i > 0) turn(i - 1);
+        if (i > 0) turn(i - 1, kept[1]);
         copy_wait<S::RING - 4>();                                          // tile i - 2, for all after the barrier
         __syncthreads();
     }
     if (LOCAL) return;
-    finish(0);
-    // sums over the tokens of a channel: the rows of a tile in order
+    finish(0, kept[0]);
+    // sums over the tokens of a channel: the threads that share it in order
+    constexpr int R = S::ROWS < K ? S::ROWS : K;
     float* cols = reinterpret_cast<float*>(sm.step);
     prepare_barrier();
-    if (it < K)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            cols[it * CC + ic + e] = sumD[e];
-            cols[(K + it) * CC + ic + e] = sumb[e];
-        }
+    if (first < K) {
+        *reinterpret_cast<f2*>(&cols[first * CC + 2 * pr]) = sumD;
+        *reinterpret_cast<f2*>(&cols[(R + first) * CC + 2 * pr]) = sumb;
+    }
     prepare_barrier();
     for (int x = tid; x < 2 * CC; x += 128) {
         const int which = x / CC, c = x % CC;
         if (c >= left) continue;
         float v = 0.f;
 #pragma unroll
-        for (int r = 0; r < K; ++r) v += cols[(which * K + r) * CC + c];
+        for (int r = 0; r < R; ++r) v += cols[(which * R + r) * CC + c];
         p.pD[(part * 2 + which) * d.D + col + c] = v;
     }
 }
