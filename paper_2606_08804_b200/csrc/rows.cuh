@@ -105,8 +105,7 @@ __device__ __forceinline__ void store_pack(IO* p, const Pack<IO, N>& r, int left
 // The logistic function.  e^{-x} overflows to infinity for x below -88, where the quotient is 0 as it should be.
 __device__ __forceinline__ float sigmoid(float x) { return __fdividef(1.f, 1.f + expf(-x)); }
 
-// 2^x on the special function unit: 2 ulp, and unbiased near x = 0 (mean relative error -5e-9 on (-0.002, -0.001)), which matters where
-// a decay of almost 1 is applied a thousand times.
+// 2^x on the special function unit: 2 ulp.
 __device__ __forceinline__ float exp2_unit(float x) {
     float y;
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));

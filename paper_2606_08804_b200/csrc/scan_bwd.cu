@@ -84,7 +84,7 @@ __global__ void __launch_bounds__(kThreads, 2) k_scan_bwd(const P p) {
                     const float2 vy = dy[t * 2 * S::PAIRS];
                     const f2 dt[2] = {both(v.x), both(v.y)}, gy[2] = {both(vy.x), both(vy.y)}, vc[2] = {pack2(c4.x, c4.y), pack2(c4.z, c4.w)};
 #pragma unroll
-                    for (int j = 0; j < 4; ++j) ga[j] = mul2(exp2_pair(mul2(dt[j >> 1], A2[j])), fma2(gy[j >> 1], vc[j & 1], ga[j]));
+                    for (int j = 0; j < 4; ++j) ga[j] = mul2(decay(dt[j >> 1], A2[j]), fma2(gy[j >> 1], vc[j & 1], ga[j]));
                     sum[0] += v.x;
                     sum[1] += v.y;
                 }
@@ -100,7 +100,7 @@ __global__ void __launch_bounds__(kThreads, 2) k_scan_bwd(const P p) {
                     const float4 v = step[t * 2 * S::PAIRS], b4 = B[t * 2 * (NS / 4)];
                     const f2 dt[2] = {both(v.x), both(v.y)}, x[2] = {both(v.z), both(v.w)}, vb[2] = {pack2(b4.x, b4.y), pack2(b4.z, b4.w)};
 #pragma unroll
-                    for (int j = 0; j < 4; ++j) hm[j] = fma2(exp2_pair(mul2(dt[j >> 1], A2[j])), hm[j], mul2(x[j >> 1], vb[j & 1]));
+                    for (int j = 0; j < 4; ++j) hm[j] = fma2(decay(dt[j >> 1], A2[j]), hm[j], mul2(x[j >> 1], vb[j & 1]));
                 }
                 auto half = [&](int base, f2(&h)[4]) {
                     f2 a[H][4], hp[H][4];
@@ -110,7 +110,7 @@ __global__ void __launch_bounds__(kThreads, 2) k_scan_bwd(const P p) {
                         const f2 dt[2] = {both(v.x), both(v.y)}, x[2] = {both(v.z), both(v.w)}, vb[2] = {pack2(b4.x, b4.y), pack2(b4.z, b4.w)};
 #pragma unroll
                         for (int j = 0; j < 4; ++j) {
-                            a[t][j] = exp2_pair(mul2(dt[j >> 1], A2[j]));
+                            a[t][j] = decay(dt[j >> 1], A2[j]);
                             hp[t][j] = h[j];
                             h[j] = fma2(a[t][j], h[j], mul2(x[j >> 1], vb[j & 1]));
                         }

@@ -9,17 +9,6 @@ namespace qd {
 namespace {
 using namespace scan;
 
-// 2^x of a pair, for |x| < 1/16 by the series of the exponential, whose rounding to nearest has no bias: what the special function unit gives
-// there is 5e-9 to 2e-8 too small on average, a decay of almost 1 is applied a thousand times, and the gradient of A grows with the
-// square of that (1.8e-6 of it off instead of 1.1e-6, fp32 sums of the definition 0.9e-6).
-__device__ __forceinline__ f2 exp2_pair_near(f2 x) {
-    f2 p = fma2(x, both(9.61812911e-3f), both(5.55041087e-2f));            // (ln 2)^k / k!
-    p = fma2(x, p, both(2.40226507e-1f));
-    p = fma2(x, p, both(6.93147181e-1f));
-    const float2 near = unpack2(fma2(x, p, both(1.f))), far = unpack2(exp2_pair(x)), t = unpack2(x);
-    return pack2(fabsf(t.x) < 0.0625f ? near.x : far.x, fabsf(t.y) < 0.0625f ? near.y : far.y);
-}
-
 template <typename IO, int NB> struct FwdSmem {
     static constexpr int CC = kWalkers / NB * kWarpChannels, NS = NB * kWarpStates;
     static constexpr int PAIRS = CC / 2, ROWS = 128 / PAIRS, PASSES = kTile / ROWS;      // of a thread that prepares: a pair of channels, PASSES tokens
@@ -31,7 +20,7 @@ template <typename IO, int NB> struct FwdSmem {
     Pack<IO, 4> bc[RING][NB][128];
 };
 
-// SAVE: for a backward; then the first two of a lane's states, which are the slow ones where A grows along a row, have the closer exponential.
+// SAVE: for a backward.
 template <typename IO, int NB, bool LOCAL, bool SAVE>
 __global__ void __launch_bounds__(kThreads, 2) k_scan_fwd(const P p) {
     using S = FwdSmem<IO, NB>;
@@ -75,10 +64,7 @@ __global__ void __launch_bounds__(kThreads, 2) k_scan_fwd(const P p) {
                 const float4 v = step[t * 2 * S::PAIRS], vb = B[t * (NS / 4)];
                 const f2 dt[2] = {both(v.x), both(v.y)}, x[2] = {both(v.z), both(v.w)}, bp[2] = {pack2(vb.x, vb.y), pack2(vb.z, vb.w)};
 #pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    const f2 arg = mul2(dt[j >> 1], A2[j]);
-                    h[j] = fma2(SAVE && !(j & 1) ? exp2_pair_near(arg) : exp2_pair(arg), h[j], mul2(x[j >> 1], bp[j & 1]));
-                }
+                for (int j = 0; j < 4; ++j) h[j] = fma2(decay(dt[j >> 1], A2[j]), h[j], mul2(x[j >> 1], bp[j & 1]));
                 if (LOCAL) {
                     sum[0] += v.x;
                     sum[1] += v.y;

@@ -105,7 +105,7 @@ __global__ void __launch_bounds__(kStepThreads, 8) k_scan_steps(const StepsP p) 
             o[r] = 0.f;
 #pragma unroll
             for (int n = 0; n < 4; ++n) {
-                h[r][n] = fmaf(exp2_unit(vr * a2[n]), h[r][n], xr * pick(fb[r], n));
+                h[r][n] = fmaf(exp2_unit(fmaf(vr, a2[n], kDecayShift)), h[r][n], xr * pick(fb[r], n));
                 o[r] = fmaf(h[r][n], pick(fc[r], n), o[r]);
             }
             if (!own) o[r] = 0.f;
