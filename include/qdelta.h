@@ -198,7 +198,8 @@ int qdelta_conv_steps(int B, int S, int D, int W, int dtype, const void *x, cons
 size_t qdelta_conv_workspace_bytes(int B, int T, int D, int W, int dtype);      /* of the backward; 0 on an invalid shape */
 
 /* Backward for  L = <y, dy> + <last, dlast>  (dlast NULL: zero).  dx [B,T,D], dstate [B,W-1,D] (NULL: skipped) in `dtype`;
- * dw [D,W], dbias [D] fp32 (dbias may be NULL only if bias is). */
+ * dw [D,W], dbias [D] fp32 (dbias may be NULL only if bias is).  dx is none of x, dy, and dstate not dlast: neighbouring runs still
+ * read those. */
 int qdelta_conv_bwd(int B, int T, int D, int W, int dtype, const void *x, const void *w, const void *bias, const void *state,
                     const void *dy, const void *dlast, void *dx, float *dw, float *dbias, void *dstate, void *workspace,
                     size_t workspace_bytes, unsigned flags, qd_stream stream);
@@ -208,7 +209,8 @@ int qdelta_conv_bwd(int B, int T, int D, int W, int dtype, const void *x, const 
  *     h_t = exp(dt_t A) h_{t-1} + dt_t u_t Bm_t ,   y_t = (<Cm_t, h_t> + D u_t) SiLU(z_t)
  *     u, dt, z, y [B,T,D]   A [D,N] fp32 (not positive where the state is to stay bounded)   D, dt_bias [D] fp32
  *     Bm, Cm [B,T,G,N], shared by the D / G channels of a group   h0, hT [B,D,N] fp32
- * D, z, dt_bias, h0 may be NULL (no skip, no factor, no bias, zero state), hT too (not returned).
+ * D, z, dt_bias, h0 may be NULL (no skip, no factor, no bias, zero state), hT too (not returned; not the same buffer as h0, which
+ * the first tokens may read after the last ones are done).
  * N from 1 to 64, T <= 2^30, D <= 2^20 a multiple of G.  A forward may need a workspace even if it does not save.
  */
 typedef struct {
@@ -225,7 +227,8 @@ int qdelta_scan_fwd(const qd_scan_shape *shape, const void *u, const void *dt, c
                     void *workspace, size_t workspace_bytes, unsigned flags, qd_stream stream);
 
 /* Backward for  L = <y, dy> + <hT, dhT>  (dhT NULL: zero).  Gradients have the shapes of what they belong to; dA, dD, ddt_bias,
- * dh0 are fp32, the others in `dtype`.  dD, dz, ddt_bias may be NULL only if D, z, dt_bias are; dh0 NULL: skipped.
+ * dh0 are fp32, the others in `dtype`.  dD, dz, ddt_bias may be NULL only if D, z, dt_bias are; dh0 NULL: skipped (else not the
+ * same buffer as dhT).
  * flags: QD_SOFTPLUS, QD_BWD_REUSE_FWD (the workspace holds what a saving forward of the same inputs left). */
 int qdelta_scan_bwd(const qd_scan_shape *shape, const void *u, const void *dt, const float *A, const void *Bm, const void *Cm,
                     const float *D, const void *z, const float *dt_bias, const float *h0, const void *dy, const float *dhT,

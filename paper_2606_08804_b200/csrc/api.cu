@@ -331,7 +331,7 @@ int qdelta_conv_bwd(int B, int T, int D, int W, int dtype, const void* x, const 
                     size_t workspace_bytes, unsigned flags, qd_stream stream) {
     const int rc = check_conv(B, T, D, W, dtype);
     if (rc != QD_OK) return rc;
-    if (!x || !w || !dy || !dx || !dw || (bias && !dbias) || dx == x || dx == dy) return QD_ERR_INVALID_ARG;
+    if (!x || !w || !dy || !dx || !dw || (bias && !dbias) || dx == x || dx == dy || (dstate && dstate == dlast)) return QD_ERR_INVALID_ARG;
     const void* const ptrs[] = {x, w, bias, state, dy, dlast, dx, dw, dbias, dstate, workspace};
     if (any_misaligned(ptrs) || (flags & ~(unsigned)QD_SILU)) return QD_ERR_INVALID_ARG;
     if (!workspace || workspace_bytes < conv_bwd_workspace(B, T, D, W)) return QD_ERR_WORKSPACE;
@@ -352,7 +352,7 @@ int qdelta_scan_fwd(const qd_scan_shape* shape, const void* u, const void* dt, c
                     size_t workspace_bytes, unsigned flags, qd_stream stream) {
     const int rc = check_scan(shape);
     if (rc != QD_OK) return rc;
-    if (!u || !dt || !A || !Bm || !Cm || !y) return QD_ERR_INVALID_ARG;
+    if (!u || !dt || !A || !Bm || !Cm || !y || (hT && hT == h0)) return QD_ERR_INVALID_ARG;
     const void* const ptrs[] = {u, dt, A, Bm, Cm, D, z, dt_bias, h0, y, hT, workspace};
     if (any_misaligned(ptrs) || (flags & ~(unsigned)(QD_SOFTPLUS | QD_FWD_SAVE_FOR_BWD))) return QD_ERR_INVALID_ARG;
     ScanArgs a{};
@@ -374,7 +374,7 @@ int qdelta_scan_bwd(const qd_scan_shape* shape, const void* u, const void* dt, c
     const int rc = check_scan(shape);
     if (rc != QD_OK) return rc;
     if (!u || !dt || !A || !Bm || !Cm || !dy || !du || !ddt || !dA || !dBm || !dCm) return QD_ERR_INVALID_ARG;
-    if ((D && !dD) || (z && !dz) || (dt_bias && !ddt_bias)) return QD_ERR_INVALID_ARG;
+    if ((D && !dD) || (z && !dz) || (dt_bias && !ddt_bias) || (dh0 && dh0 == dhT)) return QD_ERR_INVALID_ARG;
     const void* const ptrs[] = {u, dt, A, Bm, Cm, D, z, dt_bias, h0, dy, dhT, du, ddt, dA, dBm, dCm, dD, dz, ddt_bias, dh0, workspace};
     if (any_misaligned(ptrs) || (flags & ~(unsigned)(QD_SOFTPLUS | QD_BWD_REUSE_FWD))) return QD_ERR_INVALID_ARG;
     if (!workspace || workspace_bytes < scan_bwd_workspace(*shape)) return QD_ERR_WORKSPACE;

@@ -17,7 +17,7 @@ using namespace scan;
 constexpr int kStepThreads = 128;
 
 // Division of numbers below 2^31 by d <= 2^31: n m >> 31 + L for 2^L >= d and m = ceil(2^(31 + L) / d), whose error n (m d - 2^(31 + L)) / 2^(31 + L) d
-// is below 1 / d.  (A division of 64-bit numbers is 100 instructions, and a lane has 200 for its states.)
+// is below 1 / d; B D, and so the index of a channel, is 2^30 at most.  (A division of 64-bit numbers is 100 instructions, and a lane has 200 for its states.)
 struct Divisor {
     uint32_t m;
     int shift;
@@ -168,20 +168,8 @@ cudaError_t scan_steps(const ScanArgs& a) {
     p.A = a.A; p.skip = a.D; p.bias = a.dt_bias; p.softplus = a.softplus;
     p.channels = divisor(p.D);
     p.group = divisor(p.D / p.G);
-    // as many sequences at a time as a kernel can count the channels of
-    const int most = (1 << 30) / p.D;
-    const size_t size = a.s.dtype == QD_BF16 ? 2 : 4;
-    for (int b = 0; b < a.s.B; b += most) {
-        p.B = a.s.B - b < most ? a.s.B - b : most;
-        const size_t row = (size_t)b * p.S * p.D * size, bc = (size_t)b * p.S * p.G * p.N * size;
-        const auto from = [](const void* t, size_t o) { return t ? static_cast<const char*>(t) + o : nullptr; };
-        p.u = from(a.u, row); p.dt = from(a.dt, row); p.z = from(a.z, row); p.Bm = from(a.Bm, bc); p.Cm = from(a.Cm, bc);
-        p.y = static_cast<char*>(a.y) + row;
-        p.state = a.hT + (size_t)b * p.D * p.N;
-        const cudaError_t e = a.s.dtype == QD_BF16 ? launch<__nv_bfloat16>(p, a.stream) : launch<float>(p, a.stream);
-        if (e != cudaSuccess) return e;
-    }
-    return cudaSuccess;
+    p.B = a.s.B; p.u = a.u; p.dt = a.dt; p.z = a.z; p.Bm = a.Bm; p.Cm = a.Cm; p.y = a.y; p.state = a.hT;
+    return a.s.dtype == QD_BF16 ? launch<__nv_bfloat16>(p, a.stream) : launch<float>(p, a.stream);
 }
 
 }  // namespace qd

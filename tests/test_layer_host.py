@@ -37,6 +37,9 @@ def test_convolution_steps_and_backward(lib):
     assert back(FAKE, None, 2 * FAKE, FAKE, need) == 1                 # bias without dbias
     assert back(None, None, FAKE, FAKE, need) == 1                     # dx over x
     assert back(None, None, 3 * FAKE, FAKE, need) == 1                 # dx over dy
+    state = lambda dlast, dstate: lib.qdelta_conv_bwd(  # noqa: E731
+        2, 8, 64, 4, 1, FAKE, FAKE, None, None, 3 * FAKE, dlast, 2 * FAKE, FAKE, None, dstate, None, 0, 0, None)
+    assert state(4 * FAKE, 4 * FAKE) == 1 and state(4 * FAKE, 5 * FAKE) == 3        # one buffer for both; no workspace
     assert back(None, None, 2 * FAKE, FAKE, need - 1) == 3 and back(None, None, 2 * FAKE, None, need) == 3
 
 
@@ -71,6 +74,12 @@ def test_scan_arguments(lib):
     bwd = lambda D=None, dD=None, z=None, dz=None, b=None, db=None, ws=FAKE, n=need: lib.qdelta_scan_bwd(  # noqa: E731
         r, FAKE, FAKE, FAKE, FAKE, FAKE, D, z, b, None, FAKE, None, FAKE, FAKE, FAKE, FAKE, FAKE, dD, dz, db, None, ws, n, 2, None)
     assert bwd(D=FAKE) == 1 and bwd(z=FAKE) == 1 and bwd(b=FAKE) == 1 and bwd(n=need - 1) == 3 and bwd(ws=None) == 3
+    # one buffer for the states before and after, and for their gradients; with two it is the workspace that is missing
+    states = lambda h0, hT: lib.qdelta_scan_fwd(r, *[FAKE] * 5, None, None, None, h0, FAKE, hT, None, 0, 1, None)  # noqa: E731
+    assert states(FAKE, FAKE) == 1 and states(FAKE, 2 * FAKE) == 3
+    grads = lambda dhT, dh0: lib.qdelta_scan_bwd(  # noqa: E731
+        r, *[FAKE] * 5, None, None, None, FAKE, FAKE, dhT, *[FAKE] * 5, None, None, None, dh0, None, 0, 0, None)
+    assert grads(FAKE, FAKE) == 1 and grads(FAKE, 2 * FAKE) == 3
     # a forward of many channels needs no workspace, one of few long sequences does
     assert lib.qdelta_scan_workspace_bytes(ctypes.byref(_shape(B=64, D=2048)), 0) == 0
     assert lib.qdelta_scan_workspace_bytes(ctypes.byref(_shape(B=1, T=4096, D=128)), 0) > 0
