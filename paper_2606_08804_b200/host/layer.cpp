@@ -63,7 +63,10 @@ struct Params {
     at::Tensor next(c10::IntArrayRef shape) {              // each 16-byte aligned
         int64_t n = 1;
         for (const int64_t s : shape) n *= s;
-        const at::Tensor t = all.narrow(0, at, n).view(shape);
+        // a view without the dispatcher's two calls for one
+        at::Tensor t = at::detail::make_tensor<c10::TensorImpl>(c10::TensorImpl::VIEW, c10::Storage(all.storage()), all.key_set(), all.dtype());
+        t.unsafeGetTensorImpl()->set_storage_offset(all.storage_offset() + at);
+        t.unsafeGetTensorImpl()->set_sizes_contiguous(shape);
         at += (n + 3) / 4 * 4;
         return t;
     }
