@@ -8,8 +8,9 @@
 // Bound by HBM: 16384 tokens of 6144 bf16 channels take 74 us forward (5.4 TB/s) and 128 backward (4.7 TB/s, where the registers of the
 // gradients leave 16 warps to an SM), 256 decode steps 5.8 us (4.3 TB/s).  A thread owns a group of neighbouring channels and walks a run
 // of tokens with the last W - 1 inputs (and, backward, the last W - 1 dpre) in registers, so an input is read once but for the W - 1 tokens
-// in front of a run (W - 1 on either side backward); a warp reads 32 neighbouring groups of a token.  So that the arithmetic stays below HBM's time, channels are taken two at a time in the
-// packed fp32 instructions of sm_100, an input is widened once, and bf16 gates use the special function unit directly.
+// in front of a run (W - 1 on either side backward); a warp reads 32 neighbouring groups of a token.  So that the arithmetic stays below
+// HBM's time, channels are taken two at a time in the packed fp32 instructions of sm_100, an input is widened once, and bf16 gates use the
+// special function unit directly.
 // Where rows are not whole groups, the channels of a thread are `cx` apart instead, so that a warp's single loads are neighbours.
 #include "rows.cuh"
 

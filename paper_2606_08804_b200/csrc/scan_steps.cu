@@ -16,8 +16,9 @@ using namespace scan;
 
 constexpr int kStepThreads = 128;
 
-// Division of numbers below 2^31 by d <= 2^31: n m >> 31 + L for 2^L >= d and m = ceil(2^(31 + L) / d), whose error n (m d - 2^(31 + L)) / 2^(31 + L) d
-// is below 1 / d; B D, and so the index of a channel, is 2^30 at most.  (A division of 64-bit numbers is 100 instructions, and a lane has 200 for its states.)
+// Division of numbers below 2^31 by d <= 2^31: n m >> 31 + L for 2^L >= d and m = ceil(2^(31 + L) / d), whose error
+// n (m d - 2^(31 + L)) / 2^(31 + L) d is below 1 / d; B D, and so the index of a channel, is 2^30 at most.  (A division of 64-bit numbers is
+// 100 instructions, and a lane has 200 for its states.)
 struct Divisor {
     uint32_t m;
     int shift;
