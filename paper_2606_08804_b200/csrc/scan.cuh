@@ -217,6 +217,65 @@ __device__ __forceinline__ void copy_tiles(IO* const (&dst)[NA], const void* con
             if (src[a] && (SETS == 1 || a % SETS == tid / CH)) copy_group<E>(dst[a] + x * E, static_cast<const IO*>(src[a]) + at, have, how);
     }
 }
+// The same of one tile after the other where groups are whole and all tokens there: a thread's addresses move on by a step a tile.  `ring` is
+// that of the first tensor, the others' rings are behind it.
+template <int TT, int CC, int RING, typename IO, int NA>
+struct TileRun {
+    static constexpr int E = 16 / sizeof(IO), CH = TT * CC / E, SETS = CH < 128 ? 128 / CH : 1, PER = (NA + SETS - 1) / SETS, REP = (CH + 127) / 128;
+    const IO* src[PER];                      // null: absent
+    IO* dst;
+    long long step;
+    int bytes;                               // none where there are no channels
+    __device__ __forceinline__ TileRun(IO* ring, const void* const (&from)[NA], size_t row, int D, size_t col, int channels, int by, int tid) {
+        const int x = tid % CH, set = SETS > 1 ? tid / CH : 0, c = x % (CC / E) * E;
+        const bool has = channels > c;
+        bytes = has ? 16 : 0;
+        step = has ? (long long)by * D : 0;
+#pragma unroll
+        for (int j = 0; j < PER; ++j) {
+            src[j] = nullptr;
+#pragma unroll
+            for (int a = 0; a < NA; ++a)
+                if (a == set + j * SETS && from[a]) src[j] = static_cast<const IO*>(from[a]) + (has ? (row + x / (CC / E)) * D + col + c : 0);
+        }
+        dst = ring + (set * RING * CH + x) * E;
+    }
+    __device__ __forceinline__ void copy(int slot, int D) const {
+#pragma unroll
+        for (int j = 0; j < PER; ++j)
+#pragma unroll
+            for (int r = 0; r < REP; ++r)
+                if (src[j]) copy_bytes<16>(dst + ((j * SETS * RING + slot) * CH + r * 128) * E, src[j] + (bytes ? (size_t)(r * 128 / (CC / E)) * D : 0), bytes);
+    }
+    __device__ __forceinline__ void move() {
+#pragma unroll
+        for (int j = 0; j < PER; ++j)
+            if (src[j]) src[j] += step;
+    }
+};
+// And of B and C: four states of a token, of B by the first half of the threads that share a token (T tokens to a tile).
+template <int NS, typename IO>
+struct StateRun {
+    const IO* src;
+    size_t token;                            // elements from token to token
+    long long step;
+    int row, bytes;
+    __device__ __forceinline__ StateRun(const P& p, size_t first, int g, bool with_B, bool with_C, int by, int tid) {
+        const int r = tid % (NS / 2), s = r % (NS / 4) * 4;
+        const bool is_B = r < NS / 4, has = s < p.d.N && (is_B ? with_B : with_C);
+        row = tid / (NS / 2);
+        bytes = has ? 4 * sizeof(IO) : 0;
+        token = has ? (size_t)p.d.G * p.d.N : 0;
+        step = (long long)token * by;
+        src = static_cast<const IO*>(is_B ? p.Bm : p.Cm) + (has ? (first + row) * token + (size_t)g * p.d.N + s : 0);
+    }
+    template <int T, int J> __device__ __forceinline__ void copy(Pack<IO, 4> (&to)[J][128], int tid) const {
+#pragma unroll
+        for (int j = 0; j < J; ++j)
+            if (row + j * (256 / NS) < T) copy_bytes<4 * sizeof(IO)>(&to[j][tid], src + j * (256 / NS) * token, bytes);
+    }
+    __device__ __forceinline__ void move() { src += step; }
+};
 __device__ __forceinline__ void prepare_barrier() { asm volatile("bar.sync 1, 128;" ::: "memory"); }     // the half that prepares
 __device__ __forceinline__ float sum_pair(f2 v) {
     const float2 t = unpack2(v);

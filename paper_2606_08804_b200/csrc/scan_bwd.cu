@@ -29,6 +29,7 @@ template <typename IO, int NB> struct BwdSmem {
     alignas(16) float gB[2][NB][kSave][CC], gpA[2][NB][kSave][CC], y[2][NB][kSave][CC];
     alignas(16) float bc[2][kWalkers][kSave][32];          // dB, dC summed over a warp's channels
     f2x2 saved[SAVED][2][128];                             // of a thread that walks
+    // rings, each behind the one before (TileRun)
     alignas(16) IO u[RING][kSave * CC], dt[RING][kSave * CC], z[RING][kSave * CC], gy[RING][kSave * CC];
     Pack<IO, 4> rbc[RING][BCT][128];
 };
@@ -201,11 +202,18 @@ __global__ void __launch_bounds__(kThreads, 2) k_scan_bwd(const P p) {
     const f2 skip = pack2(skips[0], skips[1]);
     f2 sumD = 0, sumb = 0;
     struct Kept { f2 u, dt, dy, slope, gate; };             // slope: of the softplus; gate: dy SiLU'(z), with dy as it came in
+    const size_t begin = rows + t0 + (n - 1) * K;          // of the last tile
+    TileRun<K, CC, S::RING, IO, 4> run(&sm.u[0][0], {LOCAL ? nullptr : p.u, p.dt, p.z, p.dy}, begin, d.D, col, left, -K, tid);
+    StateRun<NS, IO> states(p, begin, g, !LOCAL, true, -K, tid);
     auto fetch = [&](int i) {
         if (i >= 0) {
             const int tt = t0 + i * K, slot = i % S::RING;
-            copy_tiles<K, CC, IO, 4>({sm.u[slot], sm.dt[slot], sm.z[slot], sm.gy[slot]}, {LOCAL ? nullptr : p.u, p.dt, p.z, p.dy}, rows, d.D, tt, t1, col, left,
+            const bool whole = tt + K <= t1;
+            if (whole && p.rows == kWhole) run.copy(slot, d.D);
+            else copy_tiles<K, CC, IO, 4>({sm.u[slot], sm.dt[slot], sm.z[slot], sm.gy[slot]}, {LOCAL ? nullptr : p.u, p.dt, p.z, p.dy}, rows, d.D, tt, t1, col, left,
                                      p.rows, tid);
+            if (whole && p.bc == kWhole) states.template copy<K>(sm.rbc[slot], tid);
+            else
 #pragma unroll
             for (int j = 0; j < S::BCT; ++j) {                             // four states of B or C of a token, which this thread prepares too
                 const int x = tid + j * 128, bt = x / (NS / 2), r = x % (NS / 2), s = r % (NS / 4) * 4;
@@ -215,6 +223,8 @@ __global__ void __launch_bounds__(kThreads, 2) k_scan_bwd(const P p) {
                               static_cast<const IO*>(r < NS / 4 ? p.Bm : p.Cm) + (have > 0 ? ((rows + tt + bt) * d.G + g) * d.N + s : 0), have, p.bc);
             }
         }
+        run.move();
+        states.move();
         copy_commit();
     };
     // Channels past the last have u = dy = 0 and any step; tokens past the last a step of 0.

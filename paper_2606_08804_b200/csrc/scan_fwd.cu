@@ -20,6 +20,7 @@ template <typename IO, int NB> struct FwdSmem {
     float4 step[2][kTile][2][PAIRS];                       // dt, dt, dt u, dt u of a pair of channels, in both orders
     float4 B[2][kTile][NS / 4], C[2][kTile][NS / 4];       // four states
     alignas(16) float y[2][NB][kTile][CC];
+    // rings, each behind the one before (TileRun)
     alignas(16) IO u[RING][kTile * CC], dt[RING][kTile * CC], z[RING][kTile * CC];
     Pack<IO, 4> bc[RING][NB][128];
 };
@@ -104,10 +105,16 @@ __global__ void __launch_bounds__(kThreads, 2) k_scan_fwd(const P p) {
     for (int e = 0; e < 2; ++e) bias[e] = p.dt_bias && 2 * pr + e < left ? p.dt_bias[col + 2 * pr + e] : 0.f;
 #pragma unroll
     for (int e = 0; e < 8; ++e) skip[e] = !LOCAL && p.D && ic + e < left ? p.D[col + ic + e] : 0.f;
+    TileRun<kTile, CC, S::RING, IO, 3> run(&sm.u[0][0], {p.u, p.dt, LOCAL ? nullptr : p.z}, rows + t0, d.D, col, left, kTile, tid);
+    StateRun<NS, IO> states(p, rows + t0, g, true, !LOCAL, kTile, tid);
     auto fetch = [&](int i) {
         if (i < n) {
             const int tt = t0 + i * kTile, slot = i % S::RING;
-            copy_tiles<kTile, CC, IO, 3>({sm.u[slot], sm.dt[slot], sm.z[slot]}, {p.u, p.dt, LOCAL ? nullptr : p.z}, rows, d.D, tt, t1, col, left, p.rows, tid);
+            const bool whole = tt + kTile <= t1;
+            if (whole && p.rows == kWhole) run.copy(slot, d.D);
+            else copy_tiles<kTile, CC, IO, 3>({sm.u[slot], sm.dt[slot], sm.z[slot]}, {p.u, p.dt, LOCAL ? nullptr : p.z}, rows, d.D, tt, t1, col, left, p.rows, tid);
+            if (whole && p.bc == kWhole) states.template copy<kTile>(sm.bc[slot], tid);
+            else
 #pragma unroll
             for (int j = 0; j < NB; ++j) {                                 // four states of B or C of a token, which this thread prepares too
                 const int x = tid + j * 128, bt = x / (NS / 2), r = x % (NS / 2), s = r % (NS / 4) * 4;
@@ -116,6 +123,8 @@ __global__ void __launch_bounds__(kThreads, 2) k_scan_fwd(const P p) {
                               static_cast<const IO*>(r < NS / 4 ? p.Bm : p.Cm) + (have > 0 ? ((rows + tt + bt) * d.G + g) * d.N + s : 0), have, p.bc);
             }
         }
+        run.move();
+        states.move();
         copy_commit();
     };
     // Channels past the last have u = 0 and any step; tokens past the last a step of 0.
