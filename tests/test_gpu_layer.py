@@ -103,7 +103,10 @@ SCAN = [  # B, T, D, N, G, dtype, softplus, gate, skip, bias, state
     (1, 2500, 20, 16, 1, F32, True, True, True, True, True),         # more segments than one joins by itself
     # segments of unequal lengths backward; in both directions; more CTAs than have room at once
     (5, 303, 40, 4, 40, F32, True, True, True, True, True), (4, 1301, 43, 3, 43, BF, True, True, True, True, True),
-    (2, 606, 50, 2, 50, F32, True, True, True, True, True), (1, 1503, 64, 2, 64, BF, True, True, True, True, True)]
+    (2, 606, 50, 2, 50, F32, True, True, True, True, True), (1, 1503, 64, 2, 64, BF, True, True, True, True, True),
+    # whole groups of channels that do not fill a CTA, of 16, 32 and 64 states
+    (1, 410, 136, 16, 1, BF, True, True, True, True, True), (1, 333, 24, 64, 3, BF, True, True, True, True, True),
+    (2, 150, 80, 32, 2, BF, True, True, True, True, True), (1, 410, 76, 20, 1, F32, True, True, True, True, True)]
 
 
 def _scan_inputs(B, T, D, N, G, dt, softplus, gate, skip, bias, state, seed=0):
@@ -209,6 +212,28 @@ def test_scan_steps_go_on_from_a_prompt(D, N, G, dt):
         y = qd.scan_steps(**p, state=one, softplus=True)
         assert torch.equal(y, torch.cat(got, 1)[:, t:t + 1])
     assert torch.equal(one, state)
+
+
+@pytest.mark.parametrize("dt", [BF, F32])
+@pytest.mark.parametrize("N", [1, 3, 4, 6, 8, 12, 16, 20, 31, 32, 44, 64])
+def test_scan_steps_of_an_odd_batch(N, dt):
+    from paper_2606_08804_b200 import binding as qd
+    B, S, D, G = 5, 3, 36, 3
+    a, _, _ = _scan_inputs(B, S, D, N, G, dt, True, True, True, True, True, seed=N)
+    h0 = a.pop("h0")
+    ry, rh = lf.scan(**{n: lf.f64(t) for n, t in a.items()}, h0=lf.f64(h0), softplus=True)
+    my, mh = lf.scan(**{n: t if n in ("A", "dt", "dt_bias") else _abs(t) for n, t in ((n, lf.f64(t)) for n, t in a.items())}, h0=_abs(lf.f64(h0)), softplus=True)
+    state = h0.clone()
+    y = qd.scan_steps(**a, state=state, softplus=True)
+    k = 2 * (10 * S + 2 * N + 40) * lf.ULP                 # as for the scan
+    lf.close("y", y, ry, k * _most(my))
+    lf.close("state", state, rh, k * _most(mh))
+    # each sequence by itself: the same bits
+    for b in range(B):
+        one = h0[b:b + 1].clone()
+        p = {n: t[b:b + 1].clone() if n in ("u", "dt", "Bm", "Cm", "z") else t for n, t in a.items()}
+        assert torch.equal(qd.scan_steps(**p, state=one, softplus=True), y[b:b + 1])
+        assert torch.equal(one, state[b:b + 1])
 
 
 # ---- norm -------------------------------------------------------------------------------------------------------------------
