@@ -236,6 +236,7 @@ def chunk_fwd_static(q, k, v, beta, alpha, lam, h0, o, hT=None, status=None, chu
         _ptr(h0, torch.float32, (B, H, dk, dv), "h0"), _ptr(o, dt, (B, T, H, dv), "o"),
         _ptr(hT, torch.float32, (B, H, dk, dv), "hT"), sp, _stream())
     _check(rc, "qdelta_chunk_fwd_static")
+    torch.autograd.graph.increment_version([t for t in (o, hT, status) if t is not None])
     return o, hT
 
 

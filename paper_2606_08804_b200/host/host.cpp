@@ -38,6 +38,8 @@ PyObject* recurrent_step(PyObject*, PyObject* const* a, Py_ssize_t n) {
             rc = qdelta_recurrent_step((int)B, (int)H, (int)dk, (int)dv, code, qp, kp, vp, bp, ap, lp, sp, op, stream());
         }
         check(rc, "qdelta_recurrent_step");
+        written(tensor(a[6], "state"));
+        written(tensor(a[7], "o"));
         return made.defined() ? THPVariable_Wrap(std::move(made)) : own(a[7]);
     });
 }
@@ -71,6 +73,8 @@ PyObject* recurrent_steps(PyObject*, PyObject* const* a, Py_ssize_t n) {
             rc = qdelta_recurrent_steps((int)B, (int)S, (int)H, (int)dk, (int)dv, code, qp, kp, vp, bp, ap, lp, sp, op, flags, stream());
         }
         check(rc, "qdelta_recurrent_steps");
+        written(&state);
+        written(tensor(a[7], "o"));
         return made.defined() ? THPVariable_Wrap(std::move(made)) : own(a[7]);
     });
 }
@@ -127,6 +131,8 @@ PyObject* chunk_fwd(PyObject*, PyObject* const* a, Py_ssize_t n) {
                                   flags, stream());
         }
         check(rc, "qdelta_chunk_fwd");
+        written(tensor(a[9], "o"));
+        written(tensor(a[10], "hT"));
         PyObject* r = PyTuple_New(3);
         if (!r) throw Raised{};
         PyTuple_SET_ITEM(r, 0, o_made.defined() ? THPVariable_Wrap(std::move(o_made)) : own(a[9]));
@@ -149,9 +155,13 @@ PyObject* chunk_bwd(PyObject*, PyObject* const* a, Py_ssize_t n) {
         if (!ws) { ws_made = c.workspace(1); ws = &ws_made; }
         if (!PyDict_Check(a[11])) { PyErr_SetString(PyExc_TypeError, "out must be a dict"); throw Raised{}; }
         // a gradient that the caller does not supply is allocated; an unwanted one is None
+        std::vector<const at::Tensor*> supplied;
         auto grad = [&](const char* name, at::ScalarType dt, c10::IntArrayRef shape, bool wanted) -> void* {
             PyObject* have = PyDict_GetItemString(a[11], name);
-            if (have) return ptr(tensor(have, name), dt, shape, name);
+            if (have) {
+                supplied.push_back(tensor(have, name));
+                return ptr(supplied.back(), dt, shape, name);
+            }
             if (!wanted) { if (PyDict_SetItemString(a[11], name, Py_None)) throw Raised{}; return nullptr; }
             at::Tensor t = empty(shape, dt, c.dev);
             void* p = t.data_ptr();
@@ -175,6 +185,7 @@ PyObject* chunk_bwd(PyObject*, PyObject* const* a, Py_ssize_t n) {
                                   ws->data_ptr(), (size_t)ws->numel(), flags, stream());
         }
         check(rc, "qdelta_chunk_bwd");
+        for (const at::Tensor* t : supplied) written(t);
         return own(a[11]);
     });
 }
@@ -196,14 +207,16 @@ struct ChunkNode : torch::autograd::Function<ChunkNode> {
         ctx->set_materialize_grads(false);         // an unused output costs no tensor of zeros
         if (need_grad) {
             auto or_none = [](const MaybeTensor& t) { return t ? *t : at::Tensor(); };
-            ctx->save_for_backward({q, k, v, beta, or_none(alpha), or_none(lam), or_none(h0), ws});
+            // not h0, which the workspace stands for: its owner may go on with it in place
+            ctx->save_for_backward({q, k, v, beta, or_none(alpha), or_none(lam), ws});
             ctx->saved_data["flags"] = flags;
+            ctx->saved_data["h0"] = h0.has_value();
         }
         return {o, hT};
     }
     static variable_list backward(AutogradContext* ctx, variable_list g) {
         const variable_list in = ctx->get_saved_variables();
-        const at::Tensor &q = in[0], &v = in[2], &beta = in[3], &alpha = in[4], &lam = in[5], &h0 = in[6], &ws = in[7];
+        const at::Tensor &q = in[0], &v = in[2], &beta = in[3], &alpha = in[4], &lam = in[5], &ws = in[6];
         if (q.dim() != 4 || v.dim() != 4) raise("q and v must have four dimensions");
         const int64_t B = q.size(0), T = q.size(1), H = q.size(2), dk = q.size(3), dv = v.size(3);
         const at::ScalarType dt = q.scalar_type();
@@ -221,7 +234,7 @@ struct ChunkNode : torch::autograd::Function<ChunkNode> {
         if (dt != at::kFloat && dt != at::kBFloat16) raise("q must be fp32 or bf16");
         seen(q, dt, {B, T, H, dk}, "q"); seen(in[1], dt, {B, T, H, dk}, "k"); seen(v, dt, {B, T, H, dv}, "v");
         seen(beta, dt, {B, T, H}, "beta"); seen(alpha, dt, {B, T, H}, "alpha"); seen(lam, dt, {B, T, H}, "lam");
-        seen(h0, at::kFloat, {B, H, dk, dv}, "h0"); seen(ws, at::kByte, {ws.numel()}, "the saved workspace");
+        seen(ws, at::kByte, {ws.numel()}, "the saved workspace");
         seen(dO, dt, {B, T, H, dv}, "dO"); seen(dhT, at::kFloat, {B, H, dk, dv}, "dhT");
         auto make = [&](c10::IntArrayRef shape, at::ScalarType t) { return at::Tensor(at::detail::empty_cuda(shape, t, dev, std::nullopt)); };
         at::Tensor gq = make({B, T, H, dk}, dt), gk = make({B, T, H, dk}, dt), gv = make({B, T, H, dv}, dt), gh;
@@ -231,10 +244,10 @@ struct ChunkNode : torch::autograd::Function<ChunkNode> {
         float* base = gates.data_ptr<float>();
         const int64_t row = B * T * H;
         float *db = base, *da = alpha.defined() ? base + row : nullptr, *dl = lam.defined() ? base + (n - 1) * row : nullptr;
-        if (h0.defined()) gh = make({B, H, dk, dv}, at::kFloat);
+        if (ctx->saved_data["h0"].toBool()) gh = make({B, H, dk, dv}, at::kFloat);
         auto p = [](const at::Tensor& t) -> void* { return t.defined() ? t.data_ptr() : nullptr; };
         const unsigned flags = (unsigned)ctx->saved_data["flags"].toInt() | QD_BWD_REUSE_FWD;
-        const int rc = qdelta_chunk_bwd(&s, p(q), p(in[1]), p(v), p(beta), p(alpha), p(lam), (const float*)p(h0), p(dO),
+        const int rc = qdelta_chunk_bwd(&s, p(q), p(in[1]), p(v), p(beta), p(alpha), p(lam), nullptr, p(dO),
                                         (const float*)p(dhT), p(gq), p(gk), p(gv), db, da, dl, (float*)p(gh), ws.data_ptr(),
                                         (size_t)ws.numel(), flags, stream());
         if (rc != QD_OK) raise("qdelta_chunk_bwd failed: " + std::string(qdelta_status_string(rc)) + " (" + std::to_string(rc) + ")");

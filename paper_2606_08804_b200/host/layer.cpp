@@ -331,6 +331,8 @@ PyObject* conv_steps(PyObject*, PyObject* const* a, Py_ssize_t n) {
             const at::Tensor o = given ? *given : c.on.make({c.B, c.T, c.D}, c.dt);
             rc_check(qdelta_conv_steps(c.b, c.t, c.d, c.w, c.code, c.xp, c.wp, c.bp, sp, c.on.p(&o, c.dt, {c.B, c.T, c.D}, "y"), flags, stream()),
                      "qdelta_conv_steps");
+            written(&state);
+            written(given);
             return o;
         });
         return given ? own(a[4]) : wrapped(y);
@@ -383,6 +385,8 @@ PyObject* scan_steps(PyObject*, PyObject* const* a, Py_ssize_t n) {
             rc_check(qdelta_scan_steps(&c.s, c.u, c.dtp, c.A, c.Bm, c.Cm, c.skip, c.z, c.bias, sp, c.on.p(&o, c.dt, {c.B, c.T, c.D}, "y"), flags,
                                        stream()),
                      "qdelta_scan_steps");
+            written(&state);
+            written(given);
             return o;
         });
         return given ? own(a[9]) : wrapped(y);
@@ -491,8 +495,10 @@ struct ScanNode : torch::autograd::Function<ScanNode> {
         const ScanOut r = scan_forward(t, maybe(h0), nullptr, true, (unsigned)flags | (need_grad ? QD_FWD_SAVE_FOR_BWD : 0));
         ctx->set_materialize_grads(false);
         if (need_grad) {
-            ctx->save_for_backward({u, dt, A, Bm, Cm, or_none(D), or_none(z), or_none(bias), or_none(h0), r.ws});
+            // not h0, which the workspace stands for: its owner may go on with it in place
+            ctx->save_for_backward({u, dt, A, Bm, Cm, or_none(D), or_none(z), or_none(bias), r.ws});
             ctx->saved_data["flags"] = flags;
+            ctx->saved_data["h0"] = h0.has_value();
         }
         return {r.y, r.hT};
     }
@@ -505,10 +511,10 @@ struct ScanNode : torch::autograd::Function<ScanNode> {
                 if (i < 5) present(in[i], names[i]);
                 t[i] = given(in[i]);
             }
-            present(in[9], "the saved workspace");
+            present(in[8], "the saved workspace");
             const at::Tensor& u = in[0];
             const at::Tensor dy = or_zeros(upstream(g[0], u.scalar_type()), u), dhT = upstream(g[1], at::kFloat);
-            const ScanGrads r = scan_backward(t, given(in[8]), dy, given(dhT), &in[9], in[8].defined(),
+            const ScanGrads r = scan_backward(t, nullptr, dy, given(dhT), &in[8], ctx->saved_data["h0"].toBool(),
                                               (unsigned)ctx->saved_data["flags"].toInt() | QD_BWD_REUSE_FWD);
             return {r.du, r.ddt, r.dA, r.dBm, r.dCm, r.dD, r.dz, r.dbias, r.dh0, at::Tensor(), at::Tensor()};
         });

@@ -107,6 +107,12 @@ inline int to_int(PyObject* o) {
     return (int)v;
 }
 
+// The caller's tensor that a call has written in place: counted as torch counts its own operations in place, so that a graph that saved
+// the tensor refuses its backward instead of computing with other values.
+inline void written(const at::Tensor* t) {
+    if (t && t->defined() && !t->is_inference()) t->unsafeGetTensorImpl()->bump_version();
+}
+
 // ---- autograd ---------------------------------------------------------------------------------------------------------
 using torch::autograd::AutogradContext;
 using torch::autograd::variable_list;
