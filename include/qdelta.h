@@ -207,7 +207,8 @@ int qdelta_conv_bwd(int B, int T, int D, int W, int dtype, const void *x, const 
 /*
  * Selective state space scan, N states to a channel:
  *     h_t = exp(dt_t A) h_{t-1} + dt_t u_t Bm_t ,   y_t = (<Cm_t, h_t> + D u_t) SiLU(z_t)
- *     u, dt, z, y [B,T,D]   A [D,N] fp32 (not positive where the state is to stay bounded)   D, dt_bias [D] fp32
+ *     u, dt, z, y [B,T,D]   A [D,N] fp32 (not positive where the state is to stay bounded; minus infinity counts as
+ *     the lowest number)   D, dt_bias [D] fp32
  *     Bm, Cm [B,T,G,N], shared by the D / G channels of a group   h0, hT [B,D,N] fp32
  * D, z, dt_bias, h0 may be NULL (no skip, no factor, no bias, zero state), hT too (not returned; not the same buffer as h0, which
  * the first tokens may read after the last ones are done).

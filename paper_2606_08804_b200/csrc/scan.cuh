@@ -28,6 +28,8 @@
 #pragma once
 #include "rows.cuh"
 
+#include <cfloat>
+
 namespace qd {
 namespace scan {
 
@@ -114,6 +116,9 @@ __device__ __forceinline__ float2 softplus(float x, float y) {
 // either sign beyond; 2^0 stays 1 exactly.  (8 x 2048 tokens of 2048 channels: dA 0.76e-6 off, without it 1.8e-6, with 1.2e-8 1.04e-6, with
 // 2.4e-8 0.77e-6; fp32 operations one by one 0.92e-6.)
 constexpr float kDecayShift = 2e-8f;
+// A log2(e) is taken no lower than the lowest number: minus infinity would make a step of 0, as that of the tokens past the last, 0 times
+// infinity, where the state has to pass through.  Every step above 1e-36 forgets the state either way.  (NaN stays NaN.)
+__device__ __forceinline__ float no_lower(float a) { return a < -FLT_MAX ? -FLT_MAX : a; }
 __device__ __forceinline__ f2 decay(f2 dt, f2 A2) { return exp2_pair(fma2(dt, A2, both(kDecayShift))); }
 
 // What a walking lane owns.  Registers [channel][pair of states], flat.
@@ -147,6 +152,15 @@ __device__ __forceinline__ void load_state(const P& p, const Map& m, const float
     each_state(p, m, g, ch, n0, [&](int r, int e, size_t at, bool in) { v[r][e] = in ? s[at] * scale : 0.f; });
 #pragma unroll
     for (int r = 0; r < 4; ++r) h[r] = pack2(v[r][0], v[r][1]);
+}
+// A log2(e)
+__device__ __forceinline__ void load_A(const P& p, const Map& m, int g, int ch, int n0, f2 (&A2)[4]) {
+    load_state(p, m, p.A, g, ch, n0, kLog2e, A2);
+#pragma unroll
+    for (f2& a : A2) {
+        const float2 v = unpack2(a);
+        a = pack2(no_lower(v.x), no_lower(v.y));
+    }
 }
 __device__ __forceinline__ void store_state(const P& p, const Map& m, float* s, int g, int ch, int n0, const f2 (&h)[4]) {
     each_state(p, m, g, ch, n0, [&](int r, int e, size_t at, bool in) {

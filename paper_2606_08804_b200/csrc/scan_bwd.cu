@@ -59,7 +59,7 @@ __global__ void __launch_bounds__(kThreads, 2) k_scan_bwd(const P p) {
         const size_t mine = (((size_t)g * d.ctas + ct) * kWalkers + warp) * kWarpTile + lane * 8, state = (size_t)b * d.D * d.N;
         f2 A2[4], ga[4] = {0, 0, 0, 0}, dA[4] = {0, 0, 0, 0};              // ga = a_{t+1} g_{t+1}
         float sum[2] = {0.f, 0.f};
-        load_state(p, m, p.A, g, ch, n0, kLog2e, A2);
+        load_A(p, m, g, ch, n0, A2);
         if (seg == p.segs - 1) {
             if (p.dhT) load_state(p, m, p.dhT + state, g, ch, n0, 1.f, ga);
         } else if (!LOCAL) load_end(p, p.segs - 2, -1, p.segs - 1 - seg, b, mine, ga);

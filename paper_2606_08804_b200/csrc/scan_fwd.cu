@@ -49,7 +49,7 @@ __global__ void __launch_bounds__(kThreads, 2) k_scan_fwd(const P p) {
         const size_t mine = (((size_t)g * d.ctas + ct) * kWalkers + warp) * kWarpTile + lane * 8, state = (size_t)b * d.D * d.N;
         f2 A2[4], h[4] = {0, 0, 0, 0};
         float sum[2] = {0.f, 0.f};
-        load_state(p, m, p.A, g, ch, n0, kLog2e, A2);
+        load_A(p, m, g, ch, n0, A2);
         if (seg == 0) {
             if (p.h0) load_state(p, m, p.h0 + state, g, ch, n0, 1.f, h);
         } else if (!LOCAL) load_end(p, 0, 1, seg, b, mine, h);

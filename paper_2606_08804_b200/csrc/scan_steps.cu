@@ -73,7 +73,7 @@ __global__ void __launch_bounds__(kStepThreads, 8) k_scan_steps(const StepsP p) 
     for (int r = 0; r < R; ++r) widen(four(state[r]), h[r]);
     widen(four(p.A + (size_t)ch * p.N + n0), a2);
 #pragma unroll
-    for (float& a : a2) a *= kLog2e;
+    for (float& a : a2) a = no_lower(a * kLog2e);
     const float bias = p.bias ? p.bias[ch] : 0.f, skip = p.skip ? p.skip[ch] : 0.f;
 #pragma unroll 1
     for (int s = 0; s < (ONE ? 1 : p.S); ++s) {
