@@ -187,6 +187,8 @@ __device__ __forceinline__ void store_end(const P& p, int k, int b, size_t lane,
     store_tile(p.ends + at, h);
     store_tile(p.decays + at, a);
 }
+// A segment's end from the state before it.  Where A is positive its decay may overflow, which a state of 0 does not notice.
+__device__ __forceinline__ float joined(float decay, float before, float end) { return before == 0.f ? end : fmaf(decay, before, end); }
 // the state behind segment ends[n - 1] of `from, from + step, ..`
 __device__ __forceinline__ void load_end(const P& p, int from, int step, int n, int b, size_t lane, f2 (&h)[4]) {
     const size_t stride = (size_t)p.d.B * p.d.states, base = (size_t)b * p.d.states + lane;
@@ -198,7 +200,10 @@ __device__ __forceinline__ void load_end(const P& p, int from, int step, int n, 
         load_tile(p.decays + (size_t)(from + k * step) * stride + base, a);
         load_tile(p.ends + (size_t)(from + k * step) * stride + base, e);
 #pragma unroll
-        for (int j = 0; j < 4; ++j) h[j] = fma2(a[j], h[j], e[j]);
+        for (int j = 0; j < 4; ++j) {
+            const float2 x = unpack2(a[j]), y = unpack2(h[j]), z = unpack2(e[j]);
+            h[j] = pack2(joined(x.x, y.x, z.x), joined(x.y, y.y, z.y));
+        }
     }
 }
 // N neighbouring elements on their way to shared memory: those from `left` on are 0.  kSingle waits for them.

@@ -204,7 +204,7 @@ __global__ void __launch_bounds__(256) k_join(float* ends, const float* decays, 
 #pragma unroll 4
     for (int k = 1; k < n; ++k) {
         const size_t at = (size_t)(from + k * step) * count + i;
-        h = fmaf(decays[at], h, ends[at]);
+        h = joined(decays[at], h, ends[at]);
         ends[at] = h;
     }
 }

@@ -35,3 +35,32 @@ def test_states_that_forget_at_every_step(B, T, D, N, dt, low):
     y, hT, _ = qd.scan_fwd(**few, h0=a["h0"], softplus=True)
     sx.close("y", y, *want["y"])
     sx.close("hT", hT, *want["hT"])
+
+
+@pytest.mark.parametrize("T", [900, 4000])                    # ends joined by each segment itself, and by a kernel of its own
+@pytest.mark.parametrize("dt", [BF, F32])
+def test_states_of_zero_that_would_have_grown(T, dt):
+    """A positive, and nothing in the state till the last tokens (a batch padded in front): zero times a growth that overflows is zero.
+    Backward likewise from a gradient that is zero till the first tokens."""
+    from paper_2606_08804_b200 import binding as qd
+    a, dy, _ = _inputs(1, T, 24, 4, 1, dt, softplus=False, bias=False, state=False)
+    a["A"] = (-a["A"]).clamp(min=0.6, max=8)
+    a["dt"].fill_(8)
+    a["dt"][:, :20] = a["dt"][:, -20:] = 0.0625
+    a["u"][:, :-20] = 0
+    dy[:, 20:] = 0
+    assert _cut(a)[0] > 0 and float(a["A"].min()) * 8 * 32 > 100           # a segment has 32 tokens at least
+    last = {n: t[:, -20:].contiguous() if n in ("u", "dt", "Bm", "Cm", "z") else t for n, t in a.items()}
+    want = sx.scan(**last)
+    y, hT, ws = qd.scan_fwd(**a, save_for_bwd=True)
+    sx.close("y", y[:, -20:], *want["y"])
+    sx.close("hT", hT, *want["hT"])
+    assert not y[:, :-20].any()
+    g = qd.scan_bwd(**a, dy=dy, dhT=torch.zeros_like(hT), workspace=ws, reuse_fwd=True)
+    first = {n: t[:, :20].contiguous() if n in ("u", "dt", "Bm", "Cm", "z") else t for n, t in a.items()}
+    want = sx.scan(**first, dy=dy[:, :20])
+    for name in ("du", "ddt", "dBm", "dCm", "dz"):
+        sx.close(name, g[name][:, :20], *want[name])
+    for name in ("du", "dBm"):                             # what later tokens send back: nothing
+        assert not g[name][:, 20:].any(), name
+    sx.close("dA", g["dA"], want["dA"][0], want["dA"][1])
