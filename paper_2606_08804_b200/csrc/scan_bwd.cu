@@ -331,7 +331,8 @@ __global__ void __launch_bounds__(kThreads, 2) k_scan_bwd(const P p) {
             for (int r = 0; r < S::PASSES; ++r) kept[0][r] = kept[1][r];
         }
         fetch(i - (S::RING - 2));                                          // where a tile stood that was finished before the last barrier
-        prepare_barrier();                                                 // the next tile takes the place of the one that is finished now
+        // (the next tile's steps, dy, B and C take the place of those of the tile before, which the walk read before the last barrier; what is
+        // finished here lies elsewhere)
         if (i > 0) turn(i - 1, kept[1]);
         copy_wait<S::RING - 4>();                                          // tile i - 2, for all after the barrier
         __syncthreads();
