@@ -86,21 +86,24 @@ bool make_tmap_tokens(CUtensorMap* map, const void* base, int B, int T, int H, i
 }
 
 cudaError_t set_max_smem_once(const void* kernel, size_t bytes) {
-    // fixed table, no heap: the largest size set so far for each (kernel, device)
-    struct Entry { const void* kernel; int dev; size_t bytes; };
+    // fixed tables, no heap: the largest size set so far for each kernel, one table a device (all of this library's kernels that ask for
+    // shared memory are 126; where a table is full, or there is none, the size is set anew every time)
+    struct Entry { const void* kernel; size_t bytes; };
+    constexpr int kDevices = 16, kKernels = 256;
     static std::mutex mu;
-    static Entry table[128];
+    static Entry tables[kDevices][kKernels];
     int dev = 0;
     cudaError_t e = cudaGetDevice(&dev);
     if (e != cudaSuccess) return e;
     std::lock_guard<std::mutex> lock(mu);
     Entry* slot = nullptr;
-    for (Entry& t : table) {
-        if (!t.kernel || (t.kernel == kernel && t.dev == dev)) { slot = &t; break; }
-    }
+    if (dev < kDevices)
+        for (Entry& t : tables[dev]) {
+            if (!t.kernel || t.kernel == kernel) { slot = &t; break; }
+        }
     if (slot && slot->kernel && slot->bytes >= bytes) return cudaSuccess;
     e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes);
-    if (e == cudaSuccess && slot) { slot->kernel = kernel; slot->dev = dev; slot->bytes = bytes; }
+    if (e == cudaSuccess && slot) { slot->kernel = kernel; slot->bytes = bytes; }
     return e;
 }
 
