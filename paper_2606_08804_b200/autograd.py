@@ -13,7 +13,11 @@ The operators around it likewise, gradients in the type of what they belong to:
     y, hT = selective_scan(u, dt, A, Bm, Cm, D, z, dt_bias, h0, softplus=False)             (binding.scan_fwd)
     y = layer_norm(x, weight, bias, eps, rms=False)                                         (binding.norm_fwd)
 
-Inputs of all of them may have any strides (they are made dense first).
+Inputs of all of them may have any strides (they are made dense first).  Types are not converted: w, bias, state and weight have the type
+of x (bf16 or fp32; pass w.to(x.dtype) where parameters are kept in fp32), A, D, dt_bias and h0 are fp32.
+
+What is saved for the backward may not be written before it, by torch or by the single-token calls (binding.conv_steps, scan_steps,
+recurrent_steps), which update a state in place: the backward then raises.  The initial states h0 are not saved.
 """
 from . import binding as qd
 

@@ -41,7 +41,7 @@ constexpr int kTile = 16;                    // tokens of a tile, forward
 constexpr size_t kWarpTile = kWarpChannels * kWarpStates;          // states of a warp, in the order [lane][channel][state]
 
 // Shared memory that two CTAs of an SM do not have: asked for where every CTA can have an SM for itself, which it would not get while the
-// kernel before still holds some of them (backward of 128 CTAs after another kernel: 680 us instead of 480).
+// kernel before still holds some of them (backward of 128 CTAs, 4 x 2048 tokens of 2048 channels, call after call: 423 us, 459 without).
 constexpr size_t kAloneSmem = 116 * 1024;
 
 // What both directions derive from the shape.

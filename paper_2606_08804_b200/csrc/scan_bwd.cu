@@ -5,8 +5,9 @@
 // a_t and h_{t-1} kept in registers, and then g is walked back, (a g) h_{t-1} being g p.  The registers hold half a tile; the first half is
 // walked once more ahead, to the state in the middle (a state saved every fourth token would be 134 MB more for each 8192 x 2048 x 16).
 // Per token, channel and state 1.5 exponentials and 13 operations of the fp32 pipe, 190 instructions a token and warp, a third of them
-// preparing: 8 x 2048 tokens of 2048 bf16 channels, 16 states, take 643 us with the sums, where two CTAs to an SM issue in 69 % of the clocks;
-// what is left are the latencies of a chain of shuffles and products, and registers leave no room for a third.
+// preparing: 8 x 2048 tokens of 2048 bf16 channels, 16 states, take 646 us with the sums (fp32 800), where two CTAs to an SM issue in 64 % of
+// the clocks, the special function unit is busy in 39 % and shared memory in 62; what is left are the latencies of a chain of shuffles and
+// products, and registers leave no room for a third.
 #include "scan.cuh"
 
 namespace qd {

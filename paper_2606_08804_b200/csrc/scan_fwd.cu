@@ -1,10 +1,10 @@
 // Forward of the selective scan (scan.cuh).  Per token, channel and state: one exponential and the products dt A, dt u B, a h + ., <C, h>.
 // The special function unit gives 4 exponentials per clock and sub-partition, so a warp's 16 x 16 states need 64 clocks of it and 32 of the
-// fp32 pipe, softplus and gate another 16.  8 x 2048 tokens of 2048 bf16 channels, 16 states: 251 us when it saves for a backward (240
-// without) against 144 of that unit and 40 of HBM.  With two walking and two preparing warps a sub-partition nothing is full: special
-// function unit 65 %, shared memory and shuffles 68 %, issue slots 63 %; the walk alone takes 189, preparing alone 170.  Not faster:
-// eight preparing warps, copies further ahead, part of the exponentials as polynomials on the fp32 pipe (766 to 771 us for 32768 tokens
-// walked in segments before the copies' addresses moved on by themselves, 257 to 271 for these).
+// fp32 pipe, softplus and gate another 16.  8 x 2048 tokens of 2048 bf16 channels, 16 states: 256 us when it saves for a backward (237
+// without) against 144 of that unit and 40 of HBM; fp32 275 (258).  With two walking and two preparing warps a sub-partition nothing is full:
+// on the SMs that have two CTAs the special function unit 65 %, shared memory and shuffles 74 %, issue slots 49 %.  Not faster, measured when
+// these took 257 (the walk alone then took 189, preparing alone 170): eight preparing warps, copies further ahead, part of the exponentials
+// as polynomials on the fp32 pipe (271).
 #include "scan.cuh"
 
 #include <algorithm>
