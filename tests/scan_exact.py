@@ -3,7 +3,7 @@
 The bounds follow the kernels' operations to first order in e = 2^-24, half a step of fp32:
   * a special function (2^x, 1 / x) is within 2 steps, 4 e; an argument of size s that is rounded k times costs s k e;
   * a decay a_t = 2^(dt A log2 e) is off by (|A| of dt's error + e (3 |dt A| + 4.24)) a_t: three roundings of the argument, 2^x, and the
-    2e-8 (0.24 e) by which the argument is shifted; where a segment's decay is one power of the sum of its steps, n e |dt A| more, n the
+    2e-8 (0.24 e) by which the argument is shifted; a power below 2^-126, the smallest that is not denormal, comes out 0; where a segment's decay is one power of the sum of its steps, n e |dt A| more, n the
     tokens of the longest segment (a sum of n terms);
   * an error of the state decays as the state does: E_t = a_t E_{t-1} + what token t adds, per state and not for the largest of them.
 Second-order terms are taken in by the factor SECOND.
@@ -40,7 +40,7 @@ def scan(u, dt, A, Bm, Cm, D=None, z=None, dt_bias=None, h0=None, softplus=False
     arg = dt[..., None] * A
     a = torch.exp(arg)
     known = A.abs() * e_dt[..., None]
-    ra = a * (known + E * (3 * arg.abs() + 4.24))                              # error of a decay
+    ra = a * (known + E * (3 * arg.abs() + 4.24)) + torch.clamp(a, max=2.0 ** -126)          # error of a decay
     ra_f, ra_b = (ra + a * E * n * arg.abs() for n in cut)
     BB, CC = grouped(Bm), grouped(Cm)
     xB = x[..., None] * BB

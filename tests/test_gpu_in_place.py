@@ -2,8 +2,6 @@
 import pytest
 import torch
 
-import gpu_util as gu  # noqa: F401  (the library is built before the first call)
-
 pytestmark = pytest.mark.gpu
 BF, F32 = torch.bfloat16, torch.float32
 SAYS = "modified by an inplace operation"
