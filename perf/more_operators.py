@@ -204,7 +204,7 @@ def _own(s):
         y, total, stats = qd.add_norm_fwd(*args, EPS, rms=rms)
         if kind == "prefill":
             return {"y": y, "total": total}
-        g = qd.add_norm_bwd(s["x"], total, s["scale"], s["weight"], s["dy"], s["dtotal"], stats, rms=rms, want_dbias=case["bias"])
+        g = qd.add_norm_bwd(s["x"], s["residual"], s["scale"], s["weight"], s["dy"], s["dtotal"], stats, rms=rms, want_dbias=case["bias"])
         return {"y": y, "total": total, **_kept(g)}
     if case["op"] == "rotary":
         how = {"positions": s["positions"], "start": s["start"], "interleaved": case["interleaved"], "scale": case["scale"]}
