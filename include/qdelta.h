@@ -96,9 +96,11 @@ typedef struct CUstream_st *qd_stream;   /* a cudaStream_t */
 
 /* flags of the operators around the delta rule */
 enum {
-    QD_SILU = 32,             /* qdelta_conv_*: y = SiLU(convolution) */
+    QD_SILU = 32,             /* qdelta_conv_*: y = SiLU(convolution); qdelta_gated_norm_*: the gate is SiLU(gate) */
     QD_SOFTPLUS = 64,         /* qdelta_scan_*: the step is softplus(dt + dt_bias); without it dt + dt_bias as given */
-    QD_RMS = 128              /* qdelta_norm_*: no mean is taken off */
+    QD_RMS = 128,             /* qdelta_*norm_*: no mean is taken off */
+    QD_INTERLEAVED = 256,     /* qdelta_rotary: pairs are neighbours */
+    QD_INVERSE = 512          /* qdelta_rotary: backwards */
 };
 
 /* Which kernels serve `shape` (the paper has no counterpart; a query for tests and benchmarks):
@@ -254,6 +256,77 @@ size_t qdelta_norm_workspace_bytes(long long rows, int width, int dtype);       
 /* Backward for  L = <y, dy>: dx in `dtype`, dweight, dbias [width] fp32 (NULL: skipped).  No workspace is needed without them. */
 int qdelta_norm_bwd(long long rows, int width, int dtype, const void *x, const void *weight, const void *dy, const float *stats,
                     void *dx, float *dweight, float *dbias, void *workspace, size_t workspace_bytes, unsigned flags, qd_stream stream);
+
+/*
+ * Linear attention with a decay for each head, d = exp(log_decay[h]):
+ *     S_t = d S_{t-1} + k_t v_t^T ,   o_t = scale S_t^T q_t
+ *     q, k [B,T,H,dk]   v, o [B,T,H,dv]   log_decay [H] fp32 (not positive where the state is to stay bounded; minus infinity: nothing
+ *     is kept)   h0, hT [B,H,dk,dv] fp32   dk, dv = 64 or 128   scale finite
+ * h0 NULL: a zero state; hT NULL: not returned (not the same buffer as h0).  T <= 2^30.  The workspace's first word is a status word
+ * (qdelta_workspace_status).  bf16 runs on the tensor cores (tcgen05), fp32 on fp32-accurate kernels.
+ */
+typedef struct {
+    int B, T, H, dk, dv;
+    int dtype;                /* qd_dtype of q, k, v, o and their gradients */
+} qd_linear_shape;
+
+/* 0 on an invalid shape */
+size_t qdelta_linear_workspace_bytes(const qd_linear_shape *shape, int for_backward);
+
+int qdelta_linear_fwd(const qd_linear_shape *shape, const void *q, const void *k, const void *v, const float *log_decay, const float *h0,
+                      void *o, float *hT, float scale, void *workspace, size_t workspace_bytes, unsigned flags, qd_stream stream);
+
+/* Backward for  L = <o, dO> + <hT, dhT>  (dhT NULL: zero): dq, dk, dv in `dtype`, dh0 fp32 (NULL: skipped; else not the same buffer as
+ * dhT).  Needs nothing of the forward but its inputs.  log_decay is a constant of the layer: it has no gradient. */
+int qdelta_linear_bwd(const qd_linear_shape *shape, const void *q, const void *k, const void *v, const float *log_decay, const float *h0,
+                      const void *dO, const float *dhT, void *dq, void *dk, void *dv, float *dh0, float scale, void *workspace,
+                      size_t workspace_bytes, unsigned flags, qd_stream stream);
+
+/* shape->T tokens of every sequence with `state` [B,H,dk,dv] fp32 updated in place: single tokens, and draft tokens.  No workspace. */
+int qdelta_linear_steps(const qd_linear_shape *shape, const void *q, const void *k, const void *v, const float *log_decay, float *state,
+                        void *o, float scale, unsigned flags, qd_stream stream);
+
+/*
+ * Layer norm with a gate, e.g. of a read-out per head: y = ((x - m) r weight + bias) f(gate), m and r as in qdelta_norm_fwd,
+ * f = SiLU with QD_SILU, else the logistic function.  x, gate, y [rows, width]; weight, bias [width] or NULL; stats [2, rows] fp32 (NULL:
+ * not returned).
+ */
+int qdelta_gated_norm_fwd(long long rows, int width, int dtype, const void *x, const void *gate, const void *weight, const void *bias, void *y,
+                          float *stats, float eps, unsigned flags, qd_stream stream);
+
+/* of the backward of gated norm and of add norm; 0 on an invalid shape */
+size_t qdelta_fused_norm_workspace_bytes(long long rows, int width, int dtype);
+
+/* Backward for  L = <y, dy>: dx, dgate in `dtype`, dweight, dbias [width] fp32 (NULL: skipped; without them no workspace is needed). */
+int qdelta_gated_norm_bwd(long long rows, int width, int dtype, const void *x, const void *gate, const void *weight, const void *bias,
+                          const void *dy, const float *stats, void *dx, void *dgate, float *dweight, float *dbias, void *workspace,
+                          size_t workspace_bytes, unsigned flags, qd_stream stream);
+
+/*
+ * Residual sum and layer norm: total = residual + scale x, y = (total - m) r weight + bias.  x, residual, total, y [rows, width]; scale,
+ * weight, bias [width] or NULL (scale NULL: 1).  y is that of the sum before it is rounded to `dtype`.  total may be residual's buffer (in
+ * place; the backward reads x and residual).
+ */
+int qdelta_add_norm_fwd(long long rows, int width, int dtype, const void *x, const void *residual, const void *scale, const void *weight,
+                        const void *bias, void *total, void *y, float *stats, float eps, unsigned flags, qd_stream stream);
+
+/* Backward for  L = <y, dy> + <total, dtotal>  (dtotal NULL: zero): dresidual and dx = scale dresidual in `dtype` (dx NULL only if scale is:
+ * dresidual is it), dscale, dweight, dbias [width] fp32 (NULL: skipped).  Adds x and residual up again, in fp32: the rounded total would
+ * cost the sums over rows half of their digits. */
+int qdelta_add_norm_bwd(long long rows, int width, int dtype, const void *x, const void *residual, const void *scale, const void *weight,
+                        const void *dy, const void *dtotal, const float *stats, void *dx, void *dresidual, float *dscale, float *dweight,
+                        float *dbias, void *workspace, size_t workspace_bytes, unsigned flags, qd_stream stream);
+
+/*
+ * Rotary positions of queries and keys: of every head the pairs (x_j, x_{j+pairs}), or (x_2j, x_{2j+1}) with QD_INTERLEAVED, j < pairs, are
+ * turned by position * turns[j] / 2^64 whole turns (backwards with QD_INVERSE: the backward of the same call) and scaled; elements from
+ * 2 pairs on are copied.
+ *     q, q_out [B,T,Hq,d]   k, k_out [B,T,Hk,d] (NULL with Hk = 0)   turns [pairs] 64-bit: what a step of one position turns by, in units
+ *     of 2^-64 turns, so that the angle of any position is exact to 2^-32 turns   positions [B,T] 64-bit, or NULL: start + t
+ * q_out may be q and k_out k (in place).  d <= 1024, 1 <= pairs <= d / 2, scale finite.
+ */
+int qdelta_rotary(int B, int T, int Hq, int Hk, int d, int pairs, int dtype, const void *q, const void *k, const long long *turns,
+                  const long long *positions, long long start, void *q_out, void *k_out, float scale, unsigned flags, qd_stream stream);
 
 /* Copies the device status word of `workspace` to *status_out (a qd_status) with a blocking
  * 4-byte device-to-host copy on `stream`.  Returns QD_OK or QD_ERR_CUDA / QD_ERR_INVALID_ARG. */

@@ -6,6 +6,7 @@ marshal natively (``host/*.cpp``), the others through ctypes.  There is no fallb
 not been built, or a call returns an error code, an exception is raised.
 """
 import ctypes
+import math
 import os
 
 import torch
@@ -15,7 +16,7 @@ LIB_PATH = os.path.join(_HERE, "libqdelta.so")
 
 QD_F32, QD_BF16 = 0, 1
 QD_FWD_SAVE_FOR_BWD, QD_BWD_REUSE_FWD, QD_COEF_LOGITS, QD_NORM_QK, QD_STATE_BF16 = 1, 2, 4, 8, 16
-QD_SILU, QD_SOFTPLUS, QD_RMS = 32, 64, 128
+QD_SILU, QD_SOFTPLUS, QD_RMS, QD_INTERLEAVED, QD_INVERSE = 32, 64, 128, 256, 512
 
 EXPORTS = ("qdelta_chunk_workspace_bytes", "qdelta_chunk_fwd", "qdelta_chunk_bwd",
            "qdelta_recurrent_step", "qdelta_workspace_status", "qdelta_status_string",
@@ -23,7 +24,10 @@ EXPORTS = ("qdelta_chunk_workspace_bytes", "qdelta_chunk_fwd", "qdelta_chunk_bwd
            "qdelta_profile_read", "qdelta_chunk_fwd_static", "qdelta_chunk_path", "qdelta_chunk_parts",
            "qdelta_recurrent_steps", "qdelta_conv_fwd", "qdelta_conv_steps", "qdelta_conv_workspace_bytes", "qdelta_conv_bwd",
            "qdelta_scan_workspace_bytes", "qdelta_scan_fwd", "qdelta_scan_bwd", "qdelta_scan_steps",
-           "qdelta_norm_fwd", "qdelta_norm_workspace_bytes", "qdelta_norm_bwd")
+           "qdelta_norm_fwd", "qdelta_norm_workspace_bytes", "qdelta_norm_bwd",
+           "qdelta_linear_workspace_bytes", "qdelta_linear_fwd", "qdelta_linear_bwd", "qdelta_linear_steps",
+           "qdelta_gated_norm_fwd", "qdelta_fused_norm_workspace_bytes", "qdelta_gated_norm_bwd", "qdelta_add_norm_fwd",
+           "qdelta_add_norm_bwd", "qdelta_rotary")
 
 
 class QdShape(ctypes.Structure):
@@ -34,6 +38,11 @@ class QdShape(ctypes.Structure):
 class QdScanShape(ctypes.Structure):
     _fields_ = [("B", ctypes.c_int), ("T", ctypes.c_int), ("D", ctypes.c_int), ("N", ctypes.c_int),
                 ("G", ctypes.c_int), ("dtype", ctypes.c_int)]
+
+
+class QdLinearShape(ctypes.Structure):
+    _fields_ = [("B", ctypes.c_int), ("T", ctypes.c_int), ("H", ctypes.c_int), ("dk", ctypes.c_int),
+                ("dv", ctypes.c_int), ("dtype", ctypes.c_int)]
 
 
 class QdeltaError(RuntimeError):
@@ -100,6 +109,19 @@ def load():
     lib.qdelta_norm_workspace_bytes.argtypes = [ll, i, i]
     lib.qdelta_norm_fwd.argtypes = [ll, i, i] + [vp] * 5 + [f, u, vp]
     lib.qdelta_norm_bwd.argtypes = [ll, i, i] + [vp] * 8 + [sz, u, vp]
+    lin = ctypes.POINTER(QdLinearShape)
+    lib.qdelta_linear_workspace_bytes.restype = sz
+    lib.qdelta_linear_workspace_bytes.argtypes = [lin, i]
+    lib.qdelta_linear_fwd.argtypes = [lin] + [vp] * 7 + [f, vp, sz, u, vp]
+    lib.qdelta_linear_bwd.argtypes = [lin] + [vp] * 11 + [f, vp, sz, u, vp]
+    lib.qdelta_linear_steps.argtypes = [lin] + [vp] * 6 + [f, u, vp]
+    lib.qdelta_fused_norm_workspace_bytes.restype = sz
+    lib.qdelta_fused_norm_workspace_bytes.argtypes = [ll, i, i]
+    lib.qdelta_gated_norm_fwd.argtypes = [ll, i, i] + [vp] * 6 + [f, u, vp]
+    lib.qdelta_gated_norm_bwd.argtypes = [ll, i, i] + [vp] * 11 + [sz, u, vp]
+    lib.qdelta_add_norm_fwd.argtypes = [ll, i, i] + [vp] * 8 + [f, u, vp]
+    lib.qdelta_add_norm_bwd.argtypes = [ll, i, i] + [vp] * 13 + [sz, u, vp]
+    lib.qdelta_rotary.argtypes = [i] * 7 + [vp] * 4 + [ll, vp, vp, f, u, vp]
     lib.qdelta_workspace_status.restype = i
     lib.qdelta_workspace_status.argtypes = [vp, ctypes.POINTER(i), vp]
     lib.qdelta_status_string.restype = ctypes.c_char_p
@@ -322,3 +344,81 @@ def norm_bwd(x, weight, dy, stats, rms=False, want_dweight=None, want_dbias=True
     wanted if there is a weight)."""
     want = weight is not None if want_dweight is None else bool(want_dweight)
     return (_native or _host()).norm_bwd(x, weight, dy, stats, want, bool(want_dbias), QD_RMS if rms else 0)
+
+
+# ---- operators of a linear attention layer --------------------------------------------------------------------------------
+# Tensors as above.
+
+def linear_fwd(q, k, v, log_decay, h0=None, scale=1.0, workspace=None, want_hT=True):
+    """Linear attention with a decay for each head: S_t = e^log_decay S_{t-1} + k_t v_t^T, o_t = scale S_t^T q_t.
+    q, k [B,T,H,dk], v [B,T,H,dv] (dk, dv = 64 or 128); log_decay [H] and h0 [B,H,dk,dv] fp32.
+    Returns (o [B,T,H,dv], hT [B,H,dk,dv] fp32, workspace, whose status word workspace_status reads)."""
+    return (_native or _host()).linear_fwd(q, k, v, log_decay, h0, workspace, bool(want_hT), scale)
+
+
+def linear_bwd(q, k, v, log_decay, h0, dO, dhT=None, scale=1.0, workspace=None, want_dh0=None):
+    """Backward of linear_fwd, of which it needs nothing but the inputs (`workspace`: memory of its own size, from the caller).
+    Returns dict(dq, dk, dv, dh0)."""
+    want = h0 is not None if want_dh0 is None else bool(want_dh0)
+    return (_native or _host()).linear_bwd(q, k, v, log_decay, h0, dO, dhT, workspace, want, scale)
+
+
+def linear_steps(q, k, v, log_decay, state, o=None, scale=1.0):
+    """S tokens of every sequence, q, k [B,S,H,dk], v [B,S,H,dv]: single tokens, and draft tokens.  `state` [B,H,dk,dv] fp32 is
+    updated in place.  Returns o."""
+    return (_native or _host()).linear_steps(q, k, v, log_decay, state, o, scale)
+
+
+def gated_norm_fwd(x, gate, weight=None, bias=None, eps=1e-5, rms=False, silu=True, want_stats=True):
+    """Layer norm over the last dimension (norm_fwd) times a gate: SiLU(gate), or sigmoid(gate) with silu=False.  gate of x's shape.
+    Returns (y, stats)."""
+    flags = (QD_RMS if rms else 0) | (QD_SILU if silu else 0)
+    return (_native or _host()).gated_norm_fwd(x, gate, weight, bias, eps, bool(want_stats), flags)
+
+
+def gated_norm_bwd(x, gate, weight, bias, dy, stats, rms=False, silu=True, want_dweight=None, want_dbias=None):
+    """Backward of gated_norm_fwd with the `stats` that it returned.  Returns dict(dx, dgate, dweight, dbias); None for unwanted ones
+    (default: wanted if there is such a parameter)."""
+    flags = (QD_RMS if rms else 0) | (QD_SILU if silu else 0)
+    dw = weight is not None if want_dweight is None else bool(want_dweight)
+    db = bias is not None if want_dbias is None else bool(want_dbias)
+    return (_native or _host()).gated_norm_bwd(x, gate, weight, bias, dy, stats, dw, db, flags)
+
+
+def add_norm_fwd(x, residual, scale=None, weight=None, bias=None, eps=1e-5, rms=False, want_stats=True):
+    """total = residual + scale x (scale per channel, or absent) and its layer norm, of the sum before it is rounded to x's type.
+    Returns (y, total, stats)."""
+    return (_native or _host()).add_norm_fwd(x, residual, scale, weight, bias, eps, bool(want_stats), QD_RMS if rms else 0)
+
+
+def add_norm_bwd(x, residual, scale, weight, dy, dtotal, stats, rms=False, want_dscale=None, want_dweight=None, want_dbias=False):
+    """Backward of add_norm_fwd with the `stats` that it returned, for gradients dy and dtotal (None: zero) of y and total.  Returns dict(dx, dresidual, dscale, dweight, dbias); dx is dresidual itself where there is no scale."""
+    ds = scale is not None if want_dscale is None else bool(want_dscale)
+    dw = weight is not None if want_dweight is None else bool(want_dweight)
+    return (_native or _host()).add_norm_bwd(x, residual, scale, weight, dy, dtotal, stats, ds, dw, bool(want_dbias), QD_RMS if rms else 0)
+
+
+def rotary_turns(pairs, base=10000.0, factor=1.0, original=None, low=1.0, high=32.0, device="cuda"):
+    """What one position turns each pair by, for rotary(): frequency_j = base^(-j / pairs) radians, as int64 fractions of a turn in units
+    of 2^-64.  For contexts longer than the trained one: all frequencies divided by `factor`; or, with `original` (the trained length),
+    those that turn less than `low` times over it divided, those that turn more than `high` times kept, and in between a blend that is
+    linear in the number of turns."""
+    if pairs < 1 or not base > 0 or not factor > 0 or (original is not None and not (original > 0 and high > low)):
+        raise QdeltaError("rotary_turns: pairs >= 1, base > 0, factor > 0, original > 0 and low < high")
+    out = []
+    for j in range(pairs):
+        turn = base ** (-j / pairs) / (2 * math.pi)
+        kept = 0.0 if original is None else min(1.0, max(0.0, (original * turn - low) / (high - low)))
+        turn *= kept + (1.0 - kept) / factor
+        out.append((int(math.ldexp(turn, 64)) + (1 << 63)) % (1 << 64) - (1 << 63))
+    return torch.tensor(out, dtype=torch.int64, device=device)
+
+
+def rotary(q, k, turns, positions=None, start=0, interleaved=False, inverse=False, scale=1.0, out=None):
+    """Rotary positions of q [B,T,Hq,d] and k [B,T,Hk,d] (or None): in each head the pairs (x_j, x_{j+pairs}), or (x_2j, x_2j+1) with
+    interleaved=True, turned by position * turns[j] and scaled; the rest of the head is copied.  turns [pairs] from rotary_turns;
+    positions [B,T] int64 (None: start + t).  inverse=True turns back, and so is the backward of the same call.
+    out: a pair of tensors to write to, (q, k) for a call in place.  Returns (q', k')."""
+    flags = (QD_INTERLEAVED if interleaved else 0) | (QD_INVERSE if inverse else 0)
+    qo, ko = out if out is not None else (None, None)
+    return (_native or _host()).rotary(q, k, turns, positions, start, scale, flags, qo, ko)

@@ -48,8 +48,8 @@ int check_shape(const qd_shape* s) {
 static bool misaligned(const void* p) { return ((uintptr_t)p & 15) != 0; }
 
 // ---- optional per-stage timing with CUDA events on the launching stream ------------------------
-enum Stage { ST_PREP = 0, ST_CHAIN_FWD, ST_CHAIN_BWD, ST_CHUNK_BWD, ST_DECODE, ST_CONV, ST_SCAN, ST_NORM, ST_COUNT };
-static const char* kStageNames[ST_COUNT] = {"prep", "chain_fwd", "chain_bwd", "chunk_bwd", "decode", "conv", "scan", "norm"};
+enum Stage { ST_PREP = 0, ST_CHAIN_FWD, ST_CHAIN_BWD, ST_CHUNK_BWD, ST_DECODE, ST_CONV, ST_SCAN, ST_NORM, ST_LINEAR, ST_ROTARY, ST_COUNT };
+static const char* kStageNames[ST_COUNT] = {"prep", "chain_fwd", "chain_bwd", "chunk_bwd", "decode", "conv", "scan", "norm", "linear", "rotary"};
 struct Pending { cudaEvent_t a, b; int stage; };
 static bool g_profile = false;
 static std::vector<Pending> g_pending;
@@ -126,6 +126,24 @@ static int check_norm(long long rows, int width, int dtype) {
     if (rows <= 0 || width <= 0) return QD_ERR_INVALID_ARG;
     if (dtype != QD_F32 && dtype != QD_BF16) return QD_ERR_UNSUPPORTED;
     if (width > 16384 || rows > kMostElements / 4 || rows > kMostElements / width) return QD_ERR_UNSUPPORTED;
+    return QD_OK;
+}
+static int check_linear(const qd_linear_shape* s) {
+    if (!s || s->B <= 0 || s->T <= 0 || s->H <= 0 || s->dk <= 0 || s->dv <= 0) return QD_ERR_INVALID_ARG;
+    if (s->dtype != QD_F32 && s->dtype != QD_BF16) return QD_ERR_UNSUPPORTED;
+    if ((s->dk != 64 && s->dk != 128) || (s->dv != 64 && s->dv != 128)) return QD_ERR_UNSUPPORTED;
+    // states, and with them CTAs of a walk, fit 31 bits whatever they are split into
+    if (s->T > 1 << 30 || s->H > 1 << 20 || (long long)s->B * s->H > 1 << 23 || (long long)s->B * s->T > kMostElements / 128 / s->H)
+        return QD_ERR_UNSUPPORTED;
+    return QD_OK;
+}
+static bool finite(float x) { return x - x == 0.f; }
+static int check_rotary(int B, int T, int Hq, int Hk, int d, int pairs, int dtype) {
+    if (B <= 0 || T <= 0 || Hq <= 0 || Hk < 0 || d <= 0 || pairs <= 0) return QD_ERR_INVALID_ARG;
+    if (dtype != QD_F32 && dtype != QD_BF16) return QD_ERR_UNSUPPORTED;
+    if (d > 1024 || pairs > d / 2 || Hq > 1 << 16 || Hk > 1 << 16) return QD_ERR_UNSUPPORTED;
+    // tokens: CTAs fit 31 bits with one token each
+    if ((long long)B * T > 0x7fffffffLL || (long long)B * T > kMostElements / d / (Hq > Hk ? Hq : Hk)) return QD_ERR_UNSUPPORTED;
     return QD_OK;
 }
 template <size_t N> static bool any_misaligned(const void* const (&ptrs)[N]) {
@@ -437,6 +455,147 @@ int qdelta_norm_bwd(long long rows, int width, int dtype, const void* x, const v
         return norm_bwd(rows, width, dtype, x, weight, dy, stats, dx, dweight, dbias, (float*)workspace, (flags & QD_RMS) != 0, s);
     });
     return e == cudaSuccess ? QD_OK : QD_ERR_CUDA;
+}
+
+size_t qdelta_linear_workspace_bytes(const qd_linear_shape* shape, int for_backward) {
+    return check_linear(shape) == QD_OK ? linear_workspace(*shape, for_backward != 0) : 0;
+}
+
+int qdelta_linear_fwd(const qd_linear_shape* shape, const void* q, const void* k, const void* v, const float* log_decay, const float* h0,
+                      void* o, float* hT, float scale, void* workspace, size_t workspace_bytes, unsigned flags, qd_stream stream) {
+    const int rc = check_linear(shape);
+    if (rc != QD_OK) return rc;
+    if (!q || !k || !v || !log_decay || !o || o == q || o == k || o == v || (hT && hT == h0) || !finite(scale) || flags) return QD_ERR_INVALID_ARG;
+    const void* const ptrs[] = {q, k, v, h0, o, hT, workspace};
+    if (any_misaligned(ptrs) || ((uintptr_t)log_decay & 3)) return QD_ERR_INVALID_ARG;
+    if (!workspace || workspace_bytes < linear_workspace(*shape, false)) return QD_ERR_WORKSPACE;
+    LinearArgs a{};
+    a.s = *shape;
+    a.q = q; a.k = k; a.v = v; a.g = log_decay; a.h0 = h0; a.o = o; a.hT = hT; a.scale = scale;
+    a.ws = (char*)workspace;
+    a.stream = (cudaStream_t)stream;
+    return timed(ST_LINEAR, a.stream, [&] { return linear_fwd(a); }) == cudaSuccess ? QD_OK : QD_ERR_CUDA;
+}
+
+int qdelta_linear_bwd(const qd_linear_shape* shape, const void* q, const void* k, const void* v, const float* log_decay, const float* h0,
+                      const void* dO, const float* dhT, void* dq, void* dk, void* dv, float* dh0, float scale, void* workspace,
+                      size_t workspace_bytes, unsigned flags, qd_stream stream) {
+    const int rc = check_linear(shape);
+    if (rc != QD_OK) return rc;
+    if (!q || !k || !v || !log_decay || !dO || !dq || !dk || !dv || (dh0 && dh0 == dhT) || !finite(scale) || flags) return QD_ERR_INVALID_ARG;
+    const void* const outs[] = {dq, dk, dv};
+    const void* const ins[] = {q, k, v, dO};
+    for (const void* x : outs)
+        for (const void* y : ins)
+            if (x == y) return QD_ERR_INVALID_ARG;          // other walks still read it
+    if (dq == dk || dq == dv || dk == dv) return QD_ERR_INVALID_ARG;
+    const void* const ptrs[] = {q, k, v, h0, dO, dhT, dq, dk, dv, dh0, workspace};
+    if (any_misaligned(ptrs) || ((uintptr_t)log_decay & 3)) return QD_ERR_INVALID_ARG;
+    if (!workspace || workspace_bytes < linear_workspace(*shape, true)) return QD_ERR_WORKSPACE;
+    LinearArgs a{};
+    a.s = *shape;
+    a.q = q; a.k = k; a.v = v; a.g = log_decay; a.h0 = h0; a.dO = dO; a.dhT = dhT; a.dq = dq; a.dk = dk; a.dv = dv; a.dh0 = dh0; a.scale = scale;
+    a.ws = (char*)workspace;
+    a.stream = (cudaStream_t)stream;
+    return timed(ST_LINEAR, a.stream, [&] { return linear_bwd(a); }) == cudaSuccess ? QD_OK : QD_ERR_CUDA;
+}
+
+int qdelta_linear_steps(const qd_linear_shape* shape, const void* q, const void* k, const void* v, const float* log_decay, float* state,
+                        void* o, float scale, unsigned flags, qd_stream stream) {
+    const int rc = check_linear(shape);
+    if (rc != QD_OK) return rc;
+    // o would be written before other CTAs have read these
+    if (!q || !k || !v || !log_decay || !state || !o || o == q || o == k || o == v || !finite(scale) || flags) return QD_ERR_INVALID_ARG;
+    const void* const ptrs[] = {q, k, v, state, o};
+    if (any_misaligned(ptrs) || ((uintptr_t)log_decay & 3)) return QD_ERR_INVALID_ARG;
+    LinearArgs a{};
+    a.s = *shape;
+    a.q = q; a.k = k; a.v = v; a.g = log_decay; a.hT = state; a.o = o; a.scale = scale;
+    a.stream = (cudaStream_t)stream;
+    return timed(ST_LINEAR, a.stream, [&] { return linear_steps(a); }) == cudaSuccess ? QD_OK : QD_ERR_CUDA;
+}
+
+size_t qdelta_fused_norm_workspace_bytes(long long rows, int width, int dtype) {
+    return check_norm(rows, width, dtype) == QD_OK ? fused_norm_workspace(rows, width, dtype) : 0;
+}
+
+int qdelta_gated_norm_fwd(long long rows, int width, int dtype, const void* x, const void* gate, const void* weight, const void* bias, void* y,
+                          float* stats, float eps, unsigned flags, qd_stream stream) {
+    const int rc = check_norm(rows, width, dtype);
+    if (rc != QD_OK) return rc;
+    if (!x || !gate || !y || !(eps >= 0.f) || eps > 3e38f) return QD_ERR_INVALID_ARG;
+    const void* const ptrs[] = {x, gate, weight, bias, y, stats};
+    if (any_misaligned(ptrs) || (flags & ~(unsigned)(QD_RMS | QD_SILU))) return QD_ERR_INVALID_ARG;
+    FusedNormArgs a{};
+    a.rows = rows; a.width = width; a.dtype = dtype; a.rms = (flags & QD_RMS) != 0; a.silu = (flags & QD_SILU) != 0;
+    a.x = x; a.gate = gate; a.weight = weight; a.bias = bias; a.y = y; a.stats = stats; a.eps = eps;
+    a.stream = (cudaStream_t)stream;
+    return timed(ST_NORM, a.stream, [&] { return fused_norm_fwd(a); }) == cudaSuccess ? QD_OK : QD_ERR_CUDA;
+}
+
+int qdelta_gated_norm_bwd(long long rows, int width, int dtype, const void* x, const void* gate, const void* weight, const void* bias,
+                          const void* dy, const float* stats, void* dx, void* dgate, float* dweight, float* dbias, void* workspace,
+                          size_t workspace_bytes, unsigned flags, qd_stream stream) {
+    const int rc = check_norm(rows, width, dtype);
+    if (rc != QD_OK) return rc;
+    if (!x || !gate || !dy || !stats || !dx || !dgate || dx == dgate) return QD_ERR_INVALID_ARG;
+    const void* const ptrs[] = {x, gate, weight, bias, dy, stats, dx, dgate, dweight, dbias, workspace};
+    if (any_misaligned(ptrs) || (flags & ~(unsigned)(QD_RMS | QD_SILU))) return QD_ERR_INVALID_ARG;
+    if ((dweight || dbias) && (!workspace || workspace_bytes < fused_norm_workspace(rows, width, dtype))) return QD_ERR_WORKSPACE;
+    FusedNormArgs a{};
+    a.rows = rows; a.width = width; a.dtype = dtype; a.rms = (flags & QD_RMS) != 0; a.silu = (flags & QD_SILU) != 0;
+    a.x = x; a.gate = gate; a.weight = weight; a.bias = bias; a.dy = dy; a.stats = const_cast<float*>(stats);
+    a.dx = dx; a.dgate = dgate; a.dweight = dweight; a.dbias = dbias; a.part = (float*)workspace;
+    a.stream = (cudaStream_t)stream;
+    return timed(ST_NORM, a.stream, [&] { return fused_norm_bwd(a); }) == cudaSuccess ? QD_OK : QD_ERR_CUDA;
+}
+
+int qdelta_add_norm_fwd(long long rows, int width, int dtype, const void* x, const void* residual, const void* scale, const void* weight,
+                        const void* bias, void* total, void* y, float* stats, float eps, unsigned flags, qd_stream stream) {
+    const int rc = check_norm(rows, width, dtype);
+    if (rc != QD_OK) return rc;
+    if (!x || !residual || !total || !y || total == y || !(eps >= 0.f) || eps > 3e38f) return QD_ERR_INVALID_ARG;
+    const void* const ptrs[] = {x, residual, scale, weight, bias, total, y, stats};
+    if (any_misaligned(ptrs) || (flags & ~(unsigned)QD_RMS)) return QD_ERR_INVALID_ARG;
+    FusedNormArgs a{};
+    a.rows = rows; a.width = width; a.dtype = dtype; a.added = true; a.rms = (flags & QD_RMS) != 0;
+    a.x = x; a.residual = residual; a.scale = scale; a.weight = weight; a.bias = bias; a.total = total; a.y = y; a.stats = stats; a.eps = eps;
+    a.stream = (cudaStream_t)stream;
+    return timed(ST_NORM, a.stream, [&] { return fused_norm_fwd(a); }) == cudaSuccess ? QD_OK : QD_ERR_CUDA;
+}
+
+int qdelta_add_norm_bwd(long long rows, int width, int dtype, const void* x, const void* residual, const void* scale, const void* weight,
+                        const void* dy, const void* dtotal, const float* stats, void* dx, void* dresidual, float* dscale, float* dweight,
+                        float* dbias, void* workspace, size_t workspace_bytes, unsigned flags, qd_stream stream) {
+    const int rc = check_norm(rows, width, dtype);
+    if (rc != QD_OK) return rc;
+    if (!x || !residual || !dy || !stats || !dresidual || (scale && !dx) || dx == dresidual) return QD_ERR_INVALID_ARG;
+    const void* const ptrs[] = {x, residual, scale, weight, dy, dtotal, stats, dx, dresidual, dscale, dweight, dbias, workspace};
+    if (any_misaligned(ptrs) || (flags & ~(unsigned)QD_RMS)) return QD_ERR_INVALID_ARG;
+    if ((dscale || dweight || dbias) && (!workspace || workspace_bytes < fused_norm_workspace(rows, width, dtype))) return QD_ERR_WORKSPACE;
+    FusedNormArgs a{};
+    a.rows = rows; a.width = width; a.dtype = dtype; a.added = true; a.rms = (flags & QD_RMS) != 0;
+    a.x = x; a.residual = residual; a.scale = scale; a.weight = weight; a.dy = dy; a.dtotal = dtotal; a.stats = const_cast<float*>(stats);
+    a.dx = dx; a.dresidual = dresidual; a.dscale = dscale; a.dweight = dweight; a.dbias = dbias; a.part = (float*)workspace;
+    a.stream = (cudaStream_t)stream;
+    return timed(ST_NORM, a.stream, [&] { return fused_norm_bwd(a); }) == cudaSuccess ? QD_OK : QD_ERR_CUDA;
+}
+
+int qdelta_rotary(int B, int T, int Hq, int Hk, int d, int pairs, int dtype, const void* q, const void* k, const long long* turns,
+                  const long long* positions, long long start, void* q_out, void* k_out, float scale, unsigned flags, qd_stream stream) {
+    const int rc = check_rotary(B, T, Hq, Hk, d, pairs, dtype);
+    if (rc != QD_OK) return rc;
+    if (!q || !q_out || !turns || (Hk && (!k || !k_out)) || !finite(scale)) return QD_ERR_INVALID_ARG;
+    if (Hk && (q_out == k || k_out == q || q_out == k_out)) return QD_ERR_INVALID_ARG;
+    const void* const ptrs[] = {q, k, q_out, k_out};
+    if (any_misaligned(ptrs) || ((uintptr_t)turns & 7) || ((uintptr_t)positions & 7)) return QD_ERR_INVALID_ARG;
+    if (flags & ~(unsigned)(QD_INTERLEAVED | QD_INVERSE)) return QD_ERR_INVALID_ARG;
+    RotaryArgs a{};
+    a.B = B; a.T = T; a.Hq = Hq; a.Hk = Hk; a.d = d; a.pairs = pairs; a.dtype = dtype;
+    a.q = q; a.k = k; a.turns = turns; a.positions = positions; a.start = start; a.q_out = q_out; a.k_out = k_out; a.scale = scale;
+    a.interleaved = (flags & QD_INTERLEAVED) != 0; a.inverse = (flags & QD_INVERSE) != 0;
+    a.stream = (cudaStream_t)stream;
+    return timed(ST_ROTARY, a.stream, [&] { return rotary(a); }) == cudaSuccess ? QD_OK : QD_ERR_CUDA;
 }
 
 int qdelta_workspace_status(const void* workspace, int* status_out, qd_stream stream) {

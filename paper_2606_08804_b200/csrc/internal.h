@@ -164,6 +164,57 @@ cudaError_t scan_fwd(const ScanArgs& a);
 cudaError_t scan_bwd(const ScanArgs& a);
 cudaError_t scan_steps(const ScanArgs& a);
 
+// layer norm with a gate, and behind a residual sum (fused_norm.cu)
+struct FusedNormArgs {
+    long long rows;
+    int width, dtype;
+    bool added, rms, silu;
+    const void *x, *gate, *residual, *scale, *weight, *bias;
+    void *total, *y;
+    float* stats;
+    const void *dy, *dtotal;
+    void *dx, *dgate, *dresidual;
+    float *dscale, *dweight, *dbias, *part;
+    float eps;
+    cudaStream_t stream;
+};
+size_t fused_norm_workspace(long long rows, int width, int dtype);
+cudaError_t fused_norm_fwd(const FusedNormArgs& a);
+cudaError_t fused_norm_bwd(const FusedNormArgs& a);
+// rotary positions (rotary.cu)
+struct RotaryArgs {
+    int B, T, Hq, Hk, d, pairs, dtype;
+    const void *q, *k;
+    const long long *turns, *positions;
+    long long start;
+    void *q_out, *k_out;
+    float scale;
+    bool interleaved, inverse;
+    cudaStream_t stream;
+};
+cudaError_t rotary(const RotaryArgs& a);
+// linear attention (linear.cu and the walks of linear.cuh)
+struct LinearP;
+struct LinearArgs {
+    qd_linear_shape s;
+    const void *q, *k, *v;
+    const float *g, *h0;
+    void* o;
+    float* hT;       // steps: the state, in place
+    const void* dO;
+    const float* dhT;
+    void *dq, *dk, *dv;
+    float* dh0;
+    float scale;
+    char* ws;
+    cudaStream_t stream;
+};
+size_t linear_workspace(const qd_linear_shape& s, bool backward);
+cudaError_t linear_fwd(const LinearArgs& a);
+cudaError_t linear_bwd(const LinearArgs& a);
+cudaError_t linear_steps(const LinearArgs& a);
+cudaError_t linear_planes(const LinearP& p, int walks, int db, int dc, int dtype, cudaStream_t stream);
+
 // ---- in-kernel L2 normalisation of q and k (QD_NORM_QK) ------------------------------------------------
 // x^ = x / sqrt(sum x^2 + kNormEps), per token and head.  Its backward: dx = r (dx^ - x^ <x^, dx^>), r = 1/sqrt(sum x^2 + eps).
 constexpr float kNormEps = 1e-6f;

@@ -1,0 +1,179 @@
+// Linear attention: which walks (linear.cuh) a forward and a backward are, in how many segments, and the recurrent form.
+#include "linear.cuh"
+#include "rows.cuh"
+
+#include <initializer_list>
+
+namespace qd {
+namespace {
+
+constexpr size_t kStatusBytes = 256;
+
+// tokens of a chunk, and CTAs that share a sequence's head in one walk (planes: 32 columns of the state each)
+int linear_chunk(const qd_linear_shape&) { return 64; }
+long long linear_ctas(const qd_linear_shape& s) { return (long long)s.B * s.H * (s.dv / 32); }
+cudaError_t linear_walks(const LinearP& p, int walks, int db, int dc, int dtype, cudaStream_t stream) {
+    return linear_planes(p, walks, db, dc, dtype, stream);
+}
+
+// Segments of a sequence: as many as make the CTAs' longest run of chunks shortest.  A segment costs its chunks and what a CTA needs
+// before its first one; where there are several, the sums of each come first, which take half as long as a walk.
+int segments_of(const qd_linear_shape& s, bool backward) {
+    const int chunk = linear_chunk(s);
+    const long long per = linear_ctas(s) * (backward ? kLinearWalks : 1);
+    const int chunks = (s.T + chunk - 1) / chunk;
+    int best = 1;
+    double least = 1e30;
+    for (int n = 1; n <= 32 && n <= chunks; ++n) {
+        const int length = (chunks + n - 1) / n;
+        if ((chunks + length - 1) / length != n) continue;
+        const double waves = (double)((per * n + kSMs - 1) / kSMs);
+        const double cost = waves * (length + 2) + (n > 1 ? 0.5 * waves * (length + 2) + 3 : 0);
+        if (cost < least) { least = cost; best = n; }
+    }
+    return best;
+}
+
+struct Plan {
+    LinearP p;
+    int chunk;
+    float* ends[2];
+};
+Plan plan(const LinearArgs& a, bool backward) {
+    Plan r{};
+    r.chunk = linear_chunk(a.s);
+    const int chunks = (a.s.T + r.chunk - 1) / r.chunk;
+    const int n = segments_of(a.s, backward);
+    r.p.T = a.s.T; r.p.H = a.s.H; r.p.BH = a.s.B * a.s.H;
+    r.p.segments = n;
+    r.p.length = (chunks + n - 1) / n * r.chunk;
+    r.p.g = a.g;
+    r.p.scale = a.scale;
+    r.p.status = reinterpret_cast<unsigned*>(a.ws);
+    const size_t state = (size_t)r.p.BH * n * a.s.dk * a.s.dv;
+    for (int i = 0; i < 2; ++i) r.ends[i] = reinterpret_cast<float*>(a.ws + kStatusBytes) + i * state;
+    return r;
+}
+// walks of one shape of state, at most kLinearWalks
+cudaError_t walk(LinearP p, std::initializer_list<LinearWalk> ws, int db, int dc, const LinearArgs& a, bool clear) {
+    int n = 0;
+    for (const LinearWalk& w : ws) p.w[n++] = w;
+    p.clear = clear;
+    return linear_walks(p, n, db, dc, a.s.dtype, a.stream);
+}
+
+}  // namespace
+
+size_t linear_workspace(const qd_linear_shape& s, bool backward) {
+    const int n = segments_of(s, backward);
+    return kStatusBytes + (n > 1 ? (size_t)(backward ? 2 : 1) * s.B * s.H * n * s.dk * s.dv * 4 : 0);
+}
+
+cudaError_t linear_fwd(const LinearArgs& a) {
+    const Plan l = plan(a, false);
+    const int dk = a.s.dk, dv = a.s.dv;
+    if (l.p.segments > 1) {
+        const cudaError_t e = walk(l.p, {LinearWalk{nullptr, a.k, a.v, nullptr, nullptr, nullptr, l.ends[0], 0, 0}}, dk, dv, a, true);
+        if (e != cudaSuccess) return e;
+    }
+    return walk(l.p, {LinearWalk{a.q, a.k, a.v, a.o, a.h0, a.hT, l.ends[0], 0, 0}}, dk, dv, a, l.p.segments == 1);
+}
+
+cudaError_t linear_bwd(const LinearArgs& a) {
+    const Plan l = plan(a, true);
+    const int dk = a.s.dk, dv = a.s.dv;
+    if (l.p.segments > 1) {
+        const cudaError_t e = walk(l.p, {LinearWalk{nullptr, a.k, a.v, nullptr, nullptr, nullptr, l.ends[0], 0, 0},
+                                         LinearWalk{nullptr, a.q, a.dO, nullptr, nullptr, nullptr, l.ends[1], 1, 0}}, dk, dv, a, true);
+        if (e != cudaSuccess) return e;
+    }
+    const LinearWalk wq{a.dO, a.v, a.k, a.dq, a.h0, nullptr, l.ends[0], 0, 1}, wk{a.v, a.dO, a.q, a.dk, a.dhT, nullptr, l.ends[1], 1, 1},
+        wv{a.k, a.q, a.dO, a.dv, a.dhT, a.dh0, l.ends[1], 1, 0};
+    const bool clear = l.p.segments == 1;
+    if (dk == dv) return walk(l.p, {wq, wk, wv}, dk, dv, a, clear);
+    const cudaError_t e = walk(l.p, {wq, wk}, dv, dk, a, clear);
+    return e == cudaSuccess ? walk(l.p, {wv}, dk, dv, a, false) : e;
+}
+
+// ---- single tokens --------------------------------------------------------------------------------------------------------
+// S tokens of every sequence, state in place: h <- e^g h + k v^T, o = scale h^T q.  Bound by HBM, one read and one write of the state: a
+// CTA has COLS columns of one state, each thread 16 bytes of every RP-th row in registers for all tokens; the read-out's sums over rows go
+// through shared memory, a barrier a token.
+namespace {
+
+constexpr int kStepThreads = 256, kStepTokens = 8;
+
+template <typename IO, int DK, int COLS>
+__global__ void __launch_bounds__(kStepThreads) k_linear_steps(int S, int H, int dv, const IO* __restrict__ q, const IO* __restrict__ k,
+                                                               const IO* __restrict__ v, const float* __restrict__ g, float* state,
+                                                               IO* __restrict__ o, float scale) {
+    constexpr int CT = COLS / 4, RP = kStepThreads / CT, NP = DK / RP;
+    static_assert(NP >= 1 && DK % RP == 0, "every thread has rows");
+    __shared__ float sq[kStepTokens][DK], sk[kStepTokens][DK];
+    __shared__ __align__(16) float sv[kStepTokens][COLS], red[2][RP][COLS];
+    const int nsl = dv / COLS, bh = blockIdx.x / nsl, j0 = blockIdx.x % nsl * COLS, b = bh / H, h = bh % H;
+    const int tid = threadIdx.x, ct = tid % CT, rg = tid / CT;
+    sm100::grid_dep_wait();
+    sm100::grid_dep_launch();
+    float4* base = reinterpret_cast<float4*>(state + ((size_t)bh * DK + rg) * dv + j0) + ct;
+    const size_t step = (size_t)RP * dv / 4;
+    float4 st[NP];
+#pragma unroll
+    for (int i = 0; i < NP; ++i) st[i] = __ldcs(base + i * step);
+    const float keep = exp2f(g[h] * 1.4426950408889634f);
+    for (int s0 = 0; s0 < S; s0 += kStepTokens) {
+        const int n = min(kStepTokens, S - s0);
+        const size_t row = ((size_t)b * S + s0) * H + h;
+        if (s0) __syncthreads();
+        for (int i = tid; i < n * DK; i += kStepThreads) {
+            const size_t at = (row + (size_t)(i / DK) * H) * DK + i % DK;
+            sq[i / DK][i % DK] = scale * ld(q, at);
+            sk[i / DK][i % DK] = ld(k, at);
+        }
+        for (int i = tid; i < n * COLS; i += kStepThreads) sv[i / COLS][i % COLS] = ld(v, (row + (size_t)(i / COLS) * H) * dv + j0 + i % COLS);
+        __syncthreads();
+        for (int t = 0; t < n; ++t) {
+            const float4 vv = *reinterpret_cast<const float4*>(&sv[t][4 * ct]);
+            float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+            for (int i = 0; i < NP; ++i) {
+                const float kk = sk[t][i * RP + rg], qq = sq[t][i * RP + rg];
+                st[i].x = fmaf(keep, st[i].x, kk * vv.x); acc.x = fmaf(qq, st[i].x, acc.x);
+                st[i].y = fmaf(keep, st[i].y, kk * vv.y); acc.y = fmaf(qq, st[i].y, acc.y);
+                st[i].z = fmaf(keep, st[i].z, kk * vv.z); acc.z = fmaf(qq, st[i].z, acc.z);
+                st[i].w = fmaf(keep, st[i].w, kk * vv.w); acc.w = fmaf(qq, st[i].w, acc.w);
+            }
+            float (*part)[COLS] = red[t & 1];
+            *reinterpret_cast<float4*>(&part[rg][4 * ct]) = acc;
+            __syncthreads();
+            if (tid < COLS) {
+                float sum = 0.f;
+#pragma unroll
+                for (int i = 0; i < RP; ++i) sum += part[i][tid];
+                qd::st(o, (row + (size_t)t * H) * dv + j0 + tid, sum);
+            }
+        }
+    }
+#pragma unroll
+    for (int i = 0; i < NP; ++i) __stcs(base + i * step, st[i]);
+}
+
+template <typename IO, int DK, int COLS>
+cudaError_t steps(const LinearArgs& a) {
+    return launch_overlapped(k_linear_steps<IO, DK, COLS>, dim3((unsigned)(a.s.B * a.s.H * (a.s.dv / COLS))), dim3(kStepThreads), 0, a.stream, a.s.T,
+                             a.s.H, a.s.dv, static_cast<const IO*>(a.q), static_cast<const IO*>(a.k), static_cast<const IO*>(a.v), a.g, a.hT,
+                             static_cast<IO*>(a.o), a.scale);
+}
+template <typename IO>
+cudaError_t steps(const LinearArgs& a) {
+    // few states: a quarter of a state to a CTA, so that more SMs read
+    const bool few = (long long)a.s.B * a.s.H * (a.s.dv / 64) < 2 * kSMs;
+    if (a.s.dk == 128) return few ? steps<IO, 128, 32>(a) : steps<IO, 128, 64>(a);
+    return few ? steps<IO, 64, 32>(a) : steps<IO, 64, 64>(a);
+}
+
+}  // namespace
+
+cudaError_t linear_steps(const LinearArgs& a) { return a.s.dtype == QD_F32 ? steps<float>(a) : steps<__nv_bfloat16>(a); }
+
+}  // namespace qd

@@ -1,0 +1,189 @@
+// Linear attention, fp32-accurate: a walk (linear.cuh) per CTA over chunks of 64 tokens, for 32 columns of the state.  All products are
+// products of bf16 planes on the warp-level tensor instruction (planes.cuh), an fp32 matrix three planes; the state stays in fp32 registers,
+// to which a chunk's sum is added, and is written as planes for the next chunk's a S.
+#include "linear.cuh"
+#include "planes.cuh"
+#include "split_common.cuh"
+
+namespace qd {
+namespace {
+
+constexpr int kRows = 64, kCols = 32, kPlanesThreads = 256;
+
+// four neighbours of a tile from global memory, rows >= live as zeros; on their way in registers, then into planes
+template <typename IO, int W>
+struct Rows4 {
+    static constexpr int kN = kRows * W / 4 / kPlanesThreads;
+    float4 r[kN];
+    __device__ __forceinline__ void get(const IO* src, size_t stride, int live) {
+#pragma unroll
+        for (int i = 0; i < kN; ++i) {
+            const int id = i * kPlanesThreads + threadIdx.x, row = id / (W / 4), c = id % (W / 4) * 4;
+            r[i] = make_float4(0.f, 0.f, 0.f, 0.f);
+            if (row < live) {
+                if constexpr (sizeof(IO) == 4) r[i] = *reinterpret_cast<const float4*>(src + row * stride + c);
+                else {
+                    const uint2 u = *reinterpret_cast<const uint2*>(src + row * stride + c);
+                    r[i] = make_float4(__uint_as_float(u.x << 16), __uint_as_float(u.x & 0xffff0000u), __uint_as_float(u.y << 16),
+                                       __uint_as_float(u.y & 0xffff0000u));
+                }
+            }
+        }
+    }
+    template <class P> __device__ __forceinline__ void put(const P& d) const {
+#pragma unroll
+        for (int i = 0; i < kN; ++i) {
+            const int id = i * kPlanesThreads + threadIdx.x;
+            d.st4(id / (W / 4), id % (W / 4) * 4, r[i]);
+        }
+    }
+    template <class P> __device__ __forceinline__ void put(const P& d, const float* factor) const {
+#pragma unroll
+        for (int i = 0; i < kN; ++i) {
+            const int id = i * kPlanesThreads + threadIdx.x;
+            const float f = factor[id / (W / 4)];
+            d.st4(id / (W / 4), id % (W / 4) * 4, make_float4(f * r[i].x, f * r[i].y, f * r[i].z, f * r[i].w));
+        }
+    }
+};
+
+template <typename IO, int DB>
+struct PlanesLayout {
+    static constexpr int NP = sizeof(IO) == 4 ? 3 : 1;
+    typedef Planes<kRows, DB, NP> Wide;
+    typedef Planes<kRows, kCols, NP> Slice;
+    typedef Planes<kRows, kCols, 3> Scaled;
+    typedef Planes<kRows, kRows, 3> Square;
+    typedef Planes<DB, kCols, 3> State;
+    static constexpr int kA = 0, kB = kA + Wide::kBytes, kC = kB + Wide::kBytes, kCh = kC + Slice::kBytes, kP = kCh + Scaled::kBytes,
+                         kS = kP + Square::kBytes, kBytes = kS + State::kBytes;
+};
+
+template <typename IO, int DB, int DC>
+__global__ void __launch_bounds__(kPlanesThreads, 1) k_linear_planes(const LinearP p) {
+    typedef PlanesLayout<IO, DB> L;
+    extern __shared__ __align__(16) unsigned char smem_planes[];
+    __shared__ float s_d[kRows], s_rho[kRows], s_kappa[kRows];
+    const typename L::Wide A(smem_planes + L::kA), B(smem_planes + L::kB);
+    const typename L::Slice Cc(smem_planes + L::kC);
+    const typename L::Scaled Ch(smem_planes + L::kCh);
+    const typename L::Square P(smem_planes + L::kP);
+    const typename L::State S(smem_planes + L::kS);
+    const LinearWalk w = p.w[blockIdx.y];
+    constexpr int kSlices = DC / kCols;
+    const int slice = blockIdx.x % kSlices, segment = blockIdx.x / kSlices % p.segments, bh = blockIdx.x / kSlices / p.segments;
+    const int b = bh / p.H, h = bh % p.H, j0 = slice * kCols, tid = threadIdx.x, warp = tid >> 5;
+    const float g2 = p.g[h] * 1.4426950408889634f;
+    sm100::grid_dep_wait();
+    sm100::grid_dep_launch();
+    if (p.clear && blockIdx.x == 0 && blockIdx.y == 0 && tid == 0) *p.status = 0;
+    // the sums of the segment that no other begins with are not asked for
+    if (!w.out && segment == (w.reverse ? 0 : p.segments - 1)) return;
+
+    // a warp's part of the state: 16 rows, 32 columns (16, where there are 64 rows)
+    constexpr int NS = DB == 128 ? 4 : 2;
+    const int sm = DB == 128 ? 16 * warp : 16 * (warp >> 1), sn = DB == 128 ? 0 : 16 * (warp & 1);
+    float st[1][NS][4];
+    const int size = DB * DC;
+    auto place = [&](int r, int c) { return w.flip ? (j0 + c) * DB + r : r * DC + j0 + c; };
+    each(st, sm, sn, [&](int r, int c, float& x, float& y) {
+        x = w.out ? linear_entry(p, w, bh, segment, size, place(r, c), g2) : 0.f;
+        y = w.out ? linear_entry(p, w, bh, segment, size, place(r, c + 1), g2) : 0.f;
+        S.st2(r, c, x, y);
+    });
+    if (tid < kRows) s_d[tid] = p.scale * decay_power(g2, tid);
+
+    const int first = segment * p.length, end = min(p.T, first + p.length), chunks = (end - first + kRows - 1) / kRows;
+    const size_t ld_b = (size_t)p.H * DB, ld_c = (size_t)p.H * DC;
+    const IO *ga = static_cast<const IO*>(w.a), *gb = static_cast<const IO*>(w.b), *gc = static_cast<const IO*>(w.c);
+    Rows4<IO, DB> ra, rb;
+    Rows4<IO, kCols> rc;
+    auto fetch = [&](int n) {
+        const int t0 = first + (w.reverse ? chunks - 1 - n : n) * kRows, live = min(kRows, end - t0);
+        const size_t row = (size_t)b * p.T + t0;
+        if (w.out) ra.get(ga + row * ld_b + (size_t)h * DB, ld_b, live);
+        rb.get(gb + row * ld_b + (size_t)h * DB, ld_b, live);
+        rc.get(gc + row * ld_c + (size_t)h * DC + j0, ld_c, live);
+    };
+    fetch(0);
+    for (int n = 0; n < chunks; ++n) {
+        const int t0 = first + (w.reverse ? chunks - 1 - n : n) * kRows, live = min(kRows, end - t0);
+        if (tid < kRows) {
+            const float fall = tid < live ? decay_power(g2, live - 1 - tid) : 0.f, rise = tid < live ? p.scale * decay_power(g2, tid + 1) : 0.f;
+            s_rho[tid] = w.reverse ? fall : rise;
+            s_kappa[tid] = w.reverse ? rise : fall;
+        }
+        __syncthreads();                                       // and the chunk before has been read
+        if (w.out) ra.put(A);
+        rb.put(B);
+        rc.put(Cc);
+        rc.put(Ch, s_kappa);
+        __syncthreads();
+        if (n + 1 < chunks) fetch(n + 1);
+        if (w.out) {
+            float acc[1][4][4];
+            const int m0 = 16 * (warp >> 1), n0 = 32 * (warp & 1);
+            zero(acc);
+            pmm<false, false>(acc, A, B, m0, n0, DB);
+            each(acc, m0, n0, [&](int r, int c, float& x, float& y) {
+                const int u = w.reverse ? c - r : r - c, v = w.reverse ? u + 1 : u - 1;
+                P.st2(r, c, u >= 0 ? x * s_d[u] : 0.f, v >= 0 ? y * s_d[v] : 0.f);
+            });
+            __syncthreads();
+            float in[1][2][4], out[1][2][4];
+            const int o0 = 16 * (warp & 1);
+            zero(in);
+            zero(out);
+            pmm<false, true>(in, P, Cc, m0, o0, w.reverse ? kRows : m0 + 16, w.reverse ? m0 : 0);
+            pmm<false, true>(out, A, S, m0, o0, DB);
+            IO* o = static_cast<IO*>(w.out) + ((size_t)b * p.T + t0) * ld_c + (size_t)h * DC + j0;
+            each2(in, out, m0, o0, [&](int r, int c, float x, float y, float x2, float y2) {
+                if (r >= live) return;
+                const float f = s_rho[r];
+                x = fmaf(f, x2, x);
+                y = fmaf(f, y2, y);
+                if constexpr (sizeof(IO) == 4) *reinterpret_cast<float2*>(o + r * ld_c + c) = make_float2(x, y);
+                else *reinterpret_cast<uint32_t*>(o + r * ld_c + c) = sm100::pack_bf16(x, y);
+            });
+        }
+        float add[1][NS][4];
+        zero(add);
+        pmm<true, true>(add, B, Ch, sm, sn, kRows);
+        if (w.out) __syncthreads();                            // the state has been read
+        const float keep = decay_power(g2, live);
+        each2(st, add, sm, sn, [&](int r, int c, float& x, float& y, float x2, float y2) {
+            x = fmaf(keep, x, x2);
+            y = fmaf(keep, y, y2);
+            if (w.out) S.st2(r, c, x, y);
+        });
+    }
+    float* left = w.out ? segment == (w.reverse ? 0 : p.segments - 1) && w.sT ? w.sT + (size_t)bh * size : nullptr
+                        : w.ends + ((size_t)bh * p.segments + segment) * size;
+    if (left)
+        each(st, sm, sn, [&](int r, int c, float& x, float& y) {
+            left[place(r, c)] = x;
+            left[place(r, c + 1)] = y;
+        });
+}
+
+template <typename IO, int DB, int DC>
+cudaError_t launch(const LinearP& p, int walks, cudaStream_t stream) {
+    constexpr int bytes = PlanesLayout<IO, DB>::kBytes;
+    const auto kern = k_linear_planes<IO, DB, DC>;
+    const cudaError_t e = set_max_smem_once((const void*)kern, bytes);
+    if (e != cudaSuccess) return e;
+    return launch_overlapped(kern, dim3((unsigned)(p.BH * p.segments * (DC / kCols)), walks), dim3(kPlanesThreads), bytes, stream, p);
+}
+
+}  // namespace
+
+cudaError_t linear_planes(const LinearP& p, int walks, int db, int dc, int dtype, cudaStream_t stream) {
+    if (dtype == QD_F32) {
+        if (db == 128) return dc == 128 ? launch<float, 128, 128>(p, walks, stream) : launch<float, 128, 64>(p, walks, stream);
+        return dc == 128 ? launch<float, 64, 128>(p, walks, stream) : launch<float, 64, 64>(p, walks, stream);
+    }
+    if (db == 128) return dc == 128 ? launch<__nv_bfloat16, 128, 128>(p, walks, stream) : launch<__nv_bfloat16, 128, 64>(p, walks, stream);
+    return dc == 128 ? launch<__nv_bfloat16, 64, 128>(p, walks, stream) : launch<__nv_bfloat16, 64, 64>(p, walks, stream);
+}
+
+}  // namespace qd

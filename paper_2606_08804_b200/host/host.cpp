@@ -301,6 +301,6 @@ PyModuleDef module_def = {PyModuleDef_HEAD_INIT, "_qdelta_host", nullptr, -1, me
 
 PyMODINIT_FUNC PyInit__qdelta_host(void) {
     PyObject* m = PyModule_Create(&module_def);
-    if (m && PyModule_AddFunctions(m, qdhost::layer_methods)) { Py_DECREF(m); return nullptr; }
+    if (m && (PyModule_AddFunctions(m, qdhost::layer_methods) || PyModule_AddFunctions(m, qdhost::linear_methods))) { Py_DECREF(m); return nullptr; }
     return m;
 }

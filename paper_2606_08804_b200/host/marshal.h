@@ -130,5 +130,6 @@ inline const at::Tensor* maybe(const MaybeTensor& t) { return t ? &*t : nullptr;
 }
 
 extern PyMethodDef layer_methods[];                // the operators around the delta rule (layer.cpp)
+extern PyMethodDef linear_methods[];               // those of a linear attention layer (linear.cpp)
 
 }  // namespace qdhost
