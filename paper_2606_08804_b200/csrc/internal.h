@@ -213,7 +213,8 @@ size_t linear_workspace(const qd_linear_shape& s, bool backward);
 cudaError_t linear_fwd(const LinearArgs& a);
 cudaError_t linear_bwd(const LinearArgs& a);
 cudaError_t linear_steps(const LinearArgs& a);
-cudaError_t linear_planes(const LinearP& p, int walks, int db, int dc, int dtype, cudaStream_t stream);
+cudaError_t linear_planes(const LinearP& p, int db, int dc, cudaStream_t stream);       // fp32
+cudaError_t linear_tc(const LinearP& p, int db, int dc, cudaStream_t stream);           // bf16
 
 // ---- in-kernel L2 normalisation of q and k (QD_NORM_QK) ------------------------------------------------
 // x^ = x / sqrt(sum x^2 + kNormEps), per token and head.  Its backward: dx = r (dx^ - x^ <x^, dx^>), r = 1/sqrt(sum x^2 + eps).

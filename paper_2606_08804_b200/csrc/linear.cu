@@ -9,12 +9,9 @@ namespace {
 
 constexpr size_t kStatusBytes = 256;
 
-// tokens of a chunk, and CTAs that share a sequence's head in one walk (planes: 32 columns of the state each)
-int linear_chunk(const qd_linear_shape&) { return 64; }
-long long linear_ctas(const qd_linear_shape& s) { return (long long)s.B * s.H * (s.dv / 32); }
-cudaError_t linear_walks(const LinearP& p, int walks, int db, int dc, int dtype, cudaStream_t stream) {
-    return linear_planes(p, walks, db, dc, dtype, stream);
-}
+// tokens of a chunk, and CTAs that share a head of a sequence in one walk (fp32: 32 columns of the state each)
+int linear_chunk(const qd_linear_shape& s) { return s.dtype == QD_BF16 ? 128 : 64; }
+long long linear_ctas(const qd_linear_shape& s) { return (long long)s.B * s.H * (s.dtype == QD_BF16 ? 1 : s.dv / 32); }
 
 // Segments of a sequence: as many as make the CTAs' longest run of chunks shortest.  A segment costs its chunks and what a CTA needs
 // before its first one; where there are several, the sums of each come first, which take half as long as a walk.
@@ -58,8 +55,9 @@ Plan plan(const LinearArgs& a, bool backward) {
 cudaError_t walk(LinearP p, std::initializer_list<LinearWalk> ws, int db, int dc, const LinearArgs& a, bool clear) {
     int n = 0;
     for (const LinearWalk& w : ws) p.w[n++] = w;
+    p.walks = n;
     p.clear = clear;
-    return linear_walks(p, n, db, dc, a.s.dtype, a.stream);
+    return a.s.dtype == QD_BF16 ? linear_tc(p, db, dc, a.stream) : linear_planes(p, db, dc, a.stream);
 }
 
 }  // namespace

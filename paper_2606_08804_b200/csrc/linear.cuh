@@ -30,6 +30,7 @@ struct LinearP {
     const float* g;
     float scale;
     unsigned* status;
+    int walks;                           // of this launch; CTAs of the walks that share a segment are neighbours
     int clear;                           // the first launch of a call: the status word starts at zero
     LinearWalk w[kLinearWalks];
 };

@@ -69,14 +69,14 @@ __global__ void __launch_bounds__(kPlanesThreads, 1) k_linear_planes(const Linea
     const typename L::Scaled Ch(smem_planes + L::kCh);
     const typename L::Square P(smem_planes + L::kP);
     const typename L::State S(smem_planes + L::kS);
-    const LinearWalk w = p.w[blockIdx.y];
     constexpr int kSlices = DC / kCols;
-    const int slice = blockIdx.x % kSlices, segment = blockIdx.x / kSlices % p.segments, bh = blockIdx.x / kSlices / p.segments;
+    const int cta = blockIdx.x / p.walks, slice = cta % kSlices, segment = cta / kSlices % p.segments, bh = cta / kSlices / p.segments;
+    const LinearWalk w = p.w[blockIdx.x % p.walks];
     const int b = bh / p.H, h = bh % p.H, j0 = slice * kCols, tid = threadIdx.x, warp = tid >> 5;
-    const float g2 = p.g[h] * 1.4426950408889634f;
     sm100::grid_dep_wait();
     sm100::grid_dep_launch();
-    if (p.clear && blockIdx.x == 0 && blockIdx.y == 0 && tid == 0) *p.status = 0;
+    const float g2 = p.g[h] * 1.4426950408889634f;
+    if (p.clear && blockIdx.x == 0 && tid == 0) *p.status = 0;
     // the sums of the segment that no other begins with are not asked for
     if (!w.out && segment == (w.reverse ? 0 : p.segments - 1)) return;
 
@@ -167,23 +167,19 @@ __global__ void __launch_bounds__(kPlanesThreads, 1) k_linear_planes(const Linea
 }
 
 template <typename IO, int DB, int DC>
-cudaError_t launch(const LinearP& p, int walks, cudaStream_t stream) {
+cudaError_t launch(const LinearP& p, cudaStream_t stream) {
     constexpr int bytes = PlanesLayout<IO, DB>::kBytes;
     const auto kern = k_linear_planes<IO, DB, DC>;
     const cudaError_t e = set_max_smem_once((const void*)kern, bytes);
     if (e != cudaSuccess) return e;
-    return launch_overlapped(kern, dim3((unsigned)(p.BH * p.segments * (DC / kCols)), walks), dim3(kPlanesThreads), bytes, stream, p);
+    return launch_overlapped(kern, dim3((unsigned)(p.BH * p.segments * (DC / kCols) * p.walks)), dim3(kPlanesThreads), bytes, stream, p);
 }
 
 }  // namespace
 
-cudaError_t linear_planes(const LinearP& p, int walks, int db, int dc, int dtype, cudaStream_t stream) {
-    if (dtype == QD_F32) {
-        if (db == 128) return dc == 128 ? launch<float, 128, 128>(p, walks, stream) : launch<float, 128, 64>(p, walks, stream);
-        return dc == 128 ? launch<float, 64, 128>(p, walks, stream) : launch<float, 64, 64>(p, walks, stream);
-    }
-    if (db == 128) return dc == 128 ? launch<__nv_bfloat16, 128, 128>(p, walks, stream) : launch<__nv_bfloat16, 128, 64>(p, walks, stream);
-    return dc == 128 ? launch<__nv_bfloat16, 64, 128>(p, walks, stream) : launch<__nv_bfloat16, 64, 64>(p, walks, stream);
+cudaError_t linear_planes(const LinearP& p, int db, int dc, cudaStream_t stream) {
+    if (db == 128) return dc == 128 ? launch<float, 128, 128>(p, stream) : launch<float, 128, 64>(p, stream);
+    return dc == 128 ? launch<float, 64, 128>(p, stream) : launch<float, 64, 64>(p, stream);
 }
 
 }  // namespace qd

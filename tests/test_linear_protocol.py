@@ -1,0 +1,69 @@
+"""What the warps of the linear attention walk tell each other, in any order of the warps and with waits that expire: the kernel's own source on
+the host, as in test_cta_protocol.py.  No GPU."""
+import os
+import re
+import subprocess
+
+import pytest
+
+import test_cta_protocol as cp
+
+ONE = r"""
+static std::string one(const std::string& name, const emu::Scenario& s, int i) {
+    const int chunks = 1 + i % 7;
+    LinearP p{};
+    p.T = 128 * chunks - (i % 3) * 40; p.H = 1; p.BH = 1; p.segments = 1; p.length = 128 * chunks; p.g = f(); p.scale = 1.f; p.status = u(); p.walks = 1;
+    LinearWalk& w = p.w[0];
+    w.a = w.b = w.c = f(); w.out = h(); w.sT = f(); w.ends = f(); w.reverse = i & 1; w.flip = i >> 1 & 1;
+    auto go = [&](auto kern, int db, int dc) {
+        LinearMaps m{};
+        m.a[0] = m.b[0] = box(128 * 64 * 2); m.c[0] = box(128 * 64 * 2); m.out[0] = box(0);
+        return emu::run(s, kTcThreads, dim3(0), dim3(1), [&] { kern(m, p); });
+    };
+    if (name == "ends") {
+        p.segments = 2; p.length = 128 * chunks; p.T = 256 * chunks; w.out = nullptr; w.reverse = 0;
+        return i & 1 ? go(k_linear_tc<128, 64, true>, 128, 64) : go(k_linear_tc<64, 128, true>, 64, 128);
+    }
+    switch (i & 3) {
+        case 0: return go(k_linear_tc<128, 128, false>, 128, 128);
+        case 1: return go(k_linear_tc<64, 64, false>, 64, 64);
+        case 2: return go(k_linear_tc<64, 128, false>, 64, 128);
+        default: return go(k_linear_tc<128, 64, false>, 128, 64);
+    }
+}
+"""
+
+
+def _source():
+    read = lambda n: open(os.path.join(cp.CSRC, n)).read()  # noqa: E731
+    src = read("linear_tc.cu")
+    src = src[:src.index("\ntemplate <int DB, int DC, bool ENDS>\ncudaError_t launch")] + "\n}\n}\n"
+    head = re.sub(r'#include "sm100\.cuh"|#pragma once', "", read("linear.cuh"))
+    src = src.replace('#include "linear.cuh"', head).replace("extern __shared__ unsigned char smem_raw[];", "unsigned char* const smem_raw = emu::smem;")
+    src = src.replace("__shared__ ", "static ").replace("__grid_constant__ ", "")
+    src = re.sub(r"__launch_bounds__\([^)]*\)", "", src)
+    assert "asm " not in src
+    return '#include "cta_emulation.h"\ntypedef __nv_bfloat16 bf16;\n' + src
+
+
+@pytest.fixture(scope="module")
+def program(tmp_path_factory):
+    d = tmp_path_factory.mktemp("emu")
+    cpp, exe = str(d / "cta.cpp"), str(d / "cta")
+    with open(cpp, "w") as fh:
+        fh.write(_source() + cp.MAIN % ONE)
+    r = subprocess.run(["g++", "-O1", "-std=c++17", "-w", "-Wno-psabi", "-I", cp.HERE, "-I", cp.CSRC, "-I", "/usr/local/cuda/include", cpp, "-o", exe],
+                       capture_output=True, text=True)
+    assert r.returncode == 0, r.stderr[:4000]
+    return exe
+
+
+@pytest.mark.parametrize("kernel", ["walk", "ends"])
+def test_any_order_of_warps(program, kernel):
+    cp._run(program, kernel, 200, 0, 0)
+
+
+@pytest.mark.parametrize("kernel", ["walk", "ends"])
+@pytest.mark.parametrize("expire,lose", [(0.0005, 0), (0.05, 0), (0.005, 0.02)], ids=["rare", "early", "lost load"])
+def test_expired_waits(program, kernel, expire, lose):
+    cp._run(program, kernel, 200, expire, lose)
