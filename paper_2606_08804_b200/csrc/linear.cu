@@ -19,6 +19,7 @@ int segments_of(const qd_linear_shape& s, bool backward) {
     const int chunk = linear_chunk(s);
     const long long per = linear_ctas(s) * (backward ? kLinearWalks : 1);
     const int chunks = (s.T + chunk - 1) / chunk;
+    if (per > 4 * kSMs) return 1;
     int best = 1;
     double least = 1e30;
     for (int n = 1; n <= 32 && n <= chunks; ++n) {
@@ -31,19 +32,51 @@ int segments_of(const qd_linear_shape& s, bool backward) {
     return best;
 }
 
+// The sums of the segments alone, in `ends`, become the states that they begin with: s0, then what is before each, decayed.  A thread has four
+// elements of a state; the loads of all segments are under way together.
+struct LinearJoin { const float* s0; float* ends; int reverse; };
+struct LinearJoins { LinearJoin j[2]; };
+constexpr int kJoinThreads = 128;
+__global__ void __launch_bounds__(kJoinThreads) k_linear_join(const LinearJoins js, const float* g, int H, int T, int segments, int length, int quads) {
+    sm100::grid_dep_wait();
+    sm100::grid_dep_launch();
+    const LinearJoin& j = js.j[blockIdx.z];
+    const int e = blockIdx.x * kJoinThreads + threadIdx.x;
+    const size_t bh = blockIdx.y;
+    if (e >= quads) return;
+    const float g2 = g[bh % H] * 1.4426950408889634f;
+    float4* ends = reinterpret_cast<float4*>(j.ends) + bh * segments * quads + e;
+    float4 s = j.s0 ? __ldcg(reinterpret_cast<const float4*>(j.s0) + bh * quads + e) : make_float4(0.f, 0.f, 0.f, 0.f);
+    constexpr int kGroup = 8;
+    for (int n0 = 0; n0 < segments; n0 += kGroup) {
+        float4 v[kGroup];
+#pragma unroll
+        for (int i = 0; i < kGroup; ++i) {
+            const int n = n0 + i, at = j.reverse ? segments - 1 - n : n;
+            if (n + 1 < segments) v[i] = __ldcg(ends + (size_t)at * quads);                // nobody begins with the sums of the last one
+        }
+#pragma unroll
+        for (int i = 0; i < kGroup; ++i) {
+            const int n = n0 + i, at = j.reverse ? segments - 1 - n : n;
+            if (n >= segments) break;
+            ends[(size_t)at * quads] = s;
+            const float keep = decay_power(g2, min(length, T - at * length));
+            if (n + 1 < segments)
+                s = make_float4(fmaf(keep, s.x, v[i].x), fmaf(keep, s.y, v[i].y), fmaf(keep, s.z, v[i].z), fmaf(keep, s.w, v[i].w));
+        }
+    }
+}
+
 struct Plan {
     LinearP p;
-    int chunk;
     float* ends[2];
 };
 Plan plan(const LinearArgs& a, bool backward) {
     Plan r{};
-    r.chunk = linear_chunk(a.s);
-    const int chunks = (a.s.T + r.chunk - 1) / r.chunk;
-    const int n = segments_of(a.s, backward);
+    const int chunk = linear_chunk(a.s), chunks = (a.s.T + chunk - 1) / chunk, n = segments_of(a.s, backward);
     r.p.T = a.s.T; r.p.H = a.s.H; r.p.BH = a.s.B * a.s.H;
     r.p.segments = n;
-    r.p.length = (chunks + n - 1) / n * r.chunk;
+    r.p.length = (chunks + n - 1) / n * chunk;
     r.p.g = a.g;
     r.p.scale = a.scale;
     r.p.status = reinterpret_cast<unsigned*>(a.ws);
@@ -59,6 +92,14 @@ cudaError_t walk(LinearP p, std::initializer_list<LinearWalk> ws, int db, int dc
     p.clear = clear;
     return a.s.dtype == QD_BF16 ? linear_tc(p, db, dc, a.stream) : linear_planes(p, db, dc, a.stream);
 }
+cudaError_t join(const LinearP& p, std::initializer_list<LinearJoin> js, const LinearArgs& a) {
+    LinearJoins all{};
+    int n = 0;
+    for (const LinearJoin& j : js) all.j[n++] = j;
+    const int quads = a.s.dk * a.s.dv / 4;
+    return launch_overlapped(k_linear_join, dim3((unsigned)(quads / kJoinThreads), (unsigned)p.BH, (unsigned)n), dim3(kJoinThreads), 0, a.stream, all, p.g,
+                             p.H, p.T, p.segments, p.length, quads);
+}
 
 }  // namespace
 
@@ -70,26 +111,30 @@ size_t linear_workspace(const qd_linear_shape& s, bool backward) {
 cudaError_t linear_fwd(const LinearArgs& a) {
     const Plan l = plan(a, false);
     const int dk = a.s.dk, dv = a.s.dv;
-    if (l.p.segments > 1) {
-        const cudaError_t e = walk(l.p, {LinearWalk{nullptr, a.k, a.v, nullptr, nullptr, nullptr, l.ends[0], 0, 0}}, dk, dv, a, true);
+    const bool cut = l.p.segments > 1;
+    if (cut) {
+        cudaError_t e = walk(l.p, {LinearWalk{nullptr, a.k, a.v, nullptr, nullptr, nullptr, l.ends[0], 0, 0}}, dk, dv, a, true);
+        if (e == cudaSuccess) e = join(l.p, {LinearJoin{a.h0, l.ends[0], 0}}, a);
         if (e != cudaSuccess) return e;
     }
-    return walk(l.p, {LinearWalk{a.q, a.k, a.v, a.o, a.h0, a.hT, l.ends[0], 0, 0}}, dk, dv, a, l.p.segments == 1);
+    return walk(l.p, {LinearWalk{a.q, a.k, a.v, a.o, cut ? l.ends[0] : a.h0, a.hT, nullptr, 0, 0}}, dk, dv, a, !cut);
 }
 
 cudaError_t linear_bwd(const LinearArgs& a) {
     const Plan l = plan(a, true);
     const int dk = a.s.dk, dv = a.s.dv;
-    if (l.p.segments > 1) {
-        const cudaError_t e = walk(l.p, {LinearWalk{nullptr, a.k, a.v, nullptr, nullptr, nullptr, l.ends[0], 0, 0},
-                                         LinearWalk{nullptr, a.q, a.dO, nullptr, nullptr, nullptr, l.ends[1], 1, 0}}, dk, dv, a, true);
+    const bool cut = l.p.segments > 1;
+    if (cut) {
+        cudaError_t e = walk(l.p, {LinearWalk{nullptr, a.k, a.v, nullptr, nullptr, nullptr, l.ends[0], 0, 0},
+                                   LinearWalk{nullptr, a.q, a.dO, nullptr, nullptr, nullptr, l.ends[1], 1, 0}}, dk, dv, a, true);
+        if (e == cudaSuccess) e = join(l.p, {LinearJoin{a.h0, l.ends[0], 0}, LinearJoin{a.dhT, l.ends[1], 1}}, a);
         if (e != cudaSuccess) return e;
     }
-    const LinearWalk wq{a.dO, a.v, a.k, a.dq, a.h0, nullptr, l.ends[0], 0, 1}, wk{a.v, a.dO, a.q, a.dk, a.dhT, nullptr, l.ends[1], 1, 1},
-        wv{a.k, a.q, a.dO, a.dv, a.dhT, a.dh0, l.ends[1], 1, 0};
-    const bool clear = l.p.segments == 1;
-    if (dk == dv) return walk(l.p, {wq, wk, wv}, dk, dv, a, clear);
-    const cudaError_t e = walk(l.p, {wq, wk}, dv, dk, a, clear);
+    const float *h = cut ? l.ends[0] : a.h0, *dh = cut ? l.ends[1] : a.dhT;
+    const LinearWalk wq{a.dO, a.v, a.k, a.dq, h, nullptr, nullptr, 0, 1}, wk{a.v, a.dO, a.q, a.dk, dh, nullptr, nullptr, 1, 1},
+        wv{a.k, a.q, a.dO, a.dv, dh, a.dh0, nullptr, 1, 0};
+    if (dk == dv) return walk(l.p, {wq, wk, wv}, dk, dv, a, !cut);
+    const cudaError_t e = walk(l.p, {wq, wk}, dv, dk, a, !cut);
     return e == cudaSuccess ? walk(l.p, {wv}, dk, dv, a, false) : e;
 }
 

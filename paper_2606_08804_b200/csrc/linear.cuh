@@ -8,7 +8,8 @@
 //   backward in time (i >= r), rho_r = e^{g (n - 1 - r)}, kappa_i = scale e^{g (i + 1)}:
 //     dv = walk(a = k,  b = q, c = dO), S = dL/dh      dk = walk(a = v,  b = dO, c = q), S = (dL/dh)^T
 // so a backward needs nothing of the forward but its inputs: no state of any chunk is ever in memory.  Where sequences and heads are
-// few, a sequence is cut into segments: the sums of a segment by itself first (`ends`), then the walks, each from the sum of what is before it.
+// few, a sequence is cut into segments: first the sums of each by itself (`ends`), which are then joined to the states that the segments
+// begin with, then the walks from there.
 #pragma once
 #include "internal.h"
 #include "sm100.cuh"
@@ -18,9 +19,9 @@ namespace qd {
 struct LinearWalk {
     const void *a, *b, *c;
     void* out;               // NULL: the sums of every segment alone, to `ends`
-    const float* s0;         // state before the first token (after the last one, backward in time); NULL: zeros
+    const float* s0;         // the states that the segments begin with, [B H][segments][state]; NULL: zeros
     float* sT;               // the state that the walk ends with; NULL: not returned
-    float* ends;             // [B H][segments][state]: written, or read where a segment begins with what others leave
+    float* ends;             // [B H][segments][state], written where out is NULL
     int reverse;
     int flip;                // s0, sT and ends hold S^T (as [DC][DB])
 };
@@ -37,19 +38,5 @@ struct LinearP {
 
 // e^{g m} for a count m of tokens, g2 = g log2(e): 1 for m = 0 whatever g is (minus infinity: nothing is kept)
 __device__ __forceinline__ float decay_power(float g2, int m) { return m == 0 ? 1.f : exp2f(g2 * (float)m); }
-
-// Element e of the state that `segment` of this walk begins with, e counted as s0 and ends count it.
-__device__ __forceinline__ float linear_entry(const LinearP& p, const LinearWalk& w, int bh, int segment, int size, int e, float g2) {
-    const int before = w.reverse ? p.T - min(p.T, (segment + 1) * p.length) : segment * p.length;      // tokens since s0
-    float s = w.s0 ? decay_power(g2, before) * __ldcg(w.s0 + (size_t)bh * size + e) : 0.f;
-    const float keep = decay_power(g2, p.length);
-    if (p.segments > 1) {
-        const float* ends = w.ends + (size_t)bh * p.segments * size + e;
-        float f = 1.f;                                                                                 // nearest first; those between are whole
-        for (int j = w.reverse ? segment + 1 : segment - 1; j >= 0 && j < p.segments; j += w.reverse ? 1 : -1, f *= keep)
-            s = fmaf(f, __ldcg(ends + (size_t)j * size), s);
-    }
-    return s;
-}
 
 }  // namespace qd

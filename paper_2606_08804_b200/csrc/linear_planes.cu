@@ -86,9 +86,10 @@ __global__ void __launch_bounds__(kPlanesThreads, 1) k_linear_planes(const Linea
     float st[1][NS][4];
     const int size = DB * DC;
     auto place = [&](int r, int c) { return w.flip ? (j0 + c) * DB + r : r * DC + j0 + c; };
+    const float* entry = w.s0 ? w.s0 + ((size_t)bh * p.segments + segment) * size : nullptr;
     each(st, sm, sn, [&](int r, int c, float& x, float& y) {
-        x = w.out ? linear_entry(p, w, bh, segment, size, place(r, c), g2) : 0.f;
-        y = w.out ? linear_entry(p, w, bh, segment, size, place(r, c + 1), g2) : 0.f;
+        x = entry ? __ldcg(entry + place(r, c)) : 0.f;
+        y = entry ? __ldcg(entry + place(r, c + 1)) : 0.f;
         S.st2(r, c, x, y);
     });
     if (tid < kRows) s_d[tid] = p.scale * decay_power(g2, tid);

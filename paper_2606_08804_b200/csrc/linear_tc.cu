@@ -1,13 +1,15 @@
 // Linear attention in bf16 on the tensor cores: a walk (linear.cuh) over chunks of 128 tokens to a CTA, every product a tcgen05.mma:
 //     P = (a b^T) o D  (rounded to bf16 as the next operand)      out = P c + rho (a S)      S <- e^{g n} S + (kappa b)^T c
-// The state stays in fp32 registers; each chunk's sum comes from tensor memory and is added there (the tensor cores cut as they
-// accumulate).  For a S it goes to shared memory in bf16; kappa b goes there in two bf16 planes, so that the state has 16 bits of every term.
+// The state stays in fp32 registers; each chunk's sum comes from tensor memory and is added there (the tensor cores cut as they accumulate).
+// For a S it goes to shared memory in bf16.  kappa b is three bf16 planes, which hold all of its 24 bits: with two the state is 2.4e-6 of its
+// length off, which is half of what a whole fp32 sum over a sequence is allowed to be.
 //
-// Bound by HBM: per token and head two tensors of its width in and one out besides c, 2.5 us a chunk of 128 x 128 with 128 CTAs; the five products of
-// a chunk are 2560 cycles.  So a chunk's steps need not overlap perfectly, only loads must never stop: five (six) tile buffers, in each of
-// which b, a and c of the chunks follow one another, and out leaves through a's.
-//   warps 0-3    P: row r = lane, from tensor memory and back to it as an operand; then kappa b in place and its rest
-//   warps 4-7    out: 32 rows each, staged in a's tile, stored by TMA
+// Bound by HBM: per token and head two tensors of its width in and one out besides c, 2.5 us a chunk of 128 x 128 with 128 CTAs; the products of
+// a chunk are 3072 cycles.  So a chunk's steps need not overlap perfectly, only loads must never stop: five (six) tile buffers, in each of
+// which b, a and c of the chunks follow one another, and out leaves through a's.  The first plane takes b's place, the others of 32 tokens at a
+// time go through two buffers.
+//   warps 0-3    P: row r = lane, from tensor memory and back to it as an operand
+//   warps 4-7    the planes of kappa b, then out: 32 rows each, staged in a's tile, stored by TMA
 //   warps 8-15   state: a row to a lane, half of the columns to a warpgroup
 //   warp 16      issues the products;  warp 17  loads
 // All waits are bounded; on expiry the status word says so, everybody leaves, what is in flight is waited for.
@@ -17,7 +19,7 @@ namespace qd {
 namespace {
 using namespace sm100;
 
-constexpr int kTokens = 128, kTcThreads = 18 * 32;
+constexpr int kTokens = 128, kPart = 32, kParts = kTokens / kPart, kTcThreads = 18 * 32;
 
 struct LinearMaps { CUtensorMap a[kLinearWalks], b[kLinearWalks], c[kLinearWalks], out[kLinearWalks]; };
 
@@ -26,7 +28,7 @@ struct TcLinear {
     static constexpr int kSlot = kTokens * (DB > DC ? DB : DC) * 2;
     static constexpr int kRing = ENDS ? 4 : DB == 128 ? 5 : 6;        // at most two chunks ahead: barriers of chunks n and n + 2 are the same
     static constexpr int kPer = ENDS ? 2 : 3;                         // tiles of a chunk: b, a, c
-    static constexpr int kState = ENDS ? 0 : DB * DC * 2, kRest = kTokens * DB * 2;
+    static constexpr int kState = ENDS ? 0 : DB * DC * 2, kPlane = kPart * DB * 2, kRest = 4 * kPlane;
     static constexpr int kOffRest = kState, kOffRing = kOffRest + kRest, kSmem = kOffRing + kRing * kSlot + 1024;
     static constexpr int kColumns = ENDS ? DC : 512;
     static_assert(kSmem <= 232448 - 1024, "shared memory");
@@ -39,12 +41,12 @@ __global__ void __launch_bounds__(kTcThreads, 1) k_linear_tc(const __grid_consta
     extern __shared__ unsigned char smem_raw[];
     unsigned char* smem = (unsigned char*)(((uintptr_t)smem_raw + 1023) & ~(uintptr_t)1023);
     unsigned char *sState = smem, *sRest = smem + L::kOffRest, *sRing = smem + L::kOffRing;
-    // bar_s, bar_o, bar_kv: products complete; bar_p, bar_k, bar_h: operands in place; bar_of: out's accumulators have been read;
-    // bar_af: a's tile is free.  bar_kv and bar_af have one for even and one for odd chunks, since the loads run up to two ahead.
-    __shared__ uint64_t bar_full[kRing], bar_s, bar_o, bar_kv[2], bar_p, bar_k, bar_h, bar_of, bar_af[2], bar_end;
+    // bar_s, bar_o, bar_kv, bar_kq: products complete; bar_p, bar_k, bar_h: operands in place; bar_of: out's accumulators have been
+    // read; bar_af: a's tile is free.  Where one side runs up to two phases ahead there is one for even and one for odd phases.
+    __shared__ uint64_t bar_full[kRing], bar_s, bar_o, bar_kv[2], bar_kq[2], bar_p, bar_k[2], bar_h, bar_of, bar_af[2], bar_end;
     __shared__ uint32_t tmem_slot;
     __shared__ volatile int s_abort;
-    __shared__ float s_d[kTokens];
+    __shared__ float s_d[2 * kTokens];                                    // D(|m|), m from -128
 
     const int tid = threadIdx.x, warp = warp_index(), lane = tid & 31, wq = warp & 3;
     const int walk = blockIdx.x % p.walks, cta = blockIdx.x / p.walks, segment = cta % p.segments, bh = cta / p.segments;
@@ -56,8 +58,8 @@ __global__ void __launch_bounds__(kTcThreads, 1) k_linear_tc(const __grid_consta
 
     if (tid == 0) {
         for (int i = 0; i < kRing; ++i) mbar_init(&bar_full[i], 1);
-        for (int i = 0; i < 2; ++i) { mbar_init(&bar_kv[i], 1); mbar_init(&bar_af[i], 4); }
-        mbar_init(&bar_s, 1); mbar_init(&bar_o, 1); mbar_init(&bar_p, 4); mbar_init(&bar_k, 4); mbar_init(&bar_h, 8); mbar_init(&bar_of, 4);
+        for (int i = 0; i < 2; ++i) { mbar_init(&bar_kv[i], 1); mbar_init(&bar_kq[i], 1); mbar_init(&bar_k[i], 4); mbar_init(&bar_af[i], 4); }
+        mbar_init(&bar_s, 1); mbar_init(&bar_o, 1); mbar_init(&bar_p, 4); mbar_init(&bar_h, 8); mbar_init(&bar_of, 4);
         mbar_init(&bar_end, 1);
         mbar_init_fence();
         s_abort = 0;
@@ -66,7 +68,7 @@ __global__ void __launch_bounds__(kTcThreads, 1) k_linear_tc(const __grid_consta
     grid_dep_wait();
     grid_dep_launch();
     const float g2 = p.g[hh] * 1.4426950408889634f;
-    if (tid < kTokens) s_d[tid] = p.scale * decay_power(g2, tid);
+    if (tid < 2 * kTokens) s_d[tid] = p.scale * decay_power(g2, abs(tid - kTokens));
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
@@ -85,87 +87,94 @@ __global__ void __launch_bounds__(kTcThreads, 1) k_linear_tc(const __grid_consta
     if (ENDS && segment == (reverse ? 0 : p.segments - 1)) {
         // nobody begins with the sums of this one
     } else if (warp < 4) {
-        // ---------------------------------- weights and scaled rows ----------------------------------
-        const int r = (int)lanes + lane;
-        for (int n = 0; n < chunks; ++n) {
-            const int live = min(kTokens, end - token0(n));
-            if (!ENDS) {
-                if (!all(wait(&bar_s, n & 1))) break;
-                tc_fence_after();
+        // ---------------------------------- weights ----------------------------------
+        const float* far = s_d + kTokens + lanes + lane;
+        for (int n = 0; n < chunks && !ENDS; ++n) {
+            if (!all(wait(&bar_s, n & 1))) break;
+            tc_fence_after();
 #pragma unroll
-                for (int j = 0; j < 4; ++j) {                      // 32 columns i, which become 16 packed ones in the place of what has been read
-                    uint32_t o[16];
-                    if (reverse ? j >= wq : j <= wq) {
-                        float v[32];
-                        tmem_ld32(tmem_addr(tS, lanes, 32 * j), v);
-                        tmem_ld_wait();
+            for (int j = 0; j < 4; ++j) {                          // 32 columns i, which become 16 packed ones in the place of what has been read
+                uint32_t o[16];
+                if (reverse ? j >= wq : j <= wq) {
+                    float v[32];
+                    tmem_ld32(tmem_addr(tS, lanes, 32 * j), v);
+                    tmem_ld_wait();
 #pragma unroll
-                        for (int e = 0; e < 32; ++e) {
-                            const int u = reverse ? 32 * j + e - r : r - 32 * j - e;
-                            v[e] = u >= 0 ? v[e] * s_d[u & (kTokens - 1)] : 0.f;
-                        }
+                    for (int e = 0; e < 32; ++e) v[e] *= far[-32 * j - e];
+                    if (j == wq)                                   // an infinite product past the diagonal leaves nothing either
 #pragma unroll
-                        for (int e = 0; e < 16; ++e) o[e] = pack_bf16(v[2 * e], v[2 * e + 1]);
-                    } else {
+                        for (int e = 0; e < 32; ++e) v[e] = (reverse ? e >= lane : e <= lane) ? v[e] : 0.f;
 #pragma unroll
-                        for (int e = 0; e < 16; ++e) o[e] = 0;
-                    }
-                    tmem_st8(tmem_addr(tS, lanes, 16 * j), o);
-                    tmem_st8(tmem_addr(tS, lanes, 16 * j + 8), o + 8);
+                    for (int e = 0; e < 16; ++e) o[e] = pack_bf16(v[2 * e], v[2 * e + 1]);
+                } else {
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) o[e] = 0;
                 }
-                tmem_st_wait();
-                tc_fence_before();
-                arrive(&bar_p);
-            } else if (n > 0 && !all(wait(&bar_kv[(n - 1) & 1], ((n - 1) >> 1) & 1))) {
-                break;
+                tmem_st8(tmem_addr(tS, lanes, 16 * j), o);
+                tmem_st8(tmem_addr(tS, lanes, 16 * j + 8), o + 8);
             }
-            // the product with b has been taken (there is none in ENDS): its rows times kappa, and what bf16 leaves of them
-            if (!all(full(n * kPer))) break;
-            const float kappa = r >= live ? 0.f : reverse ? p.scale * decay_power(g2, r + 1) : decay_power(g2, live - 1 - r);
-            unsigned char *tile = slot(n * kPer), *rest = sRest;
-#pragma unroll
-            for (int blk = 0; blk < DB / 64; ++blk, tile += kTokens * 128, rest += kTokens * 128)
-#pragma unroll 4
-                for (int ch = 0; ch < 8; ++ch) {
-                    const uint32_t off = sw128_chunk(r, ch);
-                    float x[8], y[8];
-                    load8(tile + off, x);
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) x[e] *= kappa;
-                    const uint4 hi = pack8(x);
-                    const uint32_t h[4] = {hi.x, hi.y, hi.z, hi.w};
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        y[2 * e] = x[2 * e] - __uint_as_float(h[e] << 16);
-                        y[2 * e + 1] = x[2 * e + 1] - __uint_as_float(h[e] & 0xffff0000u);
-                    }
-                    sts128(tile + off, hi);
-                    sts128(rest + off, pack8(y));
-                }
-            fence_proxy_async();
-            arrive(&bar_k);
+            tmem_st_wait();
+            tc_fence_before();
+            arrive(&bar_p);
         }
     } else if (warp < 8) {
-        // ---------------------------------- output ----------------------------------
+        // ---------------------------------- planes and output ----------------------------------
         const int r = (int)lanes + lane;
-        for (int n = 0; n < chunks && !ENDS; ++n) {
+        for (int n = 0; n < chunks; ++n) {
             const int t0 = token0(n), live = min(kTokens, end - t0);
+            // b has been multiplied with a: its rows times kappa, a row to a lane, a quarter of the columns to a warp
+            if (!ENDS && !all(wait(&bar_s, n & 1))) break;
+            if (!all(full(n * kPer))) break;
+            bool ok = true;
+            for (int q = 0; q < kParts && ok; ++q) {
+                const int i = n * kParts + q, row = q * kPart + lane;
+                if (i >= 2) ok = all(wait(&bar_kq[i & 1], ((i - 2) >> 1) & 1));
+                const float kappa = row >= live ? 0.f : reverse ? p.scale * decay_power(g2, row + 1) : decay_power(g2, live - 1 - row);
+                unsigned char *tile = slot(n * kPer), *rest = sRest + (i & 1) * 2 * L::kPlane;
+#pragma unroll
+                for (int k = 0; k < DB / 32; ++k) {
+                    const int ch = wq * (DB / 32) + k, blk = ch >> 3;
+                    const uint32_t off = sw128_chunk(row, ch & 7), part = sw128_chunk(lane, ch & 7) + blk * kPart * 128;
+                    unsigned char* at = tile + blk * kTokens * 128 + off;
+                    float x[8];
+                    load8(at, x);
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) x[e] *= kappa;
+                    uint4 plane = pack8(x);
+                    sts128(at, plane);
+#pragma unroll
+                    for (int m = 0; m < 2; ++m) {                 // what the planes before leave of it
+                        const uint32_t h[4] = {plane.x, plane.y, plane.z, plane.w};
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) {
+                            x[2 * e] -= __uint_as_float(h[e] << 16);
+                            x[2 * e + 1] -= __uint_as_float(h[e] & 0xffff0000u);
+                        }
+                        plane = pack8(x);
+                        sts128(rest + m * L::kPlane + part, plane);
+                    }
+                }
+                fence_proxy_async();
+                arrive(&bar_k[i & 1]);
+            }
+            if (!ok) break;
+            if (ENDS) continue;
             const float rho = r >= live ? 0.f : reverse ? decay_power(g2, live - 1 - r) : p.scale * decay_power(g2, r + 1);
             if (!all(wait(&bar_o, n & 1))) break;
             tc_fence_after();
             unsigned char* stage = slot(n * kPer + kA);
 #pragma unroll
-            for (int j = 0; j < DC / 32; ++j) {
-                float x[32], y[32];
-                tmem_ld32(tmem_addr(tO1, lanes, 32 * j), x);
-                tmem_ld32(tmem_addr(tO2, lanes, 32 * j), y);
+            for (int j = 0; j < DC / 16; ++j) {
+                float x[16], y[16];
+                tmem_ld16(tmem_addr(tO1, lanes, 16 * j), x);
+                tmem_ld16(tmem_addr(tO2, lanes, 16 * j), y);
                 tmem_ld_wait();
-                if (j == DC / 32 - 1) { tc_fence_before(); arrive(&bar_of); }
+                if (j == DC / 16 - 1) { tc_fence_before(); arrive(&bar_of); }
 #pragma unroll
-                for (int e = 0; e < 32; ++e) x[e] = fmaf(rho, y[e], x[e]);
+                for (int e = 0; e < 16; ++e) x[e] = fmaf(rho, y[e], x[e]);
 #pragma unroll
-                for (int ch = 0; ch < 4; ++ch)
-                    sts128(stage + (j >> 1) * kTokens * 128 + sw128_chunk(r, (j & 1) * 4 + ch), pack8(x + 8 * ch));
+                for (int ch = 0; ch < 2; ++ch)
+                    sts128(stage + (j >> 2) * kTokens * 128 + sw128_chunk(r, (j & 3) * 2 + ch), pack8(x + 8 * ch));
             }
             fence_proxy_async();
             __syncwarp();
@@ -190,8 +199,17 @@ __global__ void __launch_bounds__(kTcThreads, 1) k_linear_tc(const __grid_consta
         const bool live_row = DB == 128 || lane < 16;
         float h[HC];
         auto place = [&](int i) { return w.flip ? (c0 + i) * DB + r : r * DC + c0 + i; };
+        const float* entry = !ENDS && w.s0 && live_row ? w.s0 + ((size_t)bh * p.segments + segment) * size : nullptr;
+        if (entry && !w.flip) {
 #pragma unroll
-        for (int i = 0; i < HC; ++i) h[i] = !ENDS && live_row ? linear_entry(p, w, bh, segment, size, place(i), g2) : 0.f;
+            for (int i = 0; i < HC; i += 4) {
+                const float4 t = __ldcg(reinterpret_cast<const float4*>(entry + place(i)));
+                h[i] = t.x; h[i + 1] = t.y; h[i + 2] = t.z; h[i + 3] = t.w;
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < HC; ++i) h[i] = entry ? __ldcg(entry + place(i)) : 0.f;
+        }
         auto put = [&]() {
             if (!ENDS && live_row)
 #pragma unroll
@@ -206,21 +224,27 @@ __global__ void __launch_bounds__(kTcThreads, 1) k_linear_tc(const __grid_consta
             tc_fence_after();
             const float keep = decay_power(g2, min(kTokens, end - token0(n)));
 #pragma unroll
-            for (int j = 0; j < HC / 32; ++j) {
-                float v[32];
-                tmem_ld32(tmem_addr(tKV, lanes, c0 + 32 * j), v);
+            for (int j = 0; j < HC / 16; ++j) {
+                float v[16];
+                tmem_ld16(tmem_addr(tKV, lanes, c0 + 16 * j), v);
                 tmem_ld_wait();
 #pragma unroll
-                for (int e = 0; e < 32; ++e) h[32 * j + e] = fmaf(keep, h[32 * j + e], v[e]);
+                for (int e = 0; e < 16; ++e) h[16 * j + e] = fmaf(keep, h[16 * j + e], v[e]);
             }
             tc_fence_before();
             if (n + 1 < chunks) put();
         }
         float* left = ENDS ? w.ends + ((size_t)bh * p.segments + segment) * size
                            : segment == (reverse ? 0 : p.segments - 1) && w.sT ? w.sT + (size_t)bh * size : nullptr;
-        if (left && live_row && !s_abort)
+        if (left && live_row && !s_abort) {
+            if (!w.flip) {
 #pragma unroll
-            for (int i = 0; i < HC; ++i) left[place(i)] = h[i];
+                for (int i = 0; i < HC; i += 4) *reinterpret_cast<float4*>(left + place(i)) = make_float4(h[i], h[i + 1], h[i + 2], h[i + 3]);
+            } else {
+#pragma unroll
+                for (int i = 0; i < HC; ++i) left[place(i)] = h[i];
+            }
+        }
     } else if (warp == 16) {
         // ---------------------------------- products, by the converged warp ----------------------------------
         const uint32_t issue = elect_lane();
@@ -242,16 +266,27 @@ __global__ void __launch_bounds__(kTcThreads, 1) k_linear_tc(const __grid_consta
                 umma_product_w<false, true>(tO2, tA, blk, aState, DB * 128, DC, DB, false, issue);
             }
             if (!all(full(n * kPer + kC))) break;
-            if (!ENDS) {
-                if (!all(wait(&bar_p, n & 1))) break;
+            bool ok = true;
+#pragma unroll
+            for (int q = 0; q < kParts; ++q) {
+                if (!ENDS && q == kParts / 2) {                   // the weights have been made beside the first two parts
+                    ok = ok && all(wait(&bar_p, n & 1));
+                    if (!ok) break;
+                    tc_fence_after();
+                    umma_product_ts_w<true>(tO1, tS, tC, blk, DC, kTokens, false, issue);
+                    umma_commit_w(&bar_o, issue);
+                }
+                const int i = n * kParts + q;
+                ok = ok && all(wait(&bar_k[i & 1], (i >> 1) & 1));
+                if (!ok) break;
                 tc_fence_after();
-                umma_product_ts_w<true>(tO1, tS, tC, blk, DC, kTokens, false, issue);
-                umma_commit_w(&bar_o, issue);
+                const uint32_t rest = aRest + (uint32_t)(i & 1) * 2 * L::kPlane, line = q * kPart * 128;
+                umma_product_w<true, true, DB>(tKV, tB + line, blk, tC + line, blk, DC, kPart, q > 0, issue);
+                umma_product_w<true, true, DB>(tKV, rest, kPart * 128, tC + line, blk, DC, kPart, true, issue);
+                umma_product_w<true, true, DB>(tKV, rest + L::kPlane, kPart * 128, tC + line, blk, DC, kPart, true, issue);
+                umma_commit_w(&bar_kq[i & 1], issue);
             }
-            if (!all(wait(&bar_k, n & 1))) break;
-            tc_fence_after();
-            umma_product_w<true, true, DB>(tKV, tB, blk, tC, blk, DC, kTokens, false, issue);
-            umma_product_w<true, true, DB>(tKV, aRest, blk, tC, blk, DC, kTokens, true, issue);
+            if (!ok) break;
             umma_commit_w(&bar_kv[n & 1], issue);
         }
         umma_commit_w(&bar_end, issue);                           // leaves when its products have come to their end, whatever has expired
