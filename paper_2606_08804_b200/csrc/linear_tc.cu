@@ -21,6 +21,19 @@ using namespace sm100;
 
 constexpr int kTokens = 128, kPart = 32, kParts = kTokens / kPart, kTcThreads = 18 * 32;
 
+// The upper halves of eight fp32 values as packed bf16; what they leave stays behind, exactly.
+__device__ __forceinline__ uint4 upper8(float (&x)[8]) {
+    uint32_t r[4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+        const uint32_t lo = __float_as_uint(x[2 * e]), hi = __float_as_uint(x[2 * e + 1]) & 0xffff0000u;
+        r[e] = lo >> 16 | hi;
+        x[2 * e] -= __uint_as_float(lo & 0xffff0000u);
+        x[2 * e + 1] -= __uint_as_float(hi);
+    }
+    return make_uint4(r[0], r[1], r[2], r[3]);
+}
+
 struct LinearMaps { CUtensorMap a[kLinearWalks], b[kLinearWalks], c[kLinearWalks], out[kLinearWalks]; };
 
 template <int DB, int DC, bool ENDS>
@@ -120,6 +133,7 @@ __global__ void __launch_bounds__(kTcThreads, 1) k_linear_tc(const __grid_consta
     } else if (warp < 8) {
         // ---------------------------------- planes and output ----------------------------------
         const int r = (int)lanes + lane;
+        int stored = -1;                                           // chunk whose output this thread has stored and not seen read
         for (int n = 0; n < chunks; ++n) {
             const int t0 = token0(n), live = min(kTokens, end - t0);
             // b has been multiplied with a: its rows times kappa, a row to a lane, a quarter of the columns to a warp
@@ -128,6 +142,11 @@ __global__ void __launch_bounds__(kTcThreads, 1) k_linear_tc(const __grid_consta
             bool ok = true;
             for (int q = 0; q < kParts && ok; ++q) {
                 const int i = n * kParts + q, row = q * kPart + lane;
+                if (q == 1 && stored >= 0) {                       // the output of the chunk before has been read by now: its tile is free
+                    tma_store_wait_read();
+                    mbar_arrive(&bar_af[stored & 1]);
+                    stored = -1;
+                }
                 if (i >= 2) ok = all(wait(&bar_kq[i & 1], ((i - 2) >> 1) & 1));
                 const float kappa = row >= live ? 0.f : reverse ? p.scale * decay_power(g2, row + 1) : decay_power(g2, live - 1 - row);
                 unsigned char *tile = slot(n * kPer), *rest = sRest + (i & 1) * 2 * L::kPlane;
@@ -136,23 +155,18 @@ __global__ void __launch_bounds__(kTcThreads, 1) k_linear_tc(const __grid_consta
                     const int ch = wq * (DB / 32) + k, blk = ch >> 3;
                     const uint32_t off = sw128_chunk(row, ch & 7), part = sw128_chunk(lane, ch & 7) + blk * kPart * 128;
                     unsigned char* at = tile + blk * kTokens * 128 + off;
+                    const uint4 raw = *reinterpret_cast<const uint4*>(at);
+                    const uint32_t in[4] = {raw.x, raw.y, raw.z, raw.w};
                     float x[8];
-                    load8(at, x);
 #pragma unroll
-                    for (int e = 0; e < 8; ++e) x[e] *= kappa;
-                    uint4 plane = pack8(x);
-                    sts128(at, plane);
-#pragma unroll
-                    for (int m = 0; m < 2; ++m) {                 // what the planes before leave of it
-                        const uint32_t h[4] = {plane.x, plane.y, plane.z, plane.w};
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) {
-                            x[2 * e] -= __uint_as_float(h[e] << 16);
-                            x[2 * e + 1] -= __uint_as_float(h[e] & 0xffff0000u);
-                        }
-                        plane = pack8(x);
-                        sts128(rest + m * L::kPlane + part, plane);
+                    for (int e = 0; e < 4; ++e) {
+                        x[2 * e] = kappa * __uint_as_float(in[e] << 16);
+                        x[2 * e + 1] = kappa * __uint_as_float(in[e] & 0xffff0000u);
                     }
+                    // cut to 8 bits, three times: nothing is left of 24
+                    sts128(at, upper8(x));
+                    sts128(rest + part, upper8(x));
+                    sts128(rest + L::kPlane + part, upper8(x));
                 }
                 fence_proxy_async();
                 arrive(&bar_k[i & 1]);
@@ -184,9 +198,8 @@ __global__ void __launch_bounds__(kTcThreads, 1) k_linear_tc(const __grid_consta
                     for (int blk = 0; blk < DC / 64; ++blk)
                         tma_store_3d(&maps.out[walk], stage + blk * kTokens * 128 + lanes * 128, hh * DC + blk * 64, t0 + (int)lanes, b);
                     tma_store_commit();
-                    tma_store_wait_read();
                 }
-                mbar_arrive(&bar_af[n & 1]);
+                stored = n;
             }
             __syncwarp();
         }
@@ -250,14 +263,17 @@ __global__ void __launch_bounds__(kTcThreads, 1) k_linear_tc(const __grid_consta
         const uint32_t issue = elect_lane();
         const uint32_t aState = smem_u32(sState), aRest = smem_u32(sRest), aRing = smem_u32(sRing);
         auto tile = [&](int m) { return aRing + (uint32_t)(m % kRing) * L::kSlot; };
+        constexpr uint32_t blk = kTokens * 128;
+        auto scores = [&](int n) {
+            if (ENDS) return true;
+            if (!all(full(n * kPer) && full(n * kPer + kA))) return false;
+            umma_product_w<false, false>(tS, tile(n * kPer + kA), blk, tile(n * kPer), blk, kTokens, DB, false, issue);
+            umma_commit_w(&bar_s, issue);
+            return true;
+        };
         for (int n = 0; n < chunks; ++n) {
             const uint32_t tB = tile(n * kPer), tA = tile(n * kPer + kA), tC = tile(n * kPer + kC);
-            constexpr uint32_t blk = kTokens * 128;
-            if (!ENDS) {
-                if (!all(full(n * kPer) && full(n * kPer + kA))) break;
-                umma_product_w<false, false>(tS, tA, blk, tB, blk, kTokens, DB, false, issue);
-                umma_commit_w(&bar_s, issue);
-            }
+            if (n == 0 && !scores(0)) break;
             if (!all(wait(&bar_h, n & 1))) break;
             tc_fence_after();
             if (!ENDS) {
@@ -275,6 +291,7 @@ __global__ void __launch_bounds__(kTcThreads, 1) k_linear_tc(const __grid_consta
                     tc_fence_after();
                     umma_product_ts_w<true>(tO1, tS, tC, blk, DC, kTokens, false, issue);
                     umma_commit_w(&bar_o, issue);
+                    ok = n + 1 == chunks || scores(n + 1);        // its weights are made beside the rest of this one
                 }
                 const int i = n * kParts + q;
                 ok = ok && all(wait(&bar_k[i & 1], (i >> 1) & 1));
@@ -294,18 +311,25 @@ __global__ void __launch_bounds__(kTcThreads, 1) k_linear_tc(const __grid_consta
     } else if (lane == 0) {
         // ---------------------------------- loads ----------------------------------
         const int tiles = chunks * kPer;
+        auto each_box = [&](int m, auto f) {
+            const int j = m % kPer, width = j == kC ? DC : DB;
+            const CUtensorMap* map = j == 0 ? &maps.b[walk] : j == kC ? &maps.c[walk] : &maps.a[walk];
+            for (int blk = 0; blk < width / 64; ++blk) f(map, blk, hh * width + blk * 64, token0(m / kPer));
+        };
+        // what no buffer is free for yet comes to L2 two chunks ahead
+        constexpr int kAhead = 2 * kPer;
+        auto prefetch = [&](int m) { each_box(m, [&](const CUtensorMap* map, int, int x, int t0) { tma_prefetch_3d(map, x, t0, b); }); };
+        for (int m = kRing; m < kAhead && m < tiles; ++m) prefetch(m);
         for (int m = 0; m < tiles; ++m, ++loads) {
+            if (m + kAhead < tiles) prefetch(m + kAhead);
             if (m >= kRing) {
                 const int old = m - kRing, on = old / kPer;
                 uint64_t* bar = !ENDS && old % kPer == kA ? &bar_af[on & 1] : &bar_kv[on & 1];
                 if (!wait(bar, (on >> 1) & 1)) break;
             }
-            const int n = m / kPer, j = m % kPer, t0 = token0(n);
-            const CUtensorMap* map = j == 0 ? &maps.b[walk] : j == kC ? &maps.c[walk] : &maps.a[walk];
-            const int width = j == kC ? DC : DB;
             uint64_t* bar = &bar_full[m % kRing];
-            mbar_expect_tx(bar, kTokens * width * 2);
-            for (int blk = 0; blk < width / 64; ++blk) tma_load_3d(slot(m) + blk * kTokens * 128, map, hh * width + blk * 64, t0, b, bar);
+            mbar_expect_tx(bar, kTokens * (m % kPer == kC ? DC : DB) * 2);
+            each_box(m, [&](const CUtensorMap* map, int blk, int x, int t0) { tma_load_3d(slot(m) + blk * kTokens * 128, map, x, t0, b, bar); });
         }
     }
     __syncwarp();
