@@ -11,11 +11,12 @@
 // cycles a chunk with the planes in shared memory and two accumulators.  Six tile buffers, two chunks deep: b, a, c of each; out leaves
 // through a's.
 //   warps 0-3    planes of the first 64 tokens; P: row r = lane, from tensor memory and back to it
-//   warps 4-7    planes of the others; a S times rho; out: 32 rows each, staged in a's tile, stored by TMA
-//   warps 8-15   state, transposed: a column of S to a lane, half of the rows to a warpgroup
+//   warps 4-7    planes of the others; out: 32 rows each, staged in a's tile, stored by TMA
+//   warps 8-15   state, transposed: a column of S to a lane, half of the rows to a warpgroup; a S times rho
 //   warp 16      issues the products;  warp 17  loads
 // All waits are bounded; on expiry the status word says so, everybody leaves, what is in flight is waited for.
 #include "linear.cuh"
+#include "rows.cuh"
 
 namespace qd {
 namespace {
@@ -23,16 +24,12 @@ using namespace sm100;
 
 constexpr int kTokens = 128, kPart = 32, kParts = kTokens / kPart, kTcThreads = 18 * 32;
 
-// The upper halves of pairs of fp32 values as packed bf16; what they leave stays behind, exactly.
-template <int N>
-__device__ __forceinline__ void cut(float (&x)[2 * N], uint32_t (&r)[N]) {
-#pragma unroll
-    for (int e = 0; e < N; ++e) {
-        const uint32_t lo = __float_as_uint(x[2 * e]), hi = __float_as_uint(x[2 * e + 1]) & 0xffff0000u;
-        r[e] = lo >> 16 | hi;
-        x[2 * e] -= __uint_as_float(lo & 0xffff0000u);
-        x[2 * e + 1] -= __uint_as_float(hi);
-    }
+// The upper halves of a pair of fp32 values as packed bf16; what they leave stays behind, exactly.
+__device__ __forceinline__ uint32_t cut(f2& x) {
+    const float2 v = unpack2(x);
+    const uint32_t lo = __float_as_uint(v.x), hi = __float_as_uint(v.y);
+    x = add2(x, pack2(-__uint_as_float(lo & 0xffff0000u), -__uint_as_float(hi & 0xffff0000u)));
+    return __byte_perm(lo, hi, 0x7632);
 }
 
 struct LinearMaps { CUtensorMap a[kLinearWalks], b[kLinearWalks], c[kLinearWalks], out[kLinearWalks]; };
@@ -79,7 +76,7 @@ __global__ void __launch_bounds__(kTcThreads, 1) k_linear_tc(const __grid_consta
         for (int i = 0; i < kRing; ++i) mbar_init(&bar_full[i], 1);
         for (int i = 0; i < 2; ++i) { mbar_init(&bar_kv[i], 1); mbar_init(&bar_af[i], 4); }
         for (int i = 0; i < kParts; ++i) { mbar_init(&bar_kq[i], 1); mbar_init(&bar_k[i], 4); }
-        mbar_init(&bar_s, 1); mbar_init(&bar_o2, 1); mbar_init(&bar_o, 1); mbar_init(&bar_p, 4); mbar_init(&bar_os, 4); mbar_init(&bar_of, 4);
+        mbar_init(&bar_s, 1); mbar_init(&bar_o2, 1); mbar_init(&bar_o, 1); mbar_init(&bar_p, 4); mbar_init(&bar_os, 8); mbar_init(&bar_of, 4);
         mbar_init(&bar_h, 8); mbar_init(&bar_kr, 8);
         mbar_init(&bar_end, 1);
         mbar_init_fence();
@@ -117,23 +114,27 @@ __global__ void __launch_bounds__(kTcThreads, 1) k_linear_tc(const __grid_consta
         }
         const unsigned char* tile = slot(n * kPer + kC);
         const uint32_t to = tmem_addr(tPlanes, lanes, (i & 1) * 3 * L::kPlane);
-#pragma unroll 1
-        for (int half = 0; half < (DC == 128 ? 2 : 1); ++half) {                      // 64 rows: 16 to each of a warpgroup's four warps
+        constexpr int kHalves = DC == 128 ? 2 : 1;                                    // 64 rows: 16 to each of a warpgroup's four warps
+        uint32_t raw[kHalves][8];
+#pragma unroll
+        for (int half = 0; half < kHalves; ++half) {
             const int col = (DC == 128 ? 32 * wq + 16 * half : 16 * wq) + ((lane >> 3) & 1) * 8;
-            uint32_t raw[8];
 #pragma unroll
             for (int k = 0; k < 2; ++k)
-                ldsm4<true>(tile + (col >> 6) * kTokens * 128 + sw128_chunk(q * kPart + 16 * k + (lane >> 4) * 8 + (lane & 7), (col >> 3) & 7), raw + 4 * k);
-            float x[16];
+                ldsm4<true>(tile + (col >> 6) * kTokens * 128 + sw128_chunk(q * kPart + 16 * k + (lane >> 4) * 8 + (lane & 7), (col >> 3) & 7),
+                            raw[half] + 4 * k);
+        }
 #pragma unroll
-            for (int k = 0; k < 8; ++k) {
-                x[2 * k] = kappa[k & ~1] * __uint_as_float(raw[k] << 16);
-                x[2 * k + 1] = kappa[k | 1] * __uint_as_float(raw[k] & 0xffff0000u);
-            }
+        for (int half = 0; half < kHalves; ++half) {
+            f2 x[8];
+#pragma unroll
+            for (int k = 0; k < 8; ++k)
+                x[k] = mul2(pack2(kappa[k & ~1], kappa[k | 1]), pack2(__uint_as_float(raw[half][k] << 16), __uint_as_float(raw[half][k] & 0xffff0000u)));
 #pragma unroll
             for (int m = 0; m < 3; ++m) {                                             // cut to 8 bits, three times: nothing is left of 24
                 uint32_t r[8];
-                cut<8>(x, r);
+#pragma unroll
+                for (int k = 0; k < 8; ++k) r[k] = cut(x[k]);
                 tmem_st_frag4(tmem_addr(to, 16 * half, m * L::kPlane), r);
             }
         }
@@ -202,33 +203,18 @@ __global__ void __launch_bounds__(kTcThreads, 1) k_linear_tc(const __grid_consta
                 arrive(&bar_p);
                 continue;
             }
-            const float rho = r >= live ? 0.f : reverse ? decay_power(g2, live - 1 - r) : p.scale * decay_power(g2, r + 1);
-            if (!all(wait(&bar_o2, n & 1))) break;
-            tc_fence_after();
-#pragma unroll 1
-            for (int j = 0; j < DC / 32; ++j) {
-                float x[32];
-                tmem_ld32(tmem_addr(tO, lanes, 32 * j), x);
-                tmem_ld_wait();
-#pragma unroll
-                for (int e = 0; e < 32; ++e) x[e] *= rho;
-#pragma unroll
-                for (int e = 0; e < 32; e += 8) tmem_st8(tmem_addr(tO, lanes, 32 * j + e), reinterpret_cast<const uint32_t*>(x + e));
-            }
-            tmem_st_wait();
-            tc_fence_before();
-            arrive(&bar_os);
             if (!all(wait(&bar_o, n & 1))) break;
             tc_fence_after();
             unsigned char* stage = slot(n * kPer + kA);
-#pragma unroll 1
-            for (int j = 0; j < DC / 32; ++j) {
-                float x[32];
-                tmem_ld32(tmem_addr(tO, lanes, 32 * j), x);
-                tmem_ld_wait();
+            float x[2][16];                                        // the next columns come while these are written
+            tmem_ld16(tmem_addr(tO, lanes, 0), x[0]);
 #pragma unroll
-                for (int ch = 0; ch < 4; ++ch)
-                    sts128(stage + (j >> 1) * kTokens * 128 + sw128_chunk(r, (j & 1) * 4 + ch), pack8(x + 8 * ch));
+            for (int j = 0; j < DC / 16; ++j) {
+                tmem_ld_wait();
+                if (j + 1 < DC / 16) tmem_ld16(tmem_addr(tO, lanes, 16 * j + 16), x[(j + 1) & 1]);
+#pragma unroll
+                for (int ch = 0; ch < 2; ++ch)
+                    sts128(stage + (j >> 2) * kTokens * 128 + sw128_chunk(r, (j & 3) * 2 + ch), pack8(x[j & 1] + 8 * ch));
             }
             tc_fence_before();
             arrive(&bar_of);
@@ -275,9 +261,29 @@ __global__ void __launch_bounds__(kTcThreads, 1) k_linear_tc(const __grid_consta
         };
         put();
         for (int n = 0; n < chunks; ++n) {
+            const int live = min(kTokens, end - token0(n)), row = (int)lanes + lane;
+            if (!ENDS) {                                           // a S times rho, half of the columns to a warpgroup
+                const float rho = row >= live ? 0.f : reverse ? decay_power(g2, live - 1 - row) : p.scale * decay_power(g2, row + 1);
+                if (!all(wait(&bar_o2, n & 1))) break;
+                tc_fence_after();
+#pragma unroll
+                for (int j = 0; j < DC / 32; ++j) {
+                    const uint32_t at = tmem_addr(tO, lanes, (warp - 8) / 4 * (DC / 2) + 16 * j);
+                    float v[16];
+                    tmem_ld16(at, v);
+                    tmem_ld_wait();
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) v[e] *= rho;
+                    tmem_st8(at, reinterpret_cast<const uint32_t*>(v));
+                    tmem_st8(at + 8, reinterpret_cast<const uint32_t*>(v + 8));
+                }
+                tmem_st_wait();
+                tc_fence_before();
+                arrive(&bar_os);
+            }
             if (!all(wait(&bar_kv[n & 1], (n >> 1) & 1))) break;
             tc_fence_after();
-            const float keep = decay_power(g2, min(kTokens, end - token0(n)));
+            const float keep = decay_power(g2, live);
 #pragma unroll
             for (int j = 0; j < HC / 16; ++j) {
                 float v[16];

@@ -34,12 +34,20 @@ static std::string one(const std::string& name, const emu::Scenario& s, int i) {
 """
 
 
+# the packed arithmetic that the kernel takes from rows.cuh
+ROWS = """
+namespace qd { typedef unsigned long long f2; inline f2 pack2(float, float) { return 0; } inline float2 unpack2(f2) { return {0.f, 0.f}; }
+inline f2 mul2(f2, f2) { return 0; } inline f2 add2(f2, f2) { return 0; } }
+inline unsigned __byte_perm(unsigned, unsigned, unsigned) { return 0; }
+"""
+
+
 def _source():
     read = lambda n: open(os.path.join(cp.CSRC, n)).read()  # noqa: E731
     src = read("linear_tc.cu")
     src = src[:src.index("\ntemplate <int DB, int DC, bool ENDS>\ncudaError_t launch")] + "\n}\n}\n"
     head = re.sub(r'#include "sm100\.cuh"|#pragma once', "", read("linear.cuh"))
-    src = src.replace('#include "linear.cuh"', head).replace("extern __shared__ unsigned char smem_raw[];", "unsigned char* const smem_raw = emu::smem;")
+    src = src.replace('#include "rows.cuh"', ROWS).replace('#include "linear.cuh"', head).replace("extern __shared__ unsigned char smem_raw[];", "unsigned char* const smem_raw = emu::smem;")
     src = src.replace("__shared__ ", "static ").replace("__grid_constant__ ", "")
     src = re.sub(r"__launch_bounds__\([^)]*\)", "", src)
     assert "asm " not in src
