@@ -8,10 +8,10 @@
 // a chunk of 128 x 128 with 128 CTAs; the products of a chunk are 3072 cycles.  Next to that it is shared memory, 128 bytes a cycle, which
 // a product of 128 x 128 with both operands there takes all of; so P and the planes are operands in tensor memory (the planes of 32 tokens at a
 // time through two places, c read transposed from its tile), and the parts of out, a S and P c, share one accumulator, scaled in between: 7000
-// cycles a chunk with the planes in shared memory and two accumulators.  Six tile buffers, two chunks deep: b, a, c of each; out leaves
+// cycles a chunk with the planes in shared memory and two accumulators.  Six tile buffers, two chunks deep: b, c, a of each; out leaves
 // through a's.
-//   warps 0-3    planes of the first 64 tokens; P: row r = lane, from tensor memory and back to it
-//   warps 4-7    planes of the others; out: 32 rows each, staged in a's tile, stored by TMA
+//   warps 0-7    two warpgroups, alike: planes, every second part; P, half of the columns, from tensor memory and back to it; out, half of the
+//                columns, staged in a's tile, stored by TMA
 //   warps 8-15   state, transposed: a column of S to a lane, half of the rows to a warpgroup; a S times rho
 //   warp 16      issues the products;  warp 17  loads
 // All waits are bounded; on expiry the status word says so, everybody leaves, what is in flight is waited for.
@@ -37,7 +37,7 @@ struct LinearMaps { CUtensorMap a[kLinearWalks], b[kLinearWalks], c[kLinearWalks
 template <int DB, int DC, bool ENDS>
 struct TcLinear {
     static constexpr int kSlot = kTokens * (DB > DC ? DB : DC) * 2;
-    static constexpr int kPer = ENDS ? 2 : 3;                         // tiles of a chunk: b, a, c
+    static constexpr int kPer = ENDS ? 2 : 3;                         // tiles of a chunk: b, c, a
     static constexpr int kRing = 2 * kPer;                            // two chunks: barriers of chunks n and n + 2 are the same
     static constexpr int kState = ENDS ? 0 : DB * DC * 2;
     static constexpr int kSmem = kState + kRing * kSlot + 1024;
@@ -47,17 +47,22 @@ struct TcLinear {
     static_assert(kSmem <= 232448 - 1024, "shared memory");
 };
 
+// What follows a first poll without success, once for all waits: written out at each of them it is a third of the kernel's instructions.
+__device__ __noinline__ bool wait_longer(uint64_t* bar, uint32_t parity, volatile int* s_abort, unsigned* status) {
+    return wait_on(bar, parity, *s_abort, status);
+}
+
 template <int DB, int DC, bool ENDS>
 __global__ void __launch_bounds__(kTcThreads, 1) k_linear_tc(const __grid_constant__ LinearMaps maps, const LinearP p) {
     typedef TcLinear<DB, DC, ENDS> L;
-    constexpr int kRing = L::kRing, kPer = L::kPer, kA = 1, kC = kPer - 1;
+    constexpr int kRing = L::kRing, kPer = L::kPer, kA = 2, kC = 1;
     extern __shared__ unsigned char smem_raw[];
     unsigned char* smem = (unsigned char*)(((uintptr_t)smem_raw + 1023) & ~(uintptr_t)1023);
     unsigned char *sState = smem, *sRing = smem + L::kState;
-    // bar_s, bar_o2, bar_o, bar_kq, bar_kv: products complete (scores, a S, out, a part's and all of a chunk's sum); bar_p, bar_os, bar_k,
+    // bar_s, bar_o2, bar_o, bar_kq, bar_kv: products complete (scores, a S, out twice, a part's and all of a chunk's sum); bar_p, bar_os, bar_k,
     // bar_h: operands in place; bar_of, bar_kr: out's and the sum's accumulator have been read; bar_af: a's tile is free.  Where one side
     // runs up to two phases ahead there is one for even and one for odd phases.
-    __shared__ uint64_t bar_full[kRing], bar_s, bar_o2, bar_o, bar_kv[2], bar_kq[kParts], bar_p, bar_os, bar_k[kParts], bar_h, bar_of, bar_kr, bar_af[2], bar_end;
+    __shared__ uint64_t bar_full[kRing], bar_s, bar_o2, bar_o, bar_c[2], bar_kv[2], bar_kq[kParts], bar_p, bar_os, bar_k[kParts], bar_h, bar_of, bar_kr, bar_af[2], bar_end;
     __shared__ uint32_t tmem_slot;
     __shared__ volatile int s_abort;
     __shared__ float s_d[2 * kTokens];                                    // D(|m|), m from -128
@@ -74,9 +79,9 @@ __global__ void __launch_bounds__(kTcThreads, 1) k_linear_tc(const __grid_consta
 
     if (tid == 0) {
         for (int i = 0; i < kRing; ++i) mbar_init(&bar_full[i], 1);
-        for (int i = 0; i < 2; ++i) { mbar_init(&bar_kv[i], 1); mbar_init(&bar_af[i], 4); }
+        for (int i = 0; i < 2; ++i) { mbar_init(&bar_kv[i], 1); mbar_init(&bar_c[i], 1); mbar_init(&bar_af[i], DC == 128 ? 8 : 4); }
         for (int i = 0; i < kParts; ++i) { mbar_init(&bar_kq[i], 1); mbar_init(&bar_k[i], 4); }
-        mbar_init(&bar_s, 1); mbar_init(&bar_o2, 1); mbar_init(&bar_o, 1); mbar_init(&bar_p, 4); mbar_init(&bar_os, 8); mbar_init(&bar_of, 4);
+        mbar_init(&bar_s, 1); mbar_init(&bar_o2, 1); mbar_init(&bar_o, 1); mbar_init(&bar_p, 8); mbar_init(&bar_os, 8); mbar_init(&bar_of, DC == 128 ? 8 : 4);
         mbar_init(&bar_h, 8); mbar_init(&bar_kr, 8);
         mbar_init(&bar_end, 1);
         mbar_init_fence();
@@ -96,7 +101,7 @@ __global__ void __launch_bounds__(kTcThreads, 1) k_linear_tc(const __grid_consta
     const uint32_t tS = tb, tO = tb + L::kOut, tKV = tb + L::kSum, tPlanes = tb + L::kPlanes;
     const uint32_t lanes = (uint32_t)wq * 32;
 
-    auto wait = [&](uint64_t* bar, uint32_t parity) { return mbar_try_wait(bar, parity) || wait_on(bar, parity, s_abort, p.status); };
+    auto wait = [&](uint64_t* bar, uint32_t parity) { return mbar_try_wait(bar, parity) || wait_longer(bar, parity, &s_abort, p.status); };
     auto all = [&](bool ok) { return __all_sync(0xffffffffu, ok) != 0; };
     auto arrive = [&](uint64_t* bar) { __syncwarp(); if (lane == 0) mbar_arrive(bar); };
     auto slot = [&](int m) { return sRing + m % kRing * L::kSlot; };
@@ -148,32 +153,53 @@ __global__ void __launch_bounds__(kTcThreads, 1) k_linear_tc(const __grid_consta
     if (ENDS && segment == (reverse ? 0 : p.segments - 1)) {
         // nobody begins with the sums of this one
     } else if (warp < 8) {
-        // ---------------------------------- planes, then weights or output ----------------------------------
+        // ---------------------------------- planes, weights and output ----------------------------------
+        // Two warpgroups, alike: of the parts, of the weights' columns and of out's each takes every second, or half.
         // One copy of every piece of code, and loops as loops: what all warps go through in a chunk has to fit the instruction cache
-        // (planes and weights written out: 12000 cycles a chunk for 4500).
-        const int r = (int)lanes + lane;
+        // (planes and weights written out: 12000 cycles a chunk).
+        const int r = (int)lanes + lane, group = warp >> 2;
         const float* far = s_d + kTokens + r;
+        constexpr bool kSplit = DC == 128;                         // else the second group has all of out: 64 columns are one box
         int stored = -1;                                           // chunk whose output this thread has stored and not seen read
-        for (int n = 0; n < chunks; ++n) {
-            const int t0 = token0(n), live = min(kTokens, end - t0);
-            bool ok = all(full(n * kPer + kC));
-#pragma unroll 1
-            for (int k = 0; k < kParts / 2 && ok; ++k) {
-                ok = planes(n, (warp < 4 ? 0 : kParts / 2) + k);
-                if (stored >= 0) {                                 // the output of the chunk before has been read by now: its tile is free
-                    tma_store_wait_read();
-                    mbar_arrive(&bar_af[stored & 1]);
-                    stored = -1;
-                }
-                __syncwarp();
+        auto output = [&](int n) {
+            if (!kSplit && group == 0) return true;
+            if (!all(wait(&bar_o, n & 1))) return false;
+            tc_fence_after();
+            unsigned char* stage = slot(n * kPer + kA) + (kSplit ? group * kTokens * 128 : 0);
+            const uint32_t from = tmem_addr(tO, lanes, kSplit ? 64 * group : 0);
+            float x[2][16];                                        // the next columns come while these are written
+            tmem_ld16(from, x[0]);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                tmem_ld_wait();
+                if (j < 3) tmem_ld16(from + 16 * j + 16, x[(j + 1) & 1]);
+#pragma unroll
+                for (int ch = 0; ch < 2; ++ch) sts128(stage + sw128_chunk(r, 2 * j + ch), pack8(x[j & 1] + 8 * ch));
             }
-            if (!ok) break;
-            if (ENDS) continue;
-            if (warp < 4) {
+            tc_fence_before();
+            arrive(&bar_of);
+            fence_proxy_async();
+            __syncwarp();
+            if (lane == 0) {
+                const int t0 = token0(n) + (int)lanes;
+                if (t0 < p.T) {                                    // rows past the end of the sequence are skipped
+                    tma_store_3d(&maps.out[walk], stage + lanes * 128, hh * DC + (kSplit ? 64 * group : 0), t0, b);
+                    tma_store_commit();
+                }
+                stored = n;
+            }
+            __syncwarp();
+            return true;
+        };
+        int n = 0;
+        for (; n < chunks; ++n) {
+            if (!all(full(n * kPer + kC)) || !planes(n, group)) break;
+            if (!ENDS) {
+                if (n > 0 && !output(n - 1)) break;
                 if (!all(wait(&bar_s, n & 1))) break;
                 tc_fence_after();
 #pragma unroll 1
-                for (int j = 0; j < 4; ++j) {                      // 32 columns i, which become 16 packed ones in the place of what has been read
+                for (int j = 2 * group; j < 2 * group + 2; ++j) {  // 32 columns i, which become 16 packed ones in the place of what has been read
                     uint32_t o[16];
 #pragma unroll
                     for (int e = 0; e < 16; ++e) o[e] = 0;
@@ -195,43 +221,23 @@ __global__ void __launch_bounds__(kTcThreads, 1) k_linear_tc(const __grid_consta
 #pragma unroll
                         for (int e = 0; e < 16; ++e) o[e] = pack_bf16(v[2 * e], v[2 * e + 1]);
                     }
-                    tmem_st8(tmem_addr(tS, lanes, 16 * j), o);
-                    tmem_st8(tmem_addr(tS, lanes, 16 * j + 8), o + 8);
+                    tmem_st8(tmem_addr(tS, lanes, 32 * group + 16 * j), o);
+                    tmem_st8(tmem_addr(tS, lanes, 32 * group + 16 * j + 8), o + 8);
                 }
                 tmem_st_wait();
                 tc_fence_before();
                 arrive(&bar_p);
-                continue;
-            }
-            if (!all(wait(&bar_o, n & 1))) break;
-            tc_fence_after();
-            unsigned char* stage = slot(n * kPer + kA);
-            float x[2][16];                                        // the next columns come while these are written
-            tmem_ld16(tmem_addr(tO, lanes, 0), x[0]);
-#pragma unroll
-            for (int j = 0; j < DC / 16; ++j) {
-                tmem_ld_wait();
-                if (j + 1 < DC / 16) tmem_ld16(tmem_addr(tO, lanes, 16 * j + 16), x[(j + 1) & 1]);
-#pragma unroll
-                for (int ch = 0; ch < 2; ++ch)
-                    sts128(stage + (j >> 2) * kTokens * 128 + sw128_chunk(r, (j & 3) * 2 + ch), pack8(x[j & 1] + 8 * ch));
-            }
-            tc_fence_before();
-            arrive(&bar_of);
-            fence_proxy_async();
-            __syncwarp();
-            if (lane == 0) {
-                if (t0 + (int)lanes < p.T) {                       // rows past the end of the sequence are skipped
-#pragma unroll
-                    for (int blk = 0; blk < DC / 64; ++blk)
-                        tma_store_3d(&maps.out[walk], stage + blk * kTokens * 128 + lanes * 128, hh * DC + blk * 64, t0 + (int)lanes, b);
-                    tma_store_commit();
+                if (stored >= 0) {                                 // the output of the chunk before has been read by now: its tile is free
+                    tma_store_wait_read();
+                    mbar_arrive(&bar_af[stored & 1]);
+                    stored = -1;
                 }
-                stored = n;
+                __syncwarp();
             }
-            __syncwarp();
+            if (!planes(n, kParts / 2 + group)) break;
         }
-        if (warp >= 4 && lane == 0) tma_store_wait_all();
+        if (!ENDS && n == chunks) output(n - 1);
+        if (lane == 0) tma_store_wait_all();
     } else if (warp < 16) {
         // ---------------------------------- state ----------------------------------
         constexpr int HC = DB / 2, size = DB * DC;
@@ -266,7 +272,7 @@ __global__ void __launch_bounds__(kTcThreads, 1) k_linear_tc(const __grid_consta
                 const float rho = row >= live ? 0.f : reverse ? decay_power(g2, live - 1 - row) : p.scale * decay_power(g2, row + 1);
                 if (!all(wait(&bar_o2, n & 1))) break;
                 tc_fence_after();
-#pragma unroll
+#pragma unroll 1
                 for (int j = 0; j < DC / 32; ++j) {
                     const uint32_t at = tmem_addr(tO, lanes, (warp - 8) / 4 * (DC / 2) + 16 * j);
                     float v[16];
@@ -349,8 +355,11 @@ __global__ void __launch_bounds__(kTcThreads, 1) k_linear_tc(const __grid_consta
                 if (!ENDS) {
                     if (!all(wait(&bar_p, n & 1)) || !all(wait(&bar_os, n & 1))) break;
                     tc_fence_after();
-                    umma_product_ts_w<true>(tO, tS, tile(n * kPer + kC), blk, DC, kTokens, true, issue);
+#pragma unroll
+                    for (int g = 0; g < 2; ++g)                    // of either warpgroup
+                        umma_product_ts_w<true>(tO, tS + 64 * g, tile(n * kPer + kC) + g * kTokens * 64, blk, DC, kTokens / 2, true, issue);
                     umma_commit_w(&bar_o, issue);
+                    umma_commit_w(&bar_c[n & 1], issue);
                 }
                 if (n + 1 < chunks && !scores(n + 1)) break;
             }
@@ -369,9 +378,8 @@ __global__ void __launch_bounds__(kTcThreads, 1) k_linear_tc(const __grid_consta
         for (int m = 0; m < tiles; ++m, ++loads) {
             if (m + kAhead < tiles) each_box(m + kAhead, [&](const CUtensorMap* map, int, int x, int t0) { tma_prefetch_3d(map, x, t0, b); });
             if (m >= kRing) {
-                // out has left after all products that read c; those of the sum are the last to read b
                 const int on = m / kPer - 2, j = m % kPer;
-                if (!(ENDS || j == 0 ? wait(&bar_kv[on & 1], (on >> 1) & 1) : wait(&bar_af[on & 1], (on >> 1) & 1))) break;
+                if (!wait(ENDS || j == 0 ? &bar_kv[on & 1] : j == kC ? &bar_c[on & 1] : &bar_af[on & 1], (on >> 1) & 1)) break;
             }
             uint64_t* bar = &bar_full[m % kRing];
             mbar_expect_tx(bar, kTokens * (m % kPer == kC ? DC : DB) * 2);

@@ -48,7 +48,7 @@ def _source():
     src = src[:src.index("\ntemplate <int DB, int DC, bool ENDS>\ncudaError_t launch")] + "\n}\n}\n"
     head = re.sub(r'#include "sm100\.cuh"|#pragma once', "", read("linear.cuh"))
     src = src.replace('#include "rows.cuh"', ROWS).replace('#include "linear.cuh"', head).replace("extern __shared__ unsigned char smem_raw[];", "unsigned char* const smem_raw = emu::smem;")
-    src = src.replace("__shared__ ", "static ").replace("__grid_constant__ ", "")
+    src = src.replace("__shared__ ", "static ").replace("__grid_constant__ ", "").replace("__noinline__ ", "")
     src = re.sub(r"__launch_bounds__\([^)]*\)", "", src)
     assert "asm " not in src
     return '#include "cta_emulation.h"\ntypedef __nv_bfloat16 bf16;\n' + src
