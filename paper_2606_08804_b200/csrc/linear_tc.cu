@@ -47,11 +47,6 @@ struct TcLinear {
     static_assert(kSmem <= 232448 - 1024, "shared memory");
 };
 
-// What follows a first poll without success, once for all waits: written out at each of them it is a third of the kernel's instructions.
-__device__ __noinline__ bool wait_longer(uint64_t* bar, uint32_t parity, volatile int* s_abort, unsigned* status) {
-    return wait_on(bar, parity, *s_abort, status);
-}
-
 template <int DB, int DC, bool ENDS>
 __global__ void __launch_bounds__(kTcThreads, 1) k_linear_tc(const __grid_constant__ LinearMaps maps, const LinearP p) {
     typedef TcLinear<DB, DC, ENDS> L;
@@ -101,7 +96,7 @@ __global__ void __launch_bounds__(kTcThreads, 1) k_linear_tc(const __grid_consta
     const uint32_t tS = tb, tO = tb + L::kOut, tKV = tb + L::kSum, tPlanes = tb + L::kPlanes;
     const uint32_t lanes = (uint32_t)wq * 32;
 
-    auto wait = [&](uint64_t* bar, uint32_t parity) { return mbar_try_wait(bar, parity) || wait_longer(bar, parity, &s_abort, p.status); };
+    auto wait = [&](uint64_t* bar, uint32_t parity) { return mbar_try_wait(bar, parity) || wait_on(bar, parity, s_abort, p.status); };
     auto all = [&](bool ok) { return __all_sync(0xffffffffu, ok) != 0; };
     auto arrive = [&](uint64_t* bar) { __syncwarp(); if (lane == 0) mbar_arrive(bar); };
     auto slot = [&](int m) { return sRing + m % kRing * L::kSlot; };
@@ -120,21 +115,18 @@ __global__ void __launch_bounds__(kTcThreads, 1) k_linear_tc(const __grid_consta
         const unsigned char* tile = slot(n * kPer + kC);
         const uint32_t to = tmem_addr(tPlanes, lanes, (i & 1) * 3 * L::kPlane);
         constexpr int kHalves = DC == 128 ? 2 : 1;                                    // 64 rows: 16 to each of a warpgroup's four warps
-        uint32_t raw[kHalves][8];
-#pragma unroll
+#pragma unroll 1
         for (int half = 0; half < kHalves; ++half) {
+            uint32_t raw[8];
             const int col = (DC == 128 ? 32 * wq + 16 * half : 16 * wq) + ((lane >> 3) & 1) * 8;
 #pragma unroll
             for (int k = 0; k < 2; ++k)
                 ldsm4<true>(tile + (col >> 6) * kTokens * 128 + sw128_chunk(q * kPart + 16 * k + (lane >> 4) * 8 + (lane & 7), (col >> 3) & 7),
-                            raw[half] + 4 * k);
-        }
-#pragma unroll
-        for (int half = 0; half < kHalves; ++half) {
+                            raw + 4 * k);
             f2 x[8];
 #pragma unroll
             for (int k = 0; k < 8; ++k)
-                x[k] = mul2(pack2(kappa[k & ~1], kappa[k | 1]), pack2(__uint_as_float(raw[half][k] << 16), __uint_as_float(raw[half][k] & 0xffff0000u)));
+                x[k] = mul2(pack2(kappa[k & ~1], kappa[k | 1]), pack2(__uint_as_float(raw[k] << 16), __uint_as_float(raw[k] & 0xffff0000u)));
 #pragma unroll
             for (int m = 0; m < 3; ++m) {                                             // cut to 8 bits, three times: nothing is left of 24
                 uint32_t r[8];
@@ -191,52 +183,56 @@ __global__ void __launch_bounds__(kTcThreads, 1) k_linear_tc(const __grid_consta
             __syncwarp();
             return true;
         };
-        int n = 0;
-        for (; n < chunks; ++n) {
-            if (!all(full(n * kPer + kC)) || !planes(n, group)) break;
-            if (!ENDS) {
-                if (n > 0 && !output(n - 1)) break;
-                if (!all(wait(&bar_s, n & 1))) break;
-                tc_fence_after();
+        auto weights = [&](int n) {
+            if (!all(wait(&bar_s, n & 1))) return false;
+            tc_fence_after();
 #pragma unroll 1
-                for (int j = 2 * group; j < 2 * group + 2; ++j) {  // 32 columns i, which become 16 packed ones in the place of what has been read
-                    uint32_t o[16];
+            for (int j = 2 * group; j < 2 * group + 2; ++j) {      // 32 columns i, which become 16 packed ones in the place of what has been read
+                uint32_t o[16];
 #pragma unroll
-                    for (int e = 0; e < 16; ++e) o[e] = 0;
-                    if (reverse ? j >= wq : j <= wq) {
-                        float v[32];
-                        tmem_ld32(tmem_addr(tS, lanes, 32 * j), v);
-                        tmem_ld_wait();
-                        if (j == wq) {                             // an infinite product past the diagonal leaves nothing either
+                for (int e = 0; e < 16; ++e) o[e] = 0;
+                if (reverse ? j >= wq : j <= wq) {
+                    float v[32];
+                    tmem_ld32(tmem_addr(tS, lanes, 32 * j), v);
+                    tmem_ld_wait();
+                    if (j == wq) {                                 // an infinite product past the diagonal leaves nothing either
 #pragma unroll
-                            for (int e = 0; e < 32; ++e) v[e] = (reverse ? e >= lane : e <= lane) ? v[e] * far[-32 * j - e] : 0.f;
-                        } else {
-                            const float near = far[reverse ? -32 * j : -32 * j - 31];
+                        for (int e = 0; e < 32; ++e) v[e] = (reverse ? e >= lane : e <= lane) ? v[e] * far[-32 * j - e] : 0.f;
+                    } else {
+                        const float near = far[reverse ? -32 * j : -32 * j - 31];
 #pragma unroll
-                            for (int e = 0; e < 32; e += 4) {
-                                const float4 t = *reinterpret_cast<const float4*>(s_e + e);
-                                v[e] *= near * t.x; v[e + 1] *= near * t.y; v[e + 2] *= near * t.z; v[e + 3] *= near * t.w;
-                            }
+                        for (int e = 0; e < 32; e += 4) {
+                            const float4 t = *reinterpret_cast<const float4*>(s_e + e);
+                            v[e] *= near * t.x; v[e + 1] *= near * t.y; v[e + 2] *= near * t.z; v[e + 3] *= near * t.w;
                         }
-#pragma unroll
-                        for (int e = 0; e < 16; ++e) o[e] = pack_bf16(v[2 * e], v[2 * e + 1]);
                     }
-                    tmem_st8(tmem_addr(tS, lanes, 32 * group + 16 * j), o);
-                    tmem_st8(tmem_addr(tS, lanes, 32 * group + 16 * j + 8), o + 8);
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) o[e] = pack_bf16(v[2 * e], v[2 * e + 1]);
                 }
-                tmem_st_wait();
-                tc_fence_before();
-                arrive(&bar_p);
-                if (stored >= 0) {                                 // the output of the chunk before has been read by now: its tile is free
-                    tma_store_wait_read();
-                    mbar_arrive(&bar_af[stored & 1]);
-                    stored = -1;
-                }
-                __syncwarp();
+                tmem_st8(tmem_addr(tS, lanes, 32 * group + 16 * j), o);
+                tmem_st8(tmem_addr(tS, lanes, 32 * group + 16 * j + 8), o + 8);
             }
-            if (!planes(n, kParts / 2 + group)) break;
+            tmem_st_wait();
+            tc_fence_before();
+            arrive(&bar_p);
+            if (stored >= 0) {                                     // the output of the chunk before has been read by now: its tile is free
+                tma_store_wait_read();
+                mbar_arrive(&bar_af[stored & 1]);
+                stored = -1;
+            }
+            __syncwarp();
+            return true;
+        };
+        bool ok = true;
+#pragma unroll 1
+        for (int i = 0; i <= 2 * chunks && ok; ++i) {              // half chunks, and the last chunk's output
+            const int n = i >> 1;
+            if (n < chunks) ok = all(full(n * kPer + kC)) && planes(n, (i & 1) * 2 + group);
+            if (!ENDS && ok && !(i & 1)) {
+                if (n > 0) ok = output(n - 1);
+                if (n < chunks) ok = ok && weights(n);
+            }
         }
-        if (!ENDS && n == chunks) output(n - 1);
         if (lane == 0) tma_store_wait_all();
     } else if (warp < 16) {
         // ---------------------------------- state ----------------------------------
@@ -342,15 +338,18 @@ __global__ void __launch_bounds__(kTcThreads, 1) k_linear_tc(const __grid_consta
             for (int n = 0; n < chunks; ++n) {
                 if (n > 0 && !all(wait(&bar_kr, (n - 1) & 1))) break;
                 tc_fence_after();
-                bool ok = part(n, 0) && part(n, 1);
-                if (!ok) break;
-                if (!ENDS) {
-                    if (!all(wait(&bar_h, n & 1)) || (n > 0 && !all(wait(&bar_of, (n - 1) & 1)))) break;
+                bool ok = true;
+#pragma unroll 1
+                for (int q = 0; q < kParts && ok; ++q) {
+                    ok = part(n, q);
+                    if (ENDS || q != 1 || !ok) continue;
+                    ok = all(wait(&bar_h, n & 1)) && (n == 0 || all(wait(&bar_of, (n - 1) & 1)));
+                    if (!ok) break;
                     tc_fence_after();
                     umma_product_w<false, false>(tO, tile(n * kPer + kA), blk, aState, DC * 128, DC, DB, false, issue);
                     umma_commit_w(&bar_o2, issue);
                 }
-                if (!part(n, 2) || !part(n, 3)) break;
+                if (!ok) break;
                 umma_commit_w(&bar_kv[n & 1], issue);
                 if (!ENDS) {
                     if (!all(wait(&bar_p, n & 1)) || !all(wait(&bar_os, n & 1))) break;
