@@ -372,10 +372,7 @@ __global__ void __launch_bounds__(kTcThreads, 1) k_linear_tc(const __grid_consta
             const CUtensorMap* map = j == 0 ? &maps.b[walk] : j == kC ? &maps.c[walk] : &maps.a[walk];
             for (int blk = 0; blk < width / 64; ++blk) f(map, blk, hh * width + blk * 64, token0(m / kPer));
         };
-        // what no buffer is free for yet comes to L2 ahead of that
-        constexpr int kAhead = kRing;
         for (int m = 0; m < tiles; ++m, ++loads) {
-            if (m + kAhead < tiles) each_box(m + kAhead, [&](const CUtensorMap* map, int, int x, int t0) { tma_prefetch_3d(map, x, t0, b); });
             if (m >= kRing) {
                 const int on = m / kPer - 2, j = m % kPer;
                 if (!wait(ENDS || j == 0 ? &bar_kv[on & 1] : j == kC ? &bar_c[on & 1] : &bar_af[on & 1], (on >> 1) & 1)) break;
@@ -383,6 +380,9 @@ __global__ void __launch_bounds__(kTcThreads, 1) k_linear_tc(const __grid_consta
             uint64_t* bar = &bar_full[m % kRing];
             mbar_expect_tx(bar, kTokens * (m % kPer == kC ? DC : DB) * 2);
             each_box(m, [&](const CUtensorMap* map, int blk, int x, int t0) { tma_load_3d(slot(m) + blk * kTokens * 128, map, x, t0, b, bar); });
+            // what no buffer is free for yet comes to L2, once the first chunks are on their way (all of them at once: 6 us to the first product)
+            if (m >= kPer && m + kRing < tiles)
+                each_box(m + kRing, [&](const CUtensorMap* map, int, int x, int t0) { tma_prefetch_3d(map, x, t0, b); });
         }
     }
     __syncwarp();
