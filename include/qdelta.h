@@ -297,7 +297,8 @@ int qdelta_gated_norm_fwd(long long rows, int width, int dtype, const void *x, c
 /* of the backward of gated norm and of add norm; 0 on an invalid shape */
 size_t qdelta_fused_norm_workspace_bytes(long long rows, int width, int dtype);
 
-/* Backward for  L = <y, dy>: dx, dgate in `dtype`, dweight, dbias [width] fp32 (NULL: skipped; without them no workspace is needed). */
+/* Backward for  L = <y, dy>: dx, dgate in `dtype`, dweight, dbias [width] fp32 (NULL: skipped; without them no workspace is needed up
+ * to a width of 1024). */
 int qdelta_gated_norm_bwd(long long rows, int width, int dtype, const void *x, const void *gate, const void *weight, const void *bias,
                           const void *dy, const float *stats, void *dx, void *dgate, float *dweight, float *dbias, void *workspace,
                           size_t workspace_bytes, unsigned flags, qd_stream stream);
@@ -311,8 +312,8 @@ int qdelta_add_norm_fwd(long long rows, int width, int dtype, const void *x, con
                         const void *bias, void *total, void *y, float *stats, float eps, unsigned flags, qd_stream stream);
 
 /* Backward for  L = <y, dy> + <total, dtotal>  (dtotal NULL: zero): dresidual and dx = scale dresidual in `dtype` (dx NULL only if scale is:
- * dresidual is it), dscale, dweight, dbias [width] fp32 (NULL: skipped).  Adds x and residual up again, in fp32: the rounded total would
- * cost the sums over rows half of their digits. */
+ * dresidual is it), dscale, dweight, dbias [width] fp32 (NULL: skipped).  Workspace as there.  Adds x and residual up again, in fp32: the
+ * rounded total would cost the sums over rows half of their digits. */
 int qdelta_add_norm_bwd(long long rows, int width, int dtype, const void *x, const void *residual, const void *scale, const void *weight,
                         const void *dy, const void *dtotal, const float *stats, void *dx, void *dresidual, float *dscale, float *dweight,
                         float *dbias, void *workspace, size_t workspace_bytes, unsigned flags, qd_stream stream);

@@ -541,7 +541,9 @@ int qdelta_gated_norm_bwd(long long rows, int width, int dtype, const void* x, c
     if (!x || !gate || !dy || !stats || !dx || !dgate || dx == dgate) return QD_ERR_INVALID_ARG;
     const void* const ptrs[] = {x, gate, weight, bias, dy, stats, dx, dgate, dweight, dbias, workspace};
     if (any_misaligned(ptrs) || (flags & ~(unsigned)(QD_RMS | QD_SILU))) return QD_ERR_INVALID_ARG;
-    if ((dweight || dbias) && (!workspace || workspace_bytes < fused_norm_workspace(rows, width, dtype))) return QD_ERR_WORKSPACE;
+    if ((dweight || dbias || fused_norm_needs_workspace(rows, width, dtype)) &&
+        (!workspace || workspace_bytes < fused_norm_workspace(rows, width, dtype)))
+        return QD_ERR_WORKSPACE;
     FusedNormArgs a{};
     a.rows = rows; a.width = width; a.dtype = dtype; a.rms = (flags & QD_RMS) != 0; a.silu = (flags & QD_SILU) != 0;
     a.x = x; a.gate = gate; a.weight = weight; a.bias = bias; a.dy = dy; a.stats = const_cast<float*>(stats);
@@ -572,7 +574,9 @@ int qdelta_add_norm_bwd(long long rows, int width, int dtype, const void* x, con
     if (!x || !residual || !dy || !stats || !dresidual || (scale && !dx) || dx == dresidual) return QD_ERR_INVALID_ARG;
     const void* const ptrs[] = {x, residual, scale, weight, dy, dtotal, stats, dx, dresidual, dscale, dweight, dbias, workspace};
     if (any_misaligned(ptrs) || (flags & ~(unsigned)QD_RMS)) return QD_ERR_INVALID_ARG;
-    if ((dscale || dweight || dbias) && (!workspace || workspace_bytes < fused_norm_workspace(rows, width, dtype))) return QD_ERR_WORKSPACE;
+    if ((dscale || dweight || dbias || fused_norm_needs_workspace(rows, width, dtype)) &&
+        (!workspace || workspace_bytes < fused_norm_workspace(rows, width, dtype)))
+        return QD_ERR_WORKSPACE;
     FusedNormArgs a{};
     a.rows = rows; a.width = width; a.dtype = dtype; a.added = true; a.rms = (flags & QD_RMS) != 0;
     a.x = x; a.residual = residual; a.scale = scale; a.weight = weight; a.dy = dy; a.dtotal = dtotal; a.stats = const_cast<float*>(stats);

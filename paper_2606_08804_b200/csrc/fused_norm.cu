@@ -7,8 +7,14 @@
 // Backward of the norm, with g = dy w and x^ = (x - m) r:  dx = r (g - x^ mean(g x^) - mean(g))  (the last term not without the mean),
 // dw = sum_rows dy x^, db = sum_rows dy.
 //
-// Bound by HBM.  Rows belong to groups of lanes or to a CTA and are read once into registers, the next one on its way, as in norm.cu;
-// backward the sums over rows stay in registers, one partial per CTA, added up in a fixed order.
+// Bound by HBM, so the plan of a row decides:
+//   k_fused_fwd, _bwd   rows of whole 16-byte groups: a row belongs to 2^k lanes or to a CTA and is in registers when its sums are taken; what
+//                       the next rows need is on its way to shared memory, where each thread reads back only what it asked for (no barrier).
+//                       CTAs stay; backward the sums over rows stay in registers, one partial per CTA, added up in a fixed order.
+//   k_odd_fwd, _bwd     rows that begin anywhere: blocks of rows come to shared memory as the aligned 16-byte pieces that they lie in, and
+//                       are read from there one element at a time, neighbouring columns to neighbouring lanes.
+//   k_wide_sums, _cols  backward of rows too wide for registers: the sums of a row first, then everything else with a thread to a column
+//                       and the rows in a loop, whose sums over rows need no more than the registers of one column.  Inputs are read twice.
 #include "rows.cuh"
 
 namespace qd {
@@ -20,16 +26,16 @@ struct FusedP {
     const void *x, *e, *scale, *weight, *bias, *dy, *dt;      // e: gate or residual
     void *y, *t, *dx, *de;
     float* stats;                                              // [2][rows]: mean, r
-    float* part;                                               // backward: [gridDim.x][sums][width]
+    float* part;                                               // backward: [parts][sums][width]
+    float* rowsum;                                             // wide backward: [2][rows]: mean(g x^), mean(g)
     float eps, inv;
+    int step;                                                  // odd rows: rows that a group of lanes takes of a block; wide: rows of a CTA
     bool rms, silu;
 };
 constexpr __host__ __device__ int fused_threads(int tpr) { return tpr > 256 ? tpr : 256; }
-constexpr __host__ __device__ int fused_resident(int k, int v, int tpr, bool bwd) {
-    return tpr > 256 ? 1 : bwd ? (k * v <= 8 ? 2 : 1) : (k * v <= 8 ? 4 : k * v <= 16 ? 2 : 1);
-}
 constexpr __host__ __device__ int fused_sums(bool added) { return added ? 3 : 2; }
 
+// sums over the TPR threads of a row, the same bits in each; as in norm.cu
 template <int TPR, int M>
 __device__ __forceinline__ void row_sum(float (&v)[M], float (*red)[M][32], int& turn) {
 #pragma unroll
@@ -51,68 +57,114 @@ __device__ __forceinline__ void row_sum(float (&v)[M], float (*red)[M][32], int&
             for (int m = 0; m < M; ++m) v[m] += __shfl_xor_sync(0xffffffffu, v[m], w);
     }
 }
-template <typename IO, int V, int K, int TPR>
-__device__ __forceinline__ void columns(const void* base, long long row, int width, bool live, Pack<IO, V> (&v)[K]) {
-    const IO* p = static_cast<const IO*>(base) + row * width;
-#pragma unroll
-    for (int k = 0; k < K; ++k) {
-        const int c = (k * TPR + threadIdx.x % TPR) * V;
-        v[k] = live && c < width ? load_pack<IO, V>(p + c, V, V > 1) : zero_pack<IO, V>();
-    }
-}
 // the gate and its slope
 __device__ __forceinline__ float gate_value(float z, bool silu) { const float s = gate_sigmoid(z); return silu ? z * s : s; }
 __device__ __forceinline__ float2 gate_slope(float z, bool silu) {
     const float s = gate_sigmoid(z);
     return silu ? make_float2(z * s, s * fmaf(z, 1.f - s, 1.f)) : make_float2(s, s * (1.f - s));
 }
+// One element backward.  `in`: x, gate or residual, dy, dtotal.  Leaves x^ and g; adds to the row's sums and, where `cols`, to dw and db.
+template <bool ADDED>
+__device__ __forceinline__ void element(const FusedP& p, const float (&in)[4], float w, float v, float mean, float r, float& xh, float& g, float& dz,
+                                        float (&s)[2], float* dw, float* db) {
+    float x = in[0], d = in[2];
+    if (ADDED) x = p.scale ? fmaf(v, x, in[1]) : x + in[1];
+    xh = (x - mean) * r;
+    if (!ADDED) {
+        const float2 f = gate_slope(in[1], p.silu);
+        dz = d * fmaf(xh, w, p.bias ? v : 0.f) * f.y;
+        d *= f.x;
+    }
+    g = d * w;
+    s[0] = fmaf(g, xh, s[0]);
+    s[1] += g;
+    if (dw) { *dw = fmaf(d, xh, *dw); *db += d; }
+}
+
+// ---- rows of whole groups -----------------------------------------------------------------------------------------------------
+// A thread's K groups of STREAMS rows, DEPTH rows ahead.
+template <typename IO, int V, int K, int TPR, int STREAMS, int DEPTH>
+struct Ahead {
+    static constexpr int NT = fused_threads(TPR), kBytes = DEPTH * STREAMS * K * NT * 16;
+    unsigned char* mine;
+    __device__ __forceinline__ explicit Ahead(unsigned char* smem) : mine(smem + threadIdx.x * 16) {}
+    __device__ __forceinline__ unsigned char* at(int stage, int stream, int k) const { return mine + ((stage * STREAMS + stream) * K + k) * (NT * 16); }
+    __device__ __forceinline__ void fetch(int stage, const void* const (&src)[STREAMS], long long row, int width, bool live) const {
+#pragma unroll
+        for (int m = 0; m < STREAMS; ++m)
+#pragma unroll
+            for (int k = 0; k < K; ++k) {
+                const int c = (k * TPR + threadIdx.x % TPR) * V;
+                const bool in = live && c < width && src[m];
+                copy_bytes<16>(at(stage, m, k), in ? static_cast<const IO*>(src[m]) + row * width + c : static_cast<const IO*>(src[0]), in ? 16 : 0);
+            }
+        copy_commit();
+    }
+    __device__ __forceinline__ Pack<IO, V> take(int stage, int stream, int k) const {
+        const uint4 u = *reinterpret_cast<const uint4*>(at(stage, stream, k));
+        Pack<IO, V> r;
+        r.w[0] = u.x; r.w[1] = u.y; r.w[2] = u.z; r.w[3] = u.w;
+        return r;
+    }
+};
+constexpr int depth_of(int k, int nt) { return k * nt > 1024 ? 1 : k * nt > 512 ? 2 : 3; }
+// CTAs to an SM that the registers are shared out for
+constexpr __host__ __device__ int fused_resident(int k, int v, int tpr, bool bwd) {
+    return tpr > 256 ? (k * v <= 16 && !bwd ? 2 : 1) : bwd ? (k * v <= 8 ? 2 : 1) : (k * v <= 8 ? 4 : k * v <= 16 ? 3 : 1);
+}
 
 template <typename IO, int V, int K, int TPR, bool ADDED>
 __global__ void __launch_bounds__(fused_threads(TPR), fused_resident(K, V, TPR, false)) k_fused_fwd(const FusedP p) {
-    constexpr int RPC = fused_threads(TPR) / TPR;
+    constexpr int NT = fused_threads(TPR), RPC = NT / TPR, DEPTH = NT * K > 1024 ? 1 : NT * K > 512 ? 2 : 3;
     constexpr bool HELD = K * V <= 16;                       // scale, weight and bias stay in registers
+    extern __shared__ __align__(16) unsigned char smem_rows[];
     __shared__ float red[2][1][32];
     sm100::grid_dep_wait();
     sm100::grid_dep_launch();
     const int tr = threadIdx.x % TPR;
     const long long step = (long long)gridDim.x * RPC;
     long long row = (long long)blockIdx.x * RPC + threadIdx.x / TPR;
-    int turn = 0;
-    Pack<IO, V> nx[K], ne[K], ps[HELD && ADDED ? K : 1], pw[HELD ? K : 1], pb[HELD ? K : 1];
-    auto ahead = [&](long long at) {
-        columns<IO, V, K, TPR>(p.x, at, p.width, at < p.rows, nx);
-        columns<IO, V, K, TPR>(p.e, at, p.width, at < p.rows, ne);
-    };
-    auto param = [&](const void* base, int c) { return load_pack<IO, V>(static_cast<const IO*>(base) + c, V, V > 1); };
-    ahead(row);
-    if constexpr (HELD) {
-        if (ADDED && p.scale) columns<IO, V, K, TPR>(p.scale, 0, p.width, true, reinterpret_cast<Pack<IO, V>(&)[K]>(ps));
-        if (p.weight) columns<IO, V, K, TPR>(p.weight, 0, p.width, true, pw);
-        if (p.bias) columns<IO, V, K, TPR>(p.bias, 0, p.width, true, pb);
-    }
-    for (long long first = (long long)blockIdx.x * RPC; first < p.rows; first += step, row += step) {
-        float f[K][V], s[1] = {0.f}, mean = 0.f;
-        Pack<IO, V> e[K];
+    int turn = 0, stage = 0;
+    const Ahead<IO, V, K, TPR, 2, DEPTH> ahead(smem_rows);
+    const void* const src[2] = {p.x, p.e};
+#pragma unroll
+    for (int d = 0; d < DEPTH; ++d) ahead.fetch(d, src, row + d * step, p.width, row + d * step < p.rows);
+    auto param = [&](const void* base, int c) { return load_pack<IO, V>(static_cast<const IO*>(base) + c, V, true); };
+    Pack<IO, V> ps[HELD && ADDED ? K : 1], pw[HELD ? K : 1], pb[HELD ? K : 1];
+    if constexpr (HELD)
 #pragma unroll
         for (int k = 0; k < K; ++k) {
             const int c = (k * TPR + tr) * V;
-            e[k] = ne[k];
+            const bool in = c < p.width;
+            if constexpr (ADDED) ps[k] = p.scale && in ? param(p.scale, c) : zero_pack<IO, V>();
+            pw[k] = p.weight && in ? param(p.weight, c) : zero_pack<IO, V>();
+            pb[k] = p.bias && in ? param(p.bias, c) : zero_pack<IO, V>();
+        }
+    for (long long first = (long long)blockIdx.x * RPC; first < p.rows; first += step, row += step) {
+        float f[K][V], s[1] = {0.f}, mean = 0.f;
+        Pack<IO, V> e[K];
+        copy_wait<DEPTH - 1>();
+#pragma unroll
+        for (int k = 0; k < K; ++k) {
+            const int c = (k * TPR + tr) * V;
+            const Pack<IO, V> x = ahead.take(stage, 0, k);
+            e[k] = ahead.take(stage, 1, k);
             Pack<IO, V> sc;
-            if (ADDED && p.scale) sc = HELD ? ps[HELD ? k : 0] : c < p.width ? param(p.scale, c) : zero_pack<IO, V>();
+            if (ADDED && p.scale) sc = HELD ? ps[HELD && ADDED ? k : 0] : c < p.width ? param(p.scale, c) : zero_pack<IO, V>();
 #pragma unroll
             for (int i = 0; i < V; ++i) {
-                const float x = pick(nx[k], i);
-                f[k][i] = !ADDED ? x : p.scale ? fmaf(pick(sc, i), x, pick(ne[k], i)) : x + pick(ne[k], i);
+                f[k][i] = !ADDED ? pick(x, i) : p.scale ? fmaf(pick(sc, i), pick(x, i), pick(e[k], i)) : pick(x, i) + pick(e[k], i);
                 s[0] += f[k][i];
             }
         }
-        if (first + step < p.rows) ahead(row + step);
+        ahead.fetch(stage, src, row + DEPTH * step, p.width, row + DEPTH * step < p.rows);
+        stage = stage + 1 == DEPTH ? 0 : stage + 1;
         if (ADDED && row < p.rows) {
             IO* t = static_cast<IO*>(p.t) + row * p.width;
 #pragma unroll
             for (int k = 0; k < K; ++k) {
                 const int c = (k * TPR + tr) * V;
-                if (c < p.width) store_pack(t + c, narrow<IO, V>(f[k]), V, V > 1);
+                if (c < p.width) store_pack(t + c, narrow<IO, V>(f[k]), V, true);
             }
         }
         if (!p.rms) {
@@ -155,7 +207,7 @@ __global__ void __launch_bounds__(fused_threads(TPR), fused_resident(K, V, TPR, 
                 if (!ADDED)
 #pragma unroll
                     for (int i = 0; i < V; ++i) o[i] *= gate_value(pick(e[k], i), p.silu);
-                store_pack(y + c, narrow<IO, V>(o), V, V > 1);
+                store_pack(y + c, narrow<IO, V>(o), V, true);
             }
         }
     }
@@ -163,8 +215,9 @@ __global__ void __launch_bounds__(fused_threads(TPR), fused_resident(K, V, TPR, 
 
 template <typename IO, int V, int K, int TPR, bool ADDED>
 __global__ void __launch_bounds__(fused_threads(TPR), fused_resident(K, V, TPR, true)) k_fused_bwd(const FusedP p) {
-    constexpr int NT = fused_threads(TPR), RPC = NT / TPR, SUMS = fused_sums(ADDED);
-    constexpr bool HELD = K * V <= 16;
+    constexpr int NT = fused_threads(TPR), RPC = NT / TPR, SUMS = fused_sums(ADDED), STREAMS = ADDED ? 4 : 3,
+                  DEPTH = NT * K > 1024 ? 1 : NT * K > 512 ? 2 : 3;
+    extern __shared__ __align__(16) unsigned char smem_rows[];
     __shared__ float red[2][2][32];
     __shared__ float cols[RPC > 1 ? NT * V * K : 1];
     sm100::grid_dep_wait();
@@ -172,7 +225,7 @@ __global__ void __launch_bounds__(fused_threads(TPR), fused_resident(K, V, TPR, 
     const int tr = threadIdx.x % TPR, rg = threadIdx.x / TPR;
     const long long step = (long long)gridDim.x * RPC;
     long long row = (long long)blockIdx.x * RPC + rg;
-    int turn = 0;
+    int turn = 0, stage = 0;
     float sum[SUMS][K][V], nmean = 0.f, nr = 0.f;
 #pragma unroll
     for (int m = 0; m < SUMS; ++m)
@@ -180,58 +233,48 @@ __global__ void __launch_bounds__(fused_threads(TPR), fused_resident(K, V, TPR, 
         for (int k = 0; k < K; ++k)
 #pragma unroll
             for (int i = 0; i < V; ++i) sum[m][k][i] = 0.f;
-    // x, gate or residual, dy, and dtotal of the sum
-    Pack<IO, V> n0[K], n1[K], n2[K], n3[ADDED ? K : 1], pw[HELD ? K : 1], pv[HELD ? K : 1];
+    const Ahead<IO, V, K, TPR, STREAMS, DEPTH> ahead(smem_rows);
+    const void* src[STREAMS];
+    src[0] = p.x; src[1] = p.e; src[2] = p.dy;
+    if constexpr (ADDED) src[3] = p.dt;
     const void* vec = ADDED ? p.scale : p.bias;
-    auto ahead = [&](long long at) {
-        const bool live = at < p.rows;
-        columns<IO, V, K, TPR>(p.x, at, p.width, live, n0);
-        columns<IO, V, K, TPR>(p.e, at, p.width, live, n1);
-        columns<IO, V, K, TPR>(p.dy, at, p.width, live, n2);
-        if constexpr (ADDED) columns<IO, V, K, TPR>(p.dt, at, p.width, live && p.dt, n3);
-        nmean = live && !p.rms ? p.stats[at] : 0.f;
-        nr = live ? p.stats[p.rows + at] : 0.f;
+    auto stats = [&](long long at) {
+        nmean = at < p.rows && !p.rms ? p.stats[at] : 0.f;
+        nr = at < p.rows ? p.stats[p.rows + at] : 0.f;
     };
-    auto param = [&](const void* base, int c) { return load_pack<IO, V>(static_cast<const IO*>(base) + c, V, V > 1); };
-    ahead(row);
-    if constexpr (HELD) {
-        if (p.weight) columns<IO, V, K, TPR>(p.weight, 0, p.width, true, pw);
-        if (vec) columns<IO, V, K, TPR>(vec, 0, p.width, true, pv);
+    stats(row);
+#pragma unroll
+    for (int d = 0; d < DEPTH; ++d) ahead.fetch(d, src, row + d * step, p.width, row + d * step < p.rows);
+    auto param = [&](const void* base, int c) { return load_pack<IO, V>(static_cast<const IO*>(base) + c, V, true); };
+    Pack<IO, V> pw[K], pv[K];
+#pragma unroll
+    for (int k = 0; k < K; ++k) {
+        const int c = (k * TPR + tr) * V;
+        pw[k] = p.weight && c < p.width ? param(p.weight, c) : zero_pack<IO, V>();
+        pv[k] = vec && c < p.width ? param(vec, c) : zero_pack<IO, V>();
     }
     for (long long first = (long long)blockIdx.x * RPC; first < p.rows; first += step, row += step) {
-        const float r = nr;
+        const float r = nr, mean = nmean;
         Pack<IO, V> keep[K], kx[ADDED ? K : 1];                // dtotal, or dz as it will be written; x
         float xh[K][V], g[K][V], s[2] = {0.f, 0.f};
+        copy_wait<DEPTH - 1>();
 #pragma unroll
         for (int k = 0; k < K; ++k) {
-            const int c = (k * TPR + tr) * V;
-            const bool in = c < p.width;
-            Pack<IO, V> w, v;
-            if (p.weight) w = HELD ? pw[HELD ? k : 0] : in ? param(p.weight, c) : zero_pack<IO, V>();
-            if (vec) v = HELD ? pv[HELD ? k : 0] : in ? param(vec, c) : zero_pack<IO, V>();
+            const bool in = (k * TPR + tr) * V < p.width;
+            const Pack<IO, V> x = ahead.take(stage, 0, k), e = ahead.take(stage, 1, k), dy = ahead.take(stage, 2, k);
             float dz[V];
 #pragma unroll
             for (int i = 0; i < V; ++i) {
-                float x = pick(n0[k], i);
-                if (ADDED) x = vec ? fmaf(pick(v, i), x, pick(n1[k], i)) : x + pick(n1[k], i);
-                xh[k][i] = in ? (x - nmean) * r : 0.f;
-                float d = pick(n2[k], i);
-                const float wi = p.weight ? pick(w, i) : 1.f;
-                if (!ADDED) {
-                    const float2 fz = gate_slope(pick(n1[k], i), p.silu);
-                    dz[i] = d * fmaf(xh[k][i], wi, vec ? pick(v, i) : 0.f) * fz.y;
-                    d *= fz.x;
-                }
-                g[k][i] = d * wi;
-                s[0] = fmaf(g[k][i], xh[k][i], s[0]);
-                s[1] += g[k][i];
-                sum[0][k][i] = fmaf(d, xh[k][i], sum[0][k][i]);
-                sum[1][k][i] += d;
+                const float v[4] = {pick(x, i), pick(e, i), pick(dy, i), 0.f};
+                element<ADDED>(p, v, p.weight ? pick(pw[k], i) : 1.f, pick(pv[k], i), mean, in ? r : 0.f, xh[k][i], g[k][i], dz[i], s, &sum[0][k][i],
+                               &sum[1][k][i]);
             }
-            if constexpr (ADDED) { keep[k] = n3[k]; kx[k] = n0[k]; }
+            if constexpr (ADDED) { keep[k] = ahead.take(stage, 3, k); kx[k] = x; }
             else keep[k] = narrow<IO, V>(dz);
         }
-        if (first + step < p.rows) ahead(row + step);
+        ahead.fetch(stage, src, row + DEPTH * step, p.width, row + DEPTH * step < p.rows);
+        stage = stage + 1 == DEPTH ? 0 : stage + 1;
+        stats(row + step);
         row_sum<TPR>(s, red, turn);
         const float m1 = s[0] * p.inv, m2 = p.rms ? 0.f : s[1] * p.inv;
         if (row < p.rows) {
@@ -249,16 +292,15 @@ __global__ void __launch_bounds__(fused_threads(TPR), fused_resident(K, V, TPR, 
                         o[i] += pick(keep[k], i);
                         sum[2][k][i] = fmaf(o[i], pick(kx[k], i), sum[2][k][i]);
                     }
-                    store_pack(de + c, narrow<IO, V>(o), V, V > 1);
+                    store_pack(de + c, narrow<IO, V>(o), V, true);
                     if (vec) {
-                        const Pack<IO, V> v = HELD ? pv[HELD ? k : 0] : param(vec, c);
 #pragma unroll
-                        for (int i = 0; i < V; ++i) o[i] *= pick(v, i);
-                        store_pack(dx + c, narrow<IO, V>(o), V, V > 1);
+                        for (int i = 0; i < V; ++i) o[i] *= pick(pv[k], i);
+                        store_pack(dx + c, narrow<IO, V>(o), V, true);
                     }
                 } else {
-                    store_pack(de + c, keep[k], V, V > 1);
-                    store_pack(dx + c, narrow<IO, V>(o), V, V > 1);
+                    store_pack(de + c, keep[k], V, true);
+                    store_pack(dx + c, narrow<IO, V>(o), V, true);
                 }
             }
         }
@@ -291,6 +333,295 @@ __global__ void __launch_bounds__(fused_threads(TPR), fused_resident(K, V, TPR, 
     }
 }
 
+// ---- rows that begin anywhere ---------------------------------------------------------------------------------------------------
+// A block of rows: RPC groups of lanes, p.step rows each, one after the other in memory, two blocks under way.
+template <typename IO, int TPR, int STREAMS>
+struct Blocks {
+    static constexpr int NT = fused_threads(TPR), RPC = NT / TPR;
+    unsigned char* smem;
+    int width, rows, stride;                                   // rows of a block, bytes of a stream in a stage
+    __device__ __forceinline__ Blocks(unsigned char* s, const FusedP& p)
+        : smem(s), width(p.width), rows(RPC * p.step), stride((int)(((size_t)RPC * p.step * p.width * sizeof(IO) + 31) & ~(size_t)15)) {}
+    // bytes between an aligned address and the block's first element
+    __device__ __forceinline__ int shift(long long block) const { return (int)((unsigned long long)(block * rows) * width * sizeof(IO) & 15); }
+    __device__ __forceinline__ void fetch(int stage, const void* const (&src)[STREAMS], long long block, long long all) const {
+        const long long first = block * rows;
+        if (first < all) {
+            const long long end = first + rows < all ? first + rows : all;
+            const size_t from = (size_t)first * width * sizeof(IO) & ~(size_t)15, to = (size_t)end * width * sizeof(IO);
+            const int pieces = (int)((to - from + 15) / 16);
+#pragma unroll
+            for (int m = 0; m < STREAMS; ++m)
+                if (src[m])
+                    for (int i = threadIdx.x; i < pieces; i += NT) {
+                        const size_t at = from + (size_t)i * 16;
+                        copy_bytes<16>(smem + (stage * STREAMS + m) * stride + i * 16, static_cast<const unsigned char*>(src[m]) + at,
+                                       (int)(to - at < 16 ? to - at : 16));
+                    }
+        }
+        copy_commit();
+    }
+    __device__ __forceinline__ const IO* row(int stage, int stream, long long block, int r) const {
+        return reinterpret_cast<const IO*>(smem + (stage * STREAMS + stream) * stride + shift(block)) + r * width;
+    }
+};
+
+// STAGES: one where two do not fit (fp32 rows wider than 14500)
+template <typename IO, int K, int TPR, bool ADDED, int STAGES>
+__global__ void __launch_bounds__(fused_threads(TPR)) k_odd_fwd(const FusedP p) {
+    extern __shared__ __align__(16) unsigned char smem_rows[];
+    __shared__ float red[2][1][32];
+    sm100::grid_dep_wait();
+    sm100::grid_dep_launch();
+    const int tr = threadIdx.x % TPR, rg = threadIdx.x / TPR;
+    int turn = 0;
+    const Blocks<IO, TPR, 2> blocks(smem_rows, p);
+    const void* const src[2] = {p.x, p.e};
+    float w[K], b[K], sc[K];
+#pragma unroll
+    for (int k = 0; k < K; ++k) {
+        const int c = tr + TPR * k;
+        const bool in = c < p.width;
+        w[k] = p.weight && in ? ld(static_cast<const IO*>(p.weight), c) : 1.f;
+        b[k] = p.bias && in ? ld(static_cast<const IO*>(p.bias), c) : 0.f;
+        sc[k] = ADDED && p.scale && in ? ld(static_cast<const IO*>(p.scale), c) : 1.f;
+    }
+    long long block = blockIdx.x;
+#pragma unroll
+    for (int d = 0; d < STAGES; ++d) blocks.fetch(d, src, block + (long long)d * gridDim.x, p.rows);
+    for (int stage = 0; block * blocks.rows < p.rows; block += gridDim.x, stage = (stage + 1) % STAGES) {
+        copy_wait<STAGES - 1>();
+        __syncthreads();
+        for (int q = 0; q < p.step; ++q) {
+            const int local = q * (fused_threads(TPR) / TPR) + rg;
+            const long long row = block * blocks.rows + local;
+            const bool live = row < p.rows;
+            const IO *x = blocks.row(stage, 0, block, local), *e = blocks.row(stage, 1, block, local);
+            float f[K], z[K], s[1] = {0.f}, mean = 0.f;
+#pragma unroll
+            for (int k = 0; k < K; ++k) {
+                const int c = tr + TPR * k;
+                const bool in = live && c < p.width;
+                f[k] = in ? ld(x, c) : 0.f;
+                z[k] = in ? ld(e, c) : 0.f;
+                if (ADDED) {
+                    f[k] = fmaf(sc[k], f[k], z[k]);
+                    if (in) st(static_cast<IO*>(p.t), (size_t)(row * p.width + c), f[k]);
+                }
+                s[0] += f[k];
+            }
+            if (!p.rms) {
+                row_sum<TPR>(s, red, turn);
+                mean = s[0] * p.inv;
+#pragma unroll
+                for (int k = 0; k < K; ++k) f[k] = tr + TPR * k < p.width ? f[k] - mean : 0.f;
+            }
+            s[0] = 0.f;
+#pragma unroll
+            for (int k = 0; k < K; ++k) s[0] = fmaf(f[k], f[k], s[0]);
+            row_sum<TPR>(s, red, turn);
+            const float r = rsqrtf(fmaf(s[0], p.inv, p.eps));
+            if (!live) continue;
+            if (tr == 0 && p.stats) { p.stats[row] = mean; p.stats[p.rows + row] = r; }
+#pragma unroll
+            for (int k = 0; k < K; ++k) {
+                const int c = tr + TPR * k;
+                if (c >= p.width) break;
+                float o = fmaf(f[k] * r, w[k], b[k]);
+                if (!ADDED) o *= gate_value(z[k], p.silu);
+                st(static_cast<IO*>(p.y), (size_t)(row * p.width + c), o);
+            }
+        }
+        __syncthreads();
+        blocks.fetch(stage, src, block + (long long)STAGES * gridDim.x, p.rows);
+    }
+}
+
+template <typename IO, int K, int TPR, bool ADDED>
+__global__ void __launch_bounds__(fused_threads(TPR)) k_odd_bwd(const FusedP p) {
+    constexpr int NT = fused_threads(TPR), RPC = NT / TPR, SUMS = fused_sums(ADDED), STREAMS = ADDED ? 4 : 3;
+    extern __shared__ __align__(16) unsigned char smem_rows[];
+    __shared__ float red[2][2][32];
+    __shared__ float cols[RPC > 1 ? NT * K : 1];
+    sm100::grid_dep_wait();
+    sm100::grid_dep_launch();
+    const int tr = threadIdx.x % TPR, rg = threadIdx.x / TPR;
+    int turn = 0;
+    const Blocks<IO, TPR, STREAMS> blocks(smem_rows, p);
+    const void* src[STREAMS];
+    src[0] = p.x; src[1] = p.e; src[2] = p.dy;
+    if constexpr (ADDED) src[3] = p.dt;
+    const void* vec = ADDED ? p.scale : p.bias;
+    float w[K], v[K], sum[SUMS][K];
+#pragma unroll
+    for (int k = 0; k < K; ++k) {
+        const int c = tr + TPR * k;
+        w[k] = p.weight && c < p.width ? ld(static_cast<const IO*>(p.weight), c) : 1.f;
+        v[k] = vec && c < p.width ? ld(static_cast<const IO*>(vec), c) : 1.f;
+#pragma unroll
+        for (int m = 0; m < SUMS; ++m) sum[m][k] = 0.f;
+    }
+    long long block = blockIdx.x;
+    blocks.fetch(0, src, block, p.rows);
+    blocks.fetch(1, src, block + gridDim.x, p.rows);
+    for (int stage = 0; block * blocks.rows < p.rows; block += gridDim.x, stage ^= 1) {
+        copy_wait<1>();
+        __syncthreads();
+        for (int q = 0; q < p.step; ++q) {
+            const int local = q * RPC + rg;
+            const long long row = block * blocks.rows + local;
+            const bool live = row < p.rows;
+            const float mean = live && !p.rms ? p.stats[row] : 0.f, r = live ? p.stats[p.rows + row] : 0.f;
+            const IO *x = blocks.row(stage, 0, block, local), *e = blocks.row(stage, 1, block, local), *y = blocks.row(stage, 2, block, local),
+                     *t = ADDED && p.dt ? blocks.row(stage, STREAMS - 1, block, local) : nullptr;
+            float xh[K], g[K], dz[K], s[2] = {0.f, 0.f};
+#pragma unroll
+            for (int k = 0; k < K; ++k) {
+                const int c = tr + TPR * k;
+                const bool in = live && c < p.width;
+                const float u[4] = {in ? ld(x, c) : 0.f, in ? ld(e, c) : 0.f, in ? ld(y, c) : 0.f, 0.f};
+                element<ADDED>(p, u, w[k], v[k], mean, in ? r : 0.f, xh[k], g[k], dz[k], s, &sum[0][k], &sum[1][k]);
+            }
+            row_sum<TPR>(s, red, turn);
+            const float m1 = s[0] * p.inv, m2 = p.rms ? 0.f : s[1] * p.inv;
+            if (!live) continue;
+#pragma unroll
+            for (int k = 0; k < K; ++k) {
+                const int c = tr + TPR * k;
+                if (c >= p.width) break;
+                const size_t at = (size_t)(row * p.width + c);
+                float o = r * (g[k] - m2 - xh[k] * m1);
+                if constexpr (ADDED) {
+                    if (t) o += ld(t, c);
+                    sum[2][k] = fmaf(o, ld(x, c), sum[2][k]);
+                    st(static_cast<IO*>(p.de), at, o);
+                    if (vec) st(static_cast<IO*>(p.dx), at, o * v[k]);
+                } else {
+                    st(static_cast<IO*>(p.de), at, dz[k]);
+                    st(static_cast<IO*>(p.dx), at, o);
+                }
+            }
+        }
+        __syncthreads();
+        blocks.fetch(stage, src, block + 2LL * gridDim.x, p.rows);
+    }
+    if (!p.part) return;
+    float* part = p.part + (size_t)blockIdx.x * SUMS * p.width;
+#pragma unroll
+    for (int m = 0; m < SUMS; ++m) {
+        if constexpr (RPC > 1) {
+            __syncthreads();
+#pragma unroll
+            for (int k = 0; k < K; ++k) cols[rg * (TPR * K) + k * TPR + tr] = sum[m][k];
+            __syncthreads();
+            for (int c = threadIdx.x; c < p.width; c += NT) {
+                float t = 0.f;
+                for (int q = 0; q < RPC; ++q) t += cols[q * (TPR * K) + c];
+                part[(size_t)m * p.width + c] = t;
+            }
+        } else {
+#pragma unroll
+            for (int k = 0; k < K; ++k)
+                if (tr + TPR * k < p.width) part[(size_t)m * p.width + tr + TPR * k] = sum[m][k];
+        }
+    }
+}
+
+// ---- wide rows, backward ----------------------------------------------------------------------------------------------------------
+constexpr int kWideThreads = 256;
+template <typename IO, int V, bool ADDED>
+__device__ __forceinline__ void wide_load(const FusedP& p, long long row, int c, Pack<IO, V> (&u)[4]) {
+    const void* const src[4] = {p.x, p.e, p.dy, ADDED ? p.dt : nullptr};
+#pragma unroll
+    for (int m = 0; m < 4; ++m) u[m] = src[m] ? load_pack<IO, V>(static_cast<const IO*>(src[m]) + row * p.width + c, V, V > 1) : zero_pack<IO, V>();
+}
+template <typename IO, int V, bool ADDED>
+__global__ void __launch_bounds__(kWideThreads) k_wide_sums(const FusedP p) {
+    __shared__ float red[2][2][32];
+    sm100::grid_dep_wait();
+    sm100::grid_dep_launch();
+    const void* vec = ADDED ? p.scale : p.bias;
+    int turn = 0;
+    for (long long row = blockIdx.x; row < p.rows; row += gridDim.x) {
+        const float mean = p.rms ? 0.f : p.stats[row], r = p.stats[p.rows + row];
+        float s[2] = {0.f, 0.f};
+#pragma unroll(V > 1 ? 2 : 8)
+        for (int c = threadIdx.x * V; c < p.width; c += kWideThreads * V) {
+            Pack<IO, V> u[4];
+            wide_load<IO, V, false>(p, row, c, u);
+            const Pack<IO, V> w = p.weight ? load_pack<IO, V>(static_cast<const IO*>(p.weight) + c, V, V > 1) : zero_pack<IO, V>(),
+                              v = vec ? load_pack<IO, V>(static_cast<const IO*>(vec) + c, V, V > 1) : zero_pack<IO, V>();
+#pragma unroll
+            for (int i = 0; i < V; ++i) {
+                const float in[4] = {pick(u[0], i), pick(u[1], i), pick(u[2], i), 0.f};
+                float xh, g, dz;
+                element<ADDED>(p, in, p.weight ? pick(w, i) : 1.f, pick(v, i), mean, r, xh, g, dz, s, nullptr, nullptr);
+            }
+        }
+        row_sum<kWideThreads>(s, red, turn);
+        if (threadIdx.x == 0) { p.rowsum[row] = s[0] * p.inv; p.rowsum[p.rows + row] = p.rms ? 0.f : s[1] * p.inv; }
+    }
+}
+template <typename IO, int V, bool ADDED>
+__global__ void __launch_bounds__(kWideThreads) k_wide_cols(const FusedP p) {
+    constexpr int SUMS = fused_sums(ADDED), U = V > 1 ? 2 : 4;     // rows under way
+    sm100::grid_dep_wait();
+    sm100::grid_dep_launch();
+    const int c = (blockIdx.x * kWideThreads + threadIdx.x) * V;
+    if (c >= p.width) return;
+    const void* vec = ADDED ? p.scale : p.bias;
+    const Pack<IO, V> w = p.weight ? load_pack<IO, V>(static_cast<const IO*>(p.weight) + c, V, V > 1) : zero_pack<IO, V>(),
+                      v = vec ? load_pack<IO, V>(static_cast<const IO*>(vec) + c, V, V > 1) : zero_pack<IO, V>();
+    float sum[SUMS][V];
+#pragma unroll
+    for (int m = 0; m < SUMS; ++m)
+#pragma unroll
+        for (int i = 0; i < V; ++i) sum[m][i] = 0.f;
+    const long long first = (long long)blockIdx.y * p.step, end = first + p.step < p.rows ? first + p.step : p.rows;
+    for (long long row0 = first; row0 < end; row0 += U) {
+        Pack<IO, V> u[U][4];
+#pragma unroll
+        for (int j = 0; j < U; ++j)
+            if (row0 + j < end) wide_load<IO, V, ADDED>(p, row0 + j, c, u[j]);
+#pragma unroll
+        for (int j = 0; j < U; ++j) {
+            const long long row = row0 + j;
+            if (row >= end) break;
+            const float mean = p.rms ? 0.f : p.stats[row], r = p.stats[p.rows + row], m1 = p.rowsum[row], m2 = p.rowsum[p.rows + row];
+            float o[V], dz[V], s[2] = {0.f, 0.f};
+#pragma unroll
+            for (int i = 0; i < V; ++i) {
+                const float in[4] = {pick(u[j][0], i), pick(u[j][1], i), pick(u[j][2], i), pick(u[j][3], i)};
+                float xh, g;
+                element<ADDED>(p, in, p.weight ? pick(w, i) : 1.f, pick(v, i), mean, r, xh, g, dz[i], s, &sum[0][i], &sum[1][i]);
+                o[i] = r * (g - m2 - xh * m1);
+                if constexpr (ADDED) {
+                    o[i] += in[3];
+                    sum[2][i] = fmaf(o[i], in[0], sum[2][i]);
+                }
+            }
+            IO *dx = static_cast<IO*>(p.dx) + row * p.width + c, *de = static_cast<IO*>(p.de) + row * p.width + c;
+            if constexpr (ADDED) {
+                store_pack(de, narrow<IO, V>(o), V, V > 1);
+                if (vec) {
+#pragma unroll
+                    for (int i = 0; i < V; ++i) o[i] *= pick(v, i);
+                    store_pack(dx, narrow<IO, V>(o), V, V > 1);
+                }
+            } else {
+                store_pack(de, narrow<IO, V>(dz), V, V > 1);
+                store_pack(dx, narrow<IO, V>(o), V, V > 1);
+            }
+        }
+    }
+    if (!p.part) return;
+    float* part = p.part + (size_t)blockIdx.y * SUMS * p.width + c;
+#pragma unroll
+    for (int m = 0; m < SUMS; ++m)
+#pragma unroll
+        for (int i = 0; i < V; ++i) part[(size_t)m * p.width + i] = sum[m][i];
+}
+
 // out[m][c] = sum over p of part[p][m][c], in an order that depends on nothing but `parts`; absent outputs are skipped
 struct SumOut { float* out[3]; };
 __global__ void __launch_bounds__(32 * kSumRows) k_fused_sums(const float* part, int parts, int width, int sums, SumOut o) {
@@ -312,53 +643,115 @@ __global__ void __launch_bounds__(32 * kSumRows) k_fused_sums(const float* part,
     if (x == 0 && blockIdx.x * 32 + y < (unsigned)width) out[blockIdx.x * 32 + y] = a;
 }
 
-int fused_vector(int width, int dtype) {
-    const int v = dtype == QD_BF16 ? 8 : 4;
-    return width % v == 0 ? v : 1;
-}
-struct FusedShape { int tpr, k; };
-FusedShape fused_shape(int n, bool bwd) {
-    const int k = bwd ? 1 : 2;
-    for (int tpr = 1; tpr <= 32; tpr *= 2)
-        if (n <= k * tpr) return {tpr, k};
-    if (n <= 256) return {256, 1};
-    if (n <= 512) return {256, 2};
-    if (n <= 1024) return {256, 4};
-    if (n <= 4096) return {1024, 4};
-    return {1024, 16};
-}
-long long fused_ctas(long long rows, const FusedShape& s, int resident) {
-    const int rpc = fused_threads(s.tpr) / s.tpr;
+// ---- which plan ---------------------------------------------------------------------------------------------------------------------
+enum Kind { WHOLE, ODD, WIDE };
+struct FusedPlan {
+    Kind kind;
+    int tpr, k;              // lanes of a row, groups (odd: columns) of a lane
+    int step;                // FusedP::step
+    long long ctas;          // that write a partial each
+    int tiles;               // wide: CTAs side by side
+};
+constexpr int kOddMost = 2048;        // columns of an odd row that registers hold, eight to a lane
+FusedPlan fused_plan(long long rows, int width, int dtype, bool bwd) {
+    const int io = dtype == QD_BF16 ? 2 : 4, v = 16 / io;
+    FusedPlan q{};
+    const bool whole = width % v == 0;
+    const int n = (width + v - 1) / v;
+    if (bwd && (whole ? n > 1024 : width > kOddMost)) {
+        q.kind = WIDE;
+        q.tiles = (width + kWideThreads * (whole ? v : 1) - 1) / (kWideThreads * (whole ? v : 1));
+        const long long slabs = (6 * kSMs + q.tiles - 1) / q.tiles;
+        q.step = (int)((rows + slabs - 1) / slabs);
+        q.ctas = (rows + q.step - 1) / q.step;
+        return q;
+    }
+    q.kind = whole ? WHOLE : ODD;
+    if (whole) {
+        const int least = bwd ? 1 : 2;
+        q.k = least;
+        for (q.tpr = 1; q.tpr * q.k < n && q.tpr < (bwd ? 256 : 512); q.tpr *= 2) {}
+        if (q.tpr * q.k < n) {
+            if (bwd) { q.k = 2; if (n > 512) q.tpr = 512; }
+            else q.k = n <= 2048 ? 4 : 8;
+        }
+        q.step = 1;
+    } else {
+        q.tpr = width <= 32 ? 8 : width <= 256 ? 32 : width <= 2048 ? 256 : 512;
+        q.k = width <= 32 ? 4 : width <= 2048 ? 8 : 32;
+        // 4 KB of a stream in a block, if rows are short
+        const int block = fused_threads(q.tpr) / q.tpr * width * io;
+        q.step = block >= 4096 ? 1 : 4096 / block;
+        const long long share = rows / ((long long)(fused_threads(q.tpr) / q.tpr) * 2 * kSMs);            // few rows: as many CTAs as there are SMs
+        if (q.step > share) q.step = share < 1 ? 1 : (int)share;
+    }
+    const int rpc = fused_threads(q.tpr) / q.tpr * q.step;
+    const int resident = whole ? fused_resident(q.k, v, q.tpr, bwd) : q.tpr > 256 ? 1 : 4;
     const long long groups = (rows + rpc - 1) / rpc, most = kSMs * (long long)resident;
-    return groups < most ? groups : most;
+    q.ctas = groups < most ? groups : most;
+    return q;
 }
 
-template <typename IO, int V, bool ADDED, bool BWD>
-cudaError_t launch(const FusedP& p, cudaStream_t stream) {
-    const FusedShape s = fused_shape((p.width + V - 1) / V, BWD);
-#define QD_FUSED(TPR, K)                                                                                                            \
-    if (s.tpr == TPR && s.k == K) {                                                                                                   \
-        const dim3 grid((unsigned)fused_ctas(p.rows, s, fused_resident(K, V, TPR, BWD)));                                              \
-        if constexpr (BWD) return launch_overlapped(k_fused_bwd<IO, V, K, TPR, ADDED>, grid, dim3(fused_threads(TPR)), 0, stream, p);   \
-        else return launch_overlapped(k_fused_fwd<IO, V, K, TPR, ADDED>, grid, dim3(fused_threads(TPR)), 0, stream, p);                 \
-    }
-    constexpr int L = BWD ? 1 : 2;
-    QD_FUSED(1, L) QD_FUSED(2, L) QD_FUSED(4, L) QD_FUSED(8, L) QD_FUSED(16, L) QD_FUSED(32, L)
-    QD_FUSED(256, 1) QD_FUSED(256, 2) QD_FUSED(256, 4) QD_FUSED(1024, 4)
-    if constexpr (V == 1) QD_FUSED(1024, 16)
+template <class K>
+cudaError_t go(K kern, dim3 grid, int threads, size_t bytes, const FusedP& p, cudaStream_t stream) {
+    const cudaError_t e = bytes ? set_max_smem_once((const void*)kern, bytes) : cudaSuccess;
+    return e != cudaSuccess ? e : launch_overlapped(kern, grid, dim3(threads), bytes, stream, p);
+}
+template <typename IO, bool ADDED, bool BWD>
+cudaError_t launch(FusedP p, cudaStream_t stream) {
+    constexpr int V = 16 / sizeof(IO), STREAMS = !BWD ? 2 : ADDED ? 4 : 3;
+    const FusedPlan q = fused_plan(p.rows, p.width, V == 8 ? QD_BF16 : QD_F32, BWD);
+    p.step = q.step;
+    const dim3 grid((unsigned)q.ctas);
+    if (q.kind == WHOLE) {
+#define QD_FUSED(TPR, K)                                                                                                                       \
+        if (q.tpr == TPR && q.k == K) {                                                                                                         \
+            constexpr int NT = fused_threads(TPR);                                                                                               \
+            constexpr size_t bytes = (size_t)depth_of(K, NT) * STREAMS * K * NT * 16;                                                             \
+            if constexpr (BWD) return go(k_fused_bwd<IO, V, K, TPR, ADDED>, grid, NT, bytes, p, stream);                                           \
+            else return go(k_fused_fwd<IO, V, K, TPR, ADDED>, grid, NT, bytes, p, stream);                                                         \
+        }
+        constexpr int L = BWD ? 1 : 2;
+        QD_FUSED(1, L) QD_FUSED(2, L) QD_FUSED(4, L) QD_FUSED(8, L) QD_FUSED(16, L) QD_FUSED(32, L) QD_FUSED(64, L) QD_FUSED(128, L) QD_FUSED(256, L)
+        if constexpr (BWD) {
+            QD_FUSED(256, 2) QD_FUSED(512, 2)
+        } else {
+            QD_FUSED(512, 2) QD_FUSED(512, 4)
+            if constexpr (V == 4) QD_FUSED(512, 8)
+        }
 #undef QD_FUSED
+        return cudaErrorInvalidValue;
+    }
+    if (q.kind == ODD) {
+#define QD_ODD(TPR, K)                                                                                                                         \
+        if (q.tpr == TPR && q.k == K) {                                                                                                         \
+            constexpr int NT = fused_threads(TPR);                                                                                               \
+            const size_t block = ((size_t)NT / TPR * q.step * p.width * sizeof(IO) + 31) & ~(size_t)15;                                           \
+            if constexpr (BWD) return go(k_odd_bwd<IO, K, TPR, ADDED>, grid, NT, 2 * STREAMS * block, p, stream);                                  \
+            constexpr int STAGES = K * sizeof(IO) > 64 ? 1 : 2;                                                                                    \
+            if constexpr (!BWD) return go(k_odd_fwd<IO, K, TPR, ADDED, STAGES>, grid, NT, STAGES * STREAMS * block, p, stream);                      \
+        }
+        QD_ODD(8, 4) QD_ODD(32, 8) QD_ODD(256, 8)
+        if constexpr (!BWD) QD_ODD(512, 32)
+#undef QD_ODD
+        return cudaErrorInvalidValue;
+    }
+    if constexpr (BWD) {
+        const long long most = 8LL * kSMs;
+        const dim3 sums((unsigned)(p.rows < most ? p.rows : most)), cols((unsigned)q.tiles, (unsigned)q.ctas);
+        cudaError_t e;
+        if (p.width % V == 0) {
+            e = go(k_wide_sums<IO, V, ADDED>, sums, kWideThreads, 0, p, stream);
+            return e != cudaSuccess ? e : go(k_wide_cols<IO, V, ADDED>, cols, kWideThreads, 0, p, stream);
+        }
+        e = go(k_wide_sums<IO, 1, ADDED>, sums, kWideThreads, 0, p, stream);
+        return e != cudaSuccess ? e : go(k_wide_cols<IO, 1, ADDED>, cols, kWideThreads, 0, p, stream);
+    }
     return cudaErrorInvalidValue;
 }
 template <bool ADDED, bool BWD>
 cudaError_t launch(const FusedP& p, int dtype, cudaStream_t stream) {
-    const bool vec = fused_vector(p.width, dtype) > 1;
-    if (dtype == QD_BF16) return vec ? launch<__nv_bfloat16, 8, ADDED, BWD>(p, stream) : launch<__nv_bfloat16, 1, ADDED, BWD>(p, stream);
-    return vec ? launch<float, 4, ADDED, BWD>(p, stream) : launch<float, 1, ADDED, BWD>(p, stream);
-}
-long long fused_bwd_ctas(long long rows, int width, int dtype) {
-    const int V = fused_vector(width, dtype);
-    const FusedShape s = fused_shape((width + V - 1) / V, true);
-    return fused_ctas(rows, s, fused_resident(s.k, V, s.tpr, true));
+    return dtype == QD_BF16 ? launch<__nv_bfloat16, ADDED, BWD>(p, stream) : launch<float, ADDED, BWD>(p, stream);
 }
 FusedP fused(const FusedNormArgs& a) {
     FusedP p{};
@@ -369,26 +762,33 @@ FusedP fused(const FusedNormArgs& a) {
     p.de = a.added ? a.dresidual : a.dgate;
     return p;
 }
+// the workspace: partial sums, then the rows' sums
+size_t part_floats(const FusedPlan& q, int width) { return ((size_t)q.ctas * fused_sums(true) * width + 3) & ~(size_t)3; }
 
 }  // namespace
 
 size_t fused_norm_workspace(long long rows, int width, int dtype) {
-    return (size_t)fused_bwd_ctas(rows, width, dtype) * fused_sums(true) * width * sizeof(float);
+    const FusedPlan q = fused_plan(rows, width, dtype, true);
+    return (part_floats(q, width) + (q.kind == WIDE ? 2 * (size_t)rows : 0)) * sizeof(float);
 }
+bool fused_norm_needs_workspace(long long rows, int width, int dtype) { return fused_plan(rows, width, dtype, true).kind == WIDE; }
+
 cudaError_t fused_norm_fwd(const FusedNormArgs& a) {
     const FusedP p = fused(a);
     return a.added ? launch<true, false>(p, a.dtype, a.stream) : launch<false, false>(p, a.dtype, a.stream);
 }
 cudaError_t fused_norm_bwd(const FusedNormArgs& a) {
     FusedP p = fused(a);
+    const FusedPlan q = fused_plan(a.rows, a.width, a.dtype, true);
     const SumOut out{{a.dweight, a.dbias, a.added ? a.dscale : nullptr}};
     const bool sums = out.out[0] || out.out[1] || out.out[2];
     p.part = sums ? a.part : nullptr;
+    p.rowsum = q.kind == WIDE ? a.part + part_floats(q, a.width) : nullptr;
     const cudaError_t e = a.added ? launch<true, true>(p, a.dtype, a.stream) : launch<false, true>(p, a.dtype, a.stream);
     if (e != cudaSuccess || !sums) return e;
     const int n = fused_sums(a.added);
-    return launch_overlapped(k_fused_sums, dim3((unsigned)((a.width + 31) / 32), n), dim3(32 * kSumRows), 0, a.stream, p.part,
-                             (int)fused_bwd_ctas(a.rows, a.width, a.dtype), a.width, n, out);
+    return launch_overlapped(k_fused_sums, dim3((unsigned)((a.width + 31) / 32), n), dim3(32 * kSumRows), 0, a.stream, p.part, (int)q.ctas, a.width, n,
+                             out);
 }
 
 }  // namespace qd

@@ -179,6 +179,7 @@ struct FusedNormArgs {
     cudaStream_t stream;
 };
 size_t fused_norm_workspace(long long rows, int width, int dtype);
+bool fused_norm_needs_workspace(long long rows, int width, int dtype);      // even if no sums over rows are wanted
 cudaError_t fused_norm_fwd(const FusedNormArgs& a);
 cudaError_t fused_norm_bwd(const FusedNormArgs& a);
 // rotary positions (rotary.cu)

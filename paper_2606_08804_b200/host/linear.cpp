@@ -71,6 +71,7 @@ LinearGrads linear_backward(const at::Tensor& q, const at::Tensor& k, const at::
 }
 
 // ---- layer norm with a gate, and behind a residual sum ----------------------------------------------------------------------
+constexpr int64_t kNarrow = 1024;            // columns up to which a backward without sums over rows needs no workspace
 struct Fused {
     On on;
     int64_t rows, width;
@@ -114,7 +115,7 @@ GatedGrads gated_backward(const at::Tensor& x, const at::Tensor& gate, const at:
     g.dx = c.on.make(x.sizes(), c.dt);
     g.dgate = c.on.make(x.sizes(), c.dt);
     at::Tensor ws;
-    if (want_dweight || want_dbias) ws = c.workspace();
+    if (want_dweight || want_dbias || c.width > kNarrow) ws = c.workspace();
     Params params(c.on, {want_dweight ? c.width : 0, want_dbias ? c.width : 0});
     g.params = params.all;
     if (want_dweight) g.dweight = params.next({c.width});
@@ -149,7 +150,7 @@ AddedGrads added_backward(const at::Tensor& x, const at::Tensor& residual, const
     g.dresidual = c.on.make(x.sizes(), c.dt);
     g.dx = scale ? c.on.make(x.sizes(), c.dt) : g.dresidual;
     at::Tensor ws;
-    if (want_dscale || want_dweight || want_dbias) ws = c.workspace();
+    if (want_dscale || want_dweight || want_dbias || c.width > kNarrow) ws = c.workspace();
     Params params(c.on, {want_dscale ? c.width : 0, want_dweight ? c.width : 0, want_dbias ? c.width : 0});
     g.params = params.all;
     if (want_dscale) g.dscale = params.next({c.width});
