@@ -8,10 +8,10 @@
 // dw = sum_rows dy x^, db = sum_rows dy.
 //
 // Bound by HBM, so the plan of a row decides:
-//   k_fused_fwd, _bwd   rows of whole 16-byte groups: a row belongs to 2^k lanes or to a CTA and is in registers when its sums are taken; what
+//   k_fused_fwd, _bwd   rows of whole 16-byte (or 4-byte) groups: a row belongs to 2^k lanes or to a CTA and is in registers when its sums are taken; what
 //                       the next rows need is on its way to shared memory, where each thread reads back only what it asked for (no barrier).
 //                       CTAs stay; backward the sums over rows stay in registers, one partial per CTA, added up in a fixed order.
-//   k_odd_fwd, _bwd     rows that begin anywhere: blocks of rows come to shared memory as the aligned 16-byte pieces that they lie in, and
+//   k_odd_fwd, _bwd     bf16 rows of an odd width, which begin anywhere: blocks of rows come to shared memory as the aligned 16-byte pieces that they lie in, and
 //                       are read from there one element at a time, neighbouring columns to neighbouring lanes.
 //   k_wide_sums, _cols  backward of rows too wide for registers: the sums of a row first, then everything else with a thread to a column
 //                       and the rows in a loop, whose sums over rows need no more than the registers of one column.  Inputs are read twice.
@@ -82,13 +82,16 @@ __device__ __forceinline__ void element(const FusedP& p, const float (&in)[4], f
 }
 
 // ---- rows of whole groups -----------------------------------------------------------------------------------------------------
-// A thread's K groups of STREAMS rows, DEPTH rows ahead.
-template <typename IO, int V, int K, int TPR, int STREAMS, int DEPTH>
+// A thread's K groups of STREAMS rows, DEPTH rows ahead: one forward (with three, 262144 x 128 gated takes 36.2 us for 33.6, added 54.6 for
+// 49.8), three backward, where few threads have room (two gated rows ahead in registers instead: 74.7 for 64.7).
+constexpr int depth_of(int stage, bool bwd) { return !bwd ? 1 : 3 * stage <= 49152 ? 3 : 2 * stage <= 65536 ? 2 : 1; }
+template <typename IO, int V, int K, int TPR, int STREAMS, bool BWD>
 struct Ahead {
-    static constexpr int NT = fused_threads(TPR), kBytes = DEPTH * STREAMS * K * NT * 16;
+    static constexpr int NT = fused_threads(TPR), B = V * sizeof(IO), kStage = STREAMS * K * NT * B, DEPTH = depth_of(kStage, BWD), kBytes = DEPTH * kStage;
+    static_assert(B == 16 || B == 4, "what copies take");
     unsigned char* mine;
-    __device__ __forceinline__ explicit Ahead(unsigned char* smem) : mine(smem + threadIdx.x * 16) {}
-    __device__ __forceinline__ unsigned char* at(int stage, int stream, int k) const { return mine + ((stage * STREAMS + stream) * K + k) * (NT * 16); }
+    __device__ __forceinline__ explicit Ahead(unsigned char* smem) : mine(smem + threadIdx.x * B) {}
+    __device__ __forceinline__ unsigned char* at(int stage, int stream, int k) const { return mine + ((stage * STREAMS + stream) * K + k) * (NT * B); }
     __device__ __forceinline__ void fetch(int stage, const void* const (&src)[STREAMS], long long row, int width, bool live) const {
 #pragma unroll
         for (int m = 0; m < STREAMS; ++m)
@@ -96,18 +99,21 @@ struct Ahead {
             for (int k = 0; k < K; ++k) {
                 const int c = (k * TPR + threadIdx.x % TPR) * V;
                 const bool in = live && c < width && src[m];
-                copy_bytes<16>(at(stage, m, k), in ? static_cast<const IO*>(src[m]) + row * width + c : static_cast<const IO*>(src[0]), in ? 16 : 0);
+                copy_bytes<B>(at(stage, m, k), in ? static_cast<const IO*>(src[m]) + row * width + c : static_cast<const IO*>(src[0]), in ? B : 0);
             }
         copy_commit();
     }
     __device__ __forceinline__ Pack<IO, V> take(int stage, int stream, int k) const {
-        const uint4 u = *reinterpret_cast<const uint4*>(at(stage, stream, k));
         Pack<IO, V> r;
-        r.w[0] = u.x; r.w[1] = u.y; r.w[2] = u.z; r.w[3] = u.w;
+        if constexpr (B == 16) {
+            const uint4 u = *reinterpret_cast<const uint4*>(at(stage, stream, k));
+            r.w[0] = u.x; r.w[1] = u.y; r.w[2] = u.z; r.w[3] = u.w;
+        } else {
+            r.w[0] = *reinterpret_cast<const uint32_t*>(at(stage, stream, k));
+        }
         return r;
     }
 };
-constexpr int depth_of(int k, int nt) { return k * nt > 1024 ? 1 : k * nt > 512 ? 2 : 3; }
 // CTAs to an SM that the registers are shared out for
 constexpr __host__ __device__ int fused_resident(int k, int v, int tpr, bool bwd) {
     return tpr > 256 ? (k * v <= 16 && !bwd ? 2 : 1) : bwd ? (k * v <= 8 ? 2 : 1) : (k * v <= 8 ? 4 : k * v <= 16 ? 3 : 1);
@@ -115,7 +121,7 @@ constexpr __host__ __device__ int fused_resident(int k, int v, int tpr, bool bwd
 
 template <typename IO, int V, int K, int TPR, bool ADDED>
 __global__ void __launch_bounds__(fused_threads(TPR), fused_resident(K, V, TPR, false)) k_fused_fwd(const FusedP p) {
-    constexpr int NT = fused_threads(TPR), RPC = NT / TPR, DEPTH = NT * K > 1024 ? 1 : NT * K > 512 ? 2 : 3;
+    constexpr int NT = fused_threads(TPR), RPC = NT / TPR;
     constexpr bool HELD = K * V <= 16;                       // scale, weight and bias stay in registers
     extern __shared__ __align__(16) unsigned char smem_rows[];
     __shared__ float red[2][1][32];
@@ -125,7 +131,9 @@ __global__ void __launch_bounds__(fused_threads(TPR), fused_resident(K, V, TPR, 
     const long long step = (long long)gridDim.x * RPC;
     long long row = (long long)blockIdx.x * RPC + threadIdx.x / TPR;
     int turn = 0, stage = 0;
-    const Ahead<IO, V, K, TPR, 2, DEPTH> ahead(smem_rows);
+    typedef Ahead<IO, V, K, TPR, 2, false> Rows;
+    constexpr int DEPTH = Rows::DEPTH;
+    const Rows ahead(smem_rows);
     const void* const src[2] = {p.x, p.e};
 #pragma unroll
     for (int d = 0; d < DEPTH; ++d) ahead.fetch(d, src, row + d * step, p.width, row + d * step < p.rows);
@@ -215,8 +223,7 @@ __global__ void __launch_bounds__(fused_threads(TPR), fused_resident(K, V, TPR, 
 
 template <typename IO, int V, int K, int TPR, bool ADDED>
 __global__ void __launch_bounds__(fused_threads(TPR), fused_resident(K, V, TPR, true)) k_fused_bwd(const FusedP p) {
-    constexpr int NT = fused_threads(TPR), RPC = NT / TPR, SUMS = fused_sums(ADDED), STREAMS = ADDED ? 4 : 3,
-                  DEPTH = NT * K > 1024 ? 1 : NT * K > 512 ? 2 : 3;
+    constexpr int NT = fused_threads(TPR), RPC = NT / TPR, SUMS = fused_sums(ADDED), STREAMS = ADDED ? 4 : 3;
     extern __shared__ __align__(16) unsigned char smem_rows[];
     __shared__ float red[2][2][32];
     __shared__ float cols[RPC > 1 ? NT * V * K : 1];
@@ -233,7 +240,9 @@ __global__ void __launch_bounds__(fused_threads(TPR), fused_resident(K, V, TPR, 
         for (int k = 0; k < K; ++k)
 #pragma unroll
             for (int i = 0; i < V; ++i) sum[m][k][i] = 0.f;
-    const Ahead<IO, V, K, TPR, STREAMS, DEPTH> ahead(smem_rows);
+    typedef Ahead<IO, V, K, TPR, STREAMS, true> Rows;
+    constexpr int DEPTH = Rows::DEPTH;
+    const Rows ahead(smem_rows);
     const void* src[STREAMS];
     src[0] = p.x; src[1] = p.e; src[2] = p.dy;
     if constexpr (ADDED) src[3] = p.dt;
@@ -366,8 +375,7 @@ struct Blocks {
     }
 };
 
-// STAGES: one where two do not fit (fp32 rows wider than 14500)
-template <typename IO, int K, int TPR, bool ADDED, int STAGES>
+template <typename IO, int K, int TPR, bool ADDED>
 __global__ void __launch_bounds__(fused_threads(TPR)) k_odd_fwd(const FusedP p) {
     extern __shared__ __align__(16) unsigned char smem_rows[];
     __shared__ float red[2][1][32];
@@ -387,10 +395,10 @@ __global__ void __launch_bounds__(fused_threads(TPR)) k_odd_fwd(const FusedP p) 
         sc[k] = ADDED && p.scale && in ? ld(static_cast<const IO*>(p.scale), c) : 1.f;
     }
     long long block = blockIdx.x;
-#pragma unroll
-    for (int d = 0; d < STAGES; ++d) blocks.fetch(d, src, block + (long long)d * gridDim.x, p.rows);
-    for (int stage = 0; block * blocks.rows < p.rows; block += gridDim.x, stage = (stage + 1) % STAGES) {
-        copy_wait<STAGES - 1>();
+    blocks.fetch(0, src, block, p.rows);
+    blocks.fetch(1, src, block + gridDim.x, p.rows);
+    for (int stage = 0; block * blocks.rows < p.rows; block += gridDim.x, stage ^= 1) {
+        copy_wait<1>();
         __syncthreads();
         for (int q = 0; q < p.step; ++q) {
             const int local = q * (fused_threads(TPR) / TPR) + rg;
@@ -433,7 +441,7 @@ __global__ void __launch_bounds__(fused_threads(TPR)) k_odd_fwd(const FusedP p) 
             }
         }
         __syncthreads();
-        blocks.fetch(stage, src, block + (long long)STAGES * gridDim.x, p.rows);
+        blocks.fetch(stage, src, block + 2LL * gridDim.x, p.rows);
     }
 }
 
@@ -545,7 +553,7 @@ __global__ void __launch_bounds__(kWideThreads) k_wide_sums(const FusedP p) {
     for (long long row = blockIdx.x; row < p.rows; row += gridDim.x) {
         const float mean = p.rms ? 0.f : p.stats[row], r = p.stats[p.rows + row];
         float s[2] = {0.f, 0.f};
-#pragma unroll(V > 1 ? 2 : 8)
+#pragma unroll(V * sizeof(IO) == 16 ? 2 : 8)
         for (int c = threadIdx.x * V; c < p.width; c += kWideThreads * V) {
             Pack<IO, V> u[4];
             wide_load<IO, V, false>(p, row, c, u);
@@ -564,7 +572,7 @@ __global__ void __launch_bounds__(kWideThreads) k_wide_sums(const FusedP p) {
 }
 template <typename IO, int V, bool ADDED>
 __global__ void __launch_bounds__(kWideThreads) k_wide_cols(const FusedP p) {
-    constexpr int SUMS = fused_sums(ADDED), U = V > 1 ? 2 : 4;     // rows under way
+    constexpr int SUMS = fused_sums(ADDED), U = V * sizeof(IO) == 16 ? 2 : 4;     // rows under way
     sm100::grid_dep_wait();
     sm100::grid_dep_launch();
     const int c = (blockIdx.x * kWideThreads + threadIdx.x) * V;
@@ -647,105 +655,111 @@ __global__ void __launch_bounds__(32 * kSumRows) k_fused_sums(const float* part,
 enum Kind { WHOLE, ODD, WIDE };
 struct FusedPlan {
     Kind kind;
-    int tpr, k;              // lanes of a row, groups (odd: columns) of a lane
+    int v;                   // elements of a group: of 16 bytes where rows are whole groups of those, else of 4; 1 of an odd bf16 row
+    int tpr, k;              // lanes of a row, groups of a lane
     int step;                // FusedP::step
     long long ctas;          // that write a partial each
     int tiles;               // wide: CTAs side by side
 };
-constexpr int kOddMost = 2048;        // columns of an odd row that registers hold, eight to a lane
 FusedPlan fused_plan(long long rows, int width, int dtype, bool bwd) {
-    const int io = dtype == QD_BF16 ? 2 : 4, v = 16 / io;
+    const int io = dtype == QD_BF16 ? 2 : 4;
     FusedPlan q{};
-    const bool whole = width % v == 0;
-    const int n = (width + v - 1) / v;
-    if (bwd && (whole ? n > 1024 : width > kOddMost)) {
+    q.v = width % (16 / io) == 0 ? 16 / io : width % (4 / io) == 0 ? 4 / io : 1;
+    const bool odd = q.v * io < 4, big = q.v * io == 16;
+    const int n = width / q.v;
+    // what registers hold: 16 elements to a lane and one to three sums of each
+    if (bwd && n > (big ? 1024 : 2048)) {
         q.kind = WIDE;
-        q.tiles = (width + kWideThreads * (whole ? v : 1) - 1) / (kWideThreads * (whole ? v : 1));
+        q.tiles = (n + kWideThreads - 1) / kWideThreads;
         const long long slabs = (6 * kSMs + q.tiles - 1) / q.tiles;
         q.step = (int)((rows + slabs - 1) / slabs);
         q.ctas = (rows + q.step - 1) / q.step;
         return q;
     }
-    q.kind = whole ? WHOLE : ODD;
-    if (whole) {
-        const int least = bwd ? 1 : 2;
-        q.k = least;
-        for (q.tpr = 1; q.tpr * q.k < n && q.tpr < (bwd ? 256 : 512); q.tpr *= 2) {}
-        if (q.tpr * q.k < n) {
-            if (bwd) { q.k = 2; if (n > 512) q.tpr = 512; }
-            else q.k = n <= 2048 ? 4 : 8;
-        }
-        q.step = 1;
-    } else {
-        q.tpr = width <= 32 ? 8 : width <= 256 ? 32 : width <= 2048 ? 256 : 512;
-        q.k = width <= 32 ? 4 : width <= 2048 ? 8 : 32;
-        // 4 KB of a stream in a block, if rows are short
-        const int block = fused_threads(q.tpr) / q.tpr * width * io;
-        q.step = block >= 4096 ? 1 : 4096 / block;
-        const long long share = rows / ((long long)(fused_threads(q.tpr) / q.tpr) * 2 * kSMs);            // few rows: as many CTAs as there are SMs
+    q.kind = odd ? ODD : WHOLE;
+    q.step = 1;
+    if (odd) {
+        q.k = width <= 32 ? 4 : width <= 4096 ? 8 : 32;
+        q.tpr = width <= 32 ? 8 : 32;
+        while (q.tpr * q.k < width) q.tpr *= 2;
+        const int rpc = fused_threads(q.tpr) / q.tpr, block = rpc * width * io;
+        const long long share = rows / (rpc * 2LL * kSMs);                  // few rows: as many CTAs as there are SMs
+        q.step = block >= 4096 ? 1 : 4096 / block;                          // 4 KB of a stream in a block, if rows are short
         if (q.step > share) q.step = share < 1 ? 1 : (int)share;
+    } else {
+        const int most = bwd ? 256 : 512;
+        q.k = bwd ? (big ? 1 : 4) : (big ? 2 : 8);
+        for (q.tpr = 1; q.tpr * q.k < n && q.tpr < most; q.tpr *= 2) {}
+        if (bwd && q.tpr * q.k < n) { q.k *= 2; if (q.tpr * q.k < n) q.tpr = 512; }
+        while (q.tpr * q.k < n) q.k *= 2;
     }
     const int rpc = fused_threads(q.tpr) / q.tpr * q.step;
-    const int resident = whole ? fused_resident(q.k, v, q.tpr, bwd) : q.tpr > 256 ? 1 : 4;
-    const long long groups = (rows + rpc - 1) / rpc, most = kSMs * (long long)resident;
-    q.ctas = groups < most ? groups : most;
+    const int resident = odd ? (q.tpr > 256 ? 1 : 4) : fused_resident(q.k, q.v, q.tpr, bwd);
+    const long long groups = (rows + rpc - 1) / rpc, all = kSMs * (long long)resident;
+    q.ctas = groups < all ? groups : all;
     return q;
 }
 
 template <class K>
 cudaError_t go(K kern, dim3 grid, int threads, size_t bytes, const FusedP& p, cudaStream_t stream) {
-    const cudaError_t e = bytes ? set_max_smem_once((const void*)kern, bytes) : cudaSuccess;
+    const cudaError_t e = bytes > 32768 ? set_max_smem_once((const void*)kern, bytes) : cudaSuccess;
     return e != cudaSuccess ? e : launch_overlapped(kern, grid, dim3(threads), bytes, stream, p);
+}
+template <typename IO, int V, int K, int TPR, bool ADDED, bool BWD>
+cudaError_t whole(const FusedP& p, dim3 grid, cudaStream_t stream) {
+    constexpr int bytes = Ahead<IO, V, K, TPR, !BWD ? 2 : ADDED ? 4 : 3, BWD>::kBytes;
+    if constexpr (BWD) return go(k_fused_bwd<IO, V, K, TPR, ADDED>, grid, fused_threads(TPR), bytes, p, stream);
+    else return go(k_fused_fwd<IO, V, K, TPR, ADDED>, grid, fused_threads(TPR), bytes, p, stream);
+}
+template <typename IO, int V, bool ADDED, bool BWD>
+cudaError_t whole(const FusedP& p, const FusedPlan& q, cudaStream_t stream) {
+    const dim3 grid((unsigned)q.ctas);
+    constexpr bool BIG = V * sizeof(IO) == 16;
+    constexpr int L = BWD ? (BIG ? 1 : 4) : (BIG ? 2 : 8);
+#define QD_FUSED(TPR, K) if (q.tpr == TPR && q.k == (K)) return whole<IO, V, (K), TPR, ADDED, BWD>(p, grid, stream);
+    QD_FUSED(1, L) QD_FUSED(2, L) QD_FUSED(4, L) QD_FUSED(8, L) QD_FUSED(16, L) QD_FUSED(32, L) QD_FUSED(64, L) QD_FUSED(128, L) QD_FUSED(256, L)
+    if constexpr (BWD) {
+        QD_FUSED(256, 2 * L)
+        if constexpr (BIG) QD_FUSED(512, 2 * L)
+    } else {
+        QD_FUSED(512, L) QD_FUSED(512, 2 * L)
+        if constexpr (sizeof(IO) == 4) QD_FUSED(512, 4 * L)
+    }
+#undef QD_FUSED
+    return cudaErrorInvalidValue;
+}
+template <int K, int TPR, bool ADDED, bool BWD>
+cudaError_t odd(const FusedP& p, dim3 grid, cudaStream_t stream) {
+    constexpr int NT = fused_threads(TPR), STREAMS = !BWD ? 2 : ADDED ? 4 : 3;
+    const size_t bytes = 2 * STREAMS * (((size_t)NT / TPR * p.step * p.width * 2 + 31) & ~(size_t)15);
+    if constexpr (BWD) return go(k_odd_bwd<__nv_bfloat16, K, TPR, ADDED>, grid, NT, bytes, p, stream);
+    else return go(k_odd_fwd<__nv_bfloat16, K, TPR, ADDED>, grid, NT, bytes, p, stream);
+}
+template <typename IO, int V, bool ADDED>
+cudaError_t wide(const FusedP& p, const FusedPlan& q, cudaStream_t stream) {
+    const long long most = 8LL * kSMs;
+    const cudaError_t e = go(k_wide_sums<IO, V, ADDED>, dim3((unsigned)(p.rows < most ? p.rows : most)), kWideThreads, 0, p, stream);
+    return e != cudaSuccess ? e : go(k_wide_cols<IO, V, ADDED>, dim3((unsigned)q.tiles, (unsigned)q.ctas), kWideThreads, 0, p, stream);
 }
 template <typename IO, bool ADDED, bool BWD>
 cudaError_t launch(FusedP p, cudaStream_t stream) {
-    constexpr int V = 16 / sizeof(IO), STREAMS = !BWD ? 2 : ADDED ? 4 : 3;
-    const FusedPlan q = fused_plan(p.rows, p.width, V == 8 ? QD_BF16 : QD_F32, BWD);
+    constexpr int BIG = 16 / sizeof(IO), SMALL = 4 / sizeof(IO);
+    const FusedPlan q = fused_plan(p.rows, p.width, sizeof(IO) == 2 ? QD_BF16 : QD_F32, BWD);
     p.step = q.step;
-    const dim3 grid((unsigned)q.ctas);
-    if (q.kind == WHOLE) {
-#define QD_FUSED(TPR, K)                                                                                                                       \
-        if (q.tpr == TPR && q.k == K) {                                                                                                         \
-            constexpr int NT = fused_threads(TPR);                                                                                               \
-            constexpr size_t bytes = (size_t)depth_of(K, NT) * STREAMS * K * NT * 16;                                                             \
-            if constexpr (BWD) return go(k_fused_bwd<IO, V, K, TPR, ADDED>, grid, NT, bytes, p, stream);                                           \
-            else return go(k_fused_fwd<IO, V, K, TPR, ADDED>, grid, NT, bytes, p, stream);                                                         \
+    if (q.kind == WHOLE) return q.v == BIG ? whole<IO, BIG, ADDED, BWD>(p, q, stream) : whole<IO, SMALL, ADDED, BWD>(p, q, stream);
+    if constexpr (BWD)
+        if (q.kind == WIDE) {
+            if (q.v == BIG) return wide<IO, BIG, ADDED>(p, q, stream);
+            if constexpr (SMALL > 1)
+                if (q.v == SMALL) return wide<IO, SMALL, ADDED>(p, q, stream);
+            return wide<IO, 1, ADDED>(p, q, stream);
         }
-        constexpr int L = BWD ? 1 : 2;
-        QD_FUSED(1, L) QD_FUSED(2, L) QD_FUSED(4, L) QD_FUSED(8, L) QD_FUSED(16, L) QD_FUSED(32, L) QD_FUSED(64, L) QD_FUSED(128, L) QD_FUSED(256, L)
-        if constexpr (BWD) {
-            QD_FUSED(256, 2) QD_FUSED(512, 2)
-        } else {
-            QD_FUSED(512, 2) QD_FUSED(512, 4)
-            if constexpr (V == 4) QD_FUSED(512, 8)
-        }
-#undef QD_FUSED
-        return cudaErrorInvalidValue;
-    }
-    if (q.kind == ODD) {
-#define QD_ODD(TPR, K)                                                                                                                         \
-        if (q.tpr == TPR && q.k == K) {                                                                                                         \
-            constexpr int NT = fused_threads(TPR);                                                                                               \
-            const size_t block = ((size_t)NT / TPR * q.step * p.width * sizeof(IO) + 31) & ~(size_t)15;                                           \
-            if constexpr (BWD) return go(k_odd_bwd<IO, K, TPR, ADDED>, grid, NT, 2 * STREAMS * block, p, stream);                                  \
-            constexpr int STAGES = K * sizeof(IO) > 64 ? 1 : 2;                                                                                    \
-            if constexpr (!BWD) return go(k_odd_fwd<IO, K, TPR, ADDED, STAGES>, grid, NT, STAGES * STREAMS * block, p, stream);                      \
-        }
-        QD_ODD(8, 4) QD_ODD(32, 8) QD_ODD(256, 8)
-        if constexpr (!BWD) QD_ODD(512, 32)
+    if constexpr (sizeof(IO) == 2) {
+        const dim3 grid((unsigned)q.ctas);
+#define QD_ODD(TPR, K) if (q.tpr == TPR && q.k == K) return odd<K, TPR, ADDED, BWD>(p, grid, stream);
+        QD_ODD(8, 4) QD_ODD(32, 8) QD_ODD(64, 8) QD_ODD(128, 8) QD_ODD(256, 8)
+        if constexpr (!BWD) { QD_ODD(512, 8) QD_ODD(512, 32) }
 #undef QD_ODD
-        return cudaErrorInvalidValue;
-    }
-    if constexpr (BWD) {
-        const long long most = 8LL * kSMs;
-        const dim3 sums((unsigned)(p.rows < most ? p.rows : most)), cols((unsigned)q.tiles, (unsigned)q.ctas);
-        cudaError_t e;
-        if (p.width % V == 0) {
-            e = go(k_wide_sums<IO, V, ADDED>, sums, kWideThreads, 0, p, stream);
-            return e != cudaSuccess ? e : go(k_wide_cols<IO, V, ADDED>, cols, kWideThreads, 0, p, stream);
-        }
-        e = go(k_wide_sums<IO, 1, ADDED>, sums, kWideThreads, 0, p, stream);
-        return e != cudaSuccess ? e : go(k_wide_cols<IO, 1, ADDED>, cols, kWideThreads, 0, p, stream);
     }
     return cudaErrorInvalidValue;
 }

@@ -11,7 +11,7 @@
 namespace qd {
 namespace {
 
-constexpr int kRotaryThreads = 256, kRotaryPairs = 2048;      // sines in shared memory
+constexpr int kRotaryThreads = 256, kRotaryPairs = 2048, kOpen = 2;      // sines in shared memory; units a thread has under way
 
 struct RotaryP {
     const void *q, *k;
@@ -45,40 +45,73 @@ __global__ void __launch_bounds__(kRotaryThreads) k_rotary(const RotaryP p) {
         s_sin[i] = p.scale * (((quarter & 2) != 0) != p.inverse ? -y : y);
     }
     __syncthreads();
-    const int heads = p.Hq + p.Hk, all = p.units + p.rest, items = n * heads * all;
-    for (int i = blockIdx.y * kRotaryThreads + threadIdx.x; i < items; i += gridDim.y * kRotaryThreads) {
-        const int unit = i % all, th = i / all, head = th % heads, t = th / heads;
-        const bool is_q = head < p.Hq;
-        const long long at = is_q ? ((first + t) * p.Hq + head) * p.d : ((first + t) * p.Hk + head - p.Hq) * p.d;
-        const IO* src = static_cast<const IO*>(is_q ? p.q : p.k) + at;
-        IO* dst = static_cast<IO*>(is_q ? p.qo : p.ko) + at;
-        if (unit >= p.units) {                                                        // behind the pairs
-            const int c = 2 * p.pairs + (unit - p.units) * N;
-            store_pack(dst + c, load_pack<IO, N>(src + c, p.d - c, p.wide), p.d - c, p.wide);
-            continue;
+    const int heads = p.Hq + p.Hk, all = p.units + p.rest, items = n * heads * all, stride = gridDim.y * kRotaryThreads;
+    // a thread's next unit is `stride` further: unit, head and token of it without a division
+    const int step_u = stride % all, step_h = stride / all % heads, step_t = stride / all / heads;
+    int i0 = blockIdx.y * kRotaryThreads + threadIdx.x, nu = i0 % all, nh = i0 / all % heads, nt = i0 / all / heads;
+    // kOpen units of a thread at a time: all loads, then all stores (which might be to where the next loads read)
+    for (; i0 < items; i0 += kOpen * stride) {
+        Pack<IO, N> x[kOpen], y[INTERLEAVED ? 1 : kOpen];
+        IO* dst[kOpen];
+        int unit[kOpen], at[kOpen];                            // unit of the head, and where its sines begin
+#pragma unroll
+        for (int o = 0; o < kOpen; ++o) {
+            if (i0 + o * stride >= items) break;
+            const int head = nh, t = nt;
+            unit[o] = nu;
+            at[o] = t * p.pairs + nu * P;
+            nu += step_u; nh += step_h; nt += step_t;
+            if (nu >= all) { nu -= all; ++nh; }
+            if (nh >= heads) { nh -= heads; ++nt; }
+            const bool is_q = head < p.Hq;
+            const long long to = is_q ? ((first + t) * p.Hq + head) * p.d : ((first + t) * p.Hk + head - p.Hq) * p.d;
+            const int c = unit[o] < p.units ? unit[o] * N : 2 * p.pairs + (unit[o] - p.units) * N;
+            const IO* src = static_cast<const IO*>(is_q ? p.q : p.k) + to + c;
+            dst[o] = static_cast<IO*>(is_q ? p.qo : p.ko) + to + c;
+            const bool turned = unit[o] < p.units;
+            x[o] = load_pack<IO, N>(src, turned ? N : p.d - c, p.wide);
+            if constexpr (!INTERLEAVED)
+                if (turned) y[o] = load_pack<IO, N>(src + p.pairs, N, p.wide);
         }
-        const float *cs = s_cos + t * p.pairs + unit * P, *sn = s_sin + t * p.pairs + unit * P;
-        if constexpr (INTERLEAVED) {
-            const Pack<IO, N> x = load_pack<IO, N>(src + unit * N, N, p.wide);
-            float o[N];
 #pragma unroll
-            for (int j = 0; j < P; ++j) {
-                const float a = pick(x, 2 * j), b = pick(x, 2 * j + 1);
-                o[2 * j] = a * cs[j] - b * sn[j];
-                o[2 * j + 1] = a * sn[j] + b * cs[j];
+        for (int o = 0; o < kOpen; ++o) {
+            if (i0 + o * stride >= items) break;
+            if (unit[o] >= p.units) {                           // behind the pairs
+                store_pack(dst[o], x[o], p.d - 2 * p.pairs - (unit[o] - p.units) * N, p.wide);
+                continue;
             }
-            store_pack(dst + unit * N, narrow<IO, N>(o), N, p.wide);
-        } else {
-            const Pack<IO, N> x = load_pack<IO, N>(src + unit * N, N, p.wide), y = load_pack<IO, N>(src + p.pairs + unit * N, N, p.wide);
-            float o[N], u[N];
+            float cs[P], sn[P];
+            if constexpr (P % 4 == 0) {                         // pairs are a multiple of P, so at[o] is
 #pragma unroll
-            for (int j = 0; j < P; ++j) {
-                const float a = pick(x, j), b = pick(y, j);
-                o[j] = a * cs[j] - b * sn[j];
-                u[j] = a * sn[j] + b * cs[j];
+                for (int j = 0; j < P; j += 4) {
+                    const float4 c4 = *reinterpret_cast<const float4*>(s_cos + at[o] + j), s4 = *reinterpret_cast<const float4*>(s_sin + at[o] + j);
+                    cs[j] = c4.x; cs[j + 1] = c4.y; cs[j + 2] = c4.z; cs[j + 3] = c4.w;
+                    sn[j] = s4.x; sn[j + 1] = s4.y; sn[j + 2] = s4.z; sn[j + 3] = s4.w;
+                }
+            } else {
+#pragma unroll
+                for (int j = 0; j < P; ++j) { cs[j] = s_cos[at[o] + j]; sn[j] = s_sin[at[o] + j]; }
             }
-            store_pack(dst + unit * N, narrow<IO, N>(o), N, p.wide);
-            store_pack(dst + p.pairs + unit * N, narrow<IO, N>(u), N, p.wide);
+            if constexpr (INTERLEAVED) {
+                float u[N];
+#pragma unroll
+                for (int j = 0; j < P; ++j) {
+                    const float a = pick(x[o], 2 * j), b = pick(x[o], 2 * j + 1);
+                    u[2 * j] = a * cs[j] - b * sn[j];
+                    u[2 * j + 1] = a * sn[j] + b * cs[j];
+                }
+                store_pack(dst[o], narrow<IO, N>(u), N, p.wide);
+            } else {
+                float u[N], v[N];
+#pragma unroll
+                for (int j = 0; j < P; ++j) {
+                    const float a = pick(x[o], j), b = pick(y[o], j);
+                    u[j] = a * cs[j] - b * sn[j];
+                    v[j] = a * sn[j] + b * cs[j];
+                }
+                store_pack(dst[o], narrow<IO, N>(u), N, p.wide);
+                store_pack(dst[o] + p.pairs, narrow<IO, N>(v), N, p.wide);
+            }
         }
     }
 }
