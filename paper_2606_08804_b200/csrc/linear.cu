@@ -113,11 +113,11 @@ cudaError_t linear_fwd(const LinearArgs& a) {
     const int dk = a.s.dk, dv = a.s.dv;
     const bool cut = l.p.segments > 1;
     if (cut) {
-        cudaError_t e = walk(l.p, {LinearWalk{nullptr, a.k, a.v, nullptr, nullptr, nullptr, l.ends[0], 0, 0}}, dk, dv, a, true);
+        cudaError_t e = walk(l.p, {LinearWalk{nullptr, a.k, a.v, nullptr, nullptr, nullptr, l.ends[0], 0, a.hT != nullptr, 0}}, dk, dv, a, true);
         if (e == cudaSuccess) e = join(l.p, {LinearJoin{a.h0, l.ends[0], 0}}, a);
         if (e != cudaSuccess) return e;
     }
-    return walk(l.p, {LinearWalk{a.q, a.k, a.v, a.o, cut ? l.ends[0] : a.h0, a.hT, nullptr, 0, 0}}, dk, dv, a, !cut);
+    return walk(l.p, {LinearWalk{a.q, a.k, a.v, a.o, cut ? l.ends[0] : a.h0, a.hT, nullptr, 0, a.hT != nullptr, 0}}, dk, dv, a, !cut);
 }
 
 cudaError_t linear_bwd(const LinearArgs& a) {
@@ -125,14 +125,14 @@ cudaError_t linear_bwd(const LinearArgs& a) {
     const int dk = a.s.dk, dv = a.s.dv;
     const bool cut = l.p.segments > 1;
     if (cut) {
-        cudaError_t e = walk(l.p, {LinearWalk{nullptr, a.k, a.v, nullptr, nullptr, nullptr, l.ends[0], 0, 0},
-                                   LinearWalk{nullptr, a.q, a.dO, nullptr, nullptr, nullptr, l.ends[1], 1, 0}}, dk, dv, a, true);
+        cudaError_t e = walk(l.p, {LinearWalk{nullptr, a.k, a.v, nullptr, nullptr, nullptr, l.ends[0], 0, 0, 0},
+                                   LinearWalk{nullptr, a.q, a.dO, nullptr, nullptr, nullptr, l.ends[1], 1, a.dh0 != nullptr, 0}}, dk, dv, a, true);
         if (e == cudaSuccess) e = join(l.p, {LinearJoin{a.h0, l.ends[0], 0}, LinearJoin{a.dhT, l.ends[1], 1}}, a);
         if (e != cudaSuccess) return e;
     }
     const float *h = cut ? l.ends[0] : a.h0, *dh = cut ? l.ends[1] : a.dhT;
-    const LinearWalk wq{a.dO, a.v, a.k, a.dq, h, nullptr, nullptr, 0, 1}, wk{a.v, a.dO, a.q, a.dk, dh, nullptr, nullptr, 1, 1},
-        wv{a.k, a.q, a.dO, a.dv, dh, a.dh0, nullptr, 1, 0};
+    const LinearWalk wq{a.dO, a.v, a.k, a.dq, h, nullptr, nullptr, 0, 0, 1}, wk{a.v, a.dO, a.q, a.dk, dh, nullptr, nullptr, 1, 0, 1},
+        wv{a.k, a.q, a.dO, a.dv, dh, a.dh0, nullptr, 1, a.dh0 != nullptr, 0};
     if (dk == dv) return walk(l.p, {wq, wk, wv}, dk, dv, a, !cut);
     const cudaError_t e = walk(l.p, {wq, wk}, dv, dk, a, !cut);
     return e == cudaSuccess ? walk(l.p, {wv}, dk, dv, a, false) : e;

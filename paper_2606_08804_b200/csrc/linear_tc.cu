@@ -1,8 +1,9 @@
 // Linear attention in bf16 on the tensor cores: a walk (linear.cuh) over chunks of 128 tokens to a CTA, every product a tcgen05.mma:
 //     P = (a b^T) o D  (rounded to bf16 as the next operand)      out = P c + rho (a S)      S <- e^{g n} S + (kappa b)^T c
 // The state stays in fp32 registers; each chunk's sum comes from tensor memory and is added there (the tensor cores cut as they accumulate).
-// For a S it goes to shared memory in bf16.  In S the factor kappa stands with c, in three bf16 planes, which hold all of its 24 bits: with two
-// the state is 2.4e-6 of its length off, which is more than a whole fp32 sum over a sequence is.
+// For a S it goes to shared memory in bf16.  In S the factor kappa stands with c.  Where the state is returned it does so in three bf16 planes,
+// which hold all of its 24 bits: with two the state is 2.4e-6 of its length off, which is more than a whole fp32 sum over a sequence is.
+// Where it is not, it serves bf16 outputs alone, and kappa c is rounded to bf16 once, as the state is when it becomes an operand.
 //
 // Bound by HBM where there are CTAs enough: per token and head two tensors of its width in and one out besides c, 2.5 us (some 5000 cycles)
 // a chunk of 128 x 128 with 128 CTAs; the products of a chunk are 3072 cycles.  Next to that it is shared memory, 128 bytes a cycle, which
@@ -68,7 +69,7 @@ __global__ void __launch_bounds__(kTcThreads, 1) k_linear_tc(const __grid_consta
     const int walk = blockIdx.x % p.walks, cta = blockIdx.x / p.walks, segment = cta % p.segments, bh = cta / p.segments;
     const int b = bh / p.H, hh = bh % p.H;
     const LinearWalk& w = p.w[walk];
-    const bool reverse = w.reverse;
+    const bool reverse = w.reverse, exact = w.exact;
     const int first = segment * p.length, end = min(p.T, first + p.length), chunks = (end - first + kTokens - 1) / kTokens;
     auto token0 = [&](int n) { return first + (reverse ? chunks - 1 - n : n) * kTokens; };
 
@@ -127,9 +128,15 @@ __global__ void __launch_bounds__(kTcThreads, 1) k_linear_tc(const __grid_consta
 #pragma unroll
             for (int k = 0; k < 8; ++k)
                 x[k] = mul2(pack2(kappa[k & ~1], kappa[k | 1]), pack2(__uint_as_float(raw[k] << 16), __uint_as_float(raw[k] & 0xffff0000u)));
+            uint32_t r[8];
+            if (!exact) {
+#pragma unroll
+                for (int k = 0; k < 8; ++k) { const float2 v = unpack2(x[k]); r[k] = pack_bf16(v.x, v.y); }
+                tmem_st_frag4(tmem_addr(to, 16 * half, 0), r);
+                continue;
+            }
 #pragma unroll
             for (int m = 0; m < 3; ++m) {                                             // cut to 8 bits, three times: nothing is left of 24
-                uint32_t r[8];
 #pragma unroll
                 for (int k = 0; k < 8; ++k) r[k] = cut(x[k]);
                 tmem_st_frag4(tmem_addr(to, 16 * half, m * L::kPlane), r);
@@ -327,8 +334,8 @@ __global__ void __launch_bounds__(kTcThreads, 1) k_linear_tc(const __grid_consta
             const int i = n * kParts + q;
             if (!all(wait(&bar_k[q], n & 1))) return false;
             tc_fence_after();
-#pragma unroll
-            for (int m = 0; m < 3; ++m)
+#pragma unroll 1
+            for (int m = 0; m < (exact ? 3 : 1); ++m)
                 umma_product_ts_w<true, DC>(tKV, tPlanes + ((i & 1) * 3 + m) * L::kPlane, tile(n * kPer) + q * kPart * 128, blk, DB, kPart, q + m > 0, issue);
             umma_commit_w(&bar_kq[q], issue);
             return true;

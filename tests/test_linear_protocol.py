@@ -14,7 +14,7 @@ static std::string one(const std::string& name, const emu::Scenario& s, int i) {
     LinearP p{};
     p.T = 128 * chunks - (i % 3) * 40; p.H = 1; p.BH = 1; p.segments = 1; p.length = 128 * chunks; p.g = f(); p.scale = 1.f; p.status = u(); p.walks = 1;
     LinearWalk& w = p.w[0];
-    w.a = w.b = w.c = f(); w.out = h(); w.sT = f(); w.ends = f(); w.reverse = i & 1; w.flip = i >> 1 & 1;
+    w.a = w.b = w.c = f(); w.out = h(); w.sT = f(); w.ends = f(); w.reverse = i & 1; w.flip = i >> 1 & 1; w.exact = i >> 2 & 1;
     auto go = [&](auto kern, int db, int dc) {
         LinearMaps m{};
         m.a[0] = m.b[0] = box(128 * 64 * 2); m.c[0] = box(128 * 64 * 2); m.out[0] = box(0);
