@@ -103,43 +103,50 @@ __global__ void __launch_bounds__(kTcThreads, 1) k_linear_tc(const __grid_consta
     auto slot = [&](int m) { return sRing + m % kRing * L::kSlot; };
     auto full = [&](int m) { return wait(&bar_full[m % kRing], (m / kRing) & 1); };
 
-    // kappa c of part q, transposed: a column of c to a lane of tensor memory
+    // kappa c of part q, transposed: a column of c to a lane of tensor memory.  Four parts of 32 tokens in three planes, or two of 64 in one.
+    const int parts = exact ? kParts : kParts / 2;
     auto planes = [&](int n, int q) {
-        const int i = n * kParts + q, live = min(kTokens, end - token0(n)), late = reverse ? 0 : kTokens - live;
-        if (i >= 2 && !all(wait(&bar_kq[(q + 2) % kParts], (i - 2) / kParts & 1))) return false;       // the part before in this place
-        float kappa[8];
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            const int t = q * kPart + 8 * (e >> 1) + 2 * (lane & 3) + (e & 1);
-            kappa[e] = s_k[t >= live ? kTokens : t + late];
-        }
+        const int live = min(kTokens, end - token0(n)), late = reverse ? 0 : kTokens - live;
+        // the part before in this place: two parts before
+        const int before = q < 2 ? q + parts - 2 : q - 2;
+        if ((n > 0 || q >= 2) && !all(wait(&bar_kq[before], (q < 2 ? n - 1 : n) & 1))) return false;
         const unsigned char* tile = slot(n * kPer + kC);
-        const uint32_t to = tmem_addr(tPlanes, lanes, (i & 1) * 3 * L::kPlane);
+        uint32_t to = tmem_addr(tPlanes, lanes, (q & 1) * 3 * L::kPlane);
         constexpr int kHalves = DC == 128 ? 2 : 1;                                    // 64 rows: 16 to each of a warpgroup's four warps
 #pragma unroll 1
-        for (int half = 0; half < kHalves; ++half) {
-            uint32_t raw[8];
-            const int col = (DC == 128 ? 32 * wq + 16 * half : 16 * wq) + ((lane >> 3) & 1) * 8;
+        for (int sub = 0; sub < (exact ? 1 : 2); ++sub, to += L::kPlane) {
+            const int first_t = (exact ? q : 2 * q + sub) * kPart;
+            float kappa[8];
 #pragma unroll
-            for (int k = 0; k < 2; ++k)
-                ldsm4<true>(tile + (col >> 6) * kTokens * 128 + sw128_chunk(q * kPart + 16 * k + (lane >> 4) * 8 + (lane & 7), (col >> 3) & 7),
-                            raw + 4 * k);
-            f2 x[8];
-#pragma unroll
-            for (int k = 0; k < 8; ++k)
-                x[k] = mul2(pack2(kappa[k & ~1], kappa[k | 1]), pack2(__uint_as_float(raw[k] << 16), __uint_as_float(raw[k] & 0xffff0000u)));
-            uint32_t r[8];
-            if (!exact) {
-#pragma unroll
-                for (int k = 0; k < 8; ++k) { const float2 v = unpack2(x[k]); r[k] = pack_bf16(v.x, v.y); }
-                tmem_st_frag4(tmem_addr(to, 16 * half, 0), r);
-                continue;
+            for (int e = 0; e < 8; ++e) {
+                const int t = first_t + 8 * (e >> 1) + 2 * (lane & 3) + (e & 1);
+                kappa[e] = s_k[t >= live ? kTokens : t + late];
             }
+#pragma unroll 1
+            for (int half = 0; half < kHalves; ++half) {
+                uint32_t raw[8];
+                const int col = (DC == 128 ? 32 * wq + 16 * half : 16 * wq) + ((lane >> 3) & 1) * 8;
 #pragma unroll
-            for (int m = 0; m < 3; ++m) {                                             // cut to 8 bits, three times: nothing is left of 24
+                for (int k = 0; k < 2; ++k)
+                    ldsm4<true>(tile + (col >> 6) * kTokens * 128 + sw128_chunk(first_t + 16 * k + (lane >> 4) * 8 + (lane & 7), (col >> 3) & 7),
+                                raw + 4 * k);
+                f2 x[8];
 #pragma unroll
-                for (int k = 0; k < 8; ++k) r[k] = cut(x[k]);
-                tmem_st_frag4(tmem_addr(to, 16 * half, m * L::kPlane), r);
+                for (int k = 0; k < 8; ++k)
+                    x[k] = mul2(pack2(kappa[k & ~1], kappa[k | 1]), pack2(__uint_as_float(raw[k] << 16), __uint_as_float(raw[k] & 0xffff0000u)));
+                uint32_t r[8];
+                if (!exact) {
+#pragma unroll
+                    for (int k = 0; k < 8; ++k) { const float2 v = unpack2(x[k]); r[k] = pack_bf16(v.x, v.y); }
+                    tmem_st_frag4(tmem_addr(to, 16 * half, 0), r);
+                    continue;
+                }
+#pragma unroll
+                for (int m = 0; m < 3; ++m) {                                         // cut to 8 bits, three times: nothing is left of 24
+#pragma unroll
+                    for (int k = 0; k < 8; ++k) r[k] = cut(x[k]);
+                    tmem_st_frag4(tmem_addr(to, 16 * half, m * L::kPlane), r);
+                }
             }
         }
         tmem_st_wait();
@@ -234,7 +241,7 @@ __global__ void __launch_bounds__(kTcThreads, 1) k_linear_tc(const __grid_consta
 #pragma unroll 1
         for (int i = 0; i <= 2 * chunks && ok; ++i) {              // half chunks, and the last chunk's output
             const int n = i >> 1;
-            if (n < chunks) ok = all(full(n * kPer + kC)) && planes(n, (i & 1) * 2 + group);
+            if (n < chunks && (exact || !(i & 1))) ok = all(full(n * kPer + kC)) && planes(n, (i & 1) * 2 + group);
             if (!ENDS && ok && !(i & 1)) {
                 if (n > 0) ok = output(n - 1);
                 if (n < chunks) ok = ok && weights(n);
@@ -331,12 +338,12 @@ __global__ void __launch_bounds__(kTcThreads, 1) k_linear_tc(const __grid_consta
             return true;
         };
         auto part = [&](int n, int q) {
-            const int i = n * kParts + q;
             if (!all(wait(&bar_k[q], n & 1))) return false;
             tc_fence_after();
 #pragma unroll 1
-            for (int m = 0; m < (exact ? 3 : 1); ++m)
-                umma_product_ts_w<true, DC>(tKV, tPlanes + ((i & 1) * 3 + m) * L::kPlane, tile(n * kPer) + q * kPart * 128, blk, DB, kPart, q + m > 0, issue);
+            for (int m = 0; m < (exact ? 3 : 2); ++m)              // planes of the same tokens, or tokens
+                umma_product_ts_w<true, DC>(tKV, tPlanes + ((q & 1) * 3 + m) * L::kPlane, tile(n * kPer) + (exact ? q : 2 * q + m) * kPart * 128, blk, DB,
+                                            kPart, q + m > 0, issue);
             umma_commit_w(&bar_kq[q], issue);
             return true;
         };
@@ -347,9 +354,9 @@ __global__ void __launch_bounds__(kTcThreads, 1) k_linear_tc(const __grid_consta
                 tc_fence_after();
                 bool ok = true;
 #pragma unroll 1
-                for (int q = 0; q < kParts && ok; ++q) {
+                for (int q = 0; q < parts && ok; ++q) {
                     ok = part(n, q);
-                    if (ENDS || q != 1 || !ok) continue;
+                    if (ENDS || q != parts / 2 - 1 || !ok) continue;
                     ok = all(wait(&bar_h, n & 1)) && (n == 0 || all(wait(&bar_of, (n - 1) & 1)));
                     if (!ok) break;
                     tc_fence_after();
