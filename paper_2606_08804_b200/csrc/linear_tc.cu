@@ -1,5 +1,8 @@
 // Linear attention in bf16 on the tensor cores: a walk (linear.cuh) over chunks of 128 tokens to a CTA, every product a tcgen05.mma:
 //     P = (a b^T) o D  (rounded to bf16 as the next operand)      out = P c + rho (a S)      S <- e^{g n} S + (kappa b)^T c
+// Row r of out has the factor e^{g (r - 63)} (backward e^{g (64 - r)}) in all its terms, which is multiplied in last: what is left of D and rho
+// depends on the column alone, and is at most e^{64 |g|} either way.  Heads with |g| > 0.7, where that would leave the range in which bf16 and
+// fp32 round alike, form D as it stands and multiply a S by rho between the two products.
 // The state stays in fp32 registers; each chunk's sum comes from tensor memory and is added there (the tensor cores cut as they accumulate).
 // For a S it goes to shared memory in bf16.  In S the factor kappa stands with c.  Where the state is returned it does so in three bf16 planes,
 // which hold all of its 24 bits: with two the state is 2.4e-6 of its length off, which is more than a whole fp32 sum over a sequence is.
@@ -13,7 +16,7 @@
 // through a's.
 //   warps 0-7    two warpgroups, alike: planes, every second part; P, half of the columns, from tensor memory and back to it; out, half of the
 //                columns, staged in a's tile, stored by TMA
-//   warps 8-15   state, transposed: a column of S to a lane, half of the rows to a warpgroup; a S times rho
+//   warps 8-15   state, transposed: a column of S to a lane, half of the rows to a warpgroup; a S times rho, if |g| > 0.7
 //   warp 16      issues the products;  warp 17  loads
 // All waits are bounded; on expiry the status word says so, everybody leaves, what is in flight is waited for.
 #include "linear.cuh"
@@ -45,7 +48,7 @@ struct TcLinear {
     static constexpr int kPlane = kPart / 2;                          // columns of tensor memory: scores, out, sum, planes
     static constexpr int kOut = ENDS ? 0 : kTokens, kSum = ENDS ? 0 : kOut + DC, kPlanes = kSum + DB, kUsed = kPlanes + 6 * kPlane;
     static constexpr int kColumns = kUsed > 256 ? 512 : kUsed > 128 ? 256 : 128;
-    static_assert(kSmem <= 232448 - 1024, "shared memory");
+    static_assert(kSmem <= 232448 - 2048, "the tables and barriers below need the rest");
 };
 
 template <int DB, int DC, bool ENDS>
@@ -61,8 +64,7 @@ __global__ void __launch_bounds__(kTcThreads, 1) k_linear_tc(const __grid_consta
     __shared__ uint64_t bar_full[kRing], bar_s, bar_o2, bar_o, bar_c[2], bar_kv[2], bar_kq[kParts], bar_p, bar_os, bar_k[kParts], bar_h, bar_of, bar_kr, bar_af[2], bar_end;
     __shared__ uint32_t tmem_slot;
     __shared__ volatile int s_abort;
-    __shared__ float s_d[2 * kTokens];                                    // D(|m|), m from -128
-    __shared__ __align__(16) float s_e[32];                                        // from the nearest of 32 columns to each
+    __shared__ __align__(16) float s_d[2 * kTokens];          // what is left of D for a column; or, |g| > 0.7, D(|m|), m from -128
     __shared__ float s_k[kTokens + 1];                                             // kappa of a whole chunk; 0 behind it
 
     const int tid = threadIdx.x, warp = warp_index(), lane = tid & 31, wq = warp & 3;
@@ -86,10 +88,10 @@ __global__ void __launch_bounds__(kTcThreads, 1) k_linear_tc(const __grid_consta
     if (warp == 0) { tmem_alloc(&tmem_slot, L::kColumns); tmem_relinquish(); }
     grid_dep_wait();
     grid_dep_launch();
-    const float g2 = p.g[hh] * 1.4426950408889634f;
-    if (tid < 2 * kTokens) s_d[tid] = p.scale * decay_power(g2, abs(tid - kTokens));
+    const float g = p.g[hh], g2 = g * 1.4426950408889634f;
+    const bool steep = !(fabsf(g) <= 0.7f);
+    if (tid < 2 * kTokens) s_d[tid] = p.scale * decay_power(g2, steep ? abs(tid - kTokens) : reverse ? tid - 64 : 63 - tid);
     if (tid <= kTokens) s_k[tid] = tid == kTokens ? 0.f : reverse ? p.scale * decay_power(g2, tid + 1) : decay_power(g2, kTokens - 1 - tid);
-    if (tid < 32) s_e[tid] = decay_power(g2, reverse ? tid : 31 - tid);
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
@@ -165,6 +167,7 @@ __global__ void __launch_bounds__(kTcThreads, 1) k_linear_tc(const __grid_consta
         // (planes and weights written out: 12000 cycles a chunk).
         const int r = (int)lanes + lane, group = warp >> 2;
         const float* far = s_d + kTokens + r;
+        const float last = steep ? 1.f : decay_power(g2, reverse ? 64 - r : r - 63);
         constexpr bool kSplit = DC == 128;                         // else the second group has all of out: 64 columns are one box
         int stored = -1;                                           // chunk whose output this thread has stored and not seen read
         auto output = [&](int n) {
@@ -179,6 +182,11 @@ __global__ void __launch_bounds__(kTcThreads, 1) k_linear_tc(const __grid_consta
             for (int j = 0; j < 4; ++j) {
                 tmem_ld_wait();
                 if (j < 3) tmem_ld16(from + 16 * j + 16, x[(j + 1) & 1]);
+#pragma unroll
+                for (int e = 0; e < 16; e += 2) {
+                    const float2 y = unpack2(mul2(pack2(x[j & 1][e], x[j & 1][e + 1]), both(last)));
+                    x[j & 1][e] = y.x; x[j & 1][e + 1] = y.y;
+                }
 #pragma unroll
                 for (int ch = 0; ch < 2; ++ch) sts128(stage + sw128_chunk(r, 2 * j + ch), pack8(x[j & 1] + 8 * ch));
             }
@@ -209,17 +217,20 @@ __global__ void __launch_bounds__(kTcThreads, 1) k_linear_tc(const __grid_consta
                     float v[32];
                     tmem_ld32(tmem_addr(tS, lanes, 32 * j), v);
                     tmem_ld_wait();
-                    if (j == wq) {                                 // an infinite product past the diagonal leaves nothing either
+                    if (steep) {
 #pragma unroll
-                        for (int e = 0; e < 32; ++e) v[e] = (reverse ? e >= lane : e <= lane) ? v[e] * far[-32 * j - e] : 0.f;
+                        for (int e = 0; e < 32; ++e) v[e] *= far[-32 * j - e];
                     } else {
-                        const float near = far[reverse ? -32 * j : -32 * j - 31];
 #pragma unroll
                         for (int e = 0; e < 32; e += 4) {
-                            const float4 t = *reinterpret_cast<const float4*>(s_e + e);
-                            v[e] *= near * t.x; v[e + 1] *= near * t.y; v[e + 2] *= near * t.z; v[e + 3] *= near * t.w;
+                            const float4 t = *reinterpret_cast<const float4*>(s_d + 32 * j + e);
+                            const float2 x = unpack2(mul2(pack2(v[e], v[e + 1]), pack2(t.x, t.y))), y = unpack2(mul2(pack2(v[e + 2], v[e + 3]), pack2(t.z, t.w)));
+                            v[e] = x.x; v[e + 1] = x.y; v[e + 2] = y.x; v[e + 3] = y.y;
                         }
                     }
+                    if (j == wq)                                   // an infinite product past the diagonal leaves nothing either
+#pragma unroll
+                        for (int e = 0; e < 32; ++e) v[e] = (reverse ? e >= lane : e <= lane) ? v[e] : 0.f;
 #pragma unroll
                     for (int e = 0; e < 16; ++e) o[e] = pack_bf16(v[2 * e], v[2 * e + 1]);
                 }
@@ -266,19 +277,27 @@ __global__ void __launch_bounds__(kTcThreads, 1) k_linear_tc(const __grid_consta
 #pragma unroll
             for (int i = 0; i < HC; ++i) h[i] = entry ? __ldcg(entry + place(i)) : 0.f;
         }
-        auto put = [&]() {
+        auto put = [&](int n) {                                    // as chunk n's operand
             if (ENDS) return;
+            const float f = steep ? 1.f : reverse ? decay_power(g2, min(kTokens, end - token0(n)) - 65) : p.scale * decay_power(g2, 64);
             if (live_row)
 #pragma unroll
-                for (int ch = 0; ch < HC / 8; ++ch)
-                    sts128(sState + (c0 + 8 * ch) / 64 * (DC * 128) + sw128_chunk(r, ((c0 >> 3) + ch) & 7), pack8(h + 8 * ch));
+                for (int ch = 0; ch < HC / 8; ++ch) {
+                    float x[8];
+#pragma unroll
+                    for (int e = 0; e < 8; e += 2) {
+                        const float2 y = unpack2(mul2(pack2(h[8 * ch + e], h[8 * ch + e + 1]), both(f)));
+                        x[e] = y.x; x[e + 1] = y.y;
+                    }
+                    sts128(sState + (c0 + 8 * ch) / 64 * (DC * 128) + sw128_chunk(r, ((c0 >> 3) + ch) & 7), pack8(x));
+                }
             fence_proxy_async();
             arrive(&bar_h);
         };
-        put();
+        put(0);
         for (int n = 0; n < chunks; ++n) {
             const int live = min(kTokens, end - token0(n)), row = (int)lanes + lane;
-            if (!ENDS) {                                           // a S times rho, half of the columns to a warpgroup
+            if (!ENDS && steep) {                                  // a S times rho, half of the columns to a warpgroup
                 const float rho = row >= live ? 0.f : reverse ? decay_power(g2, live - 1 - row) : p.scale * decay_power(g2, row + 1);
                 if (!all(wait(&bar_o2, n & 1))) break;
                 tc_fence_after();
@@ -310,7 +329,7 @@ __global__ void __launch_bounds__(kTcThreads, 1) k_linear_tc(const __grid_consta
             }
             tc_fence_before();
             arrive(&bar_kr);
-            if (n + 1 < chunks) put();
+            if (n + 1 < chunks) put(n + 1);
         }
         float* left = ENDS ? w.ends + ((size_t)bh * p.segments + segment) * size
                            : segment == (reverse ? 0 : p.segments - 1) && w.sT ? w.sT + (size_t)bh * size : nullptr;
@@ -366,7 +385,7 @@ __global__ void __launch_bounds__(kTcThreads, 1) k_linear_tc(const __grid_consta
                 if (!ok) break;
                 umma_commit_w(&bar_kv[n & 1], issue);
                 if (!ENDS) {
-                    if (!all(wait(&bar_p, n & 1)) || !all(wait(&bar_os, n & 1))) break;
+                    if (!all(wait(&bar_p, n & 1)) || (steep && !all(wait(&bar_os, n & 1)))) break;
                     tc_fence_after();
 #pragma unroll
                     for (int g = 0; g < 2; ++g)                    // of either warpgroup

@@ -12,7 +12,7 @@ ONE = r"""
 static std::string one(const std::string& name, const emu::Scenario& s, int i) {
     const int chunks = 1 + i % 7;
     LinearP p{};
-    p.T = 128 * chunks - (i % 3) * 40; p.H = 1; p.BH = 1; p.segments = 1; p.length = 128 * chunks; p.g = f(); p.scale = 1.f; p.status = u(); p.walks = 1;
+    p.T = 128 * chunks - (i % 3) * 40; p.H = 1; p.BH = 1; p.segments = 1; p.length = 128 * chunks; p.g = f() + 1024; F[1024] = i & 16 ? -1.f : -0.01f; p.scale = 1.f; p.status = u(); p.walks = 1;
     LinearWalk& w = p.w[0];
     w.a = w.b = w.c = f(); w.out = h(); w.sT = f(); w.ends = f(); w.reverse = i & 1; w.flip = i >> 1 & 1; w.exact = i >> 2 & 1;
     auto go = [&](auto kern, int db, int dc) {
@@ -37,7 +37,7 @@ static std::string one(const std::string& name, const emu::Scenario& s, int i) {
 # the packed arithmetic that the kernel takes from rows.cuh
 ROWS = """
 namespace qd { typedef unsigned long long f2; inline f2 pack2(float, float) { return 0; } inline float2 unpack2(f2) { return {0.f, 0.f}; }
-inline f2 mul2(f2, f2) { return 0; } inline f2 add2(f2, f2) { return 0; } }
+inline f2 mul2(f2, f2) { return 0; } inline f2 both(float) { return 0; } inline f2 add2(f2, f2) { return 0; } }
 inline unsigned __byte_perm(unsigned, unsigned, unsigned) { return 0; }
 """
 
