@@ -680,7 +680,7 @@ FusedPlan fused_plan(long long rows, int width, int dtype, bool bwd) {
     q.step = 1;
     if (odd) {
         q.k = width <= 32 ? 4 : width <= 4096 ? 8 : 32;
-        q.tpr = width <= 32 ? 8 : 32;
+        q.tpr = width <= 32 ? 8 : width <= 4096 ? 32 : 512;
         while (q.tpr * q.k < width) q.tpr *= 2;
         const int rpc = fused_threads(q.tpr) / q.tpr, block = rpc * width * io;
         const long long share = rows / (rpc * 2LL * kSMs);                  // few rows: as many CTAs as there are SMs
