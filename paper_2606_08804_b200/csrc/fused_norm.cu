@@ -114,13 +114,14 @@ struct Ahead {
         return r;
     }
 };
-// CTAs to an SM that the registers are shared out for
-constexpr __host__ __device__ int fused_resident(int k, int v, int tpr, bool bwd) {
-    return tpr > 256 ? (k * v <= 16 && !bwd ? 2 : 1) : bwd ? (k * v <= 8 ? 2 : 1) : (k * v <= 8 ? 4 : k * v <= 16 ? 3 : 1);
+// CTAs to an SM that the registers are shared out for.  bf16 forward, 262144 x 128: gated 33.3 us with three (35.5 with two, 40.4 with four),
+// added, which writes as much as it reads, 44.3 with two (49.5, 54.2); backward 63.8 and 67.6 with two (70.8 and 84.0 with three).
+constexpr __host__ __device__ int fused_resident(int k, int v, int tpr, bool bwd, bool added) {
+    return tpr > 256 ? (k * v <= 16 && !bwd ? 2 : 1) : bwd ? (k * v <= 8 ? 2 : 1) : (k * v <= 8 ? 4 : k * v <= 16 ? (added ? 2 : 3) : 1);
 }
 
 template <typename IO, int V, int K, int TPR, bool ADDED>
-__global__ void __launch_bounds__(fused_threads(TPR), fused_resident(K, V, TPR, false)) k_fused_fwd(const FusedP p) {
+__global__ void __launch_bounds__(fused_threads(TPR), fused_resident(K, V, TPR, false, ADDED)) k_fused_fwd(const FusedP p) {
     constexpr int NT = fused_threads(TPR), RPC = NT / TPR;
     constexpr bool HELD = K * V <= 16;                       // scale, weight and bias stay in registers
     extern __shared__ __align__(16) unsigned char smem_rows[];
@@ -222,7 +223,7 @@ __global__ void __launch_bounds__(fused_threads(TPR), fused_resident(K, V, TPR, 
 }
 
 template <typename IO, int V, int K, int TPR, bool ADDED>
-__global__ void __launch_bounds__(fused_threads(TPR), fused_resident(K, V, TPR, true)) k_fused_bwd(const FusedP p) {
+__global__ void __launch_bounds__(fused_threads(TPR), fused_resident(K, V, TPR, true, ADDED)) k_fused_bwd(const FusedP p) {
     constexpr int NT = fused_threads(TPR), RPC = NT / TPR, SUMS = fused_sums(ADDED), STREAMS = ADDED ? 4 : 3;
     extern __shared__ __align__(16) unsigned char smem_rows[];
     __shared__ float red[2][2][32];
@@ -661,7 +662,7 @@ struct FusedPlan {
     long long ctas;          // that write a partial each
     int tiles;               // wide: CTAs side by side
 };
-FusedPlan fused_plan(long long rows, int width, int dtype, bool bwd) {
+FusedPlan fused_plan(long long rows, int width, int dtype, bool bwd, bool added) {
     const int io = dtype == QD_BF16 ? 2 : 4;
     FusedPlan q{};
     q.v = width % (16 / io) == 0 ? 16 / io : width % (4 / io) == 0 ? 4 / io : 1;
@@ -694,7 +695,7 @@ FusedPlan fused_plan(long long rows, int width, int dtype, bool bwd) {
         while (q.tpr * q.k < n) q.k *= 2;
     }
     const int rpc = fused_threads(q.tpr) / q.tpr * q.step;
-    const int resident = odd ? (q.tpr > 256 ? 1 : 4) : fused_resident(q.k, q.v, q.tpr, bwd);
+    const int resident = odd ? (q.tpr > 256 ? 1 : 4) : fused_resident(q.k, q.v, q.tpr, bwd, added);
     const long long groups = (rows + rpc - 1) / rpc, all = kSMs * (long long)resident;
     q.ctas = groups < all ? groups : all;
     return q;
@@ -744,7 +745,7 @@ cudaError_t wide(const FusedP& p, const FusedPlan& q, cudaStream_t stream) {
 template <typename IO, bool ADDED, bool BWD>
 cudaError_t launch(FusedP p, cudaStream_t stream) {
     constexpr int BIG = 16 / sizeof(IO), SMALL = 4 / sizeof(IO);
-    const FusedPlan q = fused_plan(p.rows, p.width, sizeof(IO) == 2 ? QD_BF16 : QD_F32, BWD);
+    const FusedPlan q = fused_plan(p.rows, p.width, sizeof(IO) == 2 ? QD_BF16 : QD_F32, BWD, ADDED);
     p.step = q.step;
     if (q.kind == WHOLE) return q.v == BIG ? whole<IO, BIG, ADDED, BWD>(p, q, stream) : whole<IO, SMALL, ADDED, BWD>(p, q, stream);
     if constexpr (BWD)
@@ -782,10 +783,10 @@ size_t part_floats(const FusedPlan& q, int width) { return ((size_t)q.ctas * fus
 }  // namespace
 
 size_t fused_norm_workspace(long long rows, int width, int dtype) {
-    const FusedPlan q = fused_plan(rows, width, dtype, true);
+    const FusedPlan q = fused_plan(rows, width, dtype, true, true);      // backward alike for both
     return (part_floats(q, width) + (q.kind == WIDE ? 2 * (size_t)rows : 0)) * sizeof(float);
 }
-bool fused_norm_needs_workspace(long long rows, int width, int dtype) { return fused_plan(rows, width, dtype, true).kind == WIDE; }
+bool fused_norm_needs_workspace(long long rows, int width, int dtype) { return fused_plan(rows, width, dtype, true, true).kind == WIDE; }
 
 cudaError_t fused_norm_fwd(const FusedNormArgs& a) {
     const FusedP p = fused(a);
@@ -793,7 +794,7 @@ cudaError_t fused_norm_fwd(const FusedNormArgs& a) {
 }
 cudaError_t fused_norm_bwd(const FusedNormArgs& a) {
     FusedP p = fused(a);
-    const FusedPlan q = fused_plan(a.rows, a.width, a.dtype, true);
+    const FusedPlan q = fused_plan(a.rows, a.width, a.dtype, true, a.added);
     const SumOut out{{a.dweight, a.dbias, a.added ? a.dscale : nullptr}};
     const bool sums = out.out[0] || out.out[1] || out.out[2];
     p.part = sums ? a.part : nullptr;

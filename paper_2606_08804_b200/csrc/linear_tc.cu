@@ -46,7 +46,9 @@ struct TcLinear {
     static constexpr int kState = ENDS ? 0 : DB * DC * 2;
     static constexpr int kSmem = kState + kRing * kSlot + 1024;
     static constexpr int kPlane = kPart / 2;                          // columns of tensor memory: scores, out, sum, planes
-    static constexpr int kOut = ENDS ? 0 : kTokens, kSum = ENDS ? 0 : kOut + DC, kPlanes = kSum + DB, kUsed = kPlanes + 6 * kPlane;
+    static constexpr int kOut = ENDS ? 0 : kTokens, kSum = ENDS ? 0 : kOut + DC, kPlanes = kSum + DB;
+    static constexpr int kPlaces = ENDS ? kParts : 2;                 // of parts of planes: all of a chunk's where there is room
+    static constexpr int kUsed = kPlanes + kPlaces * 3 * kPlane;
     static constexpr int kColumns = kUsed > 256 ? 512 : kUsed > 128 ? 256 : 128;
     static_assert(kSmem <= 232448 - 2048, "the tables and barriers below need the rest");
 };
@@ -109,11 +111,12 @@ __global__ void __launch_bounds__(kTcThreads, 1) k_linear_tc(const __grid_consta
     const int parts = exact ? kParts : kParts / 2;
     auto planes = [&](int n, int q) {
         const int live = min(kTokens, end - token0(n)), late = reverse ? 0 : kTokens - live;
-        // the part before in this place: two parts before
-        const int before = q < 2 ? q + parts - 2 : q - 2;
-        if ((n > 0 || q >= 2) && !all(wait(&bar_kq[before], (q < 2 ? n - 1 : n) & 1))) return false;
+        // the part before in this place: two parts before, or that of the chunk before
+        const bool same = !ENDS && q >= 2;
+        const int before = ENDS ? q : q < 2 ? q + parts - 2 : q - 2;
+        if ((n > 0 || same) && !all(wait(&bar_kq[before], (same ? n : n - 1) & 1))) return false;
         const unsigned char* tile = slot(n * kPer + kC);
-        uint32_t to = tmem_addr(tPlanes, lanes, (q & 1) * 3 * L::kPlane);
+        uint32_t to = tmem_addr(tPlanes, lanes, q % L::kPlaces * 3 * L::kPlane);
         constexpr int kHalves = DC == 128 ? 2 : 1;                                    // 64 rows: 16 to each of a warpgroup's four warps
 #pragma unroll 1
         for (int sub = 0; sub < (exact ? 1 : 2); ++sub, to += L::kPlane) {
@@ -361,7 +364,7 @@ __global__ void __launch_bounds__(kTcThreads, 1) k_linear_tc(const __grid_consta
             tc_fence_after();
 #pragma unroll 1
             for (int m = 0; m < (exact ? 3 : 2); ++m)              // planes of the same tokens, or tokens
-                umma_product_ts_w<true, DC>(tKV, tPlanes + ((q & 1) * 3 + m) * L::kPlane, tile(n * kPer) + (exact ? q : 2 * q + m) * kPart * 128, blk, DB,
+                umma_product_ts_w<true, DC>(tKV, tPlanes + (q % L::kPlaces * 3 + m) * L::kPlane, tile(n * kPer) + (exact ? q : 2 * q + m) * kPart * 128, blk, DB,
                                             kPart, q + m > 0, issue);
             umma_commit_w(&bar_kq[q], issue);
             return true;
