@@ -127,7 +127,7 @@ __global__ void __launch_bounds__(kTcThreads, 1) k_linear_tc(const __grid_consta
                 const int t = first_t + 8 * (e >> 1) + 2 * (lane & 3) + (e & 1);
                 kappa[e] = s_k[t >= live ? kTokens : t + late];
             }
-#pragma unroll 1
+#pragma unroll (ENDS ? 2 : 1)
             for (int half = 0; half < kHalves; ++half) {
                 uint32_t raw[8];
                 const int col = (DC == 128 ? 32 * wq + 16 * half : 16 * wq) + ((lane >> 3) & 1) * 8;
