@@ -79,6 +79,35 @@ def test_linear(B, T, H, dk, dv, dt, state):
         assert torch.equal(a, gr[name]), name
 
 
+@pytest.mark.parametrize("B,T,H,dk,dv,dt", [(1, 300, 6, 128, 128, BF), (2, 257, 6, 64, 64, BF), (1, 130, 6, 64, 128, F32), (1, 140, 6, 128, 64, BF),
+                                            (1, 1300, 6, 64, 64, BF), (1, 700, 6, 128, 128, F32)])
+@pytest.mark.parametrize("decay", [[-0.9, -3.0, -0.7, -0.7000001, -20.0, -100.0], [0.01, 0.0, -1e-6, 1e-30, -0.6999999, 0.004]], ids=["steep", "slight"])
+def test_linear_with_decays_of_every_size(B, T, H, dk, dv, dt, decay):
+    """Heads that forget within a few tokens, on both sides of where a row's factor is taken out of a chunk, and heads that grow (e^(g T) is at
+    most e^13 here: the exponents that count are at most 20)."""
+    from paper_2606_08804_b200 import binding as qd
+    (q, k, v, _, h0), dO, dh = _linear_inputs(B, T, H, dk, dv, dt, True, seed=5)
+    g = torch.tensor(decay, device="cuda")
+    ref, mag = [lf.f64(t) for t in (q, k, v, h0)], [_abs(lf.f64(t)) for t in (q, k, v, h0)]
+    ro, rh = f.linear(*ref[:3], g.double().cpu(), ref[3], 1.25)
+    mo, mh = f.linear(*mag[:3], g.double().cpu(), mag[3], 1.25)
+    rg = lf.grads((ro, rh), (dO.double().cpu(), dh.double().cpu()), ref)
+    mg = lf.grads((mo, mh), (dO.double().cpu().abs(), dh.double().cpu().abs()), mag)
+    still = torch.zeros_like(g).double().cpu()
+    whole = [_abs(lf.f64(t)) for t in (q, k, v, h0)]
+    wo, wh = f.linear(*whole[:3], still, whole[3], 1.25)
+    wg = lf.grads((wo, wh), (dO.double().cpu().abs(), dh.double().cpu().abs()), whole)
+    o, hT, ws = qd.linear_fwd(q, k, v, g, h0, 1.25)
+    out, st = _rounds(T, dk, dv, dt), _rounds(T, dk, dv, dt, True)
+    low = 2.0 ** -126
+    lf.close("o", o, ro, out * mo.detach() + low * (wo.detach() + T))
+    lf.close("hT", hT, rh, st * mh.detach() + low * (wh.detach() + T))
+    gr = qd.linear_bwd(q, k, v, g, h0, dO, dh, 1.25)
+    for name, r, m, s, w in zip(("dq", "dk", "dv", "dh0"), rg, mg, (out, out, out, st), wg):
+        lf.close(name, gr[name], r, s * m + low * (w + T))
+    assert qd.workspace_status(ws) == 0
+
+
 @pytest.mark.parametrize("B,H,dk,dv,dt", [(1, 1, 64, 64, F32), (3, 5, 128, 128, BF), (2, 3, 64, 128, BF), (2, 2, 128, 64, F32), (40, 16, 128, 128, BF)])
 def test_linear_steps_go_on_from_a_prompt(B, H, dk, dv, dt):
     from paper_2606_08804_b200 import binding as qd
