@@ -30,6 +30,22 @@ struct Rows4 {
             }
         }
     }
+    // zeros for elements that are infinite or NaN, which f(row, column) hears of
+    template <class F> __device__ __forceinline__ void settle(F f) {
+#pragma unroll
+        for (int i = 0; i < kN; ++i) {
+            float* const x = &r[i].x;
+            const float sum = 0.f * x[0] + 0.f * x[1] + 0.f * x[2] + 0.f * x[3];
+            if (sum == 0.f) continue;
+            const int id = i * kPlanesThreads + threadIdx.x;
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                if (!(fabsf(x[e]) < INFINITY)) {
+                    x[e] = 0.f;
+                    f(id / (W / 4), id % (W / 4) * 4 + e);
+                }
+        }
+    }
     template <class P> __device__ __forceinline__ void put(const P& d) const {
 #pragma unroll
         for (int i = 0; i < kN; ++i) {
@@ -64,6 +80,8 @@ __global__ void __launch_bounds__(kPlanesThreads, 1) k_linear_planes(const Linea
     typedef PlanesLayout<IO, DB> L;
     extern __shared__ __align__(16) unsigned char smem_planes[];
     __shared__ float s_d[kRows], s_rho[kRows], s_kappa[kRows];
+    __shared__ int s_first[kCols];                             // of every column of c the first element that is infinite or NaN, in the walk's order
+    __shared__ int s_unfit;
     const typename L::Wide A(smem_planes + L::kA), B(smem_planes + L::kB);
     const typename L::Slice Cc(smem_planes + L::kC);
     const typename L::Scaled Ch(smem_planes + L::kCh);
@@ -93,6 +111,8 @@ __global__ void __launch_bounds__(kPlanesThreads, 1) k_linear_planes(const Linea
         S.st2(r, c, x, y);
     });
     if (tid < kRows) s_d[tid] = p.scale * decay_power(g2, tid);
+    if (tid < kCols) s_first[tid] = 0x7fffffff;
+    if (tid == 0) s_unfit = 0;
 
     const int first = segment * p.length, end = min(p.T, first + p.length), chunks = (end - first + kRows - 1) / kRows;
     const size_t ld_b = (size_t)p.H * DB, ld_c = (size_t)p.H * DC;
@@ -117,8 +137,13 @@ __global__ void __launch_bounds__(kPlanesThreads, 1) k_linear_planes(const Linea
         __syncthreads();                                       // and the chunk before has been read
         if (w.out) ra.put(A);
         rb.put(B);
-        rc.put(Cc);
         rc.put(Ch, s_kappa);
+        // out's rows before a token take nothing of it, also where it is infinite or NaN; from there on its column of out is NaN
+        rc.settle([&](int r, int c) {
+            atomicMin(s_first + c, n * kRows + (w.reverse ? kRows - 1 - r : r));
+            s_unfit = 1;
+        });
+        rc.put(Cc);
         __syncthreads();
         if (n + 1 < chunks) fetch(n + 1);
         if (w.out) {
@@ -143,6 +168,11 @@ __global__ void __launch_bounds__(kPlanesThreads, 1) k_linear_planes(const Linea
                 const float f = s_rho[r];
                 x = fmaf(f, x2, x);
                 y = fmaf(f, y2, y);
+                if (s_unfit) {
+                    const int at = n * kRows + (w.reverse ? kRows - 1 - r : r);
+                    if (at >= s_first[c]) x = NAN;
+                    if (at >= s_first[c + 1]) y = NAN;
+                }
                 if constexpr (sizeof(IO) == 4) *reinterpret_cast<float2*>(o + r * ld_c + c) = make_float2(x, y);
                 else *reinterpret_cast<uint32_t*>(o + r * ld_c + c) = sm100::pack_bf16(x, y);
             });

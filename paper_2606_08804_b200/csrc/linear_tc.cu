@@ -18,6 +18,8 @@
 //                columns, staged in a's tile, stored by TMA
 //   warps 8-15   state, transposed: a column of S to a lane, half of the rows to a warpgroup; a S times rho, if |g| > 0.7
 //   warp 16      issues the products;  warp 17  loads
+// Out's rows before a token take nothing of it, also where it is infinite or NaN: the planes' warps, which read all of c, put a 0 in such an
+// element's place for P c and note its column and place; from there on the column of out is NaN (as the state is for later chunks).
 // All waits are bounded; on expiry the status word says so, everybody leaves, what is in flight is waited for.
 #include "linear.cuh"
 #include "rows.cuh"
@@ -65,8 +67,10 @@ __global__ void __launch_bounds__(kTcThreads, 1) k_linear_tc(const __grid_consta
     // runs up to two phases ahead there is one for even and one for odd phases.
     __shared__ uint64_t bar_full[kRing], bar_s, bar_o2, bar_o, bar_c[2], bar_kv[2], bar_kq[kParts], bar_p, bar_os, bar_k[kParts], bar_h, bar_of, bar_kr, bar_af[2], bar_end;
     __shared__ uint32_t tmem_slot;
-    __shared__ volatile int s_abort;
-    __shared__ __align__(16) float s_d[2 * kTokens];          // what is left of D for a column; or, |g| > 0.7, D(|m|), m from -128
+    __shared__ volatile int s_abort, s_unfit;                  // s_unfit: c has had an element that is infinite or NaN
+    // What is left of D for a column; or, |g| > 0.7, D(|m|), m from -128, of which one half counts.  In the other, for every column of c: the
+    // first element that is infinite or NaN, counted in the order of the walk.
+    __shared__ __align__(16) float s_d[2 * kTokens + 1];
     __shared__ float s_k[kTokens + 1];                                             // kappa of a whole chunk; 0 behind it
 
     const int tid = threadIdx.x, warp = warp_index(), lane = tid & 31, wq = warp & 3;
@@ -85,14 +89,18 @@ __global__ void __launch_bounds__(kTcThreads, 1) k_linear_tc(const __grid_consta
         mbar_init(&bar_h, 8); mbar_init(&bar_kr, 8);
         mbar_init(&bar_end, 1);
         mbar_init_fence();
-        s_abort = 0;
+        s_abort = s_unfit = 0;
     }
     if (warp == 0) { tmem_alloc(&tmem_slot, L::kColumns); tmem_relinquish(); }
     grid_dep_wait();
     grid_dep_launch();
     const float g = p.g[hh], g2 = g * 1.4426950408889634f;
     const bool steep = !(fabsf(g) <= 0.7f);
-    if (tid < 2 * kTokens) s_d[tid] = p.scale * decay_power(g2, steep ? abs(tid - kTokens) : reverse ? tid - 64 : 63 - tid);
+    const int other = !steep ? kTokens : reverse ? kTokens + 1 : 0;
+    volatile int* const s_first = reinterpret_cast<volatile int*>(s_d) + other;
+    if (tid <= 2 * kTokens)
+        s_d[tid] = tid >= other && tid < other + kTokens ? __int_as_float(0x7fffffff)
+                                                         : p.scale * decay_power(g2, steep ? abs(tid - kTokens) : reverse ? tid - 64 : 63 - tid);
     if (tid <= kTokens) s_k[tid] = tid == kTokens ? 0.f : reverse ? p.scale * decay_power(g2, tid + 1) : decay_power(g2, kTokens - 1 - tid);
     tc_fence_before();
     __syncthreads();
@@ -118,6 +126,7 @@ __global__ void __launch_bounds__(kTcThreads, 1) k_linear_tc(const __grid_consta
         const unsigned char* tile = slot(n * kPer + kC);
         uint32_t to = tmem_addr(tPlanes, lanes, q % L::kPlaces * 3 * L::kPlane);
         constexpr int kHalves = DC == 128 ? 2 : 1;                                    // 64 rows: 16 to each of a warpgroup's four warps
+        uint32_t seen = 0;
 #pragma unroll 1
         for (int sub = 0; sub < (exact ? 1 : 2); ++sub, to += L::kPlane) {
             const int first_t = (exact ? q : 2 * q + sub) * kPart;
@@ -136,6 +145,9 @@ __global__ void __launch_bounds__(kTcThreads, 1) k_linear_tc(const __grid_consta
                     ldsm4<true>(tile + (col >> 6) * kTokens * 128 + sw128_chunk(first_t + 16 * k + (lane >> 4) * 8 + (lane & 7), (col >> 3) & 7),
                                 raw + 4 * k);
                 f2 x[8];
+                if (!ENDS)
+#pragma unroll
+                    for (int k = 0; k < 8; ++k) see_unfit(seen, raw[k]);
 #pragma unroll
                 for (int k = 0; k < 8; ++k)
                     x[k] = mul2(pack2(kappa[k & ~1], kappa[k | 1]), pack2(__uint_as_float(raw[k] << 16), __uint_as_float(raw[k] & 0xffff0000u)));
@@ -153,6 +165,21 @@ __global__ void __launch_bounds__(kTcThreads, 1) k_linear_tc(const __grid_consta
                     tmem_st_frag4(tmem_addr(to, 16 * half, m * L::kPlane), r);
                 }
             }
+        }
+        if (!ENDS && __any_sync(0xffffffffu, seen != 0)) {                            // what this warp has read, element by element
+            const int rows = exact ? kPart : 2 * kPart, wide = DC / 4;
+            unsigned char* const mine = slot(n * kPer + kC);
+#pragma unroll 1
+            for (int i = lane; i < rows * wide; i += 32) {
+                const int t = q * rows + i / wide, col = wq * wide + i % wide;
+                volatile unsigned short* const x =
+                    reinterpret_cast<volatile unsigned short*>(mine + (col >> 6) * kTokens * 128 + sw128_chunk(t, (col >> 3) & 7)) + (col & 7);
+                if ((*x & 0x7f80) != 0x7f80) continue;
+                *x = 0;
+                atomicMin(const_cast<int*>(s_first) + col, n * kTokens + (reverse ? kTokens - 1 - t : t));
+                s_unfit = 1;
+            }
+            fence_proxy_async();
         }
         tmem_st_wait();
         tc_fence_before();
@@ -192,6 +219,13 @@ __global__ void __launch_bounds__(kTcThreads, 1) k_linear_tc(const __grid_consta
                 }
 #pragma unroll
                 for (int ch = 0; ch < 2; ++ch) sts128(stage + sw128_chunk(r, 2 * j + ch), pack8(x[j & 1] + 8 * ch));
+            }
+            if (s_unfit) {
+                const int at = n * kTokens + (reverse ? kTokens - 1 - r : r);
+#pragma unroll 1
+                for (int col = 0; col < 64; ++col)
+                    if (at >= s_first[(kSplit ? 64 * group : 0) + col])
+                        reinterpret_cast<volatile unsigned short*>(stage + sw128_chunk(r, col >> 3))[col & 7] = 0x7fff;
             }
             tc_fence_before();
             arrive(&bar_of);

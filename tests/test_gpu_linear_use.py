@@ -1,6 +1,7 @@
 """How linear attention, the norms with a gate and behind a residual sum, and rotary positions are used: in a layer, on streams, in graphs,
 through autograd, next to other buffers, in tensors past 2^32 elements."""
 import ctypes
+import math
 import threading
 
 import pytest
@@ -479,3 +480,65 @@ def test_offsets_past_32_bits():
     lone = qd.linear_steps(q[-1:].contiguous(), k[-1:].contiguous(), v[-1:].contiguous(), g[:16], one)
     lf.close("o", o[-1:], lone.double().cpu(), 2.0 ** -7 * lone.double().cpu().abs())        # fewer states: other columns to a CTA, another order
     assert torch.equal(state[-1:], one)
+
+
+# ---- infinite and NaN -------------------------------------------------------------------------------------------------------
+@pytest.mark.parametrize("T,at", [(1, 0), (40, 17), (128, 127), (200, 128), (333, 70), (1500, 1290)])
+@pytest.mark.parametrize("dk,dv,dtype", [(128, 128, torch.bfloat16), (64, 64, torch.bfloat16), (64, 128, torch.bfloat16), (128, 64, torch.bfloat16),
+                                         (64, 64, torch.float32), (128, 128, torch.float32)])
+@pytest.mark.parametrize("what", ["q", "k", "v", "dO"])
+def test_a_token_that_is_not_finite_reaches_what_follows_it(T, at, dk, dv, dtype, what):
+    """What comes before it, in the order of each walk, has the bits that it has without it; so have, of what comes after it, the columns that do
+    not take anything of it; the others are not finite."""
+    from paper_2606_08804_b200 import binding as qd
+    H, col = 4, 5
+    gen = torch.Generator(device="cuda").manual_seed(T + at)
+    n = lambda *s: torch.randn(*s, device="cuda", generator=gen).to(dtype)  # noqa: E731
+    t = {"q": n(1, T, H, dk), "k": n(1, T, H, dk), "v": n(1, T, H, dv), "dO": n(1, T, H, dv)}
+    g = torch.tensor([-0.02, -0.9, 0.0, -0.5], device="cuda")
+    h0, dhT = n(1, H, dk, dv).float(), n(1, H, dk, dv).float()
+
+    def run(state):
+        o, hT, ws = qd.linear_fwd(t["q"], t["k"], t["v"], g, h0 if state else None)
+        gr = qd.linear_bwd(t["q"], t["k"], t["v"], g, h0, t["dO"], dhT if state else None)
+        assert qd.workspace_status(ws) == 0
+        return dict(o=o, hT=hT, dq=gr["dq"], dk=gr["dk"], dv=gr["dv"], dh0=gr["dh0"])
+    heads = (0, 1, 3)                                                          # of all but the third
+    for state in (True, False):
+        clean = run(state)
+        keep = t[what].clone()
+        for e, h in enumerate(heads):
+            t[what][0, at, h, col] = (math.inf, -math.inf, math.nan)[e]
+        got = run(state)
+        t[what] = keep
+        for name in ("o", "dq", "dk", "dv"):
+            a, b = got[name][0], clean[name][0]
+            assert torch.equal(a[:, 2], b[:, 2]), name                         # another head
+            behind = name in ("o", "dq")                                       # these take what is before them, dk and dv what is behind
+            apart = slice(0, at) if behind else slice(at + 1, T)
+            own = slice(at, T) if behind else slice(0, at + 1)
+            # rows' own factors, by which a token reaches its own row alone: of o q, of dq dO, of dk v, of dv k
+            if {"o": "q", "dq": "dO", "dk": "v", "dv": "k"}[name] == what:
+                rest = torch.ones(T, dtype=torch.bool, device="cuda")
+                rest[at] = False
+                assert torch.equal(a[rest], b[rest]), name
+                assert not a[at, list(heads)].isfinite().any(), name
+            elif {"o": "dO", "dq": "q", "dk": "k", "dv": "v"}[name] == what:
+                assert torch.equal(a, b), name                                 # takes nothing of it
+            else:
+                assert torch.equal(a[apart], b[apart]), name
+                # the columns' factors: of o v, of dq k, of dk q, of dv dO, one column; else all of them
+                if {"o": "v", "dq": "k", "dk": "q", "dv": "dO"}[name] == what:
+                    hit = torch.zeros(a.shape[-1], dtype=torch.bool, device="cuda")
+                    hit[col] = True
+                    assert torch.equal(a[own][:, :, ~hit], b[own][:, :, ~hit]), name
+                    assert not a[own][:, list(heads)][..., hit].isfinite().any(), name
+                else:
+                    assert not a[own][:, list(heads)].isfinite().any(), name
+        for name, by in (("hT", "kv"), ("dh0", ("q", "dO"))):
+            a, b = got[name][0], clean[name][0]
+            assert torch.equal(a[2], b[2]), name
+            if what not in by:
+                assert torch.equal(a, b), name
+            else:
+                assert not (a[list(heads), col] if what in "kq" else a[list(heads), :, col]).isfinite().any(), name
