@@ -147,7 +147,7 @@ __global__ void __launch_bounds__(kTcThreads, 1) k_linear_tc(const __grid_consta
                 f2 x[8];
                 if (!ENDS)
 #pragma unroll
-                    for (int k = 0; k < 8; ++k) see_unfit(seen, raw[k]);
+                    for (int k = 0; k < 8; k += 2) see_unfit(seen, raw[k], raw[k + 1]);
 #pragma unroll
                 for (int k = 0; k < 8; ++k)
                     x[k] = mul2(pack2(kappa[k & ~1], kappa[k | 1]), pack2(__uint_as_float(raw[k] << 16), __uint_as_float(raw[k] & 0xffff0000u)));
@@ -166,7 +166,7 @@ __global__ void __launch_bounds__(kTcThreads, 1) k_linear_tc(const __grid_consta
                 }
             }
         }
-        if (!ENDS && __any_sync(0xffffffffu, seen != 0)) {                            // what this warp has read, element by element
+        if (!ENDS && __any_sync(0xffffffffu, seen_unfit(seen))) {                            // what this warp has read, element by element
             const int rows = exact ? kPart : 2 * kPart, wide = DC / 4;
             unsigned char* const mine = slot(n * kPer + kC);
 #pragma unroll 1

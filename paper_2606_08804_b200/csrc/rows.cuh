@@ -122,10 +122,12 @@ __device__ __forceinline__ void copy_bytes(void* dst, const void* src, int bytes
 __device__ __forceinline__ void copy_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
 template <int N> __device__ __forceinline__ void copy_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
 
-// Two bf16 values at a time: `seen` becomes other than 0, and stays so, where one is infinite or NaN.
-__device__ __forceinline__ void see_unfit(uint32_t& seen, uint32_t x) {
-    asm("fma.rn.bf16x2 %0, %1, %2, %0;" : "+r"(seen) : "r"(x), "r"(0u));
+// Whether any of many pairs of bf16 values is infinite or NaN, two pairs to an instruction: the sum of their products is then, too, whatever
+// else is in it.  (Products that overflow raise it as well: who is told looks again.)
+__device__ __forceinline__ void see_unfit(uint32_t& sum, uint32_t x, uint32_t y) {
+    asm("fma.rn.bf16x2 %0, %1, %2, %0;" : "+r"(sum) : "r"(x), "r"(y));
 }
+__device__ __forceinline__ bool seen_unfit(uint32_t sum) { return (sum & 0x7f80u) == 0x7f80u || (sum & 0x7f800000u) == 0x7f800000u; }
 
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 __device__ __forceinline__ float reciprocal(float x) {
