@@ -257,6 +257,10 @@ __global__ void __launch_bounds__(kTcThreads, 1) k_linear_tc(const __grid_consta
                     if (steep) {
 #pragma unroll
                         for (int e = 0; e < 32; ++e) v[e] *= far[-32 * j - e];
+                        const int live = min(kTokens, end - token0(n)) - 32 * j;
+                        if (reverse && live < 32)                  // tokens past the end, whose D may be infinite
+#pragma unroll
+                            for (int e = 0; e < 32; ++e) v[e] = e < live ? v[e] : 0.f;
                     } else {
 #pragma unroll
                         for (int e = 0; e < 32; e += 4) {

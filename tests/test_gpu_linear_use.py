@@ -9,6 +9,7 @@ import torch
 
 import gpu_util as gu
 import layer_forms as lf
+import linear_forms as f
 
 pytestmark = pytest.mark.gpu
 BF, F32 = torch.bfloat16, torch.float32
@@ -542,3 +543,51 @@ def test_a_token_that_is_not_finite_reaches_what_follows_it(T, at, dk, dv, dtype
                 assert torch.equal(a, b), name
             else:
                 assert not (a[list(heads), col] if what in "kq" else a[list(heads), :, col]).isfinite().any(), name
+
+
+@pytest.mark.parametrize("width,dtype", [(127, BF), (128, BF), (130, BF), (1001, F32), (2048, BF), (5001, BF), (9, F32), (16383, BF)])
+@pytest.mark.parametrize("value", [math.nan, math.inf])
+def test_a_row_that_is_not_finite_stays_alone(width, dtype, value):
+    from paper_2606_08804_b200 import binding as qd
+    rows, bad = 67, [0, 5, 31, 66]
+    good = [r for r in range(rows) if r not in bad]
+    t = {n: _n(rows, width, seed=i, to=dtype) for i, n in enumerate(("x", "gate", "dy", "dt"))}
+    w, b, c = (_n(width, seed=9 + i, to=dtype) for i in range(3))
+
+    def run():
+        y, st = qd.gated_norm_fwd(t["x"], t["gate"], w, b)
+        g = qd.gated_norm_bwd(t["x"], t["gate"], w, b, t["dy"], st)
+        z, total, sa = qd.add_norm_fwd(t["x"], t["gate"], c, w, b)
+        a = qd.add_norm_bwd(t["x"], t["gate"], c, w, t["dy"], t["dt"], sa)
+        return dict(y=y, dx=g["dx"], dgate=g["dgate"], z=z, total=total, ax=a["dx"], ar=a["dresidual"], s=st.t(), sa=sa.t())
+    clean = run()
+    t["x"][bad, ::3] = value
+    got = run()
+    for name in clean:
+        assert torch.equal(got[name][good], clean[name][good]), name
+        assert not got[name][bad].isfinite().all(1).any(), name
+
+
+@pytest.mark.parametrize("T", [1, 40, 80])
+@pytest.mark.parametrize("dk,dv,dtype", [(128, 128, BF), (64, 64, F32), (64, 128, BF)])
+def test_states_that_grow(T, dk, dv, dtype):
+    """Up to e^(|g| T) = e^80, just inside fp32: chunks that are not full form no factor beyond it.  Exponents cost 2 half steps of their size."""
+    from paper_2606_08804_b200 import autograd as qa
+    g = torch.tensor([1.0, 0.71, 0.3], device="cuda")
+    q, k = (_n(2, T, 3, dk, seed=i, std=dk ** -0.5, to=dtype).requires_grad_() for i in range(2))
+    v, h0 = _n(2, T, 3, dv, seed=3, to=dtype).requires_grad_(), _n(2, 3, dk, dv, seed=4, to=F32).requires_grad_()
+    o, hT = qa.linear_attention(q, k, v, g, h0)
+    leaves = (q, k, v, h0)
+    up = (_n(2, T, 3, dv, seed=5, to=dtype), _n(2, 3, dk, dv, seed=6, to=F32))
+    got = torch.autograd.grad((o, hT), leaves, up)
+    ref = [lf.f64(t) for t in leaves]
+    ro = f.linear(*ref[:3], g.double().cpu(), ref[3])
+    rg = lf.grads(ro, [u.double().cpu() for u in up], ref)
+    for name, a, r in zip(("o", "hT", "dq", "dk", "dv", "dh0"), (o, hT) + got, tuple(ro) + tuple(rg)):
+        a, r = a.detach().double().cpu(), r.detach()
+        for h in range(3):
+            x, y = (a[:, :, h], r[:, :, h]) if name not in ("hT", "dh0") else (a[:, h], r[:, h])
+            assert x.isfinite().all(), (name, h)
+            # length of the difference: sums of up to 128 products that partly cancel, and for bf16 two roundings a term
+            off = float((x - y).norm() / y.norm())
+            assert off < (2.0 ** -6 if dtype == BF and name not in ("hT", "dh0") else (2 * 80 + 128) * 2.0 ** -24), (name, h, off)
