@@ -34,8 +34,8 @@ __global__ void __launch_bounds__(kRotaryThreads) k_rotary(const RotaryP p) {
     const int n = (int)min((long long)p.per, p.tokens - first);
     for (int i = threadIdx.x; i < n * p.pairs; i += kRotaryThreads) {
         const long long tok = first + i / p.pairs;
-        const long long at = p.positions ? p.positions[tok] : p.start + tok % p.T;
-        const unsigned long long turn = (unsigned long long)at * (unsigned long long)p.turns[i % p.pairs];
+        const unsigned long long at = p.positions ? (unsigned long long)p.positions[tok] : (unsigned long long)p.start + (unsigned long long)(tok % p.T);
+        const unsigned long long turn = at * (unsigned long long)p.turns[i % p.pairs];
         const uint32_t u = (uint32_t)((turn + 0x80000000ull) >> 32);
         const uint32_t quarter = (u + 0x20000000u) >> 30;                            // nearest quarter turn
         float s, c;

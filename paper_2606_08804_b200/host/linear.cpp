@@ -178,6 +178,8 @@ std::pair<at::Tensor, at::Tensor> rotate(const at::Tensor& q, const at::Tensor* 
         dims(*k, 4, "k must be [B, T, H, d]");
         Hk = k->size(2);
         if (Hk == 0) bad("k must have heads");
+    } else if (k_out) {
+        bad("an output for k needs k");
     }
     const void *qp = on.p(&q, dt, {B, T, Hq, d}, "q"), *kp = on.p(k, dt, {B, T, Hk, d}, "k");
     const void *tp = on.p(&turns, at::kLong, {pairs}, "turns"), *pp = on.p(positions, at::kLong, {B, T}, "positions");

@@ -286,6 +286,7 @@ def test_what_is_refused():
                        (lambda: qd.rotary(q, k, turns.int()), "turns must have dtype"), (lambda: qd.rotary(q, k, turns, torch.zeros(2, 7, dtype=torch.int64, device="cuda")), "positions must have shape"),
                        (lambda: qd.rotary(q, k, turns, torch.zeros(2, 8, dtype=torch.int32, device="cuda")), "positions must have dtype"), (lambda: qd.rotary(q, _n(2, 8, 2, 32), turns), "k must have shape"),
                        (lambda: qd.rotary(q, k, qd.rotary_turns(33)), "UNSUPPORTED"), (lambda: qd.rotary(q, k, turns, out=(q, q)), "INVALID_ARG"),
+                       (lambda: qd.rotary(q, None, turns, out=(q, k)), "needs k"),
                        (lambda: qa.linear_attention(q, k, v, g.clone().requires_grad_()), "log_decay is a constant")):
         with pytest.raises(qd.QdeltaError, match=says):
             call()
