@@ -77,8 +77,9 @@ __global__ void __launch_bounds__(kTcThreads, 1) k_linear_tc(const __grid_consta
     const int walk = blockIdx.x % p.walks, cta = blockIdx.x / p.walks, segment = cta % p.segments, bh = cta / p.segments;
     const int b = bh / p.H, hh = bh % p.H;
     const LinearWalk& w = p.w[walk];
-    const bool reverse = w.reverse, exact = w.exact;
     const int first = segment * p.length, end = min(p.T, first + p.length), chunks = (end - first + kTokens - 1) / kTokens;
+    // the state that is returned is that of the last segment, and what the others' sums make of it before
+    const bool reverse = w.reverse, last_one = segment == (reverse ? 0 : p.segments - 1), exact = w.exact && (ENDS || last_one);
     auto token0 = [&](int n) { return first + (reverse ? chunks - 1 - n : n) * kTokens; };
 
     if (tid == 0) {
@@ -136,7 +137,7 @@ __global__ void __launch_bounds__(kTcThreads, 1) k_linear_tc(const __grid_consta
                 const int t = first_t + 8 * (e >> 1) + 2 * (lane & 3) + (e & 1);
                 kappa[e] = s_k[t >= live ? kTokens : t + late];
             }
-#pragma unroll (ENDS ? 2 : 1)
+#pragma unroll
             for (int half = 0; half < kHalves; ++half) {
                 uint32_t raw[8];
                 const int col = (DC == 128 ? 32 * wq + 16 * half : 16 * wq) + ((lane >> 3) & 1) * 8;
@@ -188,7 +189,7 @@ __global__ void __launch_bounds__(kTcThreads, 1) k_linear_tc(const __grid_consta
     };
     int loads = 0;                                                        // issued by this thread
     if (p.clear && blockIdx.x == 0 && tid == 0) *p.status = 0;
-    if (ENDS && segment == (reverse ? 0 : p.segments - 1)) {
+    if (ENDS && last_one) {
         // nobody begins with the sums of this one
     } else if (warp < 8) {
         // ---------------------------------- planes, weights and output ----------------------------------
@@ -373,7 +374,7 @@ __global__ void __launch_bounds__(kTcThreads, 1) k_linear_tc(const __grid_consta
             if (n + 1 < chunks) put(n + 1);
         }
         float* left = ENDS ? w.ends + ((size_t)bh * p.segments + segment) * size
-                           : segment == (reverse ? 0 : p.segments - 1) && w.sT ? w.sT + (size_t)bh * size : nullptr;
+                           : last_one && w.sT ? w.sT + (size_t)bh * size : nullptr;
         if (left && live_row && !s_abort) {
             if (w.flip) {
 #pragma unroll
