@@ -14,7 +14,9 @@ int linear_chunk(const qd_linear_shape& s) { return s.dtype == QD_BF16 ? 128 : 6
 long long linear_ctas(const qd_linear_shape& s) { return (long long)s.B * s.H * (s.dtype == QD_BF16 ? 1 : s.dv / 32); }
 
 // Segments of a sequence: as many as make the CTAs' longest run of chunks shortest.  A segment costs its chunks and what a CTA needs
-// before its first one; where there are several, the sums of each come first, which take half as long as a walk.
+// before its first one; where there are several, the sums of each come first, which take half as long as a walk.  (32768 tokens of 16 heads
+// in bf16: forward 884 us in one segment, 165 in the chosen nine, 245 in twelve; backward 686, 372 in three, 447 in four.  Of 14 numbers up to 32
+// at 16 shapes the best was 4 % better than the chosen one, but for 3 x 2048 tokens of 16 heads: 51 for 47, backward 59 for 55.)
 int segments_of(const qd_linear_shape& s, bool backward) {
     const int chunk = linear_chunk(s);
     const long long per = linear_ctas(s) * (backward ? kLinearWalks : 1);
@@ -141,7 +143,7 @@ cudaError_t linear_bwd(const LinearArgs& a) {
 // ---- single tokens --------------------------------------------------------------------------------------------------------
 // S tokens of every sequence, state in place: h <- e^g h + k v^T, o = scale h^T q.  Bound by HBM, one read and one write of the state: a
 // CTA has COLS columns of one state, each thread 16 bytes of every RP-th row in registers for all tokens; the read-out's sums over rows go
-// through shared memory, a barrier a token.
+// through shared memory, a barrier a token.  256 sequences of 16 heads of 128 x 128: 82 us, 6.5 TB/s.
 namespace {
 
 constexpr int kStepThreads = 256, kStepTokens = 8;

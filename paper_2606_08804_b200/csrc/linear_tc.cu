@@ -8,12 +8,15 @@
 // which hold all of its 24 bits: with two the state is 2.4e-6 of its length off, which is more than a whole fp32 sum over a sequence is.
 // Where it is not, it serves bf16 outputs alone, and kappa c is rounded to bf16 once, as the state is when it becomes an operand.
 //
-// Bound by HBM where there are CTAs enough: per token and head two tensors of its width in and one out besides c, 2.5 us (some 5000 cycles)
-// a chunk of 128 x 128 with 128 CTAs; the products of a chunk are 3072 cycles.  Next to that it is shared memory, 128 bytes a cycle, which
-// a product of 128 x 128 with both operands there takes all of; so P and the planes are operands in tensor memory (the planes of 32 tokens at a
-// time through two places, c read transposed from its tile), and the parts of out, a S and P c, share one accumulator, scaled in between: 7000
-// cycles a chunk with the planes in shared memory and two accumulators.  Six tile buffers, two chunks deep: b, c, a of each; out leaves
-// through a's.
+// 8 x 2048 tokens, 16 heads of 128 x 128, 128 CTAs: 57 us, 5300 cycles a chunk, at 5.6 TB/s of the 6.46 that a copy has (its bytes alone 41.5),
+// so HBM with the chunks' own start; 65 us and 6600 cycles with three planes, whose warps then have no pause.  The products of a chunk are
+// 2048 cycles, 3072 with three planes.  Next to that it is shared memory, 128 bytes a cycle, which a product of 128 x 128 with both operands
+// there takes all of; so P and the planes are operands in tensor memory (the planes of 32 tokens at a time through two places, c read
+// transposed from its tile), and the parts of out, a S and P c, share one accumulator, scaled in between: 78 us with the planes in shared memory
+// and two accumulators.  Six tile buffers, two chunks deep: b, c, a of each; out leaves through a's.  Launched again and again it runs into
+// the GPU's power limit (forward and backward 215 us in the first launches, 248 after a second).
+// The sums of segments alone (ENDS), 32768 tokens of 16 heads: 65 us, of bytes 41.5.  A second accumulator for the sum does not help them (65),
+// planes by all sixteen warps little (60, and the walk with it 62 for 57: registers).
 //   warps 0-7    two warpgroups, alike: planes, every second part; P, half of the columns, from tensor memory and back to it; out, half of the
 //                columns, staged in a's tile, stored by TMA
 //   warps 8-15   state, transposed: a column of S to a lane, half of the rows to a warpgroup; a S times rho, if |g| > 0.7

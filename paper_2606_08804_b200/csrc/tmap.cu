@@ -87,7 +87,7 @@ bool make_tmap_tokens(CUtensorMap* map, const void* base, int B, int T, int H, i
 
 cudaError_t set_max_smem_once(const void* kernel, size_t bytes) {
     // fixed tables, no heap: the largest size set so far for each kernel, one table a device (all of this library's kernels that ask for
-    // shared memory are 126; where a table is full, or there is none, the size is set anew every time)
+    // shared memory are fewer than half of that; where a table is full, or there is none, the size is set anew every time)
     struct Entry { const void* kernel; size_t bytes; };
     constexpr int kDevices = 16, kKernels = 512;
     static std::mutex mu;
