@@ -4,22 +4,24 @@
 // depends on the column alone, and is at most e^{64 |g|} either way.  Heads with |g| > 0.7, where that would leave the range in which bf16 and
 // fp32 round alike, form D as it stands and multiply a S by rho between the two products.
 // The state stays in fp32 registers; each chunk's sum comes from tensor memory and is added there (the tensor cores cut as they accumulate).
-// For a S it goes to shared memory in bf16.  In S the factor kappa stands with c.  Where the state is returned it does so in three bf16 planes,
-// which hold all of its 24 bits: with two the state is 2.4e-6 of its length off, which is more than a whole fp32 sum over a sequence is.
-// Where it is not, it serves bf16 outputs alone, and kappa c is rounded to bf16 once, as the state is when it becomes an operand.
+// For a S it goes to shared memory in bf16.  In S the factor kappa stands with c, as bf16 planes cut from kappa c: three, which hold all of its
+// 24 bits, where the state is returned (with two, even rounded ones, it is 2.4e-6 of its length off, more than a whole fp32 sum over a sequence
+// is); two, 2^-15 apart, where it serves bf16 outputs alone (with one, dq and dk are off by 1.53 times what their own rounding costs, with two
+// by 1.35).
 //
-// 8 x 2048 tokens, 16 heads of 128 x 128, 128 CTAs: 57 us, 5300 cycles a chunk, at 5.6 TB/s of the 6.46 that a copy has (its bytes alone 41.5),
-// so HBM with the chunks' own start; 65 us and 6600 cycles with three planes, whose warps then have no pause.  The products of a chunk are
-// 2048 cycles, 3072 with three planes.  Next to that it is shared memory, 128 bytes a cycle, which a product of 128 x 128 with both operands
-// there takes all of; so P and the planes are operands in tensor memory (the planes of 32 tokens at a time through two places, c read
-// transposed from its tile), and the parts of out, a S and P c, share one accumulator, scaled in between: 78 us with the planes in shared memory
-// and two accumulators.  Six tile buffers, two chunks deep: b, c, a of each; out leaves through a's.  Launched again and again it runs into
-// the GPU's power limit (forward and backward 215 us in the first launches, 248 after a second).
-// The sums of segments alone (ENDS), 32768 tokens of 16 heads: 65 us, of bytes 41.5.  A second accumulator for the sum does not help them (65),
-// planes by all sixteen warps little (60, and the walk with it 62 for 57: registers).
-//   warps 0-7    two warpgroups, alike: planes, every second part; P, half of the columns, from tensor memory and back to it; out, half of the
+// 8 x 2048 tokens, 16 heads of 128 x 128, 128 CTAs: 58 us, 5300 cycles a chunk, at 5.6 TB/s of the 6.46 that a copy has (its bytes alone 41.5),
+// so HBM with the chunks' own start; 63 us with three planes, where the state's way from sum to sum is as long.  The products of a chunk are
+// 2560 cycles, 3072 with three planes.  Next to that it is shared memory, 128 bytes a cycle, which a product of 128 x 128 with both operands
+// there takes all of; so P and the planes are operands in tensor memory (c read transposed from its tile), and the parts of out, a S and P c,
+// share one accumulator, scaled in between: 78 us with the planes in shared memory and two accumulators.  Six tile buffers, two chunks deep: b,
+// c, a of each; out leaves through a's.  All sixteen warps make planes, a quarter each; with the state's left out of it 61 us, 48 for 44 at
+// 64 x 64, backward 173 for 160.  Launched again and again it runs into the GPU's power limit (forward and backward 221 us in the first launches,
+// 250 after a second).
+// The sums of segments alone (ENDS), 32768 tokens of 16 heads: 60 us, of bytes 41.5.
+//   warps 0-7    two warpgroups: planes of the first two parts; P, half of the columns, from tensor memory and back to it; out, half of the
 //                columns, staged in a's tile, stored by TMA
-//   warps 8-15   state, transposed: a column of S to a lane, half of the rows to a warpgroup; a S times rho, if |g| > 0.7
+//   warps 8-15   planes of the other two parts; state, transposed: a column of S to a lane, half of the rows to a warpgroup; a S times rho, if
+//                |g| > 0.7
 //   warp 16      issues the products;  warp 17  loads
 // Out's rows before a token take nothing of it, also where it is infinite or NaN: the planes' warps, which read all of c, put a 0 in such an
 // element's place for P c and note its column and place; from there on the column of out is NaN (as the state is for later chunks).
@@ -32,6 +34,9 @@ namespace {
 using namespace sm100;
 
 constexpr int kTokens = 128, kPart = 32, kParts = kTokens / kPart, kTcThreads = 18 * 32;
+// Registers: 18 warps are launched with 96 a thread (five to one of the SM's quarters), too few for the state's and a part of planes.
+constexpr int kLaunchRegs = 96, kGroupRegs = 80, kStateRegs = 112;
+static_assert(kGroupRegs + kStateRegs <= 2 * kLaunchRegs, "what one takes another has given");
 
 // The upper halves of a pair of fp32 values as packed bf16; what they leave stays behind, exactly.
 __device__ __forceinline__ uint32_t cut(f2& x) {
@@ -51,9 +56,9 @@ struct TcLinear {
     static constexpr int kState = ENDS ? 0 : DB * DC * 2;
     static constexpr int kSmem = kState + kRing * kSlot + 1024;
     static constexpr int kPlane = kPart / 2;                          // columns of tensor memory: scores, out, sum, planes
-    static constexpr int kOut = ENDS ? 0 : kTokens, kSum = ENDS ? 0 : kOut + DC, kPlanes = kSum + DB;
-    static constexpr int kPlaces = ENDS ? kParts : 2;                 // of parts of planes: all of a chunk's where there is room
-    static constexpr int kUsed = kPlanes + kPlaces * 3 * kPlane;
+    static constexpr int kOut = ENDS ? 0 : kTokens, kSum = ENDS ? 0 : kOut + DC;
+    static constexpr int kSums = ENDS ? 2 : 1, kPlanes = kSum + kSums * DB;   // of a chunk's sum: one is read while the next is made, where there is room
+    static constexpr int kUsed = kPlanes + kParts * (ENDS ? 3 : 2) * kPlane;      // all of a chunk's parts; three planes through two places
     static constexpr int kColumns = kUsed > 256 ? 512 : kUsed > 128 ? 256 : 128;
     static_assert(kSmem <= 232448 - 2048, "the tables and barriers below need the rest");
 };
@@ -68,7 +73,7 @@ __global__ void __launch_bounds__(kTcThreads, 1) k_linear_tc(const __grid_consta
     // bar_s, bar_o2, bar_o, bar_kq, bar_kv: products complete (scores, a S, out twice, a part's and all of a chunk's sum); bar_p, bar_os, bar_k,
     // bar_h: operands in place; bar_of, bar_kr: out's and the sum's accumulator have been read; bar_af: a's tile is free.  Where one side
     // runs up to two phases ahead there is one for even and one for odd phases.
-    __shared__ uint64_t bar_full[kRing], bar_s, bar_o2, bar_o, bar_c[2], bar_kv[2], bar_kq[kParts], bar_p, bar_os, bar_k[kParts], bar_h, bar_of, bar_kr, bar_af[2], bar_end;
+    __shared__ uint64_t bar_full[kRing], bar_s, bar_o2, bar_o, bar_c[2], bar_kv[2], bar_kq[kParts], bar_p, bar_os, bar_k[kParts], bar_h, bar_of, bar_kr[L::kSums], bar_af[2], bar_end;
     __shared__ uint32_t tmem_slot;
     __shared__ volatile int s_abort, s_unfit;                  // s_unfit: c has had an element that is infinite or NaN
     // What is left of D for a column; or, |g| > 0.7, D(|m|), m from -128, of which one half counts.  In the other, for every column of c: the
@@ -90,7 +95,8 @@ __global__ void __launch_bounds__(kTcThreads, 1) k_linear_tc(const __grid_consta
         for (int i = 0; i < 2; ++i) { mbar_init(&bar_kv[i], 1); mbar_init(&bar_c[i], 1); mbar_init(&bar_af[i], DC == 128 ? 8 : 4); }
         for (int i = 0; i < kParts; ++i) { mbar_init(&bar_kq[i], 1); mbar_init(&bar_k[i], 4); }
         mbar_init(&bar_s, 1); mbar_init(&bar_o2, 1); mbar_init(&bar_o, 1); mbar_init(&bar_p, 8); mbar_init(&bar_os, 8); mbar_init(&bar_of, DC == 128 ? 8 : 4);
-        mbar_init(&bar_h, 8); mbar_init(&bar_kr, 8);
+        mbar_init(&bar_h, 8);
+        for (int i = 0; i < L::kSums; ++i) mbar_init(&bar_kr[i], 8);
         mbar_init(&bar_end, 1);
         mbar_init_fence();
         s_abort = s_unfit = 0;
@@ -119,63 +125,53 @@ __global__ void __launch_bounds__(kTcThreads, 1) k_linear_tc(const __grid_consta
     auto slot = [&](int m) { return sRing + m % kRing * L::kSlot; };
     auto full = [&](int m) { return wait(&bar_full[m % kRing], (m / kRing) & 1); };
 
-    // kappa c of part q, transposed: a column of c to a lane of tensor memory.  Four parts of 32 tokens in three planes, or two of 64 in one.
-    const int parts = exact ? kParts : kParts / 2;
+    // kappa c of part q, 32 tokens, transposed: a column of c to a lane of tensor memory, in three planes or in two.
+    const int count = exact ? 3 : 2;
+    const bool shared = !ENDS && exact;                            // two places for four parts
+    auto place_of = [&](int q) { return shared ? (q & 1) * 3 * L::kPlane : q * (ENDS ? 3 : 2) * L::kPlane; };
     auto planes = [&](int n, int q) {
         const int live = min(kTokens, end - token0(n)), late = reverse ? 0 : kTokens - live;
-        // the part before in this place: two parts before, or that of the chunk before
-        const bool same = !ENDS && q >= 2;
-        const int before = ENDS ? q : q < 2 ? q + parts - 2 : q - 2;
-        if ((n > 0 || same) && !all(wait(&bar_kq[before], (same ? n : n - 1) & 1))) return false;
+        // what was in this place before: this part of the chunk before, or, three planes through two places, two parts before
+        const bool same = shared && q >= 2;
+        if ((n > 0 || same) && !all(wait(&bar_kq[shared ? q ^ 2 : q], (same ? n : n - 1) & 1))) return false;
         const unsigned char* tile = slot(n * kPer + kC);
-        uint32_t to = tmem_addr(tPlanes, lanes, q % L::kPlaces * 3 * L::kPlane);
+        const uint32_t to = tmem_addr(tPlanes, lanes, place_of(q));
         constexpr int kHalves = DC == 128 ? 2 : 1;                                    // 64 rows: 16 to each of a warpgroup's four warps
         uint32_t seen = 0;
 #pragma unroll 1
-        for (int sub = 0; sub < (exact ? 1 : 2); ++sub, to += L::kPlane) {
-            const int first_t = (exact ? q : 2 * q + sub) * kPart;
-            float kappa[8];
+        for (int k = 0; k < 2; ++k) {                                                 // 16 tokens
+            float kappa[4];
 #pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                const int t = first_t + 8 * (e >> 1) + 2 * (lane & 3) + (e & 1);
+            for (int e = 0; e < 4; ++e) {
+                const int t = q * kPart + 16 * k + 8 * (e >> 1) + 2 * (lane & 3) + (e & 1);
                 kappa[e] = s_k[t >= live ? kTokens : t + late];
             }
 #pragma unroll
             for (int half = 0; half < kHalves; ++half) {
-                uint32_t raw[8];
+                uint32_t raw[4], r[4];
                 const int col = (DC == 128 ? 32 * wq + 16 * half : 16 * wq) + ((lane >> 3) & 1) * 8;
+                ldsm4<true>(tile + (col >> 6) * kTokens * 128 + sw128_chunk(q * kPart + 16 * k + (lane >> 4) * 8 + (lane & 7), (col >> 3) & 7), raw);
+                if (!ENDS) { see_unfit(seen, raw[0], raw[1]); see_unfit(seen, raw[2], raw[3]); }
+                f2 x[4];
 #pragma unroll
-                for (int k = 0; k < 2; ++k)
-                    ldsm4<true>(tile + (col >> 6) * kTokens * 128 + sw128_chunk(first_t + 16 * k + (lane >> 4) * 8 + (lane & 7), (col >> 3) & 7),
-                                raw + 4 * k);
-                f2 x[8];
-                if (!ENDS)
-#pragma unroll
-                    for (int k = 0; k < 8; k += 2) see_unfit(seen, raw[k], raw[k + 1]);
-#pragma unroll
-                for (int k = 0; k < 8; ++k)
-                    x[k] = mul2(pack2(kappa[k & ~1], kappa[k | 1]), pack2(__uint_as_float(raw[k] << 16), __uint_as_float(raw[k] & 0xffff0000u)));
-                uint32_t r[8];
-                if (!exact) {
-#pragma unroll
-                    for (int k = 0; k < 8; ++k) { const float2 v = unpack2(x[k]); r[k] = pack_bf16(v.x, v.y); }
-                    tmem_st_frag4(tmem_addr(to, 16 * half, 0), r);
-                    continue;
-                }
+                for (int e = 0; e < 4; ++e)
+                    x[e] = mul2(pack2(kappa[e & ~1], kappa[e | 1]), pack2(__uint_as_float(raw[e] << 16), __uint_as_float(raw[e] & 0xffff0000u)));
+                const uint32_t at = tmem_addr(to, 16 * half, 8 * k);
 #pragma unroll
                 for (int m = 0; m < 3; ++m) {                                         // cut to 8 bits, three times: nothing is left of 24
+                    if (m == 2 && !exact) break;
 #pragma unroll
-                    for (int k = 0; k < 8; ++k) r[k] = cut(x[k]);
-                    tmem_st_frag4(tmem_addr(to, 16 * half, m * L::kPlane), r);
+                    for (int e = 0; e < 4; ++e) r[e] = cut(x[e]);
+                    tmem_st_frag2(at + m * L::kPlane, r);
                 }
             }
         }
         if (!ENDS && __any_sync(0xffffffffu, seen_unfit(seen))) {                            // what this warp has read, element by element
-            const int rows = exact ? kPart : 2 * kPart, wide = DC / 4;
+            constexpr int wide = DC / 4;
             unsigned char* const mine = slot(n * kPer + kC);
 #pragma unroll 1
-            for (int i = lane; i < rows * wide; i += 32) {
-                const int t = q * rows + i / wide, col = wq * wide + i % wide;
+            for (int i = lane; i < kPart * wide; i += 32) {
+                const int t = q * kPart + i / wide, col = wq * wide + i % wide;
                 volatile unsigned short* const x =
                     reinterpret_cast<volatile unsigned short*>(mine + (col >> 6) * kTokens * 128 + sw128_chunk(t, (col >> 3) & 7)) + (col & 7);
                 if ((*x & 0x7f80) != 0x7f80) continue;
@@ -196,9 +192,10 @@ __global__ void __launch_bounds__(kTcThreads, 1) k_linear_tc(const __grid_consta
         // nobody begins with the sums of this one
     } else if (warp < 8) {
         // ---------------------------------- planes, weights and output ----------------------------------
-        // Two warpgroups, alike: of the parts, of the weights' columns and of out's each takes every second, or half.
+        // Two warpgroups, alike: of the weights' columns and of out's each takes half.
         // One copy of every piece of code, and loops as loops: what all warps go through in a chunk has to fit the instruction cache
         // (planes and weights written out: 12000 cycles a chunk).
+        give_registers<kGroupRegs>();
         const int r = (int)lanes + lane, group = warp >> 2;
         const float* far = s_d + kTokens + r;
         const float last = steep ? 1.f : decay_power(g2, reverse ? 64 - r : r - 63);
@@ -295,17 +292,16 @@ __global__ void __launch_bounds__(kTcThreads, 1) k_linear_tc(const __grid_consta
         };
         bool ok = true;
 #pragma unroll 1
-        for (int i = 0; i <= 2 * chunks && ok; ++i) {              // half chunks, and the last chunk's output
-            const int n = i >> 1;
-            if (n < chunks && (exact || !(i & 1))) ok = all(full(n * kPer + kC)) && planes(n, (i & 1) * 2 + group);
-            if (!ENDS && ok && !(i & 1)) {
-                if (n > 0) ok = output(n - 1);
-                if (n < chunks) ok = ok && weights(n);
-            }
+        for (int n = 0; n <= chunks && ok; ++n) {
+            if (n < chunks) ok = all(full(n * kPer + kC)) && planes(n, group);
+            if (ENDS || !ok) continue;
+            if (n > 0) ok = output(n - 1);
+            if (n < chunks) ok = ok && weights(n);
         }
         if (lane == 0) tma_store_wait_all();
     } else if (warp < 16) {
         // ---------------------------------- state ----------------------------------
+        take_registers<kStateRegs>();
         constexpr int HC = DB / 2, size = DB * DC;
         const int r = DC == 128 ? (int)lanes + lane : 16 * wq + (lane & 15), c0 = (warp - 8) / 4 * HC;
         const bool live_row = DC == 128 || lane < 16;
@@ -340,8 +336,11 @@ __global__ void __launch_bounds__(kTcThreads, 1) k_linear_tc(const __grid_consta
             arrive(&bar_h);
         };
         put(0);
-        for (int n = 0; n < chunks; ++n) {
-            const int live = min(kTokens, end - token0(n)), row = (int)lanes + lane;
+        // planes a chunk ahead of the state, where their place does not wait for a sum that waits for the state
+        for (int n = shared ? 0 : -1; n < chunks; ++n) {
+            const int live = min(kTokens, end - token0(n)), row = (int)lanes + lane, ahead = shared ? n : n + 1;
+            if (ahead < chunks && (!all(full(ahead * kPer + kC)) || !planes(ahead, warp >> 2))) break;
+            if (n < 0) continue;
             if (!ENDS && steep) {                                  // a S times rho, half of the columns to a warpgroup
                 const float rho = row >= live ? 0.f : reverse ? decay_power(g2, live - 1 - row) : p.scale * decay_power(g2, row + 1);
                 if (!all(wait(&bar_o2, n & 1))) break;
@@ -367,13 +366,13 @@ __global__ void __launch_bounds__(kTcThreads, 1) k_linear_tc(const __grid_consta
 #pragma unroll
             for (int j = 0; j < HC / 16; ++j) {
                 float v[16];
-                tmem_ld16(tmem_addr(tKV, lanes, c0 + 16 * j), v);
+                tmem_ld16(tmem_addr(tKV, lanes, n % L::kSums * DB + c0 + 16 * j), v);
                 tmem_ld_wait();
 #pragma unroll
                 for (int e = 0; e < 16; ++e) h[16 * j + e] = fmaf(keep, h[16 * j + e], v[e]);
             }
             tc_fence_before();
-            arrive(&bar_kr);
+            arrive(&bar_kr[n % L::kSums]);
             if (n + 1 < chunks) put(n + 1);
         }
         float* left = ENDS ? w.ends + ((size_t)bh * p.segments + segment) * size
@@ -405,22 +404,21 @@ __global__ void __launch_bounds__(kTcThreads, 1) k_linear_tc(const __grid_consta
             if (!all(wait(&bar_k[q], n & 1))) return false;
             tc_fence_after();
 #pragma unroll 1
-            for (int m = 0; m < (exact ? 3 : 2); ++m)              // planes of the same tokens, or tokens
-                umma_product_ts_w<true, DC>(tKV, tPlanes + (q % L::kPlaces * 3 + m) * L::kPlane, tile(n * kPer) + (exact ? q : 2 * q + m) * kPart * 128, blk, DB,
-                                            kPart, q + m > 0, issue);
+            for (int m = 0; m < count; ++m)
+                umma_product_ts_w<true, DC>(tKV + n % L::kSums * DB, tPlanes + place_of(q) + m * L::kPlane, tile(n * kPer) + q * kPart * 128, blk, DB, kPart, q + m > 0, issue);
             umma_commit_w(&bar_kq[q], issue);
             return true;
         };
         // The state that a chunk begins with is made under the two products that do not need it, the weights under those of the sum.
         if (scores(0))
             for (int n = 0; n < chunks; ++n) {
-                if (n > 0 && !all(wait(&bar_kr, (n - 1) & 1))) break;
+                if (n >= L::kSums && !all(wait(&bar_kr[n % L::kSums], (n / L::kSums - 1) & 1))) break;      // what was in this sum's place
                 tc_fence_after();
                 bool ok = true;
 #pragma unroll 1
-                for (int q = 0; q < parts && ok; ++q) {
+                for (int q = 0; q < kParts && ok; ++q) {
                     ok = part(n, q);
-                    if (ENDS || q != parts / 2 - 1 || !ok) continue;
+                    if (ENDS || q != kParts / 2 - 1 || !ok) continue;
                     ok = all(wait(&bar_h, n & 1)) && (n == 0 || all(wait(&bar_of, (n - 1) & 1)));
                     if (!ok) break;
                     tc_fence_after();

@@ -129,6 +129,10 @@ __device__ __forceinline__ void see_unfit(uint32_t& sum, uint32_t x, uint32_t y)
 }
 __device__ __forceinline__ bool seen_unfit(uint32_t sum) { return (sum & 0x7f80u) == 0x7f80u || (sum & 0x7f800000u) == 0x7f800000u; }
 
+// A warpgroup's registers a thread, from here on: fewer, or more, as soon as others have given them.
+template <int N> __device__ __forceinline__ void give_registers() { asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(N)); }
+template <int N> __device__ __forceinline__ void take_registers() { asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(N)); }
+
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 __device__ __forceinline__ float reciprocal(float x) {
     float y;

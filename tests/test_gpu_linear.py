@@ -42,8 +42,8 @@ def _linear_inputs(B, T, H, dk, dv, dt, state, seed=0):
 def _rounds(T, dk, dv, dt, state_out=False):
     """fp32: products of three planes (2^-22 together) summed over a head, then over a chunk, by an instruction that cuts (two half steps
     each); a sum a chunk; factors whose exponent is at most 20 where they count.  bf16: a term's weight is rounded to bf16 once, half a step of
-    2^-8; or, where it has gone into the state, it has been when it was added to it and the state again as an operand: twice; a state that is
-    returned has terms of three planes of 8 bits, 24 together."""
+    2^-8; or, where it has gone into the state, the state has been as an operand, and before that the term cut at 2^-15: 2^-7 and 2^-16 hold
+    either; a state that is returned has terms of three planes of 8 bits, 24 together."""
     n = 2 * (max(dk, dv) + 128) + 4 * (T // 64 + 1) + 100
     return n * lf.ULP + (0 if dt == F32 or state_out else 2.0 ** -7 + 2.0 ** -16)
 

@@ -39,6 +39,7 @@ ROWS = """
 namespace qd { typedef unsigned long long f2; inline f2 pack2(float, float) { return 0; } inline float2 unpack2(f2) { return {0.f, 0.f}; }
 inline f2 mul2(f2, f2) { return 0; } inline f2 both(float) { return 0; } inline f2 add2(f2, f2) { return 0; } }
 namespace qd { inline void see_unfit(uint32_t& seen, uint32_t, uint32_t) { seen |= emu::c->rng() % 4 == 0; } inline bool seen_unfit(uint32_t seen) { return seen; } }
+template <int N> void give_registers() {} template <int N> void take_registers() {}
 inline int atomicMin(int* p, int x) { const int o = *p; *p = std::min(o, x); return o; }
 inline float __int_as_float(int x) { return (float)x; }
 inline unsigned __byte_perm(unsigned, unsigned, unsigned) { return 0; }
@@ -78,3 +79,18 @@ def test_any_order_of_warps(program, kernel):
 @pytest.mark.parametrize("expire,lose", [(0.0005, 0), (0.05, 0), (0.005, 0.02)], ids=["rare", "early", "lost load"])
 def test_expired_waits(program, kernel, expire, lose):
     cp._run(program, kernel, 200, expire, lose)
+
+
+def test_registers_that_the_state_takes(tmp_path):
+    """setmaxnreg.inc waits until the CTA's own registers, those of its launch, have room: what the compiler launches has to be what the shares
+    were made from."""
+    from paper_2606_08804_b200 import build
+    build.build()
+    log = os.path.join(build.OBJ_DIR, "linear_tc.log")
+    if not os.path.exists(log):
+        pytest.skip("the library was not built here")
+    src = open(os.path.join(cp.CSRC, "linear_tc.cu")).read()
+    launch, group, state = map(int, re.search(r"kLaunchRegs = (\d+), kGroupRegs = (\d+), kStateRegs = (\d+)", src).groups())
+    regs = re.findall(r"Compiling entry function '\w*k_linear_tc\w*' for 'sm_100a'(?:(?!Compiling entry).)*?Used (\d+) registers", open(log).read(), re.S)
+    assert len(regs) == 8 and set(map(int, regs)) == {launch} and group + state <= 2 * launch
+    assert all(r % 8 == 0 and 24 <= r <= 256 for r in (launch, group, state))
