@@ -264,6 +264,7 @@ int qdelta_norm_bwd(long long rows, int width, int dtype, const void *x, const v
  *     is kept)   h0, hT [B,H,dk,dv] fp32   dk, dv = 64 or 128   scale finite
  * h0 NULL: a zero state; hT NULL: not returned (not the same buffer as h0).  T <= 2^30.  The workspace's first word is a status word
  * (qdelta_workspace_status).  bf16 runs on the tensor cores (tcgen05), fp32 on fp32-accurate kernels.
+ * A token that is infinite or NaN reaches the rows that the recurrence carries it to, and none before it.
  */
 typedef struct {
     int B, T, H, dk, dv;

@@ -1,8 +1,8 @@
 // Linear attention, fp32-accurate: a walk (linear.cuh) per CTA over chunks of 64 tokens, for 32 columns of the state.  All products are
 // products of bf16 planes on the warp-level tensor instruction (planes.cuh), an fp32 matrix three planes; the state stays in fp32 registers,
 // to which a chunk's sum is added, and is written as planes for the next chunk's a S.
-// Bound by that instruction: 1.2 million products of elements a chunk of 64 x 128 x 32, six times over for the planes, 3.7 us; a b^T is made once
-// for every 32 columns.  2 x 2048 tokens, 16 heads of 128 x 128: forward 236 us, backward 688 (bytes 21 and 36); 2 x 1000, 4 heads of 64 x 64 in
+// A chunk of 64 x 128 x 32 takes 7.6 us: its 1.2 million products of elements, six times over for the planes, keep the tensor pipe busy half of
+// that, what is written as planes and the barriers in between is the rest; a b^T is made once for every 32 columns.  2 x 2048 tokens, 16 heads of 128 x 128: forward 244 us, backward 714 (bytes 21 and 36); 2 x 1000, 4 heads of 64 x 64 in
 // segments: 20 and 45, latency.
 #include "linear.cuh"
 #include "planes.cuh"
@@ -65,6 +65,49 @@ struct Rows4 {
         }
     }
 };
+
+// acc += A B as pmm does (planes.cuh), of three planes each.  The tensor instruction cuts as it adds, so the products go to three sums by their
+// size, and none of them adds small products to a large sum; for all columns before the next product, so that none waits for the one before.
+// Of 128 x 128, outputs are 2e-7 of their length off for 1.1e-6 with one sum; 244 us for 235 at 2 x 2048 tokens of 16 heads, 154 for 169 at 4 x 2048
+// tokens of 16 heads of 64 x 64.
+template <bool AT, bool BT, int NTL, class MA, class MB>
+__device__ __forceinline__ void product(float (&acc)[1][NTL][4], const MA& A, const MB& B, int m0, int n0, int k1, int kb = 0) {
+    static_assert(MA::NP == 3 && MB::NP == 3 && NTL % 2 == 0, "three planes, columns in pairs of 8");
+    const int lane = threadIdx.x & 31;
+    const __nv_bfloat16* pa = A.p + (AT ? ((lane & 7) + (lane >> 4) * 8) * MA::LD + m0 + ((lane >> 3) & 1) * 8 : (m0 + (lane & 15)) * MA::LD + (lane >> 4) * 8);
+    const __nv_bfloat16* pb = B.p + (BT ? (lane & 15) * MB::LD + n0 + (lane >> 4) * 8 : (n0 + (lane & 7) + (lane >> 4) * 8) * MB::LD + ((lane >> 3) & 1) * 8);
+    float less[2][NTL][4];
+#pragma unroll
+    for (int s = 0; s < 2; ++s)
+#pragma unroll
+        for (int j = 0; j < NTL; ++j)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) less[s][j][e] = 0.f;
+#pragma unroll 2
+    for (int k0 = kb; k0 < k1; k0 += 16) {
+        uint32_t a[3][4], b[NTL / 2][3][4];
+#pragma unroll
+        for (int x = 0; x < 3; ++x) sm100::ldsm4<AT>(pa + x * MA::PS + (AT ? k0 * MA::LD : k0), a[x]);
+#pragma unroll
+        for (int j = 0; j < NTL / 2; ++j)
+#pragma unroll
+            for (int y = 0; y < 3; ++y) sm100::ldsm4<BT>(pb + y * MB::PS + (BT ? k0 * MB::LD + 16 * j : 16 * j * MB::LD + k0), b[j][y]);
+        auto all = [&](float (&to)[NTL][4], int x, int y) {
+#pragma unroll
+            for (int j = 0; j < NTL; ++j) mma_bf16(to[j], a[x], b[j / 2][y] + 2 * (j & 1));
+        };
+        all(less[1], 0, 2);
+        all(less[0], 0, 1);
+        all(acc[0], 0, 0);
+        all(less[1], 1, 1);
+        all(less[0], 1, 0);
+        all(less[1], 2, 0);
+    }
+#pragma unroll
+    for (int j = 0; j < NTL; ++j)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) acc[0][j][e] += less[0][j][e] + less[1][j][e];
+}
 
 template <typename IO, int DB>
 struct PlanesLayout {
@@ -153,7 +196,7 @@ __global__ void __launch_bounds__(kPlanesThreads, 1) k_linear_planes(const Linea
             float acc[1][4][4];
             const int m0 = 16 * (warp >> 1), n0 = 32 * (warp & 1);
             zero(acc);
-            pmm<false, false>(acc, A, B, m0, n0, DB);
+            product<false, false>(acc, A, B, m0, n0, DB);
             each(acc, m0, n0, [&](int r, int c, float& x, float& y) {
                 const int u = w.reverse ? c - r : r - c, v = w.reverse ? u + 1 : u - 1;
                 P.st2(r, c, u >= 0 ? x * s_d[u] : 0.f, v >= 0 ? y * s_d[v] : 0.f);
@@ -163,8 +206,8 @@ __global__ void __launch_bounds__(kPlanesThreads, 1) k_linear_planes(const Linea
             const int o0 = 16 * (warp & 1);
             zero(in);
             zero(out);
-            pmm<false, true>(in, P, Cc, m0, o0, w.reverse ? kRows : m0 + 16, w.reverse ? m0 : 0);
-            pmm<false, true>(out, A, S, m0, o0, DB);
+            product<false, true>(in, P, Cc, m0, o0, w.reverse ? kRows : m0 + 16, w.reverse ? m0 : 0);
+            product<false, true>(out, A, S, m0, o0, DB);
             IO* o = static_cast<IO*>(w.out) + ((size_t)b * p.T + t0) * ld_c + (size_t)h * DC + j0;
             each2(in, out, m0, o0, [&](int r, int c, float x, float y, float x2, float y2) {
                 if (r >= live) return;
@@ -182,7 +225,7 @@ __global__ void __launch_bounds__(kPlanesThreads, 1) k_linear_planes(const Linea
         }
         float add[1][NS][4];
         zero(add);
-        pmm<true, true>(add, B, Ch, sm, sn, kRows);
+        product<true, true>(add, B, Ch, sm, sn, kRows);
         if (w.out) __syncthreads();                            // the state has been read
         const float keep = decay_power(g2, live);
         each2(st, add, sm, sn, [&](int r, int c, float& x, float& y, float x2, float y2) {

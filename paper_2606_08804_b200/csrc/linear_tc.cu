@@ -11,7 +11,7 @@
 //
 // 8 x 2048 tokens, 16 heads of 128 x 128, 128 CTAs: 58 us, 5300 cycles a chunk, at 5.6 TB/s of the 6.46 that a copy has (its bytes alone 41.5),
 // so HBM with the chunks' own start; 63 us with three planes, where the state's way from sum to sum is as long.  The products of a chunk are
-// 2560 cycles, 3072 with three planes.  Next to that it is shared memory, 128 bytes a cycle, which a product of 128 x 128 with both operands
+// 2560 cycles, 512 more with three planes.  Next to that it is shared memory, 128 bytes a cycle, which a product of 128 x 128 with both operands
 // there takes all of; so P and the planes are operands in tensor memory (c read transposed from its tile), and the parts of out, a S and P c,
 // share one accumulator, scaled in between: 78 us with the planes in shared memory and two accumulators.  Six tile buffers, two chunks deep: b,
 // c, a of each; out leaves through a's.  All sixteen warps make planes, a quarter each; with the state's left out of it 61 us, 48 for 44 at
