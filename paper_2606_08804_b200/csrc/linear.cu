@@ -46,7 +46,7 @@ __global__ void __launch_bounds__(kJoinThreads) k_linear_join(const LinearJoins 
     const int e = blockIdx.x * kJoinThreads + threadIdx.x;
     const size_t bh = blockIdx.y;
     if (e >= quads) return;
-    const float g2 = g[bh % H] * 1.4426950408889634f;
+    const float decay = g[bh % H];
     float4* ends = reinterpret_cast<float4*>(j.ends) + bh * segments * quads + e;
     float4 s = j.s0 ? __ldcg(reinterpret_cast<const float4*>(j.s0) + bh * quads + e) : make_float4(0.f, 0.f, 0.f, 0.f);
     constexpr int kGroup = 8;
@@ -62,9 +62,8 @@ __global__ void __launch_bounds__(kJoinThreads) k_linear_join(const LinearJoins 
             const int n = n0 + i, at = j.reverse ? segments - 1 - n : n;
             if (n >= segments) break;
             ends[(size_t)at * quads] = s;
-            const float keep = decay_power(g2, min(length, T - at * length));
-            if (n + 1 < segments)
-                s = make_float4(fmaf(keep, s.x, v[i].x), fmaf(keep, s.y, v[i].y), fmaf(keep, s.z, v[i].z), fmaf(keep, s.w, v[i].w));
+            const Keep keep = keep_power(decay, min(length, T - at * length));
+            if (n + 1 < segments) s = make_float4(kept(keep, s.x, v[i].x), kept(keep, s.y, v[i].y), kept(keep, s.z, v[i].z), kept(keep, s.w, v[i].w));
         }
     }
 }
@@ -165,7 +164,7 @@ __global__ void __launch_bounds__(kStepThreads) k_linear_steps(int S, int H, int
     float4 st[NP];
 #pragma unroll
     for (int i = 0; i < NP; ++i) st[i] = __ldcs(base + i * step);
-    const float keep = exp2f(g[h] * 1.4426950408889634f);
+    const Keep keep = keep_power(g[h], 1);
     for (int s0 = 0; s0 < S; s0 += kStepTokens) {
         const int n = min(kStepTokens, S - s0);
         const size_t row = ((size_t)b * S + s0) * H + h;
@@ -183,10 +182,10 @@ __global__ void __launch_bounds__(kStepThreads) k_linear_steps(int S, int H, int
 #pragma unroll
             for (int i = 0; i < NP; ++i) {
                 const float kk = sk[t][i * RP + rg], qq = sq[t][i * RP + rg];
-                st[i].x = fmaf(keep, st[i].x, kk * vv.x); acc.x = fmaf(qq, st[i].x, acc.x);
-                st[i].y = fmaf(keep, st[i].y, kk * vv.y); acc.y = fmaf(qq, st[i].y, acc.y);
-                st[i].z = fmaf(keep, st[i].z, kk * vv.z); acc.z = fmaf(qq, st[i].z, acc.z);
-                st[i].w = fmaf(keep, st[i].w, kk * vv.w); acc.w = fmaf(qq, st[i].w, acc.w);
+                st[i].x = kept(keep, st[i].x, kk * vv.x); acc.x = fmaf(qq, st[i].x, acc.x);
+                st[i].y = kept(keep, st[i].y, kk * vv.y); acc.y = fmaf(qq, st[i].y, acc.y);
+                st[i].z = kept(keep, st[i].z, kk * vv.z); acc.z = fmaf(qq, st[i].z, acc.z);
+                st[i].w = kept(keep, st[i].w, kk * vv.w); acc.w = fmaf(qq, st[i].w, acc.w);
             }
             float (*part)[COLS] = red[t & 1];
             *reinterpret_cast<float4*>(&part[rg][4 * ct]) = acc;

@@ -139,7 +139,7 @@ __global__ void __launch_bounds__(kPlanesThreads, 1) k_linear_planes(const Linea
     const int b = bh / p.H, h = bh % p.H, j0 = slice * kCols, tid = threadIdx.x, warp = tid >> 5;
     sm100::grid_dep_wait();
     sm100::grid_dep_launch();
-    const float g2 = p.g[h] * 1.4426950408889634f;
+    const float g = p.g[h], g2 = g * 1.4426950408889634f;
     if (p.clear && blockIdx.x == 0 && tid == 0) *p.status = 0;
     // the sums of the segment that no other begins with are not asked for
     if (!w.out && segment == (w.reverse ? 0 : p.segments - 1)) return;
@@ -227,10 +227,10 @@ __global__ void __launch_bounds__(kPlanesThreads, 1) k_linear_planes(const Linea
         zero(add);
         product<true, true>(add, B, Ch, sm, sn, kRows);
         if (w.out) __syncthreads();                            // the state has been read
-        const float keep = decay_power(g2, live);
+        const Keep keep = keep_power(g, live);
         each2(st, add, sm, sn, [&](int r, int c, float& x, float& y, float x2, float y2) {
-            x = fmaf(keep, x, x2);
-            y = fmaf(keep, y, y2);
+            x = kept(keep, x, x2);
+            y = kept(keep, y, y2);
             if (w.out) S.st2(r, c, x, y);
         });
     }

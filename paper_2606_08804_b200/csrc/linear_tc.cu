@@ -335,6 +335,7 @@ __global__ void __launch_bounds__(kTcThreads, 1) k_linear_tc(const __grid_consta
             fence_proxy_async();
             arrive(&bar_h);
         };
+        const Keep whole = keep_power(g, kTokens);
         put(0);
         // planes a chunk ahead of the state, where their place does not wait for a sum that waits for the state
         for (int n = shared ? 0 : -1; n < chunks; ++n) {
@@ -362,14 +363,19 @@ __global__ void __launch_bounds__(kTcThreads, 1) k_linear_tc(const __grid_consta
             }
             if (!all(wait(&bar_kv[n & 1], (n >> 1) & 1))) break;
             tc_fence_after();
-            const float keep = decay_power(g2, live);
+            const Keep keep = live == kTokens ? whole : keep_power(g, live);
+            const f2 base = both(keep.base), more = both(keep.more);
 #pragma unroll
             for (int j = 0; j < HC / 16; ++j) {
                 float v[16];
                 tmem_ld16(tmem_addr(tKV, lanes, n % L::kSums * DB + c0 + 16 * j), v);
                 tmem_ld_wait();
 #pragma unroll
-                for (int e = 0; e < 16; ++e) h[16 * j + e] = fmaf(keep, h[16 * j + e], v[e]);
+                for (int e = 0; e < 16; e += 2) {
+                    const f2 x = pack2(h[16 * j + e], h[16 * j + e + 1]);
+                    const float2 y = unpack2(fma2(more, x, fma2(base, x, pack2(v[e], v[e + 1]))));
+                    h[16 * j + e] = y.x; h[16 * j + e + 1] = y.y;
+                }
             }
             tc_fence_before();
             arrive(&bar_kr[n % L::kSums]);

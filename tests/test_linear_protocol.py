@@ -37,7 +37,7 @@ static std::string one(const std::string& name, const emu::Scenario& s, int i) {
 # the packed arithmetic that the kernel takes from rows.cuh
 ROWS = """
 namespace qd { typedef unsigned long long f2; inline f2 pack2(float, float) { return 0; } inline float2 unpack2(f2) { return {0.f, 0.f}; }
-inline f2 mul2(f2, f2) { return 0; } inline f2 both(float) { return 0; } inline f2 add2(f2, f2) { return 0; } }
+inline f2 mul2(f2, f2) { return 0; } inline f2 fma2(f2, f2, f2) { return 0; } inline f2 both(float) { return 0; } inline f2 add2(f2, f2) { return 0; } }
 namespace qd { inline void see_unfit(uint32_t& seen, uint32_t, uint32_t) { seen |= emu::c->rng() % 4 == 0; } inline bool seen_unfit(uint32_t seen) { return seen; } }
 template <int N> void give_registers() {} template <int N> void take_registers() {}
 inline int atomicMin(int* p, int x) { const int o = *p; *p = std::min(o, x); return o; }
