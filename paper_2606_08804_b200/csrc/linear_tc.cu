@@ -79,6 +79,7 @@ __global__ void __launch_bounds__(kTcThreads, 1) k_linear_tc(const __grid_consta
     // What is left of D for a column; or, |g| > 0.7, D(|m|), m from -128, of which one half counts.  In the other, for every column of c: the
     // first element that is infinite or NaN, counted in the order of the walk.
     __shared__ __align__(16) float s_d[2 * kTokens + 1];
+    __shared__ Keep s_keep[2];                                 // over a whole chunk, over the sequence's last
     __shared__ float s_k[kTokens + 1];                                             // kappa of a whole chunk; 0 behind it
 
     const int tid = threadIdx.x, warp = warp_index(), lane = tid & 31, wq = warp & 3;
@@ -112,6 +113,7 @@ __global__ void __launch_bounds__(kTcThreads, 1) k_linear_tc(const __grid_consta
         s_d[tid] = tid >= other && tid < other + kTokens ? __int_as_float(0x7fffffff)
                                                          : p.scale * decay_power(g2, steep ? abs(tid - kTokens) : reverse ? tid - 64 : 63 - tid);
     if (tid <= kTokens) s_k[tid] = tid == kTokens ? 0.f : reverse ? p.scale * decay_power(g2, tid + 1) : decay_power(g2, kTokens - 1 - tid);
+    if (tid < 2) s_keep[tid] = keep_power(g, tid ? end - first - (chunks - 1) * kTokens : kTokens);
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
@@ -335,7 +337,6 @@ __global__ void __launch_bounds__(kTcThreads, 1) k_linear_tc(const __grid_consta
             fence_proxy_async();
             arrive(&bar_h);
         };
-        const Keep whole = keep_power(g, kTokens);
         put(0);
         // planes a chunk ahead of the state, where their place does not wait for a sum that waits for the state
         for (int n = shared ? 0 : -1; n < chunks; ++n) {
@@ -363,7 +364,7 @@ __global__ void __launch_bounds__(kTcThreads, 1) k_linear_tc(const __grid_consta
             }
             if (!all(wait(&bar_kv[n & 1], (n >> 1) & 1))) break;
             tc_fence_after();
-            const Keep keep = live == kTokens ? whole : keep_power(g, live);
+            const Keep keep = s_keep[live < kTokens];
             const f2 base = both(keep.base), more = both(keep.more);
 #pragma unroll
             for (int j = 0; j < HC / 16; ++j) {

@@ -108,6 +108,19 @@ def test_linear_with_decays_of_every_size(B, T, H, dk, dv, dt, decay):
     assert qd.workspace_status(ws) == 0
 
 
+@pytest.mark.parametrize("T,dk,dv", [(3000, 64, 64), (2900, 128, 128)])
+def test_slow_heads_keep_their_rate(T, dk, dv):
+    """A factor that is rounded once and multiplied in for every chunk is off by the same amount each time.  What may be left of n chunks of 64 is
+    their sums' and the state's own rounding, of any sign: 2 sqrt(n) half steps of the state's length."""
+    from paper_2606_08804_b200 import binding as qd
+    (q, k, v, _, h0), _, _ = _linear_inputs(1, T, 2, dk, dv, F32, True, seed=7)
+    g = torch.tensor([-1e-4, -3e-4], device="cuda")
+    _, hT, _ = qd.linear_fwd(q, k, v, g, h0)
+    n, g64 = torch.arange(T - 1, -1, -1, device="cuda").double(), g.double()
+    ref = torch.einsum("hi,bihd,bihv->bhdv", torch.exp(g64[:, None] * n), k.double(), v.double()) + torch.exp(g64 * T)[:, None, None] * h0.double()
+    assert float((hT.double() - ref).norm() / ref.norm()) < 2 * math.sqrt(T / 64) * lf.ULP
+
+
 @pytest.mark.parametrize("B,H,dk,dv,dt", [(1, 1, 64, 64, F32), (3, 5, 128, 128, BF), (2, 3, 64, 128, BF), (2, 2, 128, 64, F32), (40, 16, 128, 128, BF)])
 def test_linear_steps_go_on_from_a_prompt(B, H, dk, dv, dt):
     from paper_2606_08804_b200 import binding as qd
