@@ -9,14 +9,14 @@
 // is); two, 2^-15 apart, where it serves bf16 outputs alone (with one, dq and dk are off by 1.53 times what their own rounding costs, with two
 // by 1.35).
 //
-// 8 x 2048 tokens, 16 heads of 128 x 128, 128 CTAs: 58 us, 5300 cycles a chunk, at 5.6 TB/s of the 6.46 that a copy has (its bytes alone 41.5),
-// so HBM with the chunks' own start; 63 us with three planes, where the state's way from sum to sum is as long.  The products of a chunk are
+// 8 x 2048 tokens, 16 heads of 128 x 128, 128 CTAs: 59 us, 5300 cycles a chunk, at 5.6 TB/s of the 6.46 that a copy has (its bytes alone 41.5),
+// so HBM with the chunks' own start; 64 us with three planes, where the state's way from sum to sum is as long.  The products of a chunk are
 // 2560 cycles, 512 more with three planes.  Next to that it is shared memory, 128 bytes a cycle, which a product of 128 x 128 with both operands
 // there takes all of; so P and the planes are operands in tensor memory (c read transposed from its tile), and the parts of out, a S and P c,
 // share one accumulator, scaled in between: 78 us with the planes in shared memory and two accumulators.  Six tile buffers, two chunks deep: b,
 // c, a of each; out leaves through a's.  All sixteen warps make planes, a quarter each; with the state's left out of it 61 us, 48 for 44 at
-// 64 x 64, backward 173 for 160.  Launched again and again it runs into the GPU's power limit (forward and backward 221 us in the first launches,
-// 250 after a second).
+// 64 x 64, backward 173 for 160 then.  Launched again and again it runs into the GPU's power limit (forward and backward 229 us in the first launches,
+// 262 after a second).
 // The sums of segments alone (ENDS), 32768 tokens of 16 heads: 60 us, of bytes 41.5.
 //   warps 0-7    two warpgroups: planes of the first two parts; P, half of the columns, from tensor memory and back to it; out, half of the
 //                columns, staged in a's tile, stored by TMA
