@@ -199,7 +199,8 @@ __global__ void __launch_bounds__(kPlanesThreads, 1) k_linear_planes(const Linea
             product<false, false>(acc, A, B, m0, n0, DB);
             each(acc, m0, n0, [&](int r, int c, float& x, float& y) {
                 const int u = w.reverse ? c - r : r - c, v = w.reverse ? u + 1 : u - 1;
-                P.st2(r, c, u >= 0 ? x * s_d[u] : 0.f, v >= 0 ? y * s_d[v] : 0.f);
+                // past the end products are 0 and factors, of heads that grow, infinite
+                P.st2(r, c, u >= 0 && c < live ? x * s_d[u] : 0.f, v >= 0 && c + 1 < live ? y * s_d[v] : 0.f);
             });
             __syncthreads();
             float in[1][2][4], out[1][2][4];
