@@ -264,6 +264,11 @@ int qdelta_norm_bwd(long long rows, int width, int dtype, const void *x, const v
  *     is kept)   h0, hT [B,H,dk,dv] fp32   dk, dv = 64 or 128   scale finite
  * h0 NULL: a zero state; hT NULL: not returned (not the same buffer as h0).  T <= 2^30.  The workspace's first word is a status word
  * (qdelta_workspace_status).  bf16 runs on the tensor cores (tcgen05), fp32 on fp32-accurate kernels.
+ * bf16: weights scale q.k d^n and the state as an operand of o are rounded to bf16 (gradients alike); what is added to a state is cut at 2^-24 where
+ * hT or dh0 asks for it, else at 2^-15.  Weights, states and outputs have fp32's range less 2^16 at both ends: beyond 2^110 they may become
+ * infinite, below 2^-110 lose bits.
+ * Factors d^n of heads that grow have to be finite in fp32 up to n = T, at most a chunk of 128 tokens (fp32: 64): log_decay <= 0.69 (1.38) for longer
+ * sequences, else 0 times infinity gives NaN where the state itself might be finite.
  * A token that is infinite or NaN reaches the rows that the recurrence carries it to, and none before it.
  */
 typedef struct {

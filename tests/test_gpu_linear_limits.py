@@ -52,3 +52,42 @@ def _grown(T, g, dk, dv, dtype):
 def test_few_tokens_of_heads_that_grow_fast(T, g, dk, dv, dtype):
     """A chunk that is not full: past its end factors would be infinite, and nothing there may meet them."""
     _grown(T, g, dk, dv, dtype)
+
+
+@pytest.mark.parametrize("T,g", [(140, [0.55, 0.2, 0.17]), (160, [0.5, 0.4, 0.1]), (175, [0.45, 0.3, 0.01]), (460, [0.17, 0.1733, 0.1734]), (1500, [0.05, 0.03, 0.0])])
+@pytest.mark.parametrize("dk,dv,dtype", [(128, 128, BF), (64, 64, BF), (64, 128, BF), (128, 64, F32)])
+def test_heads_that_grow_over_several_chunks(T, g, dk, dv, dtype):
+    """States of up to e^80 meet no factor but those of the rows that there are."""
+    _grown(T, g, dk, dv, dtype)
+
+
+# ---- values far from 1 ------------------------------------------------------------------------------------------------------
+@pytest.mark.parametrize("powers", [(45, 45, -90), (-45, -45, 90), (-90, 0, 90), (90, 0, -90)])
+@pytest.mark.parametrize("T,dk,dv,dtype", [(100, 128, 128, BF), (300, 64, 64, BF), (270, 64, 128, BF), (260, 128, 64, BF), (130, 64, 64, F32)])
+def test_weights_and_states_far_from_one(T, dk, dv, dtype, powers):
+    """Weights q k and dO v, and states, of 2^-90 to 2^90, with outputs that are ordinary numbers; heads on both sides of where a row's factor is taken
+    out of a chunk.  A term's bounds are those of any size.  What is below 2^-126 may be lost; where the row's factor is multiplied in last, what
+    is below 2^-110."""
+    from paper_2606_08804_b200 import binding as qd
+    decay = torch.tensor([-0.69, -0.45, -0.174, -0.173, -0.01, 0.02], device="cuda")
+    H, (pq, pk, pv), scale = len(decay), powers, 0.75
+    q, k, v = _n(1, T, H, dk, std=2.0 ** pq, to=dtype), _n(1, T, H, dk, seed=1, std=2.0 ** pk, to=dtype), _n(1, T, H, dv, seed=2, std=2.0 ** pv, to=dtype)
+    h0, dO, dhT = _n(1, H, dk, dv, std=2.0 ** (pk + pv), to=F32), _n(1, T, H, dv, seed=3, to=dtype), _n(1, H, dk, dv, seed=4, std=2.0 ** pq, to=F32)
+    ref = [lf.f64(t) for t in (q, k, v, h0)]
+    mag = [t.detach().abs().requires_grad_() for t in ref]
+    up, gd = [t.double().cpu() for t in (dO, dhT)], decay.double().cpu()
+    r, m = f.linear(*ref[:3], gd, ref[3], scale), f.linear(*mag[:3], gd, mag[3], scale)
+    r, m = tuple(r) + tuple(lf.grads(r, up, ref)), tuple(m) + tuple(lf.grads(m, [t.abs() for t in up], mag))
+    o, hT, ws = qd.linear_fwd(q, k, v, decay, h0, scale)
+    g = qd.linear_bwd(q, k, v, decay, h0, dO, dhT, scale)
+    # sums and factors as in test_gpu_linear.py: exponents that count are at most 20
+    n = (2 * (max(dk, dv) + 128) + 4 * (T // 64 + 1) + 100) * lf.ULP
+    bits, low = (n, 2.0 ** -124) if dtype == F32 else (n + 2.0 ** -7 + 2.0 ** -16, 2.0 ** -110)
+    top = lambda t: float(t.float().abs().max())  # noqa: E731
+    for i, (name, got, a, b, c) in enumerate((("o", o, q, k, v), ("hT", hT, None, k, None), ("dq", g["dq"], dO, v, k), ("dk", g["dk"], v, dO, q),
+                                              ("dv", g["dv"], k, q, dO), ("dh0", g["dh0"], None, q, None))):
+        if a is None:            # a term's planes, times the other factor
+            lf.close(name, got, r[i], n * m[i].detach() + T * 2.0 ** -124 * top(b))
+        else:                    # a weight, times its row of c; an element of the state, times its one of a
+            lf.close(name, got, r[i], bits * m[i].detach() + low * (T * top(c) + 128 * top(a)))
+    assert qd.workspace_status(ws) == 0
