@@ -317,9 +317,9 @@ int qdelta_gated_norm_bwd(long long rows, int width, int dtype, const void *x, c
 int qdelta_add_norm_fwd(long long rows, int width, int dtype, const void *x, const void *residual, const void *scale, const void *weight,
                         const void *bias, void *total, void *y, float *stats, float eps, unsigned flags, qd_stream stream);
 
-/* Backward for  L = <y, dy> + <total, dtotal>  (dtotal NULL: zero): dresidual and dx = scale dresidual in `dtype` (dx NULL only if scale is:
- * dresidual is it), dscale, dweight, dbias [width] fp32 (NULL: skipped).  Workspace as there.  Adds x and residual up again, in fp32: the
- * rounded total would cost the sums over rows half of their digits. */
+/* Backward for  L = <y, dy> + <total, dtotal>  (dtotal NULL: zero): dresidual and dx = scale dresidual in `dtype`, dscale, dweight, dbias [width]
+ * fp32.  Gradients that are NULL are skipped; dx may be so only without a scale, where it is dresidual.  Workspace as there.  Adds x and
+ * residual up again, in fp32: the rounded total would cost the sums over rows half of their digits. */
 int qdelta_add_norm_bwd(long long rows, int width, int dtype, const void *x, const void *residual, const void *scale, const void *weight,
                         const void *dy, const void *dtotal, const float *stats, void *dx, void *dresidual, float *dscale, float *dweight,
                         float *dbias, void *workspace, size_t workspace_bytes, unsigned flags, qd_stream stream);

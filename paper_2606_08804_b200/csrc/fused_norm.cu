@@ -799,11 +799,16 @@ cudaError_t fused_norm_bwd(const FusedNormArgs& a) {
     const bool sums = out.out[0] || out.out[1] || out.out[2];
     p.part = sums ? a.part : nullptr;
     p.rowsum = q.kind == WIDE ? a.part + part_floats(q, a.width) : nullptr;
-    const cudaError_t e = a.added ? launch<true, true>(p, a.dtype, a.stream) : launch<false, true>(p, a.dtype, a.stream);
-    if (e != cudaSuccess || !sums) return e;
+    cudaError_t e = a.added ? launch<true, true>(p, a.dtype, a.stream) : launch<false, true>(p, a.dtype, a.stream);
     const int n = fused_sums(a.added);
-    return launch_overlapped(k_fused_sums, dim3((unsigned)((a.width + 31) / 32), n), dim3(32 * kSumRows), 0, a.stream, p.part, (int)q.ctas, a.width, n,
-                             out);
+    if (e == cudaSuccess && sums)
+        e = launch_overlapped(k_fused_sums, dim3((unsigned)((a.width + 31) / 32), n), dim3(32 * kSumRows), 0, a.stream, p.part, (int)q.ctas, a.width, n,
+                              out);
+    // without a scale the kernels write dresidual alone: a caller who wants it in two places has it copied (a store of both, under a condition
+    // of its own, made the call with a scale 1.5 % slower)
+    if (e == cudaSuccess && a.added && !a.scale && a.dx)
+        e = cudaMemcpyAsync(a.dx, a.dresidual, (size_t)a.rows * a.width * (a.dtype == QD_BF16 ? 2 : 4), cudaMemcpyDeviceToDevice, a.stream);
+    return e;
 }
 
 }  // namespace qd

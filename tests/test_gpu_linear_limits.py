@@ -91,3 +91,23 @@ def test_weights_and_states_far_from_one(T, dk, dv, dtype, powers):
         else:                    # a weight, times its row of c; an element of the state, times its one of a
             lf.close(name, got, r[i], bits * m[i].detach() + low * (T * top(c) + 128 * top(a)))
     assert qd.workspace_status(ws) == 0
+
+
+# ---- outputs that a call names or leaves out --------------------------------------------------------------------------------
+@pytest.mark.parametrize("rows,width,to", [(33, 64, BF), (40, 36, F32), (7, 129, BF), (300, 2048, BF), (9, 9000, BF), (9, 5001, BF), (5, 4097, F32)])
+def test_residual_norm_without_a_scale_writes_both_gradients(rows, width, to):
+    """dx has a buffer of its own although it is dresidual: it is written, too."""
+    from paper_2606_08804_b200 import binding as qd
+    lib, code, stream = qd.load(), 1 if to == BF else 0, torch.cuda.current_stream().cuda_stream
+    x, e, dy, dt = (_n(rows, width, seed=i, to=to) for i in range(4))
+    w = _n(width, seed=5, to=to)
+    _, _, stats = qd.add_norm_fwd(x, e, None, w)
+    want = qd.add_norm_bwd(x, e, None, w, dy, dt, stats)
+    n = lib.qdelta_fused_norm_workspace_bytes(rows, width, code)
+    dx, dr, dw = gu.Guarded((rows, width), to), gu.Guarded((rows, width), to), gu.Guarded((width,), F32)
+    ws = torch.empty(n, dtype=torch.uint8, device="cuda")
+    p = lambda t: t.data_ptr()  # noqa: E731
+    assert lib.qdelta_add_norm_bwd(rows, width, code, p(x), p(e), None, p(w), p(dy), p(dt), p(stats), p(dx.t), p(dr.t), None, p(dw.t), None, p(ws), n, 0, stream) == 0
+    torch.cuda.synchronize()
+    assert torch.equal(dr.t, want["dresidual"]) and torch.equal(dx.t, want["dresidual"]) and torch.equal(dw.t, want["dweight"])
+    assert dx.intact() and dr.intact() and dw.intact()
