@@ -283,7 +283,7 @@ int qdelta_linear_fwd(const qd_linear_shape *shape, const void *q, const void *k
                       void *o, float *hT, float scale, void *workspace, size_t workspace_bytes, unsigned flags, qd_stream stream);
 
 /* Backward for  L = <o, dO> + <hT, dhT>  (dhT NULL: zero): dq, dk, dv in `dtype`, dh0 fp32 (NULL: skipped; else not the same buffer as
- * dhT).  Needs nothing of the forward but its inputs.  log_decay is a constant of the layer: it has no gradient. */
+ * dhT or h0).  Needs nothing of the forward but its inputs.  log_decay is a constant of the layer: it has no gradient. */
 int qdelta_linear_bwd(const qd_linear_shape *shape, const void *q, const void *k, const void *v, const float *log_decay, const float *h0,
                       const void *dO, const float *dhT, void *dq, void *dk, void *dv, float *dh0, float scale, void *workspace,
                       size_t workspace_bytes, unsigned flags, qd_stream stream);

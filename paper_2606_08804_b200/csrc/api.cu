@@ -482,7 +482,8 @@ int qdelta_linear_bwd(const qd_linear_shape* shape, const void* q, const void* k
                       size_t workspace_bytes, unsigned flags, qd_stream stream) {
     const int rc = check_linear(shape);
     if (rc != QD_OK) return rc;
-    if (!q || !k || !v || !log_decay || !dO || !dq || !dk || !dv || (dh0 && dh0 == dhT) || !finite(scale) || flags) return QD_ERR_INVALID_ARG;
+    // the walk that writes dh0 runs beside those that read h0
+    if (!q || !k || !v || !log_decay || !dO || !dq || !dk || !dv || (dh0 && (dh0 == dhT || dh0 == h0)) || !finite(scale) || flags) return QD_ERR_INVALID_ARG;
     const void* const outs[] = {dq, dk, dv};
     const void* const ins[] = {q, k, v, dO};
     for (const void* x : outs)
