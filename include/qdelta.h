@@ -263,7 +263,8 @@ int qdelta_norm_bwd(long long rows, int width, int dtype, const void *x, const v
  *     q, k [B,T,H,dk]   v, o [B,T,H,dv]   log_decay [H] fp32 (not positive where the state is to stay bounded; minus infinity: nothing
  *     is kept)   h0, hT [B,H,dk,dv] fp32   dk, dv = 64 or 128   scale finite
  * h0 NULL: a zero state; hT NULL: not returned (not the same buffer as h0).  T <= 2^30.  The workspace's first word is a status word
- * (qdelta_workspace_status).  bf16 runs on the tensor cores (tcgen05), fp32 on fp32-accurate kernels.
+ * (qdelta_workspace_status); where a wait has expired, what depends on it is NaN as well.  bf16 runs on the tensor cores (tcgen05), fp32 on
+ * fp32-accurate kernels.
  * bf16: weights scale q.k d^n and the state as an operand of o are rounded to bf16 (gradients alike); what is added to a state is cut at 2^-24 where
  * hT or dh0 asks for it, else at 2^-15.  Weights, states and outputs have fp32's range less 2^16 at both ends: beyond 2^110 they may become
  * infinite, below 2^-110 lose bits.

@@ -357,8 +357,8 @@ def linear_fwd(q, k, v, log_decay, h0=None, scale=1.0, workspace=None, want_hT=T
 
 
 def linear_bwd(q, k, v, log_decay, h0, dO, dhT=None, scale=1.0, workspace=None, want_dh0=None):
-    """Backward of linear_fwd, of which it needs nothing but the inputs (`workspace`: memory of its own size, from the caller).
-    Returns dict(dq, dk, dv, dh0)."""
+    """Backward of linear_fwd, of which it needs nothing but the inputs (`workspace`: memory of its own size, from the caller, whose
+    status word workspace_status reads; without it a wait that expired shows as gradients of NaN).  Returns dict(dq, dk, dv, dh0)."""
     want = h0 is not None if want_dh0 is None else bool(want_dh0)
     return (_native or _host()).linear_bwd(q, k, v, log_decay, h0, dO, dhT, workspace, want, scale)
 

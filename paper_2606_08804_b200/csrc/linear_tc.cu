@@ -26,7 +26,8 @@
 //   warp 16      issues the products;  warp 17  loads
 // Out's rows before a token take nothing of it, also where it is infinite or NaN: the planes' warps, which read all of c, put a 0 in such an
 // element's place for P c and note its column and place; from there on the column of out is NaN (as the state is for later chunks).
-// All waits are bounded; on expiry the status word says so, everybody leaves, what is in flight is waited for.
+// All waits are bounded; on expiry the status word says so, everybody leaves, what is in flight is waited for, and what the CTA was to write
+// becomes NaN: calls whose workspace nobody sees, those through autograd, do not go on with half a result.
 #include "linear.cuh"
 #include "rows.cuh"
 
@@ -474,6 +475,18 @@ __global__ void __launch_bounds__(kTcThreads, 1) k_linear_tc(const __grid_consta
     tc_fence_before();
     __syncthreads();
     if (s_abort && loads) mbar_drain_ring(bar_full, kRing, loads);       // unless a wait has expired somebody has waited for every one
+    if (s_abort) {                                             // nobody takes half a result for one: NaN, in either type
+        auto spoil = [&](void* at, size_t words) {
+#pragma unroll 1
+            for (size_t i = tid; i < words; i += kTcThreads) static_cast<uint32_t*>(at)[i] = 0x7fff7fffu;
+        };
+        const size_t state = (size_t)DB * DC;
+        if (ENDS) spoil(w.ends + ((size_t)bh * p.segments + segment) * state, state);
+        else
+#pragma unroll 1
+            for (int t = first; t < end; ++t) spoil(static_cast<unsigned short*>(w.out) + (((size_t)b * p.T + t) * p.H + hh) * DC, DC / 2);
+        if (!ENDS && last_one && w.sT) spoil(w.sT + (size_t)bh * state, state);
+    }
     if (warp == 0) tmem_dealloc(tb, L::kColumns);
 }
 
