@@ -322,6 +322,7 @@ struct LinearNode : torch::autograd::Function<LinearNode> {
         if (need_grad) {
             ctx->save_for_backward({q, k, v, g, or_none(h0)});
             ctx->saved_data["scale"] = scale;
+            ctx->saved_data["dh0"] = h0 && h0->requires_grad();
         }
         return {r.o, r.hT};
     }
@@ -332,8 +333,8 @@ struct LinearNode : torch::autograd::Function<LinearNode> {
             for (int i = 0; i < 4; ++i) present(in[i], names[i]);
             const at::Tensor &v = in[2], &h0 = in[4];
             const at::Tensor dO = or_zeros(upstream(up[0], v.scalar_type()), v), dhT = upstream(up[1], at::kFloat);
-            const LinearGrads r = linear_backward(in[0], in[1], v, in[3], given(h0), dO, given(dhT), nullptr, h0.defined(),
-                                                  ctx->saved_data["scale"].toDouble());
+            const LinearGrads r = linear_backward(in[0], in[1], v, in[3], given(h0), dO, given(dhT), nullptr,
+                                                  h0.defined() && ctx->saved_data["dh0"].toBool(), ctx->saved_data["scale"].toDouble());
             return {r.dq, r.dk, r.dv, at::Tensor(), r.dh0, at::Tensor(), at::Tensor()};
         });
     }

@@ -111,3 +111,26 @@ def test_residual_norm_without_a_scale_writes_both_gradients(rows, width, to):
     torch.cuda.synchronize()
     assert torch.equal(dr.t, want["dresidual"]) and torch.equal(dx.t, want["dresidual"]) and torch.equal(dw.t, want["dweight"])
     assert dx.intact() and dr.intact() and dw.intact()
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+def test_a_constant_initial_state_gets_no_gradient(dtype):
+    """No memory for it, and the other gradients are those of a call that does not ask for it."""
+    from paper_2606_08804_b200 import autograd as qa
+    from paper_2606_08804_b200 import binding as qd
+    B, T, H, d = 64, 20, 16, 128
+    q, k, v, dO = (_n(B, T, H, d, seed=i, std=0.3, to=dtype) for i in range(4))
+    decay, h0 = -torch.linspace(0.01, 0.9, H, device="cuda"), _n(B, H, d, d, to=F32)
+    leaves = [t.requires_grad_() for t in (q, k, v)]
+    o, _ = qa.linear_attention(q, k, v, decay, h0)
+    torch.cuda.synchronize()
+    before = torch.cuda.memory_allocated()
+    torch.cuda.reset_peak_memory_stats()
+    got = torch.autograd.grad(o, leaves, dO)
+    used = torch.cuda.max_memory_allocated() - before
+    assert used < 3 * q.numel() * q.element_size() + h0.numel() * 2, used
+    want = qd.linear_bwd(*(t.detach() for t in leaves), decay, h0, dO, want_dh0=False)
+    assert want["dh0"] is None and all(torch.equal(a, want[n]) for a, n in zip(got, ("dq", "dk", "dv")))
+    h0.requires_grad_()                                                  # asked for, it comes
+    o, _ = qa.linear_attention(q, k, v, decay, h0)
+    assert torch.equal(torch.autograd.grad(o, h0, dO)[0], qd.linear_bwd(*(t.detach() for t in leaves), decay, h0.detach(), dO)["dh0"])
