@@ -63,7 +63,9 @@ __global__ void __launch_bounds__(kJoinThreads) k_linear_join(const LinearJoins 
             if (n >= segments) break;
             ends[(size_t)at * quads] = s;
             const Keep keep = keep_power(decay, min(length, T - at * length));
-            if (n + 1 < segments) s = make_float4(kept(keep, s.x, v[i].x), kept(keep, s.y, v[i].y), kept(keep, s.z, v[i].z), kept(keep, s.w, v[i].w));
+            // a state of 0 stays 0, also across a segment over which a head's factor is beyond fp32 (a batch padded in front)
+            auto on = [&](float h, float add) { return h == 0.f ? add : kept(keep, h, add); };
+            if (n + 1 < segments) s = make_float4(on(s.x, v[i].x), on(s.y, v[i].y), on(s.z, v[i].z), on(s.w, v[i].w));
         }
     }
 }

@@ -134,3 +134,26 @@ def test_a_constant_initial_state_gets_no_gradient(dtype):
     h0.requires_grad_()                                                  # asked for, it comes
     o, _ = qa.linear_attention(q, k, v, decay, h0)
     assert torch.equal(torch.autograd.grad(o, h0, dO)[0], qd.linear_bwd(*(t.detach() for t in leaves), decay, h0.detach(), dO)["dh0"])
+
+
+def test_a_state_of_zero_stays_zero_whatever_a_head_grows_by():
+    """Long sequences that begin with tokens of zeros (a padded batch): across a segment of them a head's factor is beyond fp32, 0 times it is 0."""
+    from paper_2606_08804_b200 import binding as qd
+    T, H, d, real = 32768, 2, 64, 700
+    decay = torch.tensor([0.1, 0.02], device="cuda")
+    for dtype in (BF, F32):
+        q, k, v, dO = (_n(1, T, H, d, seed=i, std=0.3, to=dtype) for i in range(4))
+        for t in (k, v, dO):
+            t[:, :-real] = 0
+        o, hT, _ = qd.linear_fwd(q, k, v, decay)
+        g = qd.linear_bwd(q, k, v, decay, None, dO)
+        assert not o[:, :-real].any() and not g["dq"][:, :-real].any()
+        ref = [lf.f64(t[:, -real:]) for t in (q, k, v)]
+        ro = f.linear(*ref, decay.double().cpu())
+        rg = lf.grads(ro, [dO[:, -real:].double().cpu(), None], ref)
+        for name, a, r in zip(("o", "hT", "dq", "dk", "dv"), (o[:, -real:], hT, g["dq"][:, -real:], g["dk"][:, -real:], g["dv"][:, -real:]), ro + tuple(rg)):
+            a, r = a.double().cpu(), r.detach()
+            assert a.isfinite().all(), name
+            off = float((a - r).norm() / r.norm())
+            # exponents of at most 70 in two half steps each, a rounding a chunk and sums of 64, or bf16's two roundings a term and its own
+            assert off < (2.0 ** -6 if dtype == BF and name != "hT" else (140 + 128 + 40) * lf.ULP), (name, off)
