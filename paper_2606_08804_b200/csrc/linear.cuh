@@ -23,7 +23,7 @@ struct LinearWalk {
     float* sT;               // the state that the walk ends with; NULL: not returned
     float* ends;             // [B H][segments][state], written where out is NULL
     int reverse;
-    int exact;               // the state ends in fp32, so bf16 walks take three planes of what is added to it (see linear_tc.cu), not one
+    int exact;               // the state is returned in fp32, so bf16 walks take three planes of what is added to it (see linear_tc.cu), not two
     int flip;                // s0, sT and ends hold S^T (as [DC][DB])
 };
 constexpr int kLinearWalks = 3;

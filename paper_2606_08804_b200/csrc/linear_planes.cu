@@ -14,23 +14,15 @@ namespace {
 constexpr int kRows = 64, kCols = 32, kPlanesThreads = 256;
 
 // four neighbours of a tile from global memory, rows >= live as zeros; on their way in registers, then into planes
-template <typename IO, int W>
+template <int W>
 struct Rows4 {
     static constexpr int kN = kRows * W / 4 / kPlanesThreads;
     float4 r[kN];
-    __device__ __forceinline__ void get(const IO* src, size_t stride, int live) {
+    __device__ __forceinline__ void get(const float* src, size_t stride, int live) {
 #pragma unroll
         for (int i = 0; i < kN; ++i) {
             const int id = i * kPlanesThreads + threadIdx.x, row = id / (W / 4), c = id % (W / 4) * 4;
-            r[i] = make_float4(0.f, 0.f, 0.f, 0.f);
-            if (row < live) {
-                if constexpr (sizeof(IO) == 4) r[i] = *reinterpret_cast<const float4*>(src + row * stride + c);
-                else {
-                    const uint2 u = *reinterpret_cast<const uint2*>(src + row * stride + c);
-                    r[i] = make_float4(__uint_as_float(u.x << 16), __uint_as_float(u.x & 0xffff0000u), __uint_as_float(u.y << 16),
-                                       __uint_as_float(u.y & 0xffff0000u));
-                }
-            }
+            r[i] = row < live ? *reinterpret_cast<const float4*>(src + row * stride + c) : make_float4(0.f, 0.f, 0.f, 0.f);
         }
     }
     // zeros for elements that are infinite or NaN, which f(row, column) hears of
@@ -109,28 +101,26 @@ __device__ __forceinline__ void product(float (&acc)[1][NTL][4], const MA& A, co
         for (int e = 0; e < 4; ++e) acc[0][j][e] += less[0][j][e] + less[1][j][e];
 }
 
-template <typename IO, int DB>
+template <int DB>
 struct PlanesLayout {
-    static constexpr int NP = sizeof(IO) == 4 ? 3 : 1;
-    typedef Planes<kRows, DB, NP> Wide;
-    typedef Planes<kRows, kCols, NP> Slice;
-    typedef Planes<kRows, kCols, 3> Scaled;
+    typedef Planes<kRows, DB, 3> Wide;
+    typedef Planes<kRows, kCols, 3> Slice;
     typedef Planes<kRows, kRows, 3> Square;
     typedef Planes<DB, kCols, 3> State;
-    static constexpr int kA = 0, kB = kA + Wide::kBytes, kC = kB + Wide::kBytes, kCh = kC + Slice::kBytes, kP = kCh + Scaled::kBytes,
+    static constexpr int kA = 0, kB = kA + Wide::kBytes, kC = kB + Wide::kBytes, kCh = kC + Slice::kBytes, kP = kCh + Slice::kBytes,
                          kS = kP + Square::kBytes, kBytes = kS + State::kBytes;
 };
 
-template <typename IO, int DB, int DC>
+template <int DB, int DC>
 __global__ void __launch_bounds__(kPlanesThreads, 1) k_linear_planes(const LinearP p) {
-    typedef PlanesLayout<IO, DB> L;
+    typedef PlanesLayout<DB> L;
     extern __shared__ __align__(16) unsigned char smem_planes[];
     __shared__ float s_d[kRows], s_rho[kRows], s_kappa[kRows];
     __shared__ int s_first[kCols];                             // of every column of c the first element that is infinite or NaN, in the walk's order
     __shared__ int s_unfit;
     const typename L::Wide A(smem_planes + L::kA), B(smem_planes + L::kB);
     const typename L::Slice Cc(smem_planes + L::kC);
-    const typename L::Scaled Ch(smem_planes + L::kCh);
+    const typename L::Slice Ch(smem_planes + L::kCh);
     const typename L::Square P(smem_planes + L::kP);
     const typename L::State S(smem_planes + L::kS);
     constexpr int kSlices = DC / kCols;
@@ -162,9 +152,9 @@ __global__ void __launch_bounds__(kPlanesThreads, 1) k_linear_planes(const Linea
 
     const int first = segment * p.length, end = min(p.T, first + p.length), chunks = (end - first + kRows - 1) / kRows;
     const size_t ld_b = (size_t)p.H * DB, ld_c = (size_t)p.H * DC;
-    const IO *ga = static_cast<const IO*>(w.a), *gb = static_cast<const IO*>(w.b), *gc = static_cast<const IO*>(w.c);
-    Rows4<IO, DB> ra, rb;
-    Rows4<IO, kCols> rc;
+    const float *ga = static_cast<const float*>(w.a), *gb = static_cast<const float*>(w.b), *gc = static_cast<const float*>(w.c);
+    Rows4<DB> ra, rb;
+    Rows4<kCols> rc;
     auto fetch = [&](int n) {
         const int t0 = first + (w.reverse ? chunks - 1 - n : n) * kRows, live = min(kRows, end - t0);
         const size_t row = (size_t)b * p.T + t0;
@@ -209,7 +199,7 @@ __global__ void __launch_bounds__(kPlanesThreads, 1) k_linear_planes(const Linea
             zero(out);
             product<false, true>(in, P, Cc, m0, o0, w.reverse ? kRows : m0 + 16, w.reverse ? m0 : 0);
             product<false, true>(out, A, S, m0, o0, DB);
-            IO* o = static_cast<IO*>(w.out) + ((size_t)b * p.T + t0) * ld_c + (size_t)h * DC + j0;
+            float* o = static_cast<float*>(w.out) + ((size_t)b * p.T + t0) * ld_c + (size_t)h * DC + j0;
             each2(in, out, m0, o0, [&](int r, int c, float x, float y, float x2, float y2) {
                 if (r >= live) return;
                 const float f = s_rho[r];
@@ -220,8 +210,7 @@ __global__ void __launch_bounds__(kPlanesThreads, 1) k_linear_planes(const Linea
                     if (at >= s_first[c]) x = NAN;
                     if (at >= s_first[c + 1]) y = NAN;
                 }
-                if constexpr (sizeof(IO) == 4) *reinterpret_cast<float2*>(o + r * ld_c + c) = make_float2(x, y);
-                else *reinterpret_cast<uint32_t*>(o + r * ld_c + c) = sm100::pack_bf16(x, y);
+                *reinterpret_cast<float2*>(o + r * ld_c + c) = make_float2(x, y);
             });
         }
         float add[1][NS][4];
@@ -244,10 +233,10 @@ __global__ void __launch_bounds__(kPlanesThreads, 1) k_linear_planes(const Linea
         });
 }
 
-template <typename IO, int DB, int DC>
+template <int DB, int DC>
 cudaError_t launch(const LinearP& p, cudaStream_t stream) {
-    constexpr int bytes = PlanesLayout<IO, DB>::kBytes;
-    const auto kern = k_linear_planes<IO, DB, DC>;
+    constexpr int bytes = PlanesLayout<DB>::kBytes;
+    const auto kern = k_linear_planes<DB, DC>;
     const cudaError_t e = set_max_smem_once((const void*)kern, bytes);
     if (e != cudaSuccess) return e;
     return launch_overlapped(kern, dim3((unsigned)(p.BH * p.segments * (DC / kCols) * p.walks)), dim3(kPlanesThreads), bytes, stream, p);
@@ -256,8 +245,8 @@ cudaError_t launch(const LinearP& p, cudaStream_t stream) {
 }  // namespace
 
 cudaError_t linear_planes(const LinearP& p, int db, int dc, cudaStream_t stream) {
-    if (db == 128) return dc == 128 ? launch<float, 128, 128>(p, stream) : launch<float, 128, 64>(p, stream);
-    return dc == 128 ? launch<float, 64, 128>(p, stream) : launch<float, 64, 64>(p, stream);
+    if (db == 128) return dc == 128 ? launch<128, 128>(p, stream) : launch<128, 64>(p, stream);
+    return dc == 128 ? launch<64, 128>(p, stream) : launch<64, 64>(p, stream);
 }
 
 }  // namespace qd
