@@ -9,26 +9,29 @@ namespace {
 
 constexpr size_t kStatusBytes = 256;
 
-// tokens of a chunk, and CTAs that share a head of a sequence in one walk (fp32: 32 columns of the state each)
-int linear_chunk(const qd_linear_shape& s) { return s.dtype == QD_BF16 ? 128 : 64; }
-long long linear_ctas(const qd_linear_shape& s) { return (long long)s.B * s.H * (s.dtype == QD_BF16 ? 1 : s.dv / 32); }
+int linear_chunk(const qd_linear_shape& s) { return s.dtype == QD_BF16 ? 128 : 64; }          // tokens
+// CTAs of one walk over whole sequences, for columns of c (fp32: 32 columns of the state to a CTA)
+long long linear_ctas(const qd_linear_shape& s, int dc) { return (long long)s.B * s.H * (s.dtype == QD_BF16 ? 1 : dc / 32); }
 
-// Segments of a sequence: as many as make the CTAs' longest run of chunks shortest.  A segment costs its chunks and what a CTA needs
-// before its first one; where there are several, the sums of each come first, which take half as long as a walk.  (32768 tokens of 16 heads
-// in bf16: forward 884 us in one segment, 165 in the chosen nine, 245 in twelve; backward 686, 372 in three, 447 in four.  Of 14 numbers up to 32
-// at 16 shapes the best was 4 % better than the chosen one, but for 3 x 2048 tokens of 16 heads: 51 for 47, backward 59 for 55.)
+// Segments of a sequence: as many as make the CTAs' longest run of chunks shortest, launch by launch.  A segment costs its chunks and what a CTA
+// needs before its first one; where there are several, the sums of all but the last come first, which take half as long as a walk.
+// (32768 tokens of 16 heads in bf16, four of which form every factor: forward 813 us in one segment, 184 in the chosen nine, 224 in ten, 193 in
+// eight; backward 883, 427 in the chosen nine, 457 in ten, 434 in five.  Of 14 numbers up to 32 at 14 shapes in bf16 and 19 at eight in fp32 the
+// best was at most 6 % faster than the chosen one, but for 777 tokens of 16 heads of 128 x 128 in fp32: 77 for 98, backward 178 for 194.)
 int segments_of(const qd_linear_shape& s, bool backward) {
-    const int chunk = linear_chunk(s);
-    const long long per = linear_ctas(s) * (backward ? kLinearWalks : 1);
-    const int chunks = (s.T + chunk - 1) / chunk;
-    if (per > 4 * kSMs) return 1;
+    const int chunk = linear_chunk(s), chunks = (s.T + chunk - 1) / chunk;
+    // walks of each launch: o; dq, dk and dv together, or the first two, whose state is transposed, and dv
+    const bool together = !backward || s.dk == s.dv;
+    const long long first = backward ? linear_ctas(s, s.dk) * (together ? kLinearWalks : 2) : linear_ctas(s, s.dv), second = together ? 0 : linear_ctas(s, s.dv),
+                    sums = linear_ctas(s, s.dv) * (backward ? 2 : 1);
+    if (first + second > 4 * kSMs) return 1;
+    const auto waves = [](long long ctas) { return (double)((ctas + kSMs - 1) / kSMs); };
     int best = 1;
     double least = 1e30;
     for (int n = 1; n <= 32 && n <= chunks; ++n) {
         const int length = (chunks + n - 1) / n;
         if ((chunks + length - 1) / length != n) continue;
-        const double waves = (double)((per * n + kSMs - 1) / kSMs);
-        const double cost = waves * (length + 2) + (n > 1 ? 0.5 * waves * (length + 2) + 3 : 0);
+        const double cost = (waves(first * n) + waves(second * n)) * (length + 2) + (n > 1 ? 0.5 * waves(sums * (n - 1)) * (length + 2) + 3 : 0);
         if (cost < least) { least = cost; best = n; }
     }
     return best;
