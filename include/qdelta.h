@@ -271,6 +271,8 @@ int qdelta_norm_bwd(long long rows, int width, int dtype, const void *x, const v
  * Factors d^n of heads that grow have to be finite in fp32 up to n = T, at most a chunk of 128 tokens (fp32: 64): log_decay <= 0.69 (1.38) for longer
  * sequences, else 0 times infinity gives NaN where the state itself might be finite.
  * A token that is infinite or NaN reaches the rows that the recurrence carries it to, and none before it.
+ * The same call gives the same bits; how many sequences and heads are in a call decides the order of sums, so a sequence by itself and the same in a
+ * batch may differ in the last ones.
  */
 typedef struct {
     int B, T, H, dk, dv;

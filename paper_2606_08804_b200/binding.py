@@ -351,7 +351,8 @@ def norm_bwd(x, weight, dy, stats, rms=False, want_dweight=None, want_dbias=True
 
 def linear_fwd(q, k, v, log_decay, h0=None, scale=1.0, workspace=None, want_hT=True):
     """Linear attention with a decay for each head: S_t = e^log_decay S_{t-1} + k_t v_t^T, o_t = scale S_t^T q_t.
-    q, k [B,T,H,dk], v [B,T,H,dv] (dk, dv = 64 or 128); log_decay [H] and h0 [B,H,dk,dv] fp32.
+    q, k [B,T,H,dk], v [B,T,H,dv] (dk, dv = 64 or 128); log_decay [H] and h0 [B,H,dk,dv] fp32 (what bf16 rounds, and the ranges of values:
+    include/qdelta.h).
     Returns (o [B,T,H,dv], hT [B,H,dk,dv] fp32, workspace, whose status word workspace_status reads)."""
     return (_native or _host()).linear_fwd(q, k, v, log_decay, h0, workspace, bool(want_hT), scale)
 

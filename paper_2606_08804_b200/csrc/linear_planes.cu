@@ -2,8 +2,8 @@
 // products of bf16 planes on the warp-level tensor instruction (planes.cuh), an fp32 matrix three planes; the state stays in fp32 registers,
 // to which a chunk's sum is added, and is written as planes for the next chunk's a S.
 // A chunk of 64 x 128 x 32 takes 7.6 us: its 1.2 million products of elements, six times over for the planes, keep the tensor pipe busy half of
-// that, what is written as planes and the barriers in between is the rest; a b^T is made once for every 32 columns.  2 x 2048 tokens, 16 heads of 128 x 128: forward 244 us, backward 714 (bytes 21 and 36); 2 x 1000, 4 heads of 64 x 64 in
-// segments: 20 and 45, latency.
+// that, what is written as planes and the barriers in between is the rest; a b^T is made once for every 32 columns.  2 x 2048 tokens, 16 heads
+// of 128 x 128: forward 247 us, backward 722 (bytes 21 and 36); 2 x 1000, 4 heads of 64 x 64 in segments: 21 and 46, latency.
 #include "linear.cuh"
 #include "planes.cuh"
 #include "split_common.cuh"

@@ -3,21 +3,21 @@
 // Row r of out has the factor e^{g (r - 63)} (backward e^{g (64 - r)}) in all its terms, which is multiplied in last: what is left of D and rho
 // depends on the column alone, and is at most e^{64 |g|} either way.  That much of fp32's range is lost at both ends, for weights, states and
 // outputs, so heads with |g| > kSlight, 2^16, form D as it stands and multiply a S by rho between the two products: 8 x 2048 x 16 forward
-// 69 us for 66, without the state 69 for 61, backward 172 for 165 if one head of them does (188 if all do).
+// 65 us for 64, without the state 67 for 59, backward 170 for 163 where four heads do (66, 66 and 186 where all do).
 // The state stays in fp32 registers; each chunk's sum comes from tensor memory and is added there (the tensor cores cut as they accumulate).
 // For a S it goes to shared memory in bf16.  In S the factor kappa stands with c, as bf16 planes cut from kappa c: three, which hold all of its
 // 24 bits, where the state is returned (with two, even rounded ones, it is 2.4e-6 of its length off, more than a whole fp32 sum over a sequence
 // is); two, 2^-15 apart, where it serves bf16 outputs alone (with one, dq and dk are off by 1.53 times what their own rounding costs, with two
 // by 1.35).
 //
-// 8 x 2048 tokens, 16 heads of 128 x 128, 128 CTAs: 59 us, 5300 cycles a chunk, at 5.6 TB/s of the 6.46 that a copy has (its bytes alone 41.5),
-// so HBM with the chunks' own start; 64 us with three planes, where the state's way from sum to sum is as long.  The products of a chunk are
-// 2560 cycles, 512 more with three planes.  Next to that it is shared memory, 128 bytes a cycle, which a product of 128 x 128 with both operands
-// there takes all of; so P and the planes are operands in tensor memory (c read transposed from its tile), and the parts of out, a S and P c,
-// share one accumulator, scaled in between: 78 us with the planes in shared memory and two accumulators.  Six tile buffers, two chunks deep: b,
-// c, a of each; out leaves through a's.  All sixteen warps make planes, a quarter each; with the state's left out of it 61 us, 48 for 44 at
-// 64 x 64, backward 173 for 160 then.  Launched again and again it runs into the GPU's power limit (forward and backward 229 us in the first launches,
-// 262 after a second).
+// 8 x 2048 tokens, 16 heads of 128 x 128, 128 CTAs: 59 us, 5300 cycles a chunk, 4.5 TB/s of the 6.46 that a copy has (its bytes alone 41.5); 64 us with
+// three planes.  No unit is full (tensor pipe 43 %, issue slots 47 %): it is a chunk's chain, scores to weights to out, and sum to state to a S,
+// with one CTA to an SM and 20 SMs without any.  The products of a chunk are 2560 cycles, 512 more with three planes.  Next to that it is
+// shared memory, 128 bytes a cycle, which a product of 128 x 128 with both operands there takes all of; so P and the planes are operands in
+// tensor memory (c read transposed from its tile), and the parts of out, a S and P c, share one accumulator, scaled in between: 78 us with the
+// planes in shared memory and two accumulators.  Six tile buffers, two chunks deep: b, c, a of each; out leaves through a's.  All sixteen warps make planes, a quarter each; with the state's left out of it 61 us, 48 for 44 at
+// 64 x 64, backward 173 for 160 then.  Launched again and again it runs into the GPU's power limit (forward and backward 235 us in short loops, 271
+// in long ones).
 // The sums of segments alone (ENDS), 32768 tokens of 16 heads: 60 us, of bytes 41.5.
 //   warps 0-7    two warpgroups: planes of the first two parts; P, half of the columns, from tensor memory and back to it; out, half of the
 //                columns, staged in a's tile, stored by TMA
